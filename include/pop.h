@@ -274,6 +274,121 @@ int pop_layer_step_kind(pop_layer_t *layer, int *workgroups);
 int pop_probe_read(const void *buf, size_t bytes, int workgroups, unsigned int *sink, void *stream);
 int pop_probe_step_read(pop_layer_t *layer, int k, int workgroups, unsigned int *sink, void *stream);
 
+/* ---- around the FFN: what a decoder needs that serves several beams of a prompt ----
+ *
+ * The beams of one prompt are the natural batch of the decode calls above: they share the partition that the prompt
+ * determined.  The calls below give them a cache of keys and values, attention over it, beam search's selection and the
+ * reordering of the cached states after it.  None of them needs a layer or keeps state: the caller owns all buffers.
+ *
+ * The cache (one decoder layer's keys and values) is held in 4 bits: e2m1 codes (0 .5 1 1.5 2 3 4 6 and a sign) and one
+ * scale byte for 32 channels, value = code * 2^(byte - 127) (the OCP microscaling format MXFP4), 17/16 byte for the key and
+ * the value of a channel together.  It is [n_pages][n_kv_heads][page_tokens / 16] tiles of 16 (D + D/16) bytes, D = head_dim:
+ *     K codes [16 tokens][D/2], V codes [4 groups of 4 tokens][16][4 tokens][D/32] (the 16 are D/16 channels each),
+ *     K scales [16 tokens][D/32], V scales [4 groups][D/32][4 tokens];  the lower channel of a byte is its low nibble.
+ * A token's *slot* is page * page_tokens + its place in the page.  A row of `block_table` (dev [n_seq][table_stride]) names
+ * the pages of a sequence in order; entries outside [0, n_pages) are no page.  All layers of a model can share the tables.
+ * head_dim is 64, 128 or 256, page_tokens 16, 32, 64, 128 or 256, else POP_EUNSUPPORTED; n_pages * page_tokens and
+ * table_stride * page_tokens stay below 2^31, else POP_EUNSUPPORTED.  cache, q, k, v, y, logits, workspaces: 16-byte aligned.
+ *
+ * Free pages stand in a ring: `ring` (dev [n_pages]) and `pool` (dev, two ints): the place of the first free page, and how many
+ * are free.  Pages are taken at the front and given back at the end, so a call's inputs stay as they are and its outputs
+ * (pool_out, and the new lengths and tables) are buffers of their own: a caller keeps two of each and takes turns.
+ * Status words (dev, one int, read it when you next synchronise): 0, or a sum of */
+enum {
+    POP_PLAN_PAGES = 1,   /* more pages needed than are free */
+    POP_PLAN_TOKENS = 2,  /* more new tokens than max_tokens */
+    POP_PLAN_INVALID = 4  /* a negative length, a table row that is too short, a pool that is none */
+};
+/* With a status other than 0 the call changed nothing: its outputs say that every sequence is as it was. */
+
+#define POP_MAX_BEAMS 16 /* rows of one request in pop_beam_select and pop_cache_reorder */
+
+/* Host only.  Bytes of one layer's cache.  Errors: sizes < 1 -> POP_ESHAPE; NULL -> POP_EINVAL. */
+int pop_cache_bytes(int n_kv_heads, int head_dim, int page_tokens, int n_pages, size_t *bytes);
+
+/* Pages and slots of a step from request lengths, in one launch.  cached_len, new_len: dev [n_seq], tokens that each sequence
+ * has in the cache and tokens that this step adds.  Every sequence keeps its pages and gets as many of the ring's as
+ * its new tokens call for, in sequence order.  Outputs (dev): block_table's entries for the new blocks; context_len [n_seq] =
+ * cached + new; q_start [n_seq + 1], the exclusive sums of new_len; and for the new tokens, sequence by sequence,
+ * slots [max_tokens] and positions [max_tokens] (may be NULL), -1 behind the last; pool_out; status.
+ * Errors: NULL pointers, outputs that are their inputs -> POP_EINVAL; negative sizes -> POP_ESHAPE. */
+int pop_cache_plan(const int *cached_len, const int *new_len, int n_seq, int page_tokens, int *block_table,
+                   int table_stride, const int *ring, int n_pages, const int *pool, int *pool_out, int max_tokens,
+                   int *context_len, int *q_start, int *slots, int *positions, int *status, void *stream);
+
+/* Stores tokens.  k, v: dev, one row of [n_kv_heads][head_dim] for each of n_tokens, k_stride and v_stride elements apart (so
+ * both may be parts of one projection's rows; multiples of 8 for bf16, of 4 for float32).  Tokens whose slot is negative or
+ * beyond the cache are left out.  A block's scale is 2^(e - 2), e the exponent of its largest magnitude, and twice that from a
+ * significand of 1.75 on; values go to the nearest code, halves to the even one, magnitudes above 6 to 6.  An infinity is stored
+ * as the largest float32, a NaN as zero: nothing that the format holds is infinite or no number.
+ * Errors: NULL or misaligned pointers, bad dtype -> POP_EINVAL; sizes, strides -> POP_ESHAPE. */
+int pop_cache_write(void *cache, int n_kv_heads, int head_dim, int page_tokens, int n_pages, const void *k,
+                    const void *v, pop_dtype_t dtype, long long k_stride, long long v_stride, const int *slots,
+                    int n_tokens, void *stream);
+
+/* The values stored at n_tokens slots, k and v: dev [n_tokens][n_kv_heads][head_dim] (exact in bf16 as in float32); zeros
+ * where a slot is negative or beyond the cache.  Errors: as pop_cache_write. */
+int pop_cache_read(const void *cache, int n_kv_heads, int head_dim, int page_tokens, int n_pages, const int *slots,
+                   int n_tokens, void *k, void *v, pop_dtype_t dtype, void *stream);
+
+/* y = softmax(scale * q k^T) v.  q: dev [n_tokens][n_heads][head_dim] of dtype; the new tokens of sequence s are rows q_start[s] ..
+ * q_start[s + 1] - 1 and the last of them is at position context_len[s] - 1; all of them
+ * have been written.  A token sees the positions up to its own, with window > 0 only the last `window` of them; query head h reads kv
+ * head h / (n_heads / n_kv_heads).  A token that sees nothing (pages that are none, a context shorter than the new tokens)
+ * gives zeros.  y: dev [n_tokens][n_heads][head_dim] of ydtype; rows of no sequence are not written.  A sequence whose rows leave
+ * [0, n_tokens) is left out and its rows are undefined.
+ * max_new, max_context: the longest that the caller expects; longer ones are right too, but may be slow.  float32 q is
+ * taken in full (three bf16 terms of q and of the softmax weights), with bf16 q the weights are rounded to bf16.
+ * workspace: dev, of pop_cache_attention_workspace bytes for the same sizes, any content, for this call alone.
+ * Errors: NULL or misaligned pointers, bad dtype, a scale that is not finite -> POP_EINVAL; sizes, n_heads no multiple of
+ * n_kv_heads, a workspace that is too small -> POP_ESHAPE. */
+int pop_cache_attention(const void *q, pop_dtype_t dtype, int n_tokens, const void *cache, int n_kv_heads,
+                        int head_dim, int page_tokens, int n_pages, const int *block_table, int table_stride,
+                        const int *q_start, const int *context_len, int n_seq, int n_heads, int max_new,
+                        int max_context, float scale, int window, void *y, pop_dtype_t ydtype, void *workspace,
+                        size_t workspace_bytes, void *stream);
+/* Host only. */
+int pop_cache_attention_workspace(int n_tokens, int n_seq, int n_heads, int n_kv_heads, int head_dim, int max_new,
+                                  int max_context, size_t *bytes);
+
+/* Beam search's selection.  logits: dev [n_requests * n_beams][vocab] (float32 or bf16), scores: dev [n_requests * n_beams]
+ * float32, the beams' sums of log-probabilities (-inf: not alive), done: dev, a byte for each beam (may be NULL).
+ * A beam proposes scores + logit - logsumexp(logits) for every token; one that is done proposes pad_token at its own score
+ * and nothing else.  Per request the k best: scores, tokens and the beams they come from (dev [n_requests][k]), best first, equal
+ * scores by lower beam, then lower token.  (Tokens of one beam are first ranked by their logits, equal ones by lower token.)
+ * What is proposed at -inf fills up a list that is short.  n_beams <= POP_MAX_BEAMS, k <= 64 and <= n_beams * vocab.
+ * NaN logits count as -inf; with +inf ones results are unspecified.
+ * workspace: dev, of pop_beam_workspace bytes for the same sizes, any content.
+ * Errors: NULL or misaligned pointers, bad dtype -> POP_EINVAL; sizes, pad_token outside the vocabulary, a workspace that is
+ * too small -> POP_ESHAPE; beyond the limits above, vocab > 2^24 -> POP_EUNSUPPORTED. */
+int pop_beam_select(const void *logits, pop_dtype_t dtype, const float *scores, const unsigned char *done,
+                    int n_requests, int n_beams, int vocab, int k, int pad_token, float *out_scores, int *out_tokens,
+                    int *out_parents, void *workspace, size_t workspace_bytes, void *stream);
+/* Host only. */
+int pop_beam_workspace(int n_requests, int n_beams, int vocab, int k, size_t *bytes);
+
+/* The cached states after a selection: n_seq rows in groups of n_beams, and row c of a group becomes what row parents[c]
+ * (0 .. n_beams - 1, within the group; anything else ends the row) of it was.  Rows share the full pages they have in common.
+ * A last page that is partly filled goes on with the parent's first child; each further child gets a page of the ring and
+ * copies = {the parent's page, its own} (dev [n_seq][2], {-1, -1} for none), for pop_cache_copy_pages on every layer.  Pages
+ * that no row of the group holds any more go to the end of the ring, by group, block and row.  n_beams = 1 and parents of -1
+ * release sequences.  Rows of a group may share pages only at the same block, and groups none, as these calls leave them.
+ * Outputs (dev): new_table [n_seq][table_stride] (-1 behind a row's last page), new_len [n_seq], copies, pool_out, status, and
+ * the ring's free places.  workspace: dev, of pop_cache_reorder_workspace bytes, any content.
+ * Errors: NULL pointers, outputs that are their inputs -> POP_EINVAL; sizes, n_seq no multiple of n_beams, a workspace
+ * that is too small -> POP_ESHAPE; n_beams > POP_MAX_BEAMS -> POP_EUNSUPPORTED. */
+int pop_cache_reorder(const int *block_table, const int *len, const int *parents, int n_seq, int n_beams,
+                      int page_tokens, int table_stride, int *new_table, int *new_len, int *copies, int *ring,
+                      int n_pages, const int *pool, int *pool_out, void *workspace, size_t workspace_bytes, int *status,
+                      void *stream);
+/* Host only. */
+int pop_cache_reorder_workspace(int n_seq, int n_beams, int table_stride, size_t *bytes);
+
+/* Page copies {from, to} of one layer's cache: copies dev [n_copies][2]; pairs with a number that is no page do nothing.  No page
+ * may be copied to twice, or from and to.  Errors: NULL or misaligned pointers -> POP_EINVAL; sizes -> POP_ESHAPE. */
+int pop_cache_copy_pages(void *cache, int n_kv_heads, int head_dim, int page_tokens, int n_pages, const int *copies,
+                         int n_copies, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

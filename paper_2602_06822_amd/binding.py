@@ -28,6 +28,7 @@ POP_MAX_BATCH = 8
 
 _vp, _i, _dbl = C.c_void_p, C.c_int, C.c_double
 _ip = C.POINTER(C.c_int)
+_szp = C.POINTER(C.c_size_t)
 
 _SIGS = {
     "pop_version": (C.c_int, []),
@@ -59,6 +60,18 @@ _SIGS = {
     "pop_layer_set_wait_limit": (_i, [_vp, _i]),
     "pop_layer_set_shared_batch_mask": (_i, [_vp, _i]),
     "pop_layer_set_importance": (_i, [_vp, _i]),
+    "pop_cache_bytes": (_i, [_i, _i, _i, _i, _szp]),
+    "pop_cache_plan": (_i, [_vp, _vp, _i, _i, _vp, _i, _vp, _i, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "pop_cache_write": (_i, [_vp, _i, _i, _i, _i, _vp, _vp, _i, C.c_longlong, C.c_longlong, _vp, _i, _vp]),
+    "pop_cache_read": (_i, [_vp, _i, _i, _i, _i, _vp, _i, _vp, _vp, _i, _vp]),
+    "pop_cache_attention": (_i, [_vp, _i, _i, _vp, _i, _i, _i, _i, _vp, _i, _vp, _vp, _i, _i, _i, _i, C.c_float, _i, _vp, _i,
+                                 _vp, C.c_size_t, _vp]),
+    "pop_cache_attention_workspace": (_i, [_i, _i, _i, _i, _i, _i, _i, _szp]),
+    "pop_beam_select": (_i, [_vp, _i, _vp, _vp, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp, C.c_size_t, _vp]),
+    "pop_beam_workspace": (_i, [_i, _i, _i, _i, _szp]),
+    "pop_cache_reorder": (_i, [_vp, _vp, _vp, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp, _vp, _vp, C.c_size_t, _vp, _vp]),
+    "pop_cache_reorder_workspace": (_i, [_i, _i, _i, _szp]),
+    "pop_cache_copy_pages": (_i, [_vp, _i, _i, _i, _i, _vp, _i, _vp]),
 }
 for _name, (_res, _args) in _SIGS.items():
     _fn = getattr(_lib, _name)
@@ -263,6 +276,99 @@ def pop_layer_step_kind(layer):
     if kind < 0:
         raise PopError(kind, "pop_layer_step_kind")
     return kind, wg.value
+
+
+POP_PLAN_PAGES, POP_PLAN_TOKENS, POP_PLAN_INVALID = 1, 2, 4
+POP_MAX_BEAMS = 16
+
+
+def _size(fn, name, *args) -> int:
+    n = C.c_size_t()
+    _check(fn(*args, C.byref(n)), name)
+    return n.value
+
+
+def _rows(t, width, stride):
+    """(address, elements from row to row) of token rows that may be part of longer ones; a raw address needs `stride`."""
+    if t is None or isinstance(t, int):
+        return t, width if stride is None else stride
+    if not t.is_cuda:
+        raise ValueError("device tensor expected")
+    if t.numel() and not t[0].is_contiguous():
+        raise ValueError("contiguous rows expected")
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else width) if stride is None else stride
+
+
+def _workspace(t):
+    return (None, 0) if t is None else (_ptr(t), t.numel() * t.element_size())
+
+
+def pop_cache_bytes(n_kv_heads, head_dim, page_tokens, n_pages) -> int:
+    return _size(_lib.pop_cache_bytes, "pop_cache_bytes", n_kv_heads, head_dim, page_tokens, n_pages)
+
+
+def pop_cache_plan(cached_len, new_len, n_seq, page_tokens, block_table, table_stride, ring, n_pages, pool, pool_out,
+                   max_tokens, context_len, q_start, slots, positions, status, stream=None):
+    _check(_lib.pop_cache_plan(_ptr(cached_len), _ptr(new_len), n_seq, page_tokens, _ptr(block_table), table_stride,
+                               _ptr(ring), n_pages, _ptr(pool), _ptr(pool_out), max_tokens, _ptr(context_len),
+                               _ptr(q_start), _ptr(slots), _ptr(positions), _ptr(status), _stream(stream)), "pop_cache_plan")
+
+
+def pop_cache_write(cache, n_kv_heads, head_dim, page_tokens, n_pages, k, v, dtype, slots, n_tokens, k_stride=None,
+                    v_stride=None, stream=None):
+    k, k_stride = _rows(k, n_kv_heads * head_dim, k_stride)
+    v, v_stride = _rows(v, n_kv_heads * head_dim, v_stride)
+    _check(_lib.pop_cache_write(_ptr(cache), n_kv_heads, head_dim, page_tokens, n_pages, k, v, dtype, k_stride, v_stride,
+                                _ptr(slots), n_tokens, _stream(stream)), "pop_cache_write")
+
+
+def pop_cache_read(cache, n_kv_heads, head_dim, page_tokens, n_pages, slots, n_tokens, k, v, dtype, stream=None):
+    _check(_lib.pop_cache_read(_ptr(cache), n_kv_heads, head_dim, page_tokens, n_pages, _ptr(slots), n_tokens, _ptr(k),
+                               _ptr(v), dtype, _stream(stream)), "pop_cache_read")
+
+
+def pop_cache_attention(q, dtype, n_tokens, cache, n_kv_heads, head_dim, page_tokens, n_pages, block_table, table_stride,
+                        q_start, context_len, n_seq, n_heads, max_new, max_context, scale, window, y, ydtype, workspace,
+                        stream=None):
+    ws, ws_bytes = _workspace(workspace)
+    _check(_lib.pop_cache_attention(_ptr(q), dtype, n_tokens, _ptr(cache), n_kv_heads, head_dim, page_tokens, n_pages,
+                                    _ptr(block_table), table_stride, _ptr(q_start), _ptr(context_len), n_seq, n_heads,
+                                    max_new, max_context, scale, window, _ptr(y), ydtype, ws, ws_bytes, _stream(stream)),
+           "pop_cache_attention")
+
+
+def pop_cache_attention_workspace(n_tokens, n_seq, n_heads, n_kv_heads, head_dim, max_new, max_context) -> int:
+    return _size(_lib.pop_cache_attention_workspace, "pop_cache_attention_workspace", n_tokens, n_seq, n_heads, n_kv_heads,
+                 head_dim, max_new, max_context)
+
+
+def pop_beam_select(logits, dtype, scores, done, n_requests, n_beams, vocab, k, pad_token, out_scores, out_tokens,
+                    out_parents, workspace, stream=None):
+    ws, ws_bytes = _workspace(workspace)
+    _check(_lib.pop_beam_select(_ptr(logits), dtype, _ptr(scores), _ptr(done), n_requests, n_beams, vocab, k, pad_token,
+                                _ptr(out_scores), _ptr(out_tokens), _ptr(out_parents), ws, ws_bytes, _stream(stream)),
+           "pop_beam_select")
+
+
+def pop_beam_workspace(n_requests, n_beams, vocab, k) -> int:
+    return _size(_lib.pop_beam_workspace, "pop_beam_workspace", n_requests, n_beams, vocab, k)
+
+
+def pop_cache_reorder(block_table, length, parents, n_seq, n_beams, page_tokens, table_stride, new_table, new_len, copies,
+                      ring, n_pages, pool, pool_out, workspace, status, stream=None):
+    ws, ws_bytes = _workspace(workspace)
+    _check(_lib.pop_cache_reorder(_ptr(block_table), _ptr(length), _ptr(parents), n_seq, n_beams, page_tokens, table_stride,
+                                  _ptr(new_table), _ptr(new_len), _ptr(copies), _ptr(ring), n_pages, _ptr(pool),
+                                  _ptr(pool_out), ws, ws_bytes, _ptr(status), _stream(stream)), "pop_cache_reorder")
+
+
+def pop_cache_reorder_workspace(n_seq, n_beams, table_stride) -> int:
+    return _size(_lib.pop_cache_reorder_workspace, "pop_cache_reorder_workspace", n_seq, n_beams, table_stride)
+
+
+def pop_cache_copy_pages(cache, n_kv_heads, head_dim, page_tokens, n_pages, copies, n_copies, stream=None):
+    _check(_lib.pop_cache_copy_pages(_ptr(cache), n_kv_heads, head_dim, page_tokens, n_pages, _ptr(copies), n_copies,
+                                     _stream(stream)), "pop_cache_copy_pages")
 
 
 def raw():

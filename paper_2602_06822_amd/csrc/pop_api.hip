@@ -18,11 +18,15 @@ namespace {
 
 thread_local char g_hip_err[256] = "";
 
-int hip_fail(hipError_t e, const char *what)
+}  // namespace
+
+int pop::hip_fail(hipError_t e, const char *what)
 {
     snprintf(g_hip_err, sizeof g_hip_err, "%s: %s", what, hipGetErrorString(e));
     return POP_EHIP;
 }
+
+namespace {
 
 #define POP_HIP(call)                                      \
     do {                                                   \

@@ -11,6 +11,9 @@ namespace pop {
 
 constexpr int kWave = 64;
 
+// Keeps the text of a failed HIP call for pop_last_hip_error and returns POP_EHIP.
+int hip_fail(hipError_t e, const char *what);
+
 // Order-preserving key of a float32 score: larger score <=> larger key; -0.0 maps to the key of +0.0.
 __device__ __forceinline__ uint32_t score_key(float s)
 {
