@@ -287,8 +287,8 @@ int pop_probe_step_read(pop_layer_t *layer, int k, int workgroups, unsigned int 
  *     K scales [16 tokens][D/32], V scales [4 groups][D/32][4 tokens];  the lower channel of a byte is its low nibble.
  * A token's *slot* is page * page_tokens + its place in the page.  A row of `block_table` (dev [n_seq][table_stride]) names
  * the pages of a sequence in order; entries outside [0, n_pages) are no page.  All layers of a model can share the tables.
- * head_dim is 64, 128 or 256, page_tokens 16, 32, 64, 128 or 256, else POP_EUNSUPPORTED; n_pages * page_tokens and
- * table_stride * page_tokens stay below 2^31, else POP_EUNSUPPORTED.  cache, q, k, v, y, logits, workspaces: 16-byte aligned.
+ * head_dim is 64, 128 or 256, page_tokens 16, 32, 64, 128 or 256, else POP_EUNSUPPORTED; n_pages * page_tokens stays
+ * below 2^31 and table_stride * page_tokens does not pass 2^30, else POP_EUNSUPPORTED.  cache, q, k, v, y, logits, workspaces: 16-byte aligned.
  *
  * Free pages stand in a ring: `ring` (dev [n_pages]) and `pool` (dev, two ints): the place of the first free page, and how many
  * are free.  Pages are taken at the front and given back at the end, so a call's inputs stay as they are and its outputs

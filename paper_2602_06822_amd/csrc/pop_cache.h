@@ -60,6 +60,33 @@ __device__ __forceinline__ uint32_t cache_pair_at(uint32_t codes, float scale, i
 
 __device__ __forceinline__ float cache_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
 
+// Workgroups of one launch that hand their results to the last of them count themselves in a word {tag, number}.  The tag (48 bits)
+// is the launch's own: a word with any other content counts as none, and the last one to arrive leaves it 0, so nothing has to be
+// cleared before a launch, and a captured launch can be replayed.  Nobody waits.  A word that has the tag is added to; exchanges, which
+// cost 0.6 us each where many arrive together (64 of them: 40 us), are left to whoever finds it without.
+//
+// Called by one thread once the workgroup's results are on their way past the caches and acknowledged; true for the last of
+// `expected` (2 .. 65535).
+__device__ __forceinline__ bool arrive_last(unsigned long long *word, unsigned long long tag, int expected)
+{
+    unsigned long long seen = __hip_atomic_fetch_add(word, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if ((seen & ~0xffffull) != tag) {  // not there yet: that addition does not count, whatever it was added to
+        for (seen += 1; (seen & ~0xffffull) != tag;)
+            if (__hip_atomic_compare_exchange_strong(word, &seen, tag | 1, __ATOMIC_RELAXED, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) return false;
+        seen = __hip_atomic_fetch_add(word, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    if ((int)(seen & 0xffffull) + 1 != expected) return false;
+    __hip_atomic_store(word, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return true;
+}
+// Puts the tag there ahead of time, so that those who arrive add: `seen` is what coherent_load(word) gave.
+__device__ __forceinline__ void announce(unsigned long long *word, unsigned long long seen, unsigned long long tag)
+{
+    if ((seen & ~0xffffull) != tag)
+        __hip_atomic_compare_exchange_strong(word, &seen, tag, __ATOMIC_RELAXED, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+unsigned long long launch_tag();  // host: another one for every launch, never 0
+
 // Launchers.  Arguments have been checked; each returns the launch's status.
 struct PlanArgs {
     const int *cached, *fresh;  // [n_seq] tokens in the cache, new tokens
@@ -106,7 +133,7 @@ struct AttentionArgs {
     int y_bf16;
     float *ws;
 };
-size_t cache_attention_ws(int n_tokens, int n_seq, int n_heads, int n_kv, int d, int max_new, int max_context);
+size_t cache_attention_ws(int n_seq, int n_heads, int n_kv, int d, int max_new, int max_context);
 hipError_t launch_cache_attention(const AttentionArgs &a, hipStream_t s);
 
 struct BeamArgs {

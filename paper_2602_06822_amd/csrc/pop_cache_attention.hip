@@ -17,6 +17,8 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef const __attribute__((address_space(4))) int *scalar_ints;  // read by scalar loads
 
 constexpr float kLog2e = 1.44269504088896340736f;
 // A column's maximum starts here: below every finite score, and a difference with it is no NaN.
@@ -49,26 +51,41 @@ struct TileRegs {
     uint32_t k[D / 32], v[D / 32], ks, vs;
 };
 
+// Loads of a lane go through a descriptor of the tile: its address is in scalar registers, a lane's offsets within a tile stay the
+// same for all tiles, and a descriptor of no bytes stands for a tile that is not there: its loads give zeros and fetch nothing, so
+// that a wave always has the same number of loads in flight.
 template <int D>
-__device__ __forceinline__ void load_tile(TileRegs<D> &r, const unsigned char *tile, int n, int g)
+struct TileOffsets {
+    int k, v, ks, vs;
+    __device__ __forceinline__ TileOffsets(int n, int g)
+    {
+        constexpr int W = D / 32;
+        k = n * (D / 2) + g * (D / 8);
+        v = 8 * D + (g * 16 + n) * (4 * W);
+        ks = 16 * D + n * W + g * D / 128;
+        vs = 16 * D + 16 * W + (g * W + n * (D / 16) / 32) * 4;
+    }
+};
+
+template <int D, bool PAST>
+__device__ __forceinline__ void load_tile(TileRegs<D> &r, const unsigned char *tile, bool there, const TileOffsets<D> &o)
 {
-    constexpr int W = D / 32;
-    const unsigned char *k = tile + n * (D / 2) + g * (D / 8), *v = tile + 8 * D + (g * 16 + n) * (4 * W);
+    constexpr int kAux = PAST ? 2 : 0;  // non-temporal
+    const __amdgpu_buffer_rsrc_t d = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(tile), 0, there ? cache_tile_bytes(D) : 0, 0x00020000);
     if constexpr (D == 64) {
-        const uint2 a = *reinterpret_cast<const uint2 *>(k), b = *reinterpret_cast<const uint2 *>(v);
-        r.k[0] = a.x, r.k[1] = a.y, r.v[0] = b.x, r.v[1] = b.y;
+        const u32x2 a = __builtin_amdgcn_raw_buffer_load_b64(d, o.k, 0, kAux), b = __builtin_amdgcn_raw_buffer_load_b64(d, o.v, 0, kAux);
+        r.k[0] = a[0], r.k[1] = a[1], r.v[0] = b[0], r.v[1] = b[1];
     } else {
 #pragma unroll
         for (int i = 0; i < D / 128; ++i) {
-            const uint4 a = reinterpret_cast<const uint4 *>(k)[i], b = reinterpret_cast<const uint4 *>(v)[i];
-            r.k[4 * i] = a.x, r.k[4 * i + 1] = a.y, r.k[4 * i + 2] = a.z, r.k[4 * i + 3] = a.w;
-            r.v[4 * i] = b.x, r.v[4 * i + 1] = b.y, r.v[4 * i + 2] = b.z, r.v[4 * i + 3] = b.w;
+            const u32x4 a = __builtin_amdgcn_raw_buffer_load_b128(d, o.k + 16 * i, 0, kAux), b = __builtin_amdgcn_raw_buffer_load_b128(d, o.v + 16 * i, 0, kAux);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) r.k[4 * i + j] = a[j], r.v[4 * i + j] = b[j];
         }
     }
-    const unsigned char *ks = tile + 16 * D + n * W + g * D / 128;
-    if constexpr (D == 256) r.ks = *reinterpret_cast<const uint16_t *>(ks);
-    else r.ks = *ks;
-    r.vs = *reinterpret_cast<const uint32_t *>(tile + 16 * D + 16 * W + (g * W + n * (D / 16) / 32) * 4);
+    if constexpr (D == 256) r.ks = __builtin_amdgcn_raw_buffer_load_b16(d, o.ks, 0, kAux);
+    else r.ks = __builtin_amdgcn_raw_buffer_load_b8(d, o.ks, 0, kAux);
+    r.vs = __builtin_amdgcn_raw_buffer_load_b32(d, o.vs, 0, kAux);
 }
 
 // Operand of the s-th 32 channels: 8 of the lane's D/4, in the order of their bytes.
@@ -89,9 +106,6 @@ struct Columns {
     int window;     // INT_MAX for none
 };
 
-// The general kernel.  Workgroup: 4 waves; grid: (splits, column blocks, kv heads x sequences).  Wave w takes steps w, w + 4, .. of
-// the split's tokens.  QT, PT: bf16 terms that q and the softmax weights are split into: q one if it is bf16 (exact), else three (24
-// bits); the weights one if the output is bf16 (rounded to 8 significant bits, as the output is), else three.  K and V are exact in bf16.
 template <int TERMS>
 __device__ __forceinline__ void split_terms(const float (&x)[8], bf16x8 (&t)[TERMS])
 {
@@ -109,254 +123,480 @@ __device__ __forceinline__ void split_terms(const float (&x)[8], bf16x8 (&t)[TER
     }
 }
 
-__device__ __forceinline__ void store_y(const AttentionArgs &a, size_t at, float y)
+__device__ __forceinline__ void store_y2(const AttentionArgs &a, size_t at, float x, float y)
 {
-    if (a.y_bf16) static_cast<uint16_t *>(a.y)[at] = (uint16_t)pack_bf16(y, 0.0f);
-    else static_cast<float *>(a.y)[at] = y;
+    if (a.y_bf16) *reinterpret_cast<uint32_t *>(static_cast<uint16_t *>(a.y) + at) = pack_bf16(x, y);
+    else *reinterpret_cast<float2 *>(static_cast<float *>(a.y) + at) = {x, y};
 }
 
-// Sequences' rows of q and y: rows outside the tensors are not touched.
-__device__ __forceinline__ bool sequence_columns(const AttentionArgs &a, int seq, int share, int *first_row, Columns *c)
+// Sum over the lanes up to this one.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_add(int v)
 {
-    const int start = a.start[seq], fresh = a.start[seq + 1] - start;
-    c->length = min(max(a.context[seq], 0), (int)min((long long)a.stride << a.c.log_page, (long long)0x7fffffff));
-    c->first_pos = a.context[seq] - fresh;
+    return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ int wave_scan(int v)
+{
+    v = dpp_add<0x111, 0xf>(v), v = dpp_add<0x112, 0xf>(v), v = dpp_add<0x114, 0xf>(v), v = dpp_add<0x118, 0xf>(v);  // rows of 16
+    v = dpp_add<0x142, 0xa>(v);                                                                                      // pairs of rows
+    return dpp_add<0x143, 0xc>(v);
+}
+
+constexpr int kNoWindow = 0x7fffffff, kMostTokens = 1 << 30;  // (a sequence's table holds no more: checked by the caller)
+
+// Sequences' rows of q and y: rows outside the tensors are not touched.
+__device__ __forceinline__ bool sequence_columns(const AttentionArgs &a, int start, int next, int context, int share, Columns *c)
+{
+    const int fresh = next - start;
+    context = min(max(context, 0), kMostTokens);
+    c->length = min(context, a.stride << a.c.log_page);
+    c->first_pos = context - fresh;
     c->share = share;
     c->n = fresh * share;
-    c->window = a.window > 0 ? a.window : 0x7fffffff;
-    *first_row = start;
+    c->window = a.window > 0 ? min(a.window, kMostTokens) : kNoWindow;
     return start >= 0 && fresh > 0 && fresh <= a.n_tokens - start;
 }
 
+// Tokens [lo, hi) that some of the columns [begin, end) see, lo a multiple of 32, and the first and the last of the columns' positions.
+struct SeenTokens {
+    int lo, hi, first_pos, last_pos;
+};
+__device__ __forceinline__ SeenTokens seen_tokens(const Columns &c, int begin, int end)
+{
+    SeenTokens s;
+    s.first_pos = c.first_pos + begin / c.share, s.last_pos = c.first_pos + (end - 1) / c.share;
+    s.hi = max(min(s.last_pos + 1, c.length), 0);
+    s.lo = c.window == kNoWindow ? 0 : min(max(s.first_pos - c.window + 1, 0) & ~31, s.hi);
+    return s;
+}
+
+// One step of a wave: 32 tokens of one kv head against 16 columns.
 template <int D, int QT, int PT>
-__global__ __launch_bounds__(256) void cache_attention_kernel(AttentionArgs a, int splits)
+struct WaveSums {
+    bf16x8 q[D / 32][QT];  // the lane's part of q: channels [g D/4, (g + 1) D/4) of column n
+    f32x4 o[D / 16];       // O^T: channel (4 g + i) D/16 + j of column n in o[j][i]
+    float m, l;            // maximum that the weights are relative to; the lane's part of their sum
+
+    // limit[u]: tokens of tile u from this position on are not there; masked: some of the 32 are not seen by some column.
+    __device__ __forceinline__ void step(const TileRegs<D> (&r)[2], const int (&limit)[2], bool masked, int t0, int pos, int window, int g,
+                                         float scale)
+    {
+        f32x4 s[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            s[u] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) {
+                const bf16x8 k = k_operand<D>(r[u], c);
+#pragma unroll
+                for (int t = QT - 1; t >= 0; --t) s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[c][t], s[u], 0, 0, 0);
+            }
+        }
+        uint32_t vs[2] = {r[0].vs, r[1].vs};
+        if (masked) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int t = t0 + 16 * u + 4 * g;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (!(t + i < limit[u] && t + i <= pos && pos - (t + i) < window)) s[u][i] = -INFINITY;
+                // scale bytes of tokens that are not there become 2^-127, so that whatever stands in their place is finite
+                const int left = limit[u] - t;
+                vs[u] = left >= 4 ? vs[u] : left <= 0 ? 0u : vs[u] & ((1u << (8 * left)) - 1);
+            }
+        }
+        float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+        top *= scale;  // (scale > 0)
+        if (__any(top > m + kSlack)) {
+            top = fmaxf(top, __shfl_xor(top, 16, kWave));
+            top = fmaxf(top, __shfl_xor(top, 32, kWave));
+            const float next = fmaxf(m, top), factor = __builtin_amdgcn_exp2f(m - next);
+            m = next;
+            l *= factor;
+#pragma unroll
+            for (int j = 0; j < D / 16; ++j) o[j] *= factor;
+        }
+        float p[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            p[i] = __builtin_amdgcn_exp2f(fmaf(s[i / 4][i % 4], scale, -m));
+            l += p[i];
+        }
+        bf16x8 w[PT];
+        split_terms<PT>(p, w);
+        float sv[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sv[i] = cache_scale((vs[i / 4] >> (8 * (i % 4))) & 255u);
+        constexpr int W = D / 32;  // bytes of a token: channels 2 b and 2 b + 1 of the lane's D/16 in byte b
+#pragma unroll
+        for (int b = 0; b < W; ++b) {
+            uint32_t c[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int at = (i % 4) * W + b;
+                c[i] = cache_pair_at(r[i / 4].v[at / 4], sv[i], at % 4);
+            }
+            const bf16x8 even = as_bf16x8(low_halves(c[0], c[1]), low_halves(c[2], c[3]), low_halves(c[4], c[5]), low_halves(c[6], c[7]));
+            const bf16x8 odd = as_bf16x8(high_halves(c[0], c[1]), high_halves(c[2], c[3]), high_halves(c[4], c[5]), high_halves(c[6], c[7]));
+#pragma unroll
+            for (int t = PT - 1; t >= 0; --t) {
+                o[2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, w[t], o[2 * b], 0, 0, 0);
+                o[2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, w[t], o[2 * b + 1], 0, 0, 0);
+            }
+        }
+    }
+};
+
+constexpr int kBuffers = 2;   // steps that a wave has in registers: the one it uses and the next
+constexpr int kRound = 128;   // tokens of a round: a step of each of the four waves
+constexpr int kWorkgroups = 512;
+constexpr int kPieces = 32;    // of a unit, as a rule
+
+// How the work is dealt.  A unit is one kv head's block of 16 columns of one sequence: a number of rounds over the tokens that the
+// sequence's columns see.  All units stand in one row (sequence, block, head), and every workgroup takes the same number of rounds of
+// it, wherever units begin and end: ragged batches and single long sequences load all compute units alike.  A piece of a unit
+// is what one workgroup has of it.
+struct SequenceWork {
+    int rounds;  // of a unit
+    int blocks;
+    Columns cols;
+    SeenTokens seen;
+    int row0;
+};
+__device__ __forceinline__ SequenceWork sequence_work(const AttentionArgs &a, int start, int next, int context, int share)
+{
+    SequenceWork w;
+    w.rounds = 0, w.blocks = 0, w.row0 = start;
+    if (!sequence_columns(a, start, next, context, share, &w.cols)) return w;
+    w.blocks = (w.cols.n + 15) / 16;
+    w.seen = seen_tokens(w.cols, 0, w.cols.n);
+    w.rounds = max((w.seen.hi - w.seen.lo + kRound - 1) / kRound, 1);
+    return w;
+}
+
+// Partial results: two places for each workgroup, its first piece if the unit began in front of it and its last if the unit goes on
+// behind it; then the counters of the units' pieces, by the workgroup that has the first.
+template <int D>
+__device__ __forceinline__ float *partial_of(const AttentionArgs &a, int place)
+{
+    return a.ws + (size_t)place * 16 * (D + 4);
+}
+
+__device__ __forceinline__ void store_pair(float *p, float x, float y)
+{
+    const unsigned long long v = (unsigned long long)__float_as_uint(y) << 32 | __float_as_uint(x);
+    __hip_atomic_store(reinterpret_cast<unsigned long long *>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 load_pair(const float *p)
+{
+    const unsigned long long v = coherent_load(reinterpret_cast<const unsigned long long *>(p));
+    return {__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))};
+}
+
+// Workgroup: 4 waves.  In a round wave w takes tokens 32 w .. 32 w + 31 and asks for the next round's codes before it uses this one's.
+// Units that end and begin with a workgroup are written to y; the pieces of others are joined by the last workgroup that finishes
+// one, in the order of the tokens.  QT, PT: bf16 terms that q and the softmax weights are split into: q one if it is bf16 (exact),
+// else three (24 bits); the weights one if the output is bf16 (rounded to 8 significant bits, as the output is), else three.  K and V
+// are exact in bf16.
+template <int D, int QT, int PT, bool PAST>
+__global__ __launch_bounds__(256, D == 256 || QT == 3 ? 1 : 3) void cache_attention_kernel(AttentionArgs a, unsigned long long tag)
 {
     constexpr int kTile = cache_tile_bytes(D);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
-    const int share = a.n_heads / a.c.n_kv;
-    const int head = blockIdx.z % a.c.n_kv, seq = blockIdx.z / a.c.n_kv;
-    Columns cols;
-    int row0;
-    if (!sequence_columns(a, seq, share, &row0, &cols)) return;
-    const int *table = a.table + (size_t)seq * a.stride;
-
-    __shared__ float s_o[16][D + 1];
+    constexpr int kPass = D > 128 ? 128 : D;  // channels of a pass of the join through LDS
+    __shared__ float s_o[4][16][kPass + 4];
     __shared__ float s_m[4][16], s_l[4][16];
+    __shared__ int s_last;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+    const int share = a.n_heads / a.c.n_kv, n_kv = a.c.n_kv;
+    // a positive scale: the sign, or all of it where it is zero, goes into q (a masked score stays -inf)
+    const float scale = a.scale != 0.0f ? fabsf(a.scale) * kLog2e : 1.0f;
+    const TileOffsets<D> offsets(n, g);
 
-    for (int block = blockIdx.y; block * 16 < cols.n; block += gridDim.y) {
+    // this workgroup's rounds, and the sequence that the first of them belongs to: every wave sums all sequences' for itself, a lane
+    // those of a run of sequences
+    const int per_lane = (a.n_seq + 63) / 64;
+    int mine = 0, my_start = 0, my_next = 0, my_context = 0;
+    for (int i = 0; i < per_lane; ++i) {
+        const int s = lane * per_lane + i;
+        if (s < a.n_seq) {
+            my_start = a.start[s], my_next = a.start[s + 1], my_context = a.context[s];
+            const SequenceWork w = sequence_work(a, my_start, my_next, my_context, share);
+            mine += w.rounds * w.blocks * n_kv;
+        }
+    }
+    const int upto = wave_scan(mine);
+    const unsigned total = (unsigned)__builtin_amdgcn_readlane(upto, 63);
+    const unsigned n_wg = min(gridDim.x, total);
+    if (blockIdx.x >= n_wg) return;
+    // the first `longer` workgroups have one round more than the others
+    const unsigned fewest = total / n_wg, longer = total - fewest * n_wg;
+    const auto workgroup_of = [&](unsigned round) {
+        const unsigned of_longer = longer * (fewest + 1);
+        return (int)(round < of_longer ? round / (fewest + 1) : longer + (round - of_longer) / fewest);
+    };
+    const int first_round = blockIdx.x * fewest + min(blockIdx.x, longer), end = first_round + (int)fewest + (blockIdx.x < longer);
+    int at = first_round;
+    const int owner = __ffsll((unsigned long long)__ballot(upto > at)) - 1;
+    int seq = owner * per_lane, seq_at = __builtin_amdgcn_readlane(upto - mine, owner);  // the sequence's first round
+    unsigned long long *const counters = reinterpret_cast<unsigned long long *>(partial_of<D>(a, 2 * (int)gridDim.x));
+    const unsigned page_bytes = n_kv * (a.c.page >> 4) * kTile;
+
+    while (at < end) {
+        int start, next, context;
+        if (per_lane == 1) {  // (a lane has them)
+            start = __builtin_amdgcn_readlane(my_start, seq), next = __builtin_amdgcn_readlane(my_next, seq);
+            context = __builtin_amdgcn_readlane(my_context, seq);
+        } else {
+            start = a.start[seq], next = a.start[seq + 1], context = a.context[seq];
+        }
+        const SequenceWork w = sequence_work(a, start, next, context, share);
+        const int of_seq = w.rounds * w.blocks * n_kv;
+        if (at >= seq_at + of_seq) {
+            seq_at += of_seq, ++seq;
+            continue;
+        }
+        const int unit = (int)((unsigned)(at - seq_at) / (unsigned)w.rounds), block = (int)((unsigned)unit / (unsigned)n_kv), head = unit - block * n_kv;
+        const int unit_at = seq_at + unit * w.rounds, begin = at - unit_at, stop = min(w.rounds, end - unit_at);
+        const Columns &cols = w.cols;
+        const SeenTokens seen = seen_tokens(cols, block * 16, min(block * 16 + 16, cols.n));
+        const scalar_ints table = (scalar_ints)(uintptr_t)(a.table + (size_t)seq * a.stride);
         const int col = block * 16 + n, token = col / share, qh = head * share + col % share;
         const bool live = col < cols.n;
         const int pos = live ? cols.first_pos + token : -1;  // a column that is not there sees nothing
-        // the lane's part of q: channels [g D/4, (g + 1) D/4)
-        bf16x8 q[D / 32][QT];
+        WaveSums<D, QT, PT> sums;
+        {
+            const int t1 = min(seen.hi, w.seen.lo + stop * kRound), first = w.seen.lo + begin * kRound + wave * 32;
+            const unsigned char *const cache = a.cache + (size_t)(head * (a.c.page >> 4)) * kTile;
+            TileRegs<D> r[kBuffers][2];
+            int limit[kBuffers][2], page[2];
+            // the pages of a step's tiles; past the last step that of the last token again, of which nothing is loaded
+            auto look_up = [&](int t0) {
+                if (a.c.page == 16) {
 #pragma unroll
-        for (int s = 0; s < D / 32; ++s) {
-            float x[8];
+                    for (int u = 0; u < 2; ++u) page[u] = table[min(t0 + 16 * u, t1 - 1) >> 4];
+                } else {  // one page holds both
+                    page[0] = page[1] = table[min(t0, t1 - 1) >> a.c.log_page];
+                }
+            };
+            auto load = [&](TileRegs<D> (&to)[2], int (&lim)[2], int t0) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = 0.0f;
-            if (live) {
-                const size_t at = ((size_t)(row0 + token) * a.n_heads + qh) * D + g * (D / 4) + 8 * s;
-                if (QT == 1) {
-                    const uint4 w = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.q) + at);
-                    x[0] = bf16_lo(w.x), x[1] = bf16_hi(w.x), x[2] = bf16_lo(w.y), x[3] = bf16_hi(w.y);
-                    x[4] = bf16_lo(w.z), x[5] = bf16_hi(w.z), x[6] = bf16_lo(w.w), x[7] = bf16_hi(w.w);
+                for (int u = 0; u < 2; ++u) {
+                    const int t = t0 + 16 * u;
+                    lim[u] = (unsigned)page[u] < (unsigned)a.c.n_pages ? t1 : 0;
+                    const unsigned char *tile = cache + (size_t)(lim[u] ? (unsigned)page[u] : 0u) * page_bytes + ((t & (a.c.page - 1)) >> 4) * kTile;
+                    load_tile<D, PAST>(to[u], tile, t < lim[u], offsets);
+                }
+            };
+            if (first < t1) look_up(first);
+            else page[0] = page[1] = -1;
+            // the lane's q, and for the first unit the counter of the one that goes on behind this workgroup: all under way together
+            constexpr int kQ = QT == 1 ? D / 32 : D / 16;
+            u32x4 q[kQ];
+            const size_t q_at = ((size_t)(w.row0 + token) * a.n_heads + qh) * D + g * (D / 4);
+            const u32x4 *q_from = QT == 1 ? reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(a.q) + q_at)
+                                          : reinterpret_cast<const u32x4 *>(static_cast<const float *>(a.q) + q_at);
+#pragma unroll
+            for (int i = 0; i < kQ; ++i) {
+                q[i] = u32x4{0, 0, 0, 0};
+                if (live) q[i] = q_from[i];
+            }
+            unsigned long long counted = 0;
+            const bool first_unit = at == first_round && threadIdx.x == 0;
+            if (first_unit) counted = coherent_load(counters + blockIdx.x);
+#pragma unroll
+            for (int i = 0; i < kBuffers - 1; ++i) {
+                load(r[i], limit[i], first + kRound * i);
+                if (first < t1) look_up(first + kRound * (i + 1));
+            }
+            if (first_unit) announce(counters + blockIdx.x, counted, tag);
+            const uint32_t sign = a.scale < 0.0f ? (QT == 1 ? 0x80008000u : 0x80000000u) : 0u, keep = a.scale != 0.0f ? ~0u : 0u;
+#pragma unroll
+            for (int i = 0; i < kQ; ++i) q[i] = (q[i] ^ sign) & keep;
+#pragma unroll
+            for (int s = 0; s < D / 32; ++s) {
+                if constexpr (QT == 1) {
+                    sums.q[s][0] = __builtin_bit_cast(bf16x8, q[s]);
                 } else {
-                    const float4 *f = reinterpret_cast<const float4 *>(static_cast<const float *>(a.q) + at);
-                    const float4 u = f[0], w = f[1];
-                    x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w, x[4] = w.x, x[5] = w.y, x[6] = w.z, x[7] = w.w;
+                    float x[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(q[2 * s + i / 4][i % 4]);
+                    split_terms<QT>(x, sums.q[s]);
                 }
             }
-            split_terms<QT>(x, q[s]);
-        }
-        // tokens that some column of the block sees
-        const int last_col = min(block * 16 + 15, cols.n - 1);
-        const int lo_pos = cols.first_pos + block * 16 / share, hi_pos = cols.first_pos + last_col / share;
-        const int hi = min(hi_pos + 1, cols.length);
-        const int lo = (int)max((long long)lo_pos - cols.window + 1, 0ll) & ~31;
-        // a split's share of them, in whole rounds of the four waves
-        const long long steps = hi > lo ? (hi - lo + 31) / 32 : 0, per = (steps + splits * 4 - 1) / (splits * 4) * 4;
-        const long long begin = blockIdx.x * per, end = min(steps, begin + per);
-
-        f32x4 o[D / 16];
 #pragma unroll
-        for (int j = 0; j < D / 16; ++j) o[j] = f32x4{0, 0, 0, 0};
-        float m = kLowest, l = 0.0f;
-        const float scale = a.scale * kLog2e;
-
-        for (long long step = begin + wave; step < end; step += 4) {
-            const int t0 = lo + (int)step * 32;
-            TileRegs<D> r[2];
-            int there[2];  // tokens of each tile that the cache holds
+            for (int j = 0; j < D / 16; ++j) sums.o[j] = f32x4{0, 0, 0, 0};
+            sums.m = kLowest, sums.l = 0.0f;
+            for (int t0 = first; t0 < t1;) {
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int t = t0 + 16 * u;
-                int page = t < hi ? table[t >> a.c.log_page] : -1;
-                there[u] = page >= 0 && page < a.c.n_pages ? min(hi - t, 16) : 0;
-                if (there[u] == 0) page = 0;
-                load_tile<D>(r[u], a.cache + cache_tile_offset(page, head, t & (a.c.page - 1), a.c.n_kv, a.c.log_page, kTile), n, g);
-            }
-            f32x4 s[2];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                s[u] = f32x4{0, 0, 0, 0};
-#pragma unroll
-                for (int c = 0; c < D / 32; ++c) {
-                    const bf16x8 k = k_operand<D>(r[u], c);
-#pragma unroll
-                    for (int t = QT - 1; t >= 0; --t) s[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[c][t], s[u], 0, 0, 0);
-                }
-            }
-            float p[8];
-            float top = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int u = i / 4, at = 4 * g + i % 4, t = t0 + 16 * u + at;
-                const bool sees = at < there[u] && t <= pos && pos - t < cols.window;
-                p[i] = sees ? s[u][i % 4] * scale : -INFINITY;
-                top = fmaxf(top, p[i]);
-            }
-            if (__any(top > m + kSlack)) {
-                top = fmaxf(top, __shfl_xor(top, 16, kWave));
-                top = fmaxf(top, __shfl_xor(top, 32, kWave));
-                const float next = fmaxf(m, top), factor = exp2f(m - next);
-                m = next;
-                l *= factor;
-#pragma unroll
-                for (int j = 0; j < D / 16; ++j) o[j] *= factor;
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                p[i] = __builtin_amdgcn_exp2f(p[i] - m);
-                l += p[i];
-            }
-            bf16x8 w[PT];
-            split_terms<PT>(p, w);
-            // V: four tokens a tile, D/16 channels; scale bytes of tokens that are not there become 2^-127, so that whatever
-            // stands in their place is finite
-            float sv[8];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int left = there[u] - 4 * g;
-                const uint32_t vs = left >= 4 ? r[u].vs : left <= 0 ? 0u : r[u].vs & ((1u << (8 * left)) - 1);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) sv[4 * u + i] = cache_scale((vs >> (8 * i)) & 255u);
-            }
-            constexpr int W = D / 32;  // bytes of a token: channels 2 b and 2 b + 1 of the lane's D/16 in byte b
-#pragma unroll
-            for (int b = 0; b < W; ++b) {
-                uint32_t c[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int at = (i % 4) * W + b;
-                    c[i] = cache_pair_at(r[i / 4].v[at / 4], sv[i], at % 4);
-                }
-                const bf16x8 even = as_bf16x8(low_halves(c[0], c[1]), low_halves(c[2], c[3]), low_halves(c[4], c[5]), low_halves(c[6], c[7]));
-                const bf16x8 odd = as_bf16x8(high_halves(c[0], c[1]), high_halves(c[2], c[3]), high_halves(c[4], c[5]), high_halves(c[6], c[7]));
-#pragma unroll
-                for (int t = PT - 1; t >= 0; --t) {
-                    o[2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, w[t], o[2 * b], 0, 0, 0);
-                    o[2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, w[t], o[2 * b + 1], 0, 0, 0);
+                for (int i = 0; i < kBuffers; ++i) {
+                    constexpr int kAhead = kBuffers - 1;
+                    load(r[(i + kAhead) % kBuffers], limit[(i + kAhead) % kBuffers], t0 + kRound * kAhead);
+                    look_up(t0 + kRound * kBuffers);
+                    const bool all = t0 + 32 <= min(limit[i][0], limit[i][1]) && t0 + 31 <= seen.first_pos && seen.last_pos - t0 < cols.window;
+                    if (t0 < t1) sums.step(r[i], limit[i], !all, t0, pos, cols.window, g, scale);
+                    t0 += kRound;
                 }
             }
         }
-        // the four waves' sums, joined in their order; a lane has channels [g D/4, (g + 1) D/4) of column n
-        l += __shfl_xor(l, 16, kWave);
-        l += __shfl_xor(l, 32, kWave);
-        __syncthreads();
-        if (g == 0) s_m[wave][n] = m, s_l[wave][n] = l;
-        __syncthreads();
-        const float top = fmaxf(fmaxf(s_m[0][n], s_m[1][n]), fmaxf(s_m[2][n], s_m[3][n]));
-        const float factor = exp2f(m - top);
-        for (int w = 0; w < 4; ++w) {
-            if (wave == w) {
+        sums.l += __shfl_xor(sums.l, 16, kWave);
+        sums.l += __shfl_xor(sums.l, 32, kWave);
+
+        // the four waves' sums, joined in their order: into y, or for the workgroup that joins the unit's pieces
+        const int n_live = min(16, cols.n - block * 16);
+        const bool whole = begin == 0 && stop == w.rounds;
+        // what the four waves left in s_m, s_l and s_o, each relative to its own maximum
+        const auto merge = [&](int pass, bool to_y, float *part) {
+            for (int e = threadIdx.x; e < n_live * (kPass / 2); e += 256) {
+                const int c = e / (kPass / 2), ch = e % (kPass / 2) * 2, gc = block * 16 + c;
+                float most = kLowest, sum = 0.0f, x = 0.0f, y = 0.0f;
 #pragma unroll
-                for (int j = 0; j < D / 16; ++j)
+                for (int i = 0; i < 4; ++i) most = fmaxf(most, s_m[i][c]);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        float *at = &s_o[n][(4 * g + i) * (D / 16) + j];
-                        *at = (w ? *at : 0.0f) + factor * o[j][i];
-                    }
+                for (int i = 0; i < 4; ++i) {
+                    const float f = __builtin_amdgcn_exp2f(s_m[i][c] - most);
+                    sum += f * s_l[i][c], x += f * s_o[i][c][ch], y += f * s_o[i][c][ch + 1];
+                }
+                if (to_y) {
+                    const size_t row = (size_t)(w.row0 + gc / share) * a.n_heads + head * share + gc % share;
+                    const float by = sum > 0.0f ? 1.0f / sum : 0.0f;
+                    store_y2(a, row * D + pass * kPass + ch, x * by, y * by);
+                } else {
+                    store_pair(part + c * (D + 4) + pass * kPass + ch, x, y);
+                    if (ch == 0 && pass == 0) store_pair(part + c * (D + 4) + D, most, sum);
+                }
+            }
+        };
+        if (g == 0) s_m[wave][n] = sums.m, s_l[wave][n] = sums.l;
+        float *const part = partial_of<D>(a, 2 * blockIdx.x + (begin == 0));
+#pragma unroll
+        for (int pass = 0; pass < D / kPass; ++pass) {
+            // a lane has channels [g D/4, (g + 1) D/4) of column n, D/16 at a time; a pass takes those of some of the groups
+            constexpr int kPer = kPass / (D / 4);
+            if (live && g / kPer == pass) {
+                float *to = &s_o[wave][n][(g % kPer) * (D / 4)];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < D / 16; j += 4)
+                        *reinterpret_cast<float4 *>(to + i * (D / 16) + j) = {sums.o[j][i], sums.o[j + 1][i], sums.o[j + 2][i], sums.o[j + 3][i]};
             }
             __syncthreads();
+            merge(pass, whole, part);
+            __syncthreads();
         }
-        for (int e = threadIdx.x; e < 16 * D; e += 256) {
-            const int c = e / D, ch = e % D, gc = block * 16 + c;
-            if (gc >= cols.n) continue;
-            float most = kLowest, sum = 0.0f;
+        if (!whole) {
+            // pieces of the unit: one for each of the workgroups that its first and its last round fall to and those between them
+            const int wg0 = workgroup_of(unit_at), pieces = workgroup_of(unit_at + w.rounds - 1) - wg0 + 1;
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's stores are acknowledged
+            __syncthreads();
+            if (threadIdx.x == 0)
+                s_last = arrive_last(counters + wg0, tag, pieces);
+            __syncthreads();
+            if (s_last) {
+                // wave w takes pieces w, w + 4, .. , a lane's maxima and sums those of two of them
+                const auto piece = [&](int i, int c) { return partial_of<D>(a, i == 0 ? 2 * wg0 + 1 : 2 * (wg0 + i)) + c * (D + 4); };
+#pragma unroll 1
+                for (int pass = 0; pass < D / kPass; ++pass) {
+#pragma unroll 1
+                    for (int c0 = 0; c0 < n_live; c0 += 2) {
+                        float2 ml[2][kWorkgroups / 256], v[2][8];
+                        const auto load_values = [&](int i0) {
 #pragma unroll
-            for (int w = 0; w < 4; ++w) most = fmaxf(most, s_m[w][c]);
+                            for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int w = 0; w < 4; ++w) sum += exp2f(s_m[w][c] - most) * s_l[w][c];
-            const float acc = s_o[c][ch];
-            const size_t row = (size_t)(row0 + gc / share) * a.n_heads + head * share + gc % share;
-            if (splits == 1) {
-                store_y(a, row * D + ch, sum > 0.0f ? acc / sum : 0.0f);
-            } else {
-                float *part = a.ws + (row * splits + blockIdx.x) * (D + 2);
-                part[ch] = acc;
-                if (ch == 0) part[D] = most, part[D + 1] = sum;
+                                for (int k = 0; k < 8; ++k) {
+                                    const int i = i0 + 4 * k;
+                                    v[j][k] = {0, 0};
+                                    if (i < pieces && c0 + j < n_live && 2 * lane < kPass) v[j][k] = load_pair(piece(i, c0 + j) + pass * kPass + 2 * lane);
+                                }
+                        };
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+#pragma unroll
+                            for (int h = 0; h < kWorkgroups / 256; ++h) {
+                                const int i = wave + 4 * lane + 256 * h;
+                                ml[j][h] = {kLowest, 0.0f};
+                                if (i < pieces && c0 + j < n_live) ml[j][h] = load_pair(piece(i, c0 + j) + D);
+                            }
+                        load_values(wave);  // the first of them
+                        float most[2], x[2] = {0, 0}, y[2] = {0, 0};
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            most[j] = kLowest;
+#pragma unroll
+                            for (int h = 0; h < kWorkgroups / 256; ++h) most[j] = fmaxf(most[j], ml[j][h].x);
+#pragma unroll
+                            for (int off = 32; off > 0; off >>= 1) most[j] = fmaxf(most[j], __shfl_xor(most[j], off, kWave));
+                            float sum = 0.0f;
+#pragma unroll
+                            for (int h = 0; h < kWorkgroups / 256; ++h) {
+                                ml[j][h].x = __builtin_amdgcn_exp2f(ml[j][h].x - most[j]);
+                                sum += ml[j][h].x * ml[j][h].y;
+                            }
+                            sum = wave_sum(sum);
+                            if (lane == 0 && c0 + j < n_live) s_m[wave][c0 + j] = most[j], s_l[wave][c0 + j] = sum;
+                        }
+#pragma unroll
+                        for (int h = 0; h < kWorkgroups / 256; ++h)
+#pragma unroll 1
+                            for (int k0 = 0; k0 < 64 && wave + 4 * k0 + 256 * h < pieces; k0 += 8) {
+                                if (k0 + 64 * h > 0) load_values(wave + 4 * k0 + 256 * h);
+#pragma unroll
+                                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                                    for (int k = 0; k < 8; ++k) {
+                                        const float f = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(ml[j][h].x), k0 + k));
+                                        x[j] += f * v[j][k].x, y[j] += f * v[j][k].y;
+                                    }
+                            }
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+                            if (c0 + j < n_live && 2 * lane < kPass) s_o[wave][c0 + j][2 * lane] = x[j], s_o[wave][c0 + j][2 * lane + 1] = y[j];
+                    }
+                    __syncthreads();
+                    merge(pass, true, nullptr);
+                    __syncthreads();
+                }
             }
         }
-        __syncthreads();
+        at = unit_at + stop;
     }
 }
 
-// Joins the splits of each row, in their order.
-template <int D>
-__global__ __launch_bounds__(256) void cache_join_kernel(AttentionArgs a, int splits)
+// Two workgroups to a compute unit hide each other's beginnings and ends, but cost the last of a unit's workgroups more pieces to join,
+// about 0.15 us each: two where there are 128 units, else one, and 32 pieces of a unit at most.  (Microseconds with 512 / 256 workgroups,
+// D 128: 8 sequences x 40 heads x 4096 tokens 26.3 / 30.6, 64 x 8 x 1000 26.8 / 31.0; 2 x 8 x 131072 47.5 / 45.6, 1 x 8 x 131072 33.6 /
+// 29.9, 1 x 32 x 4096 10.8 / 10.1.)  D = 256 has registers for one.
+int attention_workgroups(int n_seq, int n_heads, int n_kv, int d, int max_new, long long max_context)
 {
-    const int per = 256 / D;
-    const long long row = (long long)blockIdx.x * per + threadIdx.x / D;
-    const int ch = threadIdx.x % D;
-    const int token = (int)(row / a.n_heads);
-    if (token >= a.n_tokens || token < a.start[0] || token >= a.start[a.n_seq]) return;
-    const float *part = a.ws + row * splits * (D + 2);
-    float top = kLowest, sum = 0.0f, acc = 0.0f;
-    for (int i = 0; i < splits; ++i) top = fmaxf(top, part[i * (D + 2) + D]);
-    for (int i = 0; i < splits; ++i) {
-        const float f = exp2f(part[i * (D + 2) + D] - top);
-        sum += f * part[i * (D + 2) + D + 1];
-        acc += f * part[i * (D + 2) + ch];
-    }
-    store_y(a, row * D + ch, sum > 0.0f ? acc / sum : 0.0f);
+    const long long blocks = ((long long)max_new * (n_heads / n_kv) + 15) / 16, rounds = (max_context + kRound - 1) / kRound;
+    const long long units = max((long long)n_seq * n_kv * blocks, 1ll);
+    return (int)min(min(units * rounds, units * kPieces), units >= 128 && d < 256 ? (long long)kWorkgroups : kWorkgroups / 2ll);
 }
 
-// Column blocks of 16, and how many ways the tokens of each are split: enough workgroups for every compute unit to hold four,
-// splits of 256 tokens at least.
-struct AttentionGrid {
-    int blocks, splits;
-};
-AttentionGrid attention_grid(int n_seq, int n_heads, int n_kv, int max_new, int max_context)
-{
-    AttentionGrid g;
-    g.blocks = (int)min(((long long)max_new * (n_heads / n_kv) + 15) / 16, 65535ll);
-    const long long units = (long long)n_seq * n_kv * g.blocks;
-    const long long want = (1024 + units - 1) / units, most = ((long long)max_context + 255) / 256;
-    g.splits = (int)max(1ll, min(want, most));
-    return g;
-}
+// From this many bytes of cache on (at the longest length) codes are loaded past the caches: what one layer's attention reads, another
+// layer's and the FFN's weights have displaced by the next step.  Three caches in turn: of 224 MB 47.5 us against 52.7, of 87 MB 23.2
+// against 22.2 (the last-level cache of 256 MB still has some of them).
+constexpr long long kPastBytes = 160ll << 20;
 
 template <int D>
 hipError_t launch_d(const AttentionArgs &a, hipStream_t s)
 {
-    const AttentionGrid g = attention_grid(a.n_seq, a.n_heads, a.c.n_kv, a.max_new, a.max_context);
-    const dim3 grid((unsigned)g.splits, (unsigned)g.blocks, (unsigned)(a.n_seq * a.c.n_kv));
-    if (!a.q_bf16) cache_attention_kernel<D, 3, 3><<<grid, 256, 0, s>>>(a, g.splits);
-    else if (!a.y_bf16) cache_attention_kernel<D, 1, 3><<<grid, 256, 0, s>>>(a, g.splits);
-    else cache_attention_kernel<D, 1, 1><<<grid, 256, 0, s>>>(a, g.splits);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || g.splits == 1) return e;
-    const long long rows = (long long)a.n_tokens * a.n_heads;
-    cache_join_kernel<D><<<(unsigned)((rows + 256 / D - 1) / (256 / D)), 256, 0, s>>>(a, g.splits);
+    const long long seen = a.window > 0 ? min((long long)a.max_context, (long long)a.window + a.max_new + 31) : a.max_context;
+    const unsigned grid = (unsigned)attention_workgroups(a.n_seq, a.n_heads, a.c.n_kv, D, a.max_new, seen);
+    const unsigned long long tag = launch_tag();
+    if (!a.q_bf16) cache_attention_kernel<D, 3, 3, false><<<grid, 256, 0, s>>>(a, tag);
+    else if (!a.y_bf16) cache_attention_kernel<D, 1, 3, false><<<grid, 256, 0, s>>>(a, tag);
+    else if (a.n_seq * seen * a.c.n_kv * (D + D / 16) < kPastBytes) cache_attention_kernel<D, 1, 1, false><<<grid, 256, 0, s>>>(a, tag);
+    else cache_attention_kernel<D, 1, 1, true><<<grid, 256, 0, s>>>(a, tag);
     return hipGetLastError();
 }
 
 }  // namespace
 
-size_t cache_attention_ws(int n_tokens, int n_seq, int n_heads, int n_kv, int d, int max_new, int max_context)
+size_t cache_attention_ws(int n_seq, int n_heads, int n_kv, int d, int max_new, int max_context)
 {
-    const AttentionGrid g = attention_grid(n_seq, n_heads, n_kv, max_new, max_context);
-    return g.splits == 1 ? 0 : (size_t)n_tokens * n_heads * g.splits * (d + 2) * sizeof(float);
+    return (size_t)attention_workgroups(n_seq, n_heads, n_kv, d, max_new, max_context) * (2 * 16 * (d + 4) * sizeof(float) + 8);
 }
 
 hipError_t launch_cache_attention(const AttentionArgs &a, hipStream_t s)

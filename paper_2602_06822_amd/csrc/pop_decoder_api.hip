@@ -3,6 +3,9 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <atomic>
+#include <chrono>
+
 #include "pop_cache.h"  // pop_cache.hip, pop_cache_attention.hip, pop_beam.hip
 
 using namespace pop;
@@ -37,6 +40,15 @@ int cache_shape(int n_kv, int d, int page, int n_pages, CacheShape *c)
 
 }  // namespace
 
+unsigned long long pop::launch_tag()
+{
+    // odd multiples of one number below 2^48, from a place that differs from process to process: what an earlier program left in a
+    // workspace is no tag of this one's
+    static std::atomic<unsigned long long> n{(unsigned long long)std::chrono::steady_clock::now().time_since_epoch().count() * 2};
+    const unsigned long long t = (n.fetch_add(2, std::memory_order_relaxed) | 1) * 0x9e3779b97f4b15ull;
+    return t << 16;
+}
+
 extern "C" {
 
 int pop_cache_bytes(int n_kv, int d, int page, int n_pages, size_t *bytes)
@@ -58,7 +70,7 @@ int pop_cache_plan(const int *cached_len, const int *new_len, int n_seq, int pag
     if (n_seq && (!cached_len || !new_len || !block_table || !context_len)) return POP_EINVAL;
     if (pool_out == pool || (n_seq && (context_len == cached_len || context_len == new_len))) return POP_EINVAL;
     const int l = log_of_page(page);
-    if (l < 0 || (long long)n_pages * page > INT_MAX || (long long)table_stride * page > INT_MAX) return POP_EUNSUPPORTED;
+    if (l < 0 || (long long)n_pages * page > INT_MAX || (long long)table_stride * page > 1 << 30) return POP_EUNSUPPORTED;
     PlanArgs a = {cached_len, new_len, n_seq, l, block_table, table_stride, ring, pool, n_pages, pool_out, max_tokens, context_len,
                   q_start, slots, positions, status};
     POP_HIP(launch_cache_plan(a, as_stream(stream)));
@@ -109,7 +121,7 @@ int pop_cache_attention_workspace(int n_tokens, int n_seq, int n_heads, int n_kv
     if (!bytes) return POP_EINVAL;
     const int rc = attention_sizes(n_tokens, n_seq, n_heads, n_kv, d, max_new, max_context);
     if (rc != POP_OK) return rc;
-    *bytes = n_seq ? cache_attention_ws(n_tokens, n_seq, n_heads, n_kv, d, max_new, max_context) : 0;
+    *bytes = n_seq ? cache_attention_ws(n_seq, n_heads, n_kv, d, max_new, max_context) : 0;
     return POP_OK;
 }
 
@@ -123,12 +135,14 @@ int pop_cache_attention(const void *q, pop_dtype_t dtype, int n_tokens, const vo
     if (rc == POP_OK) rc = attention_sizes(n_tokens, n_seq, n_heads, n_kv, d, max_new, max_context);
     if (rc != POP_OK) return rc;
     if (table_stride < 1 || window < 0) return POP_ESHAPE;
-    if ((long long)table_stride * page > INT_MAX) return POP_EUNSUPPORTED;
+    if ((long long)table_stride * page > 1 << 30) return POP_EUNSUPPORTED;
     if (!is_dtype(dtype) || !is_dtype(ydtype) || !isfinite(scale)) return POP_EINVAL;
+    // rounds of 128 tokens are counted in 32 bits
+    if (((long long)n_tokens * (n_heads / n_kv) / 16 + n_seq) * n_kv * ((long long)table_stride * page / 128 + 1) > INT_MAX) return POP_EUNSUPPORTED;
     if (n_seq == 0 || n_tokens == 0) return POP_OK;
     if (!q || !cache || !block_table || !q_start || !context_len || !y) return POP_EINVAL;
     if (!aligned16(q) || !aligned16(cache) || !aligned16(y) || !aligned16(workspace)) return POP_EINVAL;
-    const size_t need = cache_attention_ws(n_tokens, n_seq, n_heads, n_kv, d, max_new, max_context);
+    const size_t need = cache_attention_ws(n_seq, n_heads, n_kv, d, max_new, max_context);
     if (need && !workspace) return POP_EINVAL;
     if (workspace_bytes < need) return POP_ESHAPE;
     AttentionArgs a = {q, dtype == POP_BF16, n_tokens, static_cast<const unsigned char *>(cache), c, block_table, table_stride, q_start,
@@ -195,7 +209,7 @@ int pop_cache_reorder(const int *block_table, const int *len, const int *parents
     if (rc != POP_OK) return rc;
     if (page < 1 || n_pages < 1) return POP_ESHAPE;
     const int l = log_of_page(page);
-    if (l < 0 || (long long)n_pages * page > INT_MAX || (long long)table_stride * page > INT_MAX) return POP_EUNSUPPORTED;
+    if (l < 0 || (long long)n_pages * page > INT_MAX || (long long)table_stride * page > 1 << 30) return POP_EUNSUPPORTED;
     if (!ring || !pool || !pool_out || !status || pool_out == pool) return POP_EINVAL;
     if (!block_table || !len || !parents || !new_table || !new_len || !copies || new_table == block_table || new_len == len || !workspace)
         return POP_EINVAL;
