@@ -563,6 +563,245 @@ __global__ __launch_bounds__(256, D == 256 || QT == 3 ? 1 : 3) void cache_attent
     }
 }
 
+// ---------------------------------------------------------------- prompts
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int kPromptTile = 64;  // tokens that the workgroup has in LDS at a time: a tile of the cache for each wave
+
+// Where a tile's keys and values stand in LDS, as operands of 32 x 32 x 16 products.  K: 16-byte runs of 8 channels, [D/8][64 tokens].
+// V: for 16 tokens and each half of a wave, 16-byte runs of that half's 8 tokens, [4 x 2][D]; a lane that converts four tokens of channels
+// n D/16 + c writes its halves of the runs at place c 16 + n, so that neighbouring lanes write neighbouring runs.  O^T's rows are in
+// the order of those places.
+// Keys are read in the half of an iteration in front of its barrier, values behind it too: two and three tiles of them, and one
+// barrier a tile.  80 KB for D = 128: two workgroups to a compute unit.
+template <int D>
+struct PromptTiles {
+    uint32_t k[2][D / 8 * kPromptTile * 4], v[3][8 * D * 4];
+};
+
+// One wave's tile of the cache, converted into LDS.
+template <int D>
+__device__ __forceinline__ void convert_tile(uint32_t *to_k, uint32_t *to_v, const TileRegs<D> &r, int j, int left, int n, int g)
+{
+    constexpr int W = D / 32;
+#pragma unroll
+    for (int q = 0; q < W; ++q)
+        *reinterpret_cast<bf16x8 *>(&to_k[((g * W + q) * kPromptTile + 16 * j + n) * 4]) = k_operand<D>(r, q);
+    // scale bytes of tokens that are not there become 2^-127, so that whatever stands in their place is finite
+    left -= 4 * g;
+    const uint32_t vs = left >= 4 ? r.vs : left <= 0 ? 0u : r.vs & ((1u << (8 * left)) - 1);
+    float sv[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sv[i] = cache_scale((vs >> (8 * i)) & 255u);
+#pragma unroll
+    for (int b = 0; b < W; ++b) {
+        uint32_t c[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int at = i * W + b;
+            c[i] = cache_pair_at(r.v[at / 4], sv[i], at % 4);
+        }
+        uint32_t *run = &to_v[((2 * j + (g & 1)) * D + 2 * b * 16 + n) * 4 + (g >> 1) * 2];
+        *reinterpret_cast<u32x2 *>(run) = u32x2{low_halves(c[0], c[1]), low_halves(c[2], c[3])};
+        *reinterpret_cast<u32x2 *>(run + 16 * 4) = u32x2{high_halves(c[0], c[1]), high_halves(c[2], c[3])};
+    }
+}
+
+// Matrix-bound.  Workgroup: 4 waves, 32 columns each, of one kv head and sequence; 64 tokens at a time are converted to bf16 in LDS, a
+// tile of the cache by each wave, while the tokens before them are used.  A step is 32 tokens: S^T = K q^T (32 tokens x 32 columns),
+// softmax, O^T += V^T P^T; S^T of a step is asked for before the softmax of the one before, so that the matrix pipe has work
+// meanwhile.  Three buffers: one barrier a tile.  Columns of the longest reach come first, since workgroups start in order.
+template <int D>
+__global__ __launch_bounds__(256, 2) void cache_prompt_kernel(AttentionArgs a, int blocks)
+{
+    constexpr int kTile = cache_tile_bytes(D), NT = 1, kCols = 32 * NT, kBlock = 4 * kCols;
+    extern __shared__ __align__(16) unsigned char s_raw[];
+    PromptTiles<D> &s_tiles = *reinterpret_cast<PromptTiles<D> *>(s_raw);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+    const int lc = lane & 31, h = lane >> 5;
+    const int share = a.n_heads / a.c.n_kv, n_kv = a.c.n_kv;
+    const int head = blockIdx.x % n_kv, seq = blockIdx.x / n_kv % a.n_seq, rank = blockIdx.x / n_kv / a.n_seq;
+    Columns cols;
+    const int row0 = a.start[seq];
+    if (!sequence_columns(a, row0, a.start[seq + 1], a.context[seq], share, &cols)) return;
+    const float scale = a.scale != 0.0f ? fabsf(a.scale) * kLog2e : 1.0f;
+    const TileOffsets<D> offsets(n, g);
+    const scalar_ints table = (scalar_ints)(uintptr_t)(a.table + (size_t)seq * a.stride);
+    const unsigned page_bytes = n_kv * (a.c.page >> 4) * kTile;
+    const unsigned char *const cache = a.cache + (size_t)(head * (a.c.page >> 4)) * kTile;
+
+    for (int block = (cols.n + kBlock - 1) / kBlock - 1 - rank; block >= 0; block -= blocks) {
+        const SeenTokens seen = seen_tokens(cols, block * kBlock, min((block + 1) * kBlock, cols.n));
+        const int col0 = block * kBlock + wave * kCols;
+        // positions of the wave's columns (of columns that are not there: none)
+        const int wave_first = cols.first_pos + col0 / share;
+        const int wave_last = col0 < cols.n ? cols.first_pos + (min(col0 + kCols, cols.n) - 1) / share : -1;
+        int pos[NT];
+        bf16x8 q[NT][D / 16];
+        const uint32_t sign = a.scale < 0.0f ? 0x80008000u : 0u, keep = a.scale != 0.0f ? ~0u : 0u;
+#pragma unroll
+        for (int c = 0; c < NT; ++c) {
+            const int col = col0 + 32 * c + lc;
+            const bool live = col < cols.n;
+            pos[c] = live ? cols.first_pos + col / share : -1;
+            const u32x4 *from = reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(a.q) +
+                                                                ((size_t)(row0 + col / share) * a.n_heads + head * share + col % share) * D);
+#pragma unroll
+            for (int s = 0; s < D / 16; ++s) {
+                u32x4 x = {0, 0, 0, 0};
+                if (live) x = from[2 * s + h];
+                q[c][s] = __builtin_bit_cast(bf16x8, (x ^ sign) & keep);
+            }
+        }
+        f32x16 o[NT][D / 32], s0[NT], s1[NT];
+        float m[NT], l[NT];
+#pragma unroll
+        for (int c = 0; c < NT; ++c) {
+            m[c] = kLowest, l[c] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[c][j][i] = 0.0f;
+        }
+        // tokens in front of this one are all there: 0 if some page is none
+        int full = seen.hi;
+        for (int i = (seen.lo >> a.c.log_page) + lane; i << a.c.log_page < seen.hi; i += 64)
+            if ((unsigned)table[i] >= (unsigned)a.c.n_pages) full = 0;
+        full = __any(full == 0) ? 0 : full;
+        const int first = seen.lo, n_tiles = (seen.hi - seen.lo + kPromptTile - 1) / kPromptTile;
+
+        TileRegs<D> regs;
+        int limit = 0;
+        auto load = [&](int tile) {  // this wave's 16 tokens
+            const int t = first + tile * kPromptTile + 16 * wave;
+            const int page = t < seen.hi ? table[t >> a.c.log_page] : -1;
+            limit = (unsigned)page < (unsigned)a.c.n_pages ? seen.hi : 0;
+            load_tile<D, false>(regs, cache + (size_t)(limit ? (unsigned)page : 0u) * page_bytes + ((t & (a.c.page - 1)) >> 4) * kTile, t < limit, offsets);
+        };
+        auto convert = [&](int tile) {
+            convert_tile<D>(s_tiles.k[tile % 2], s_tiles.v[tile % 3], regs, wave, limit - (first + tile * kPromptTile + 16 * wave), n, g);
+        };
+        auto scores = [&](f32x16 (&s)[NT], int tile, int half) {
+            const uint32_t *const from = s_tiles.k[tile % 2];
+#pragma unroll
+            for (int c = 0; c < NT; ++c)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[c][i] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) {
+                const bf16x8 x = *reinterpret_cast<const bf16x8 *>(&from[((2 * k + h) * kPromptTile + 32 * half + lc) * 4]);
+#pragma unroll
+                for (int c = 0; c < NT; ++c) s[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[c][k], s[c], 0, 0, 0);
+            }
+        };
+        auto weights = [&](f32x16 (&s)[NT], bf16x8 (&p)[NT][2], int tile, int half) {
+            const int t0 = first + tile * kPromptTile + 32 * half;
+            if (!(t0 + 32 <= full && t0 + 31 <= wave_first && wave_last - t0 < cols.window)) {
+                int lim0 = seen.hi, lim1 = seen.hi;
+                if (full == 0) {
+                    if (t0 < seen.hi && (unsigned)table[t0 >> a.c.log_page] >= (unsigned)a.c.n_pages) lim0 = 0;
+                    if (t0 + 16 < seen.hi && (unsigned)table[(t0 + 16) >> a.c.log_page] >= (unsigned)a.c.n_pages) lim1 = 0;
+                }
+#pragma unroll
+                for (int c = 0; c < NT; ++c)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int t = t0 + 8 * (i / 4) + 4 * h + i % 4;
+                        if (!(t < (i < 8 ? lim0 : lim1) && t <= pos[c] && pos[c] - t < cols.window)) s[c][i] = -INFINITY;
+                    }
+            }
+#pragma unroll
+            for (int c = 0; c < NT; ++c) {
+                float top = s[c][0];
+#pragma unroll
+                for (int i = 1; i < 16; ++i) top = fmaxf(top, s[c][i]);
+                top *= scale;
+                if (__any(top > m[c] + kSlack)) {
+                    top = fmaxf(top, __shfl_xor(top, 32, kWave));
+                    const float next = fmaxf(m[c], top), factor = __builtin_amdgcn_exp2f(m[c] - next);
+                    m[c] = next;
+                    l[c] *= factor;
+#pragma unroll
+                    for (int j = 0; j < D / 32; ++j) o[c][j] *= factor;
+                }
+                float x[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    x[i] = __builtin_amdgcn_exp2f(fmaf(s[c][i], scale, -m[c]));
+                    l[c] += x[i];
+                }
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    p[c][j] = as_bf16x8(pack_bf16(x[8 * j], x[8 * j + 1]), pack_bf16(x[8 * j + 2], x[8 * j + 3]), pack_bf16(x[8 * j + 4], x[8 * j + 5]),
+                                        pack_bf16(x[8 * j + 6], x[8 * j + 7]));
+            }
+        };
+        auto values = [&](bf16x8 (&p)[NT][2], int tile, int half) {
+            const uint32_t *const from = s_tiles.v[tile % 3];
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const bf16x8 x = *reinterpret_cast<const bf16x8 *>(&from[((2 * (2 * half + k) + h) * D + 32 * j + lc) * 4]);
+#pragma unroll
+                    for (int c = 0; c < NT; ++c) o[c][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p[c][k], o[c][j], 0, 0, 0);
+                }
+        };
+
+        bf16x8 p[NT][2];
+        if (n_tiles > 0) {
+            load(0);
+            convert(0);
+            if (n_tiles > 1) load(1);
+            __syncthreads();
+            scores(s0, 0, 0);
+            for (int tile = 0; tile < n_tiles; ++tile) {
+                const int t0 = first + tile * kPromptTile;
+                const bool more = tile + 1 < n_tiles, active = t0 <= wave_last;  // (uniform)
+                if (active) {
+                    scores(s1, tile, 1);
+                    weights(s0, p, tile, 0);
+                    values(p, tile, 0);
+                }
+                if (more) {
+                    convert(tile + 1);
+                    if (tile + 2 < n_tiles) load(tile + 2);
+                }
+                __syncthreads();
+                if (active) {
+                    if (more) scores(s0, tile + 1, 0);
+                    weights(s1, p, tile, 1);
+                    values(p, tile, 1);
+                }
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < NT; ++c) {
+            const int col = col0 + 32 * c + lc;
+            const float sum = l[c] + __shfl_xor(l[c], 32, kWave), by = sum > 0.0f ? 1.0f / sum : 0.0f;
+            if (col >= cols.n) continue;
+            uint16_t *y = static_cast<uint16_t *>(a.y) + ((size_t)(row0 + col / share) * a.n_heads + head * share + col % share) * D;
+            // channels r D/16 .. of the lane's eight r: the places c 16 + r of all c
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    constexpr int C = D / 16;
+                    uint32_t w[C / 2];
+#pragma unroll
+                    for (int e = 0; e < C; e += 2) w[e / 2] = pack_bf16(o[c][e / 2][4 * b + i] * by, o[c][e / 2][8 + 4 * b + i] * by);
+                    uint32_t *to = reinterpret_cast<uint32_t *>(y + (8 * b + 4 * h + i) * C);
+                    if constexpr (C == 4) *reinterpret_cast<u32x2 *>(to) = u32x2{w[0], w[1]};
+                    else
+#pragma unroll
+                        for (int e = 0; e < C / 2; e += 4) *reinterpret_cast<u32x4 *>(to + e) = u32x4{w[e], w[e + 1], w[e + 2], w[e + 3]};
+                }
+        }
+        __syncthreads();  // (the next block's tiles take these buffers)
+    }
+}
+
 // Two workgroups to a compute unit hide each other's beginnings and ends, but cost the last of a unit's workgroups more pieces to join,
 // about 0.15 us each: two where there are 128 units, else one, and 32 pieces of a unit at most.  (Microseconds with 512 / 256 workgroups,
 // D 128: 8 sequences x 40 heads x 4096 tokens 26.3 / 30.6, 64 x 8 x 1000 26.8 / 31.0; 2 x 8 x 131072 47.5 / 45.6, 1 x 8 x 131072 33.6 /
@@ -579,9 +818,25 @@ int attention_workgroups(int n_seq, int n_heads, int n_kv, int d, int max_new, l
 // against 22.2 (the last-level cache of 256 MB still has some of them).
 constexpr long long kPastBytes = 160ll << 20;
 
+constexpr int kPromptColumns = 64;  // columns of a kv head from which the prompt kernel takes over
+
+template <int D>
+hipError_t launch_prompt(const AttentionArgs &a, hipStream_t s)
+{
+    constexpr int kBytes = (int)sizeof(PromptTiles<D>);
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(cache_prompt_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+    if (e != hipSuccess) return e;
+    const long long blocks = ((long long)a.max_new * (a.n_heads / a.c.n_kv) + 127) / 128, units = (long long)a.n_seq * a.c.n_kv;
+    const int n = (int)min(blocks, 0x7fffffffll / units);
+    cache_prompt_kernel<D><<<(unsigned)(n * units), 256, kBytes, s>>>(a, n);
+    return hipGetLastError();
+}
+
 template <int D>
 hipError_t launch_d(const AttentionArgs &a, hipStream_t s)
 {
+    if constexpr (D <= 128)
+        if (a.q_bf16 && a.y_bf16 && (long long)a.max_new * (a.n_heads / a.c.n_kv) >= kPromptColumns) return launch_prompt<D>(a, s);
     const long long seen = a.window > 0 ? min((long long)a.max_context, (long long)a.window + a.max_new + 31) : a.max_context;
     const unsigned grid = (unsigned)attention_workgroups(a.n_seq, a.n_heads, a.c.n_kv, D, a.max_new, seen);
     const unsigned long long tag = launch_tag();
