@@ -8,6 +8,8 @@
 // of the cache's bytes: a lane's K and V codes are loads of D/8 bytes each, a wave's loads are contiguous kilobytes.
 #include <math.h>
 
+#include <type_traits>
+
 #include "pop_cache.h"
 
 namespace pop {
@@ -274,6 +276,18 @@ __device__ __forceinline__ SequenceWork sequence_work(const AttentionArgs &a, in
     return w;
 }
 
+// What workgroups hand to each other goes past the caches (scope of the device), 16 bytes a lane at a time: the descriptor is a wave's.
+__device__ __forceinline__ void store_past(f32x4 *wave_base, int vector, int lane, f32x4 v)
+{
+    const __amdgpu_buffer_rsrc_t d = __builtin_amdgcn_make_buffer_rsrc(wave_base, 0, 0x7fffffff, 0x00020000);
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), d, (vector * 64 + lane) * 16, 0, 16);
+}
+__device__ __forceinline__ f32x4 load_past(const void *wave_base, int bytes)
+{
+    const __amdgpu_buffer_rsrc_t d = __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(wave_base), 0, 0x7fffffff, 0x00020000);
+    return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(d, bytes, 0, 16));
+}
+
 // Partial results: two places for each workgroup, its first piece if the unit began in front of it and its last if the unit goes on
 // behind it; then the counters of the units' pieces, by the workgroup that has the first.
 template <int D>
@@ -299,7 +313,7 @@ __device__ __forceinline__ float2 load_pair(const float *p)
 // else three (24 bits); the weights one if the output is bf16 (rounded to 8 significant bits, as the output is), else three.  K and V
 // are exact in bf16.
 template <int D, int QT, int PT, bool PAST>
-__global__ __launch_bounds__(256, D == 256 || QT == 3 ? 1 : 3) void cache_attention_kernel(AttentionArgs a, unsigned long long tag)
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_kernel(AttentionArgs a, unsigned long long tag)
 {
     constexpr int kTile = cache_tile_bytes(D);
     constexpr int kPass = D > 128 ? 128 : D;  // channels of a pass of the join through LDS
@@ -493,66 +507,56 @@ __global__ __launch_bounds__(256, D == 256 || QT == 3 ? 1 : 3) void cache_attent
                 s_last = arrive_last(counters + wg0, tag, pieces);
             __syncthreads();
             if (s_last) {
-                // wave w takes pieces w, w + 4, .. , a lane's maxima and sums those of two of them
-                const auto piece = [&](int i, int c) { return partial_of<D>(a, i == 0 ? 2 * wg0 + 1 : 2 * (wg0 + i)) + c * (D + 4); };
+                // wave w takes pieces w, w + 4, ..; four channels to a lane, so several columns to a load; G such groups of columns
+                // and P pieces under way together
+                constexpr int kLanes = kPass / 4, kColumns = 64 / kLanes;
+                const auto join = [&](auto groups, auto at_once, int pass) {
+                    constexpr int G = decltype(groups)::value, P = decltype(at_once)::value;
 #pragma unroll 1
-                for (int pass = 0; pass < D / kPass; ++pass) {
+                    for (int c0 = 0; c0 < n_live; c0 += G * kColumns) {
+                        f32x4 acc[G];
+                        float most[G], sum[G];
+#pragma unroll
+                        for (int i = 0; i < G; ++i) acc[i] = f32x4{0, 0, 0, 0}, most[i] = kLowest, sum[i] = 0.0f;
 #pragma unroll 1
-                    for (int c0 = 0; c0 < n_live; c0 += 2) {
-                        float2 ml[2][kWorkgroups / 256], v[2][8];
-                        const auto load_values = [&](int i0) {
+                        for (int i0 = wave; i0 < pieces; i0 += 4 * P) {
+                            f32x4 v[G][P];
+                            float2 ml[G][P];
 #pragma unroll
-                            for (int j = 0; j < 2; ++j)
+                            for (int i = 0; i < G; ++i)
 #pragma unroll
-                                for (int k = 0; k < 8; ++k) {
-                                    const int i = i0 + 4 * k;
-                                    v[j][k] = {0, 0};
-                                    if (i < pieces && c0 + j < n_live && 2 * lane < kPass) v[j][k] = load_pair(piece(i, c0 + j) + pass * kPass + 2 * lane);
+                                for (int k = 0; k < P; ++k) {
+                                    const int c = c0 + i * kColumns + lane / kLanes, from = i0 + 4 * k;
+                                    v[i][k] = f32x4{0, 0, 0, 0}, ml[i][k] = {kLowest, 0.0f};
+                                    if (c < n_live && from < pieces) {
+                                        const float *p = partial_of<D>(a, from == 0 ? 2 * wg0 + 1 : 2 * (wg0 + from)) + c * (D + 4);
+                                        ml[i][k] = load_pair(p + D);
+                                        v[i][k] = load_past(a.ws, (int)(p - a.ws) * 4 + pass * kPass * 4 + lane % kLanes * 16);
+                                    }
                                 }
-                        };
 #pragma unroll
-                        for (int j = 0; j < 2; ++j)
+                            for (int i = 0; i < G; ++i)
 #pragma unroll
-                            for (int h = 0; h < kWorkgroups / 256; ++h) {
-                                const int i = wave + 4 * lane + 256 * h;
-                                ml[j][h] = {kLowest, 0.0f};
-                                if (i < pieces && c0 + j < n_live) ml[j][h] = load_pair(piece(i, c0 + j) + D);
-                            }
-                        load_values(wave);  // the first of them
-                        float most[2], x[2] = {0, 0}, y[2] = {0, 0};
-#pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            most[j] = kLowest;
-#pragma unroll
-                            for (int h = 0; h < kWorkgroups / 256; ++h) most[j] = fmaxf(most[j], ml[j][h].x);
-#pragma unroll
-                            for (int off = 32; off > 0; off >>= 1) most[j] = fmaxf(most[j], __shfl_xor(most[j], off, kWave));
-                            float sum = 0.0f;
-#pragma unroll
-                            for (int h = 0; h < kWorkgroups / 256; ++h) {
-                                ml[j][h].x = __builtin_amdgcn_exp2f(ml[j][h].x - most[j]);
-                                sum += ml[j][h].x * ml[j][h].y;
-                            }
-                            sum = wave_sum(sum);
-                            if (lane == 0 && c0 + j < n_live) s_m[wave][c0 + j] = most[j], s_l[wave][c0 + j] = sum;
+                                for (int k = 0; k < P; ++k) {
+                                    const float next = fmaxf(most[i], ml[i][k].x);
+                                    const float f = __builtin_amdgcn_exp2f(most[i] - next), e = __builtin_amdgcn_exp2f(ml[i][k].x - next);
+                                    most[i] = next, sum[i] = f * sum[i] + e * ml[i][k].y, acc[i] = f * acc[i] + e * v[i][k];
+                                }
                         }
 #pragma unroll
-                        for (int h = 0; h < kWorkgroups / 256; ++h)
-#pragma unroll 1
-                            for (int k0 = 0; k0 < 64 && wave + 4 * k0 + 256 * h < pieces; k0 += 8) {
-                                if (k0 + 64 * h > 0) load_values(wave + 4 * k0 + 256 * h);
-#pragma unroll
-                                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                                    for (int k = 0; k < 8; ++k) {
-                                        const float f = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(ml[j][h].x), k0 + k));
-                                        x[j] += f * v[j][k].x, y[j] += f * v[j][k].y;
-                                    }
+                        for (int i = 0; i < G; ++i) {
+                            const int c = c0 + i * kColumns + lane / kLanes;
+                            if (c < n_live) {
+                                *reinterpret_cast<f32x4 *>(&s_o[wave][c][lane % kLanes * 4]) = acc[i];
+                                if (lane % kLanes == 0) s_m[wave][c] = most[i], s_l[wave][c] = sum[i];
                             }
-#pragma unroll
-                        for (int j = 0; j < 2; ++j)
-                            if (c0 + j < n_live && 2 * lane < kPass) s_o[wave][c0 + j][2 * lane] = x[j], s_o[wave][c0 + j][2 * lane + 1] = y[j];
+                        }
                     }
+                };
+#pragma unroll 1
+                for (int pass = 0; pass < D / kPass; ++pass) {
+                    if (pieces <= 8) join(std::integral_constant<int, 8>(), std::integral_constant<int, 2>(), pass);
+                    else join(std::integral_constant<int, 2>(), std::integral_constant<int, 8>(), pass);
                     __syncthreads();
                     merge(pass, true, nullptr);
                     __syncthreads();
@@ -611,9 +615,11 @@ __device__ __forceinline__ void convert_tile(uint32_t *to_k, uint32_t *to_v, con
 // Matrix-bound.  Workgroup: 4 waves, 32 columns each, of one kv head and sequence; 64 tokens at a time are converted to bf16 in LDS, a
 // tile of the cache by each wave, while the tokens before them are used.  A step is 32 tokens: S^T = K q^T (32 tokens x 32 columns),
 // softmax, O^T += V^T P^T; S^T of a step is asked for before the softmax of the one before, so that the matrix pipe has work
-// meanwhile.  Three buffers: one barrier a tile.  Columns of the longest reach come first, since workgroups start in order.
+// meanwhile.  Columns of the longest reach come first, since workgroups start in order.  Grid: (units, splits): where units are few the
+// tokens of each are split, and the last workgroup to finish a unit joins its pieces, which stand in memory as they stood in the
+// registers of each wave, in the order of the tokens.
 template <int D>
-__global__ __launch_bounds__(256, 2) void cache_prompt_kernel(AttentionArgs a, int blocks)
+__global__ __launch_bounds__(256, 2) void cache_prompt_kernel(AttentionArgs a, int blocks, int splits, unsigned long long tag)
 {
     constexpr int kTile = cache_tile_bytes(D), NT = 1, kCols = 32 * NT, kBlock = 4 * kCols;
     extern __shared__ __align__(16) unsigned char s_raw[];
@@ -631,7 +637,14 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(AttentionArgs a, i
     const unsigned page_bytes = n_kv * (a.c.page >> 4) * kTile;
     const unsigned char *const cache = a.cache + (size_t)(head * (a.c.page >> 4)) * kTile;
 
-    for (int block = (cols.n + kBlock - 1) / kBlock - 1 - rank; block >= 0; block -= blocks) {
+    // a unit's pieces, and behind all of them the units' counters
+    constexpr int kVectors = D / 8 + 1;  // of four floats a lane and piece: O^T, and the maxima and sums
+    f32x4 *const pieces = reinterpret_cast<f32x4 *>(a.ws) + ((size_t)blockIdx.x * splits * 4 + wave) * kVectors * 64;
+    unsigned long long *const counter =
+        reinterpret_cast<unsigned long long *>(reinterpret_cast<f32x4 *>(a.ws) + (size_t)gridDim.x * splits * 4 * kVectors * 64) + blockIdx.x;
+    bool announced = true;  // (units that the caller did not announce have no room for pieces: one workgroup sees to each)
+
+    for (int block = (cols.n + kBlock - 1) / kBlock - 1 - rank; block >= 0; block -= blocks, announced = false) {
         const SeenTokens seen = seen_tokens(cols, block * kBlock, min((block + 1) * kBlock, cols.n));
         const int col0 = block * kBlock + wave * kCols;
         // positions of the wave's columns (of columns that are not there: none)
@@ -669,7 +682,12 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(AttentionArgs a, i
         for (int i = (seen.lo >> a.c.log_page) + lane; i << a.c.log_page < seen.hi; i += 64)
             if ((unsigned)table[i] >= (unsigned)a.c.n_pages) full = 0;
         full = __any(full == 0) ? 0 : full;
-        const int first = seen.lo, n_tiles = (seen.hi - seen.lo + kPromptTile - 1) / kPromptTile;
+        const int first = seen.lo, all_tiles = (seen.hi - seen.lo + kPromptTile - 1) / kPromptTile;
+        const int parts = announced ? max(min(splits, all_tiles), 1) : 1, part = blockIdx.y;
+        if (part >= parts) continue;
+        const int tile0 = (int)((long long)all_tiles * part / parts), n_tiles = (int)((long long)all_tiles * (part + 1) / parts);  // [tile0, n_tiles)
+        unsigned long long counted = 0;
+        if (parts > 1 && threadIdx.x == 0) counted = coherent_load(counter);
 
         TileRegs<D> regs;
         int limit = 0;
@@ -750,13 +768,14 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(AttentionArgs a, i
         };
 
         bf16x8 p[NT][2];
-        if (n_tiles > 0) {
-            load(0);
-            convert(0);
-            if (n_tiles > 1) load(1);
+        if (n_tiles > tile0) {
+            load(tile0);
+            if (parts > 1 && threadIdx.x == 0) announce(counter, counted, tag);
+            convert(tile0);
+            if (n_tiles > tile0 + 1) load(tile0 + 1);
             __syncthreads();
-            scores(s0, 0, 0);
-            for (int tile = 0; tile < n_tiles; ++tile) {
+            scores(s0, tile0, 0);
+            for (int tile = tile0; tile < n_tiles; ++tile) {
                 const int t0 = first + tile * kPromptTile;
                 const bool more = tile + 1 < n_tiles, active = t0 <= wave_last;  // (uniform)
                 if (active) {
@@ -774,6 +793,42 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(AttentionArgs a, i
                     weights(s1, p, tile, 1);
                     values(p, tile, 1);
                 }
+            }
+        }
+        if (parts > 1) {
+            f32x4 *const mine = pieces + (size_t)part * 4 * kVectors * 64;
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+                    store_past(mine, 4 * j + b, lane, f32x4{o[0][j][4 * b], o[0][j][4 * b + 1], o[0][j][4 * b + 2], o[0][j][4 * b + 3]});
+            store_past(mine, kVectors - 1, lane, f32x4{m[0], l[0], 0.0f, 0.0f});
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's stores are acknowledged
+            __syncthreads();
+            int *const s_last = reinterpret_cast<int *>(s_raw);
+            if (threadIdx.x == 0) *s_last = arrive_last(counter, tag, parts);
+            __syncthreads();
+            const bool last = *s_last;
+            __syncthreads();  // (the next unit's tiles take its place)
+            if (!last) continue;
+            m[0] = kLowest, l[0] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[0][j][i] = 0.0f;
+#pragma unroll 1
+            for (int i = 0; i < parts; ++i) {
+                const f32x4 *from = pieces + (size_t)i * 4 * kVectors * 64;
+                f32x4 x[kVectors];
+#pragma unroll
+                for (int v = 0; v < kVectors; ++v) x[v] = load_past(from, (v * 64 + lane) * 16);
+                const float top = fmaxf(m[0], x[kVectors - 1][0]);
+                const float f = __builtin_amdgcn_exp2f(m[0] - top), e = __builtin_amdgcn_exp2f(x[kVectors - 1][0] - top);
+                m[0] = top, l[0] = f * l[0] + e * x[kVectors - 1][1];
+#pragma unroll
+                for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[0][j][r] = f * o[0][j][r] + e * x[4 * j + r / 4][r % 4];
             }
         }
 #pragma unroll
@@ -802,10 +857,10 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(AttentionArgs a, i
     }
 }
 
-// Two workgroups to a compute unit hide each other's beginnings and ends, but cost the last of a unit's workgroups more pieces to join,
-// about 0.15 us each: two where there are 128 units, else one, and 32 pieces of a unit at most.  (Microseconds with 512 / 256 workgroups,
-// D 128: 8 sequences x 40 heads x 4096 tokens 26.3 / 30.6, 64 x 8 x 1000 26.8 / 31.0; 2 x 8 x 131072 47.5 / 45.6, 1 x 8 x 131072 33.6 /
-// 29.9, 1 x 32 x 4096 10.8 / 10.1.)  D = 256 has registers for one.
+// Two workgroups to a compute unit hide each other's beginnings and ends, but cost the last of a unit's workgroups more pieces to join:
+// two where there are 128 units, else one, and 32 pieces of a unit at most.  (Microseconds with 512 / 256 workgroups, D 128: 8 sequences x
+// 40 heads x 4096 tokens 26.3 / 30.6, 64 x 8 x 1000 26.8 / 31.0; 2 x 8 x 131072 47.5 / 45.6, 1 x 8 x 131072 33.6 / 29.9, 1 x 32 x 4096 10.8 /
+// 10.1; 1 x 1 x 131072 80 with 512 pieces, 46 with 256, 29 with 32.)  D = 256 has registers for one.
 int attention_workgroups(int n_seq, int n_heads, int n_kv, int d, int max_new, long long max_context)
 {
     const long long blocks = ((long long)max_new * (n_heads / n_kv) + 15) / 16, rounds = (max_context + kRound - 1) / kRound;
@@ -813,12 +868,33 @@ int attention_workgroups(int n_seq, int n_heads, int n_kv, int d, int max_new, l
     return (int)min(min(units * rounds, units * kPieces), units >= 128 && d < 256 ? (long long)kWorkgroups : kWorkgroups / 2ll);
 }
 
-// From this many bytes of cache on (at the longest length) codes are loaded past the caches: what one layer's attention reads, another
-// layer's and the FFN's weights have displaced by the next step.  Three caches in turn: of 224 MB 47.5 us against 52.7, of 87 MB 23.2
-// against 22.2 (the last-level cache of 256 MB still has some of them).
-constexpr long long kPastBytes = 160ll << 20;
+// From this many bytes of cache on (at the longest length) codes are loaded past the caches: what one layer's attention reads, other
+// layers and the FFN's weights have displaced from the 256 MB last-level cache by the next step.  Microseconds, ordinary / past: caches
+// of 62 MB, three in turn 21.1 / 21.4, eight 24.1 / 21.7; of 83 MB, three 22.2 / 22.8, six 25.2 / 23.0; of 136 MB, three 32.8 / 29.6; of 22 MB,
+// three 14.1 / 14.6, twelve 14.9 / 14.7.
+constexpr long long kPastBytes = 48ll << 20;
 
-constexpr int kPromptColumns = 64;  // columns of a kv head from which the prompt kernel takes over
+// Blocks of 128 columns of the longest chunk, and the parts that the tokens of each are split into.
+struct PromptGrid {
+    int blocks, splits;
+    long long bytes(int n_seq, int n_kv, int d) const
+    {
+        return splits == 1 ? 0 : (long long)blocks * n_seq * n_kv * (splits * 4ll * (d / 8 + 1) * 64 * 16 + 8);
+    }
+};
+PromptGrid prompt_grid(int n_seq, int n_heads, int n_kv, int max_new, long long max_context)
+{
+    PromptGrid g;
+    const long long units = (long long)n_seq * n_kv;
+    g.blocks = (int)min(((long long)max_new * (n_heads / n_kv) + 127) / 128, 0x7fffffffll / units);
+    const long long tiles = (max_context + kPromptTile - 1) / kPromptTile;
+    g.splits = (int)max(1ll, min(min(512 / (units * g.blocks), tiles / 2), 8ll));
+    return g;
+}
+
+// Columns of a kv head from which the prompt kernel takes over.  Microseconds, general / prompt kernel: 32 kv heads x 6000 tokens, one
+// sequence 16 columns 29.9 / 30.3, 32 columns 36.7 / 30.4, 128 columns 56.8 / 34.3; 8 kv heads, 32 columns 28.1 / 28.6; 700 tokens 22.5 / 13.8.
+constexpr int kPromptColumns = 32;
 
 template <int D>
 hipError_t launch_prompt(const AttentionArgs &a, hipStream_t s)
@@ -826,9 +902,8 @@ hipError_t launch_prompt(const AttentionArgs &a, hipStream_t s)
     constexpr int kBytes = (int)sizeof(PromptTiles<D>);
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(cache_prompt_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, kBytes);
     if (e != hipSuccess) return e;
-    const long long blocks = ((long long)a.max_new * (a.n_heads / a.c.n_kv) + 127) / 128, units = (long long)a.n_seq * a.c.n_kv;
-    const int n = (int)min(blocks, 0x7fffffffll / units);
-    cache_prompt_kernel<D><<<(unsigned)(n * units), 256, kBytes, s>>>(a, n);
+    const PromptGrid g = prompt_grid(a.n_seq, a.n_heads, a.c.n_kv, a.max_new, a.max_context);
+    cache_prompt_kernel<D><<<dim3((unsigned)(g.blocks * a.n_seq * a.c.n_kv), (unsigned)g.splits), 256, kBytes, s>>>(a, g.blocks, g.splits, launch_tag());
     return hipGetLastError();
 }
 
@@ -851,7 +926,8 @@ hipError_t launch_d(const AttentionArgs &a, hipStream_t s)
 
 size_t cache_attention_ws(int n_seq, int n_heads, int n_kv, int d, int max_new, int max_context)
 {
-    return (size_t)attention_workgroups(n_seq, n_heads, n_kv, d, max_new, max_context) * (2 * 16 * (d + 4) * sizeof(float) + 8);
+    const long long prompt = d <= 128 ? prompt_grid(n_seq, n_heads, n_kv, max_new, max_context).bytes(n_seq, n_kv, d) : 0;
+    return max((size_t)prompt, (size_t)attention_workgroups(n_seq, n_heads, n_kv, d, max_new, max_context) * (2 * 16 * (d + 4) * sizeof(float) + 8));
 }
 
 hipError_t launch_cache_attention(const AttentionArgs &a, hipStream_t s)

@@ -254,6 +254,8 @@ def _attend(pop, c, q, start, dtype, ydtype, heads, scale, window=0, max_new=Non
             heads, max_new, max_context, scale, window, y, ydtype, ws)
     torch.cuda.synchronize()
     pop.pop_cache_attention(*args, stream=stream)
+    if stream is not None:
+        torch.cuda.synchronize()  # (the caller's own stream does not wait for this one)
     return y
 
 
@@ -324,6 +326,24 @@ def test_long_sequences_are_split(pop, dtype, ydtype, context, new):
     _check(c, y, q, start, dtype, ydtype, 128 ** -0.5)
     again = _attend(pop, c, q, start, dtype, ydtype, 4, 128 ** -0.5)
     assert torch.equal(y, again)
+
+
+@pytest.mark.parametrize("dtype,ydtype", [(BF16, BF16), (BF16, F32)])
+@pytest.mark.parametrize("window", [0, 333])
+@pytest.mark.parametrize("heads,n_kv,d", [(4, 2, 128), (3, 1, 64), (2, 2, 256)])
+def test_long_chunks_of_few_heads(pop, dtype, ydtype, window, heads, n_kv, d):
+    """Chunks whose tokens are split over workgroups, with a hole, and sizes that the caller underestimates in part."""
+    rng = np.random.default_rng(d + window)
+    context, new = [2100, 900, 130], [130, 65, 130]
+    c = Cached(pop, rng, context, n_kv, d, 32)
+    table = c.table.copy()
+    table[0, [5, 40]] = -1
+    there = [np.repeat((t >= 0) & (t < c.n_pages), 32) for t in table]
+    start = np.concatenate([[0], np.cumsum(new)])
+    q = _queries(rng, start[-1], heads, d, dtype)
+    for max_new, max_context in ((130, 2100), (70, 2100), (130, 1000), (64, 600)):
+        y = _attend(pop, c, q, start, dtype, ydtype, heads, 0.08, window, max_new=max_new, max_context=max_context, table=table)
+        _check(c, y, q, start, dtype, ydtype, 0.08, window, there=there)
 
 
 @pytest.mark.parametrize("new", [1, 40])
