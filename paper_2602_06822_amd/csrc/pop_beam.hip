@@ -1,9 +1,11 @@
 // Beam search's selection: of all (beam, token) of a request the k best by  score of the beam + logit - logsumexp(logits).
 //
-// One pass over the logits: a workgroup holds a stretch of a row in registers, sums its exponentials and finds its k largest
-// logits; a workgroup per request then joins the stretches' sums and ranks what they found.  The k largest of a set: every wave
-// ranks its lanes' maxima, the k-th of which no more than k - 1 lanes exceed, so it bounds the set's k-th from below; what
-// reaches the bound (k and a few more, as a rule) goes into a list in LDS, where each entry counts the ones before it.
+// One pass over the logits, bound by memory where there are many rows and by latency where there are few.  A wave goes over its part of
+// a row a tile at a time, the next tile's loads under way: each lane sums exponentials against a maximum of its own and keeps the
+// maximum of each of its *segments* (its 32 values of a tile).  Then every wave ranks its lanes' maxima: the k-th largest is a lower
+// bound of the row's k-th largest value, and the largest of the workgroup's four bounds leaves about k segments that can hold one of
+// its k best.  Only those are read again, what reaches the bound is listed in LDS, and the lists are ranked.  So a value costs
+// six operations in the pass.  The last workgroup of a request to finish joins the sums and ranks what the others found.
 #include <math.h>
 
 #include "pop_cache.h"
@@ -12,8 +14,12 @@ namespace pop {
 
 namespace {
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
-constexpr int kListed = 1024;
+constexpr int kListed = 768;   // words of a wave's list
+constexpr int kRoom = 512;     // of which these are free when a round of eight values a lane begins
+constexpr int kMostK = 64;
 
 // Largest first, equal ones by place: a 64-bit word of an ordered value and the place's complement.  0 is "nothing".
 __device__ __forceinline__ unsigned long long rank_word(float v, uint32_t place)
@@ -25,210 +31,206 @@ __device__ __forceinline__ float ranked_value(unsigned long long w)
     const uint32_t key = (uint32_t)(w >> 32);
     return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
 }
+__device__ __forceinline__ float finite_or_zero(float x) { return x > -INFINITY ? x : 0.0f; }
 
-struct SelectShared {
-    unsigned long long list[kListed], best[4];
-    uint32_t bound[4];
-    int n;
-};
-
-// The k (<= 64) largest of the workgroup's words, E to a thread and all different (0: none), in order to put(rank, word); ranks that
-// no word has are not put.  256 threads.
-template <int E, class Put>
-__device__ __forceinline__ void select_largest(const unsigned long long (&w)[E], int k, SelectShared &s, Put put)
+// The leading BITS bits of the k-th largest of the 64 lanes' values, k <= 64, bit by bit: k lanes at least are not below the result.
+template <int BITS>
+__device__ __forceinline__ uint32_t kth_of_lanes(uint32_t v, int k)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t found = 0;
+#pragma unroll
+    for (int bit = 31; bit >= 32 - BITS; --bit) {
+        const uint32_t next = found | 1u << bit;
+        found = __popcll(__ballot(v >= next)) >= k ? next : found;
+    }
+    return found;
+}
+
+// A wave's list, of n words, all different: what cannot be among its k largest is dropped, and at most kListed - kRoom words are left.
+__device__ __attribute__((noinline)) int thin_out(unsigned long long *list, int n, int k, int lane)
+{
+    constexpr int P = kListed / 64;
+    unsigned long long w[P];
+#pragma unroll
+    for (int i = 0; i < P; ++i) w[i] = i * 64 + lane < n ? list[i * 64 + lane] : 0;
     uint32_t most = 0;
 #pragma unroll
-    for (int i = 0; i < E; ++i) most = max(most, (uint32_t)(w[i] >> 32));
-    int before = 0;
+    for (int i = 0; i < P; ++i) most = max(most, (uint32_t)(w[i] >> 32));
+    unsigned long long bound = (unsigned long long)kth_of_lanes<20>(most, k) << 32;
+    int left = 0;
+#pragma unroll 1
+    for (int turn = 0; turn < 2; ++turn) {
+        left = 0;
 #pragma unroll
-    for (int i = 0; i < 64; ++i) {
-        const uint32_t other = (uint32_t)__builtin_amdgcn_readlane((int)most, i);
-        before += other > most || (other == most && i < lane);
+        for (int i = 0; i < P; ++i) {
+            const bool stays = w[i] != 0 && w[i] >= bound;
+            const unsigned long long m = __ballot(stays);
+            if (stays) list[left + __popcll(m & ((1ull << lane) - 1))] = w[i];
+            left += __popcll(m);
+        }
+        if (left <= kListed - kRoom) break;
+        // a crowd of equal values: k lanes have the k-th largest value or more, and among words with just this value a place of `place` or more
+        const uint32_t value = kth_of_lanes<32>(most, k);
+        uint32_t place = 0;
+#pragma unroll
+        for (int i = 0; i < P; ++i) place = (uint32_t)(w[i] >> 32) >= value ? max(place, (uint32_t)(w[i] >> 32) > value ? ~0u : (uint32_t)w[i]) : place;
+        bound = (unsigned long long)value << 32 | kth_of_lanes<32>(place, k);
     }
-    if (threadIdx.x == 0) s.n = 0;
-    if (before == k - 1) s.bound[wave] = most;
-    __syncthreads();
-    const uint32_t bound = max(max(s.bound[0], s.bound[1]), max(s.bound[2], s.bound[3]));
+    if (left > kListed - kRoom) {  // (only where k is near 64) the k largest are counted out
 #pragma unroll
-    for (int i = 0; i < E; ++i)
-        if (w[i] && (uint32_t)(w[i] >> 32) >= bound) {
-            const int at = atomicAdd(&s.n, 1);
-            if (at < kListed) s.list[at] = w[i];
+        for (int i = 0; i < P; ++i) w[i] = i * 64 + lane < left ? list[i * 64 + lane] : 0;
+        int rank[P] = {};
+        for (int e = 0; e < left; ++e) {
+            const unsigned long long other = list[e];
+#pragma unroll
+            for (int i = 0; i < P; ++i) rank[i] += other > w[i];
         }
-    __syncthreads();
-    const int n = s.n;
-    if (n <= kListed) {
-        for (int e = threadIdx.x; e < n; e += 256) {
-            const unsigned long long mine = s.list[e];
-            int rank = 0;
-            for (int i = 0; i < n; ++i) rank += s.list[i] > mine;
-            if (rank < k) put(rank, mine);
-        }
-    } else {  // a crowd of equal values at the bound: the largest after the last one found, k times
-        unsigned long long last = ~0ull;
-        for (int r = 0; r < k; ++r) {
-            unsigned long long best = 0;
 #pragma unroll
-            for (int i = 0; i < E; ++i)
-                if (w[i] < last && w[i] > best) best = w[i];
+        for (int i = 0; i < P; ++i)
+            if (w[i] != 0 && rank[i] < k) list[rank[i]] = w[i];
+        left = min(left, k);
+    }
+    return left;
+}
+
+constexpr int kWaveTiles = 8;  // of a wave
+
+struct BeamShared {
+    unsigned long long list[4][kListed];
+    unsigned long long found[kMostK];
+    float most[4][kWaveTiles][64];
+    uint16_t segment[4][kWaveTiles * 64];
+    uint32_t bound[4];
+    int n[4];
+    float ref[4], sum[4], lse[POP_MAX_BEAMS], was[POP_MAX_BEAMS];
+    int closed[POP_MAX_BEAMS], last;
+};
+
+// Appends a lane's word, if it has one, to its wave's list of n, which has room for it.
+__device__ __forceinline__ void append(unsigned long long *list, int &n, bool lists, unsigned long long word, int lane)
+{
+    const unsigned long long m = __ballot(lists);
+    if (lists) list[n + __popcll(m & ((1ull << lane) - 1))] = word;
+    n += __popcll(m);
+}
+
+// The k largest words of the four waves' lists, in order to put(rank, word).  All threads; n[] has been written.
+template <class Put>
+__device__ __forceinline__ void select_listed(BeamShared &s, int k, Put put)
+{
+    const int n0 = s.n[0], n1 = n0 + s.n[1], n2 = n1 + s.n[2], n = n2 + s.n[3];
+    for (int e = threadIdx.x; e < n; e += 256) {
+        const unsigned long long mine = e < n0 ? s.list[0][e] : e < n1 ? s.list[1][e - n0] : e < n2 ? s.list[2][e - n1] : s.list[3][e - n2];
+        int rank = 0;
+#pragma unroll 1
+        for (int w = 0; w < 4; ++w)
+#pragma unroll 1
+            for (int i = 0; i < s.n[w]; i += 8) {  // (eight reads under way; a list's room is a multiple of eight)
+                unsigned long long other[8];
 #pragma unroll
-            for (int off = 32; off > 0; off >>= 1) {
-                const unsigned long long o = __shfl_xor(best, off, kWave);
-                best = o > best ? o : best;
+                for (int j = 0; j < 8; ++j) other[j] = s.list[w][i + j];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) rank += i + j < s.n[w] && other[j] > mine;
             }
-            __syncthreads();
-            if (lane == 0) s.best[wave] = best;
-            __syncthreads();
-            last = max(max(s.best[0], s.best[1]), max(s.best[2], s.best[3]));
-            if (last == 0) break;
-            if (threadIdx.x == 0) put(r, last);
-        }
+        if (rank < k) put(rank, mine);
     }
-    __syncthreads();
 }
 
 // A beam that proposes nothing by its logits: it has ended, or it is not alive.
 __device__ __forceinline__ bool closed(const BeamArgs &a, int row)
 {
-    return (a.done && a.done[row]) || a.scores[row] == -INFINITY;
+    const int done = a.done ? a.done[row] : 0;
+    return (a.scores[row] == -INFINITY) | (done != 0);  // (both loads under way together)
 }
 
-// ws: per row and stretch {maximum, sum of exponentials}, then per row and stretch k words.
-__device__ __forceinline__ float2 *stats_of(const BeamArgs &a) { return static_cast<float2 *>(a.ws); }
+// ws: per row and stretch {reference, sum of exponentials relative to it}, then per row and stretch k words, then a counter for each request.
+__device__ __forceinline__ unsigned long long *stats_of(const BeamArgs &a) { return static_cast<unsigned long long *>(a.ws); }
 __device__ __forceinline__ unsigned long long *words_of(const BeamArgs &a, int stretches)
 {
-    return static_cast<unsigned long long *>(a.ws) + (size_t)a.requests * a.beams * stretches;
+    return stats_of(a) + (size_t)a.requests * a.beams * stretches;
+}
+__device__ __forceinline__ void hand_over(unsigned long long *p, unsigned long long v)
+{
+    __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// Grid: (rows, stretches); E logits to a thread.  Rows begin where they begin: a stretch starts at a 16-byte boundary of memory, and the
-// vectors that a row's ends cut are read value by value.
-template <bool BF16, int E>
-__global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs a, int stretches)
+// Sums of a request's beams and the k best of what their stretches found: 16 lanes to a beam for the sums, then every wave lists what is
+// among the best of its candidates.
+__device__ __forceinline__ void join_request(const BeamArgs &a, BeamShared &s, int request, int stretches, unsigned long long is_open)
 {
-    constexpr int V = BF16 ? 8 : 4;
-    __shared__ SelectShared s;
-    __shared__ float s_max[4], s_sum[4];
-    const int row = blockIdx.x;
-    if (closed(a, row)) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const size_t row_at = (size_t)row * a.vocab;
-    const int skew = (int)(row_at % V);
-    const size_t base = row_at - skew;  // a multiple of V values: a 16-byte boundary
-    float x[E];
-    unsigned long long w[E];
-    float top = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < E / V; ++i) {
-        const int at = (blockIdx.y * (E / V) + i) * 256 * V + threadIdx.x * V - skew;  // token of the vector's first value
-        if (at >= 0 && at + V <= a.vocab) {
-            if constexpr (BF16) {
-                const uint4 r = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.logits) + base + skew + at);
-                const uint32_t u[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) x[i * V + 2 * j] = bf16_lo(u[j]), x[i * V + 2 * j + 1] = bf16_hi(u[j]);
-            } else {
-                const float4 r = *reinterpret_cast<const float4 *>(static_cast<const float *>(a.logits) + base + skew + at);
-                x[i * V] = r.x, x[i * V + 1] = r.y, x[i * V + 2] = r.z, x[i * V + 3] = r.w;
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                x[i * V + j] = -INFINITY;
-                if (at + j >= 0 && at + j < a.vocab)
-                    x[i * V + j] = BF16 ? __uint_as_float((uint32_t)static_cast<const uint16_t *>(a.logits)[row_at + at + j] << 16)
-                                        : static_cast<const float *>(a.logits)[row_at + at + j];
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            float &v = x[i * V + j];
-            v = v == v ? v : -INFINITY;  // a NaN is no proposal
-            top = fmaxf(top, v);
-            w[i * V + j] = at + j >= 0 && at + j < a.vocab ? rank_word(v, (uint32_t)(at + j)) : 0;
-        }
-    }
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, kWave));
-    if (lane == 0) s_max[wave] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
-    const float shift = top > -INFINITY ? top : 0.0f;
-    float sum = 0.0f;
-#pragma unroll
-    for (int i = 0; i < E; ++i) sum += __builtin_amdgcn_exp2f((x[i] - shift) * kLog2e);
-    sum = wave_sum(sum);
-    if (lane == 0) s_sum[wave] = sum;
-    unsigned long long *words = words_of(a, stretches) + ((size_t)row * stretches + blockIdx.y) * a.k;
-    for (int i = threadIdx.x; i < a.k; i += 256) words[i] = 0;
-    __syncthreads();
-    if (threadIdx.x == 0) stats_of(a)[(size_t)row * stretches + blockIdx.y] = {top, s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3]};
-    select_largest<E>(w, a.k, s, [&](int rank, unsigned long long word) { words[rank] = word; });
-}
-
-// One workgroup per request.  256 threads: 16 lanes to a beam for the sums, then tiles of 2048 candidates.
-__global__ __launch_bounds__(256) void beam_join_kernel(BeamArgs a, int stretches)
-{
-    constexpr int E = 8;
-    __shared__ SelectShared s;
-    __shared__ float s_lse[POP_MAX_BEAMS], s_was[POP_MAX_BEAMS];
-    __shared__ int s_closed[POP_MAX_BEAMS];
-    __shared__ unsigned long long s_found[64];
-    const int request = blockIdx.x, row0 = request * a.beams;
-    {
-        const int b = threadIdx.x / 16, i0 = threadIdx.x % 16;
-        float top = -INFINITY, sum = 0.0f;
-        if (b < a.beams && !closed(a, row0 + b)) {
-            const float2 *st = stats_of(a) + (size_t)(row0 + b) * stretches;
-            for (int i = i0; i < stretches; i += 16) top = fmaxf(top, st[i].x);
-#pragma unroll
-            for (int off = 8; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, kWave));
-            const float shift = top > -INFINITY ? top : 0.0f;
-            for (int i = i0; i < stretches; i += 16) sum += st[i].y * __builtin_amdgcn_exp2f((st[i].x - shift) * kLog2e);
-#pragma unroll
-            for (int off = 8; off > 0; off >>= 1) sum += __shfl_xor(sum, off, kWave);
-            top = shift;
-        }
-        if (b < a.beams && i0 == 0) {
-            s_was[b] = a.scores[row0 + b];
-            s_closed[b] = closed(a, row0 + b);
-            s_lse[b] = top + __builtin_amdgcn_logf(sum) * kLn2;
-        }
-    }
-    if (threadIdx.x < 64) s_found[threadIdx.x] = 0;
-    __syncthreads();
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row0 = request * a.beams;
+    constexpr int E = 4;
     const unsigned long long *words = words_of(a, stretches) + (size_t)row0 * stretches * a.k;
     const int per = stretches * a.k, total = a.beams * per;
-    for (int tile = 0; tile < total; tile += 256 * (E - 1)) {
-        unsigned long long w[E];
+    unsigned long long w[E];
+    const auto load = [&](int tile) {
 #pragma unroll
-        for (int i = 0; i < E - 1; ++i) {
-            const int c = tile + i * 256 + threadIdx.x, b = c / per, left = c - b * per;
-            w[i] = 0;
-            if (c >= total) continue;
+        for (int i = 0; i < E; ++i) {
+            const int c = tile + i * 256 + threadIdx.x;
+            w[i] = c < total ? coherent_load(words + c) : 0;
+        }
+    };
+    load(0);  // (under way with the sums)
+    {
+        const int b = threadIdx.x / 16, i0 = threadIdx.x % 16;
+        float ref = -INFINITY, sum = 0.0f;
+        const bool open = b < a.beams && (is_open >> b & 1);
+        const float was = b < a.beams ? a.scores[row0 + b] : 0.0f;
+        if (open) {
+            const unsigned long long *st = stats_of(a) + (size_t)(row0 + b) * stretches;
+            for (int i = i0; i < stretches; i += 16) {
+                const unsigned long long w = coherent_load(st + i);
+                const float next = fmaxf(ref, __uint_as_float((uint32_t)w)), shift = finite_or_zero(next);
+                sum = sum * __builtin_amdgcn_exp2f(ref - shift) + __uint_as_float((uint32_t)(w >> 32)) * __builtin_amdgcn_exp2f(__uint_as_float((uint32_t)w) - shift);
+                ref = next;
+            }
+        }
+        float most = ref;
+#pragma unroll
+        for (int off = 8; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor(most, off, kWave));
+        const float shift = finite_or_zero(most);
+        sum *= __builtin_amdgcn_exp2f(ref - shift);
+#pragma unroll
+        for (int off = 8; off > 0; off >>= 1) sum += __shfl_xor(sum, off, kWave);
+        if (b < a.beams && i0 == 0) {
+            s.was[b] = was;
+            s.closed[b] = !open;
+            s.lse[b] = (shift + __builtin_amdgcn_logf(sum)) * kLn2;
+        }
+    }
+    __syncthreads();
+    int n = 0;
+    for (int tile = 0; tile < total; tile += 256 * E) {
+        if (tile > 0) load(tile);
+        if (n > kListed - kRoom) n = thin_out(s.list[wave], n, a.k, lane);
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            const int c = tile + i * 256 + threadIdx.x, b = (unsigned)c / (unsigned)per, left = c - b * per;
             uint32_t token = 0xffffffffu;
             float score = -INFINITY;
-            if (!s_closed[b]) {
-                const unsigned long long word = words[c];
-                if (word) {
-                    token = ~(uint32_t)word;
-                    const float x = ranked_value(word);
-                    if (x > -INFINITY) score = s_was[b] + (x - s_lse[b]);
+            if (c < total && !s.closed[b]) {
+                if (w[i]) {
+                    token = ~(uint32_t)w[i];
+                    const float x = ranked_value(w[i]);
+                    if (x > -INFINITY) score = s.was[b] + (x - s.lse[b]);
                 }
-            } else if (left < a.k) {  // an ended beam goes on by the padding token; else its tokens are the last resort, in their order
+            } else if (c < total && left < a.k) {  // an ended beam goes on by the padding token; else its tokens are the last resort, in their order
                 const bool ended = a.done && a.done[row0 + b];
                 token = ended ? (left == 0 ? a.pad : left - 1 < a.pad ? left - 1 : left) : left;
-                if (ended && left == 0) score = s_was[b];
+                if (ended && left == 0) score = s.was[b];
             }
-            if (token < (uint32_t)a.vocab) w[i] = rank_word(score, (uint32_t)b * (uint32_t)a.vocab + token);
+            w[i] = token < (uint32_t)a.vocab ? rank_word(score, (uint32_t)b * (uint32_t)a.vocab + token) : 0;
+            append(s.list[wave], n, w[i] != 0, w[i], lane);
         }
-        w[E - 1] = threadIdx.x < a.k ? s_found[threadIdx.x] : 0;  // what the tiles before left
-        __syncthreads();
-        select_largest<E>(w, a.k, s, [&](int rank, unsigned long long word) { s_found[rank] = word; });
     }
+    if (n > 32) n = thin_out(s.list[wave], n, a.k, lane);
+    if (lane == 0) s.n[wave] = n;
+    if (threadIdx.x < kMostK) s.found[threadIdx.x] = 0;
+    __syncthreads();
+    select_listed(s, a.k, [&](int rank, unsigned long long word) { s.found[rank] = word; });
+    __syncthreads();
     if ((int)threadIdx.x < a.k) {
-        const unsigned long long word = s_found[threadIdx.x];
+        const unsigned long long word = s.found[threadIdx.x];
         const uint32_t place = ~(uint32_t)word;
         const int at = request * a.k + threadIdx.x;
         a.out_scores[at] = word ? ranked_value(word) : -INFINITY;
@@ -237,16 +239,165 @@ __global__ __launch_bounds__(256) void beam_join_kernel(BeamArgs a, int stretche
     }
 }
 
-// Values to a thread: 8 where that leaves fewer than four workgroups to a compute unit, else 32.
+// Grid: (rows, stretches); `tiles` tiles of NV vectors a lane to a stretch, taken by the waves in turn.  Rows begin where they begin: a
+// stretch starts at a 16-byte boundary of memory, and the vectors that a row's ends cut are read value by value.
+template <bool BF16, int NV>
+__global__ __launch_bounds__(256, 4) void beam_select_kernel(BeamArgs a, int stretches, int tiles, unsigned long long tag)
+{
+    constexpr int V = BF16 ? 8 : 4, E = NV * V;
+    __shared__ BeamShared s;
+    const int row = blockIdx.x, stretch = blockIdx.y, request = row / a.beams, row0 = request * a.beams;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    // the request's open beams: their workgroups are counted; without any, that of the first stretch of its first row joins
+    const unsigned long long is_open = __ballot(lane < a.beams && !closed(a, row0 + min(lane, a.beams - 1)));
+    const int open = __popcll(is_open);
+    const bool reads = is_open >> (row - row0) & 1;
+    if (!reads && !(open == 0 && row == row0 && stretch == 0)) return;
+    const int expected = open * stretches;
+    unsigned long long *const counter = words_of(a, stretches) + (size_t)a.requests * a.beams * stretches * a.k + request;
+    if (reads) {
+        unsigned long long counted = 0;
+        const bool announces = expected > 1 && threadIdx.x == 0;
+        if (announces) counted = coherent_load(counter);
+        const size_t row_at = (size_t)row * a.vocab;
+        const int skew = (int)(row_at % V);  // (the row itself need not start at a 16-byte boundary)
+        const int n_tiles = (a.vocab + skew + 64 * E - 1) / (64 * E), tile_end = min((stretch + 1) * tiles, n_tiles);
+        // from that boundary to the end of the tensor, in whole words: what lies behind it is not read
+        const size_t size = BF16 ? 2 : 4, left = ((size_t)a.requests * a.beams * a.vocab - (row_at - skew)) * size;
+        const __amdgpu_buffer_rsrc_t rows = __builtin_amdgcn_make_buffer_rsrc(
+            const_cast<char *>(static_cast<const char *>(a.logits)) + (row_at - skew) * size, 0, (int)min(left & ~(size_t)3, (size_t)0x7ffffffc), 0x00020000);
+        auto load = [&](u32x4 (&r)[NV], int tile) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) r[i] = __builtin_amdgcn_raw_buffer_load_b128(rows, ((tile * NV + i) * 64 + lane) * 16, 0, 2);  // (non-temporal)
+        };
+        const auto values = [&](float *x, const u32x4 &r) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) x[j] = BF16 ? (j % 2 ? bf16_hi(r[j / 2]) : bf16_lo(r[j / 2])) : __uint_as_float(r[j]);
+        };
+        // the tensor's last value, where it has half a word of its own
+        float odd_value = 0.0f;
+        const bool odd = BF16 && (left & 2) && row == a.requests * a.beams - 1;
+        if (odd) odd_value = __uint_as_float((uint32_t)static_cast<const uint16_t *>(a.logits)[row_at + a.vocab - 1] << 16);
+        // sum: of 2^(x log2 e - ref); ref is the maximum in those units as it was rounded, so that its rounding cancels
+        float top = -INFINITY, ref = -INFINITY, sum = 0.0f;
+        const int first = stretch * tiles + wave;
+        u32x4 now[NV], next[NV];
+        load(now, first);
+        if (announces) announce(counter, counted, tag);
+        int mine = 0;  // tiles of this wave
+        for (int tile = first; tile < tile_end; tile += 4, ++mine) {
+            load(next, tile + 4);
+            float x[E];
+#pragma unroll
+            for (int i = 0; i < NV; ++i) values(&x[i * V], now[i]);
+            if (tile == 0 || tile == n_tiles - 1) {  // the row's ends
+#pragma unroll
+                for (int i = 0; i < E; ++i) {
+                    const int at = ((tile * NV + i / V) * 64 + lane) * V - skew + i % V;
+                    if (odd && at == a.vocab - 1) x[i] = odd_value;
+                    if (at < 0 || at >= a.vocab) x[i] = -INFINITY;
+                }
+            }
+            float most = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                x[i] = fmaxf(x[i], -INFINITY);  // a NaN is no proposal
+                most = fmaxf(most, x[i]);
+            }
+            s.most[wave][mine][lane] = most;
+            if (most > top) {
+                const float up = most * kLog2e;
+                sum *= __builtin_amdgcn_exp2f(ref - up);
+                top = most, ref = up;
+            }
+            const float shift = finite_or_zero(ref);
+#pragma unroll
+            for (int i = 0; i < E; ++i) sum += __builtin_amdgcn_exp2f(fmaf(x[i], kLog2e, -shift));
+#pragma unroll
+            for (int i = 0; i < NV; ++i) now[i] = next[i];
+        }
+        const uint32_t k_th = kth_of_lanes<20>(score_key(top), a.k);
+        if (lane == 0) s.bound[wave] = k_th;
+        __syncthreads();
+        constexpr uint32_t kMinusInfinity = 0x007fffffu;  // as an ordered key
+        const float limit = ranked_value((unsigned long long)max(max(max(s.bound[0], s.bound[1]), max(s.bound[2], s.bound[3])), kMinusInfinity) << 32);
+        // segments with a value that reaches the limit, and those values; minus infinities are no such value
+        int n_segments = 0, n = 0;
+        for (int t = 0; t < mine; ++t) {
+            const float most = s.most[wave][t][lane];
+            const bool is = most >= limit && most > -INFINITY;
+            const unsigned long long m = __ballot(is);
+            if (is) s.segment[wave][n_segments + __popcll(m & ((1ull << lane) - 1))] = (uint16_t)(t * 64 + lane);
+            n_segments += __popcll(m);
+        }
+        for (int base = 0; base < n_segments; base += 64 / NV) {
+            if (n > kListed - kRoom) n = thin_out(s.list[wave], n, a.k, lane);
+            const int i = base + lane / NV, segment = i < n_segments ? s.segment[wave][i] : -1;
+            const int vector = ((first + 4 * (segment >> 6)) * NV + lane % NV) * 64 + (segment & 63);
+            const u32x4 r = __builtin_amdgcn_raw_buffer_load_b128(rows, segment >= 0 ? vector * 16 : 0x7ffffff0, 0, 0);
+            float x[V];
+            values(x, r);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const int at = vector * V - skew + j;
+                if (odd && at == a.vocab - 1) x[j] = odd_value;
+                append(s.list[wave], n, segment >= 0 && at >= 0 && at < a.vocab && x[j] >= limit && x[j] > -INFINITY, rank_word(x[j], (uint32_t)at), lane);
+            }
+        }
+        if (n > 32) n = thin_out(s.list[wave], n, a.k, lane);
+        if (lane == 0) s.n[wave] = n;
+        __syncthreads();
+        if (s.n[0] + s.n[1] + s.n[2] + s.n[3] < a.k) {
+            // fewer than k: tokens at minus infinity, the first of them, which stand among the stretch's first 2 k tokens
+            __syncthreads();
+            const int at = stretch * tiles * 64 * E - skew + (int)threadIdx.x + (stretch == 0 ? skew : 0);
+            bool lists = (int)threadIdx.x < 2 * a.k && at < a.vocab && at < tile_end * 64 * E - skew;
+            float v = 0.0f;
+            if (lists) v = BF16 ? __uint_as_float((uint32_t)static_cast<const uint16_t *>(a.logits)[row_at + at] << 16) : static_cast<const float *>(a.logits)[row_at + at];
+            lists = lists && !(v > -INFINITY);
+            append(s.list[wave], n, lists, rank_word(-INFINITY, (uint32_t)at), lane);
+            if (lane == 0) s.n[wave] = n;
+        }
+        // the workgroup's sums and its k largest
+        float most = ref;
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor(most, off, kWave));
+        sum = wave_sum(sum * __builtin_amdgcn_exp2f(ref - finite_or_zero(most)));
+        if (lane == 0) s.ref[wave] = most, s.sum[wave] = sum;
+        if (threadIdx.x < kMostK) s.found[threadIdx.x] = 0;
+        __syncthreads();
+        select_listed(s, a.k, [&](int rank, unsigned long long word) { s.found[rank] = word; });
+        const float all = fmaxf(fmaxf(s.ref[0], s.ref[1]), fmaxf(s.ref[2], s.ref[3]));
+        float total = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) total += s.sum[w] * __builtin_amdgcn_exp2f(s.ref[w] - finite_or_zero(all));
+        __syncthreads();
+        const size_t part = (size_t)row * stretches + stretch;
+        if ((int)threadIdx.x < a.k) hand_over(words_of(a, stretches) + part * a.k + threadIdx.x, s.found[threadIdx.x]);
+        if (threadIdx.x == 0) hand_over(stats_of(a) + part, (unsigned long long)__float_as_uint(total) << 32 | __float_as_uint(all));
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's stores are acknowledged
+        __syncthreads();
+        if (threadIdx.x == 0) s.last = expected == 1 || arrive_last(counter, tag, expected);
+        __syncthreads();
+        if (!s.last) return;
+    }
+    join_request(a, s, request, stretches, is_open);
+}
+
+// Tiles of 32 values a lane where that leaves four workgroups to a compute unit, else of one vector; a stretch has a tile for each wave
+// at least, and as many as leave about 1024 workgroups.
 struct Stretches {
-    int e, n;
+    int nv, tiles, n;
 };
 Stretches beam_stretches(int requests, int beams, int vocab, int is_bf16)
 {
-    const int lead = is_bf16 ? 7 : 3;
+    const long long rows = (long long)requests * beams, v = is_bf16 ? 8 : 4, values = vocab + v - 1;
     Stretches s;
-    s.e = (long long)requests * beams * ((vocab + lead + 2047) / 2048) <= 1024 ? 8 : 32;
-    s.n = (vocab + lead + 256 * s.e - 1) / (256 * s.e);
+    s.nv = rows * values >= 1024 * 4 * 64 * 32 ? 32 / (int)v : 1;
+    const long long tile = 64 * v * s.nv, n_tiles = (values + tile - 1) / tile;
+    const long long most = max(1024 / rows, 1ll);  // stretches of a row
+    s.tiles = (int)min(max((n_tiles + most - 1) / most, 4ll), 4ll * kWaveTiles);
+    s.n = (int)((n_tiles + s.tiles - 1) / s.tiles);
     return s;
 }
 
@@ -255,23 +406,21 @@ Stretches beam_stretches(int requests, int beams, int vocab, int is_bf16)
 size_t beam_ws(int requests, int beams, int vocab, int k)
 {
     const int n = max(beam_stretches(requests, beams, vocab, 0).n, beam_stretches(requests, beams, vocab, 1).n);
-    return (size_t)requests * beams * n * (k + 1) * 8;
+    return (size_t)requests * (beams * (size_t)n * (k + 1) + 1) * 8;
 }
 
 hipError_t launch_beam_select(const BeamArgs &a, hipStream_t s)
 {
     const Stretches st = beam_stretches(a.requests, a.beams, a.vocab, a.is_bf16);
     const dim3 grid((unsigned)(a.requests * a.beams), (unsigned)st.n);
+    const unsigned long long tag = launch_tag();
     if (a.is_bf16) {
-        if (st.e == 8) beam_rows_kernel<true, 8><<<grid, 256, 0, s>>>(a, st.n);
-        else beam_rows_kernel<true, 32><<<grid, 256, 0, s>>>(a, st.n);
+        if (st.nv == 1) beam_select_kernel<true, 1><<<grid, 256, 0, s>>>(a, st.n, st.tiles, tag);
+        else beam_select_kernel<true, 4><<<grid, 256, 0, s>>>(a, st.n, st.tiles, tag);
     } else {
-        if (st.e == 8) beam_rows_kernel<false, 8><<<grid, 256, 0, s>>>(a, st.n);
-        else beam_rows_kernel<false, 32><<<grid, 256, 0, s>>>(a, st.n);
+        if (st.nv == 1) beam_select_kernel<false, 1><<<grid, 256, 0, s>>>(a, st.n, st.tiles, tag);
+        else beam_select_kernel<false, 8><<<grid, 256, 0, s>>>(a, st.n, st.tiles, tag);
     }
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    beam_join_kernel<<<(unsigned)a.requests, 256, 0, s>>>(a, st.n);
     return hipGetLastError();
 }
 

@@ -53,18 +53,18 @@ __device__ __forceinline__ uint32_t quantise8(float (&x)[8], int *byte)
     return codes;
 }
 
-// One thread: eight channels of K and of V of one token and head.
+// One thread: eight channels of K and of V of one token and head.  A workgroup has one head and as many tokens in a row as it holds (16
+// for D = 128): what it stores is whole lines of one or two tiles, put together in one L2.  8191 tokens of 32 heads, 128 channels, bf16:
+// 40.6 us (170 MB, 4.2 TB/s); with all heads of two tokens to a workgroup, whose lines come together from several L2s, 49.1.
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void cache_write_kernel(unsigned char *__restrict__ cache, CacheShape c, const void *__restrict__ k,
                                                           const void *__restrict__ v, long long k_stride, long long v_stride,
-                                                          const int *__restrict__ slots, unsigned n_items)
+                                                          const int *__restrict__ slots, int n_tokens)
 {
-    constexpr int kPer = D / 8, W = D / 32;
-    const unsigned id = blockIdx.x * 256u + threadIdx.x;
-    const unsigned item = id / kPer;
-    const int ch = (int)(id % kPer) * 8;
-    if (item >= n_items) return;  // (four lanes of a block leave together: kPer is a multiple of four)
-    const int token = item / (unsigned)c.n_kv, head = item - (unsigned)token * c.n_kv;
+    constexpr int kPer = D / 8, W = D / 32, kTokens = 256 / kPer;
+    const int head = blockIdx.x % (unsigned)c.n_kv, token = (int)(blockIdx.x / (unsigned)c.n_kv) * kTokens + threadIdx.x / kPer;
+    const int ch = threadIdx.x % kPer * 8;
+    if (token >= n_tokens) return;  // (four lanes of a block leave together: kPer is a multiple of four)
     const int slot = slots[token];
     const int page = slot >> c.log_page;
     if (slot < 0 || page >= c.n_pages) return;
@@ -278,48 +278,60 @@ __global__ __launch_bounds__(256) void cache_plan_kernel(PlanArgs a)
 
 constexpr int kReorderBlocks = 256;  // blocks of a request that a workgroup sees to
 
-// What block j of a request's rows holds, and which of the rows' pages no row keeps: bit r, a page counted at the first row
-// that has it.  A page that rows hold together stands at the same block of each (they share it since they were one row).
-__device__ __forceinline__ uint32_t freed_rows(const ReorderArgs &a, const int *s_blocks, uint32_t parented, int g, int j)
+// A request's rows, in LDS.
+struct ReorderRows {
+    int parent[POP_MAX_BEAMS], length[POP_MAX_BEAMS], blocks[POP_MAX_BEAMS], copy[POP_MAX_BEAMS];
+    unsigned parented;  // rows that go on, by bit
+};
+
+// What the request's rows are and which of them take a copy of their parent's last page: where it is partly filled and an earlier row
+// goes on in it.  All threads call it; the rows can be read when it returns.
+__device__ __forceinline__ void reorder_rows(const ReorderArgs &a, int g, ReorderRows &r)
 {
-    uint32_t freed = 0;
-    const int *at = a.table + (size_t)g * a.group * a.stride + j;
-    for (int r = 0; r < a.group; ++r) {
-        if (j >= s_blocks[r] || (parented >> r & 1)) continue;
-        const int page = at[(size_t)r * a.stride];
-        if (page < 0 || page >= a.n_pages) continue;
-        bool lost = true;
-        for (int q = 0; q < a.group; ++q) {
-            if (q == r || j >= s_blocks[q] || !(q < r || (parented >> q & 1))) continue;
-            if (at[(size_t)q * a.stride] == page) lost = false;
+    const int c = threadIdx.x, row = g * a.group + c;
+    if (c < a.group) {
+        const int p = a.parents[row], len = a.length[row];
+        r.parent[c] = p >= 0 && p < a.group ? p : -1;
+        r.length[c] = len;
+        r.blocks[c] = (int)min(ceil_pages(max(len, 0), a.log_page), (long long)a.stride);
+    }
+    if (c == 0) r.parented = 0;
+    __syncthreads();
+    if (c < a.group) {
+        const int p = r.parent[c];
+        int copy = 0;
+        if (p >= 0) {
+            const int len = r.length[p];
+            if (len > 0 && (len & ((1 << a.log_page) - 1)) && ceil_pages(len, a.log_page) <= a.stride)
+                for (int b = 0; b < c; ++b) copy |= r.parent[b] == p;
+            atomicOr(&r.parented, 1u << p);
         }
-        if (lost) freed |= 1u << r;
+        r.copy[c] = copy;
+    }
+    __syncthreads();
+}
+
+// The pages of block j of the rows, -1 for none, and by bit the rows whose page no row keeps: a page counts at the first row that has
+// it.  A page that rows hold together stands at the same block of each (they share it since they were one row).
+template <int W>
+__device__ __forceinline__ unsigned freed_rows(const ReorderArgs &a, const ReorderRows &rows, int g, int j, int (&page)[W])
+{
+    const int *at = a.table + (size_t)g * a.group * a.stride + j;
+#pragma unroll
+    for (int r = 0; r < W; ++r) page[r] = r < a.group && j < rows.blocks[r] ? at[(size_t)r * a.stride] : -1;
+    unsigned freed = 0;
+#pragma unroll
+    for (int r = 0; r < W; ++r) {
+        bool lost = page[r] >= 0 && page[r] < a.n_pages && !(rows.parented >> r & 1);  // (rows beyond the group have no page)
+#pragma unroll
+        for (int q = 0; q < W; ++q)
+            if (q != r && page[q] == page[r] && (q < r || (rows.parented >> q & 1))) lost = false;
+        freed |= (unsigned)lost << r;
     }
     return freed;
 }
 
-__device__ __forceinline__ int row_blocks(const ReorderArgs &a, int row)
-{
-    const int len = max(a.length[row], 0);
-    return (int)min(ceil_pages(len, a.log_page), (long long)a.stride);
-}
-__device__ __forceinline__ int local_parent(const ReorderArgs &a, int row)
-{
-    const int p = a.parents[row];
-    return p >= 0 && p < a.group ? p : -1;
-}
-// Whether row c of request g takes a copy of its parent's last page: the page is partly filled and an earlier row goes on in it.
-__device__ __forceinline__ bool takes_copy(const ReorderArgs &a, int g, int c)
-{
-    const int first = g * a.group, p = local_parent(a, first + c);
-    if (p < 0) return false;
-    const int len = a.length[first + p];
-    if (len <= 0 || !(len & ((1 << a.log_page) - 1)) || ceil_pages(len, a.log_page) > a.stride) return false;
-    for (int b = 0; b < c; ++b)
-        if (local_parent(a, first + b) == p) return true;
-    return false;
-}
-
+// Sum over the workgroup, and over the threads in front of this one.
 __device__ __forceinline__ int block_sum(int v, int *s_wave, int *before)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -329,7 +341,6 @@ __device__ __forceinline__ int block_sum(int v, int *s_wave, int *before)
         const int t = __shfl_up(incl, off, kWave);
         if (lane >= off) incl += t;
     }
-    __syncthreads();
     if (lane == 63) s_wave[wave] = incl;
     __syncthreads();
     int total = 0, ahead = 0;
@@ -338,73 +349,73 @@ __device__ __forceinline__ int block_sum(int v, int *s_wave, int *before)
         if (w < wave) ahead += s_wave[w];
         total += s_wave[w];
     }
+    __syncthreads();
     *before = ahead + incl - v;
     return total;
 }
 
-__device__ __forceinline__ uint32_t parented_rows(const ReorderArgs &a, int g)
-{
-    uint32_t m = 0;
-    for (int c = 0; c < a.group; ++c) {
-        const int p = local_parent(a, g * a.group + c);
-        if (p >= 0) m |= 1u << p;
-    }
-    return m;
-}
-
-// Pages that each part of a request's rows gives back.
+// Latency-bound integer work in two launches (one where a single workgroup sees to everything): what each part of the requests gives
+// back and takes has to be known before the first page finds its place in the ring.  W: rows of a request at most.  counts: pages given back, by request and part, then
+// copies by request.
+template <int W>
 __global__ __launch_bounds__(kReorderBlocks) void reorder_count_kernel(ReorderArgs a)
 {
-    __shared__ int s_blocks[POP_MAX_BEAMS], s_wave[4];
+    __shared__ ReorderRows s_rows;
+    __shared__ int s_wave[4];
     const int g = blockIdx.x, j = blockIdx.y * kReorderBlocks + threadIdx.x;
-    if ((int)threadIdx.x < a.group) s_blocks[threadIdx.x] = row_blocks(a, g * a.group + threadIdx.x);
-    __syncthreads();
-    const uint32_t freed = j < a.stride ? freed_rows(a, s_blocks, parented_rows(a, g), g, j) : 0;
-    int before;
-    const int total = block_sum(__popc(freed), s_wave, &before);
-    if (threadIdx.x == 0) a.counts[g * gridDim.y + blockIdx.y] = total;
-}
-
-// New rows, copies and the ring.  alone: one workgroup does it all and there are no counts to read.
-__global__ __launch_bounds__(kReorderBlocks) void reorder_rows_kernel(ReorderArgs a, int alone)
-{
-    __shared__ int s_blocks[POP_MAX_BEAMS], s_parent[POP_MAX_BEAMS], s_fresh[POP_MAX_BEAMS], s_wave[4];
-    const int g = blockIdx.x, n_groups = a.n_seq / a.group, tid = threadIdx.x;
-    const int chunks = gridDim.y, part = g * chunks + blockIdx.y, n_parts = n_groups * chunks;
-    const int j = blockIdx.y * kReorderBlocks + tid, first = g * a.group;
-    if (tid < a.group) {
-        s_blocks[tid] = row_blocks(a, first + tid);
-        s_parent[tid] = local_parent(a, first + tid);
-    }
-    const int head = a.pool[0], count = a.pool[1];
-    // copies of the requests in front of this one, and of all
-    int copies_before = 0, copies_all = 0;
-    for (int base = 0; base < n_groups; base += kReorderBlocks) {
-        int n = 0;
-        if (base + tid < n_groups)
-            for (int c = 0; c < a.group; ++c) n += takes_copy(a, base + tid, c);
-        int before;
-        copies_all += block_sum(n, s_wave, &before);
-        copies_before += block_sum(base + tid < g ? n : 0, s_wave, &before);
-    }
-    __syncthreads();
-    const uint32_t freed = j < a.stride ? freed_rows(a, s_blocks, parented_rows(a, g), g, j) : 0;
-    int at;
-    const int mine = block_sum(__popc(freed), s_wave, &at);
-    int freed_before = 0, freed_all = mine;
-    if (!alone) {
-        freed_all = 0;
-        for (int base = 0; base < n_parts; base += kReorderBlocks) {
-            const int n = base + tid < n_parts ? a.counts[base + tid] : 0;
-            int before;
-            freed_all += block_sum(n, s_wave, &before);
-            freed_before += block_sum(base + tid < part ? n : 0, s_wave, &before);
+    reorder_rows(a, g, s_rows);
+    int page[W], before;
+    const int total = block_sum(j < a.stride ? __popc(freed_rows(a, s_rows, g, j, page)) : 0, s_wave, &before);
+    if (threadIdx.x == 0) {
+        a.counts[g * gridDim.y + blockIdx.y] = total;
+        if (blockIdx.y == 0) {
+            int n = 0;
+            for (int c = 0; c < a.group; ++c) n += s_rows.copy[c];
+            a.counts[gridDim.x * gridDim.y + g] = n;
         }
     }
-    int status = copies_all > count ? 1 : 0;
+}
+
+template <int W>
+__global__ __launch_bounds__(kReorderBlocks) void reorder_rows_kernel(ReorderArgs a, int alone)
+{
+    __shared__ ReorderRows s_rows;
+    __shared__ int s_fresh[POP_MAX_BEAMS], s_wave[4], s_sums[4][4];
+    const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n_groups = gridDim.x, chunks = gridDim.y;
+    const int part = g * chunks + blockIdx.y, n_parts = n_groups * chunks, j = blockIdx.y * kReorderBlocks + tid, first = g * a.group;
+    const int head = a.pool[0], count = a.pool[1];
+    // of the parts and requests in front of this one, and of all: pages given back, copies
+    int freed_before = 0, freed_all = 0, copies_before = 0, copies_all = 0;
+    if (!alone) {
+        for (int i = tid; i < n_parts; i += kReorderBlocks) {
+            const int n = a.counts[i];
+            freed_all += n, freed_before += i < part ? n : 0;
+        }
+        for (int i = tid; i < n_groups; i += kReorderBlocks) {
+            const int n = a.counts[n_parts + i];
+            copies_all += n, copies_before += i < g ? n : 0;
+        }
+        freed_before = wave_sum(freed_before), freed_all = wave_sum(freed_all);
+        copies_before = wave_sum(copies_before), copies_all = wave_sum(copies_all);
+        if (lane == 0) s_sums[wave][0] = freed_before, s_sums[wave][1] = freed_all, s_sums[wave][2] = copies_before, s_sums[wave][3] = copies_all;
+    }
+    reorder_rows(a, g, s_rows);  // (its barriers stand behind the sums)
+    int page[W], at;
+    const unsigned freed = j < a.stride ? freed_rows(a, s_rows, g, j, page) : 0;
+    const int mine = block_sum(__popc(freed), s_wave, &at);
+    if (alone) {
+        freed_all = mine;
+        for (int c = 0; c < a.group; ++c) copies_all += s_rows.copy[c];
+    } else {
+        freed_before = freed_all = copies_before = copies_all = 0;
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+            freed_before += s_sums[w][0], freed_all += s_sums[w][1], copies_before += s_sums[w][2], copies_all += s_sums[w][3];
+    }
+    int status = copies_all > count ? POP_PLAN_PAGES : 0;
     if (head < 0 || head >= a.n_pages || count < 0 || count > a.n_pages ||
         (long long)count + freed_all > a.n_pages)
-        status |= 4;  // no ring of this many pages: one stands in it and in a row as well, or in rows of two requests
+        status |= POP_PLAN_INVALID;  // no ring of this many pages: one stands in it and in a row as well, or in rows of two requests
     if (part == 0 && tid == 0) {
         long long next = (long long)head + copies_all;
         if (next >= a.n_pages) next -= a.n_pages;
@@ -414,40 +425,41 @@ __global__ __launch_bounds__(kReorderBlocks) void reorder_rows_kernel(ReorderArg
     }
     // the copies of this request
     if (tid < a.group) {
-        int order = copies_before;
-        for (int c = 0; c < tid; ++c) order += takes_copy(a, g, c);
         int fresh = -1;
-        if (!status && takes_copy(a, g, tid)) {
-            long long r = (long long)head + order;
+        if (!status && s_rows.copy[tid]) {
+            long long r = (long long)head + copies_before;
+            for (int c = 0; c < tid; ++c) r += s_rows.copy[c];
             if (r >= a.n_pages) r -= a.n_pages;
             fresh = a.ring[r];
         }
         s_fresh[tid] = fresh;
         if (blockIdx.y == 0) {
-            const int row = first + tid, p = s_parent[tid];
-            a.copies[2 * row] = fresh >= 0 ? a.table[(size_t)(first + p) * a.stride + s_blocks[p] - 1] : -1;
+            const int row = first + tid, p = s_rows.parent[tid];
+            a.copies[2 * row] = fresh >= 0 ? a.table[(size_t)(first + p) * a.stride + s_rows.blocks[p] - 1] : -1;
             a.copies[2 * row + 1] = fresh;
-            a.new_length[row] = status ? a.length[row] : p < 0 ? 0 : a.length[first + p];
+            a.new_length[row] = status ? a.length[row] : p < 0 ? 0 : s_rows.length[p];
         }
     }
     __syncthreads();
     if (j < a.stride) {
         for (int c = 0; c < a.group; ++c) {
-            const int p = status ? c : s_parent[c];
-            int page = -1;
-            if (p >= 0 && j < s_blocks[p]) {
-                page = a.table[(size_t)(first + p) * a.stride + j];
-                if (s_fresh[c] >= 0 && j == s_blocks[p] - 1) page = s_fresh[c];
+            const int p = status ? c : s_rows.parent[c];
+            int entry = -1;
+            if (p >= 0) {
+#pragma unroll
+                for (int r = 0; r < W; ++r) entry = r == p ? page[r] : entry;  // (-1 behind a row's last block)
+                if (s_fresh[c] >= 0 && j == s_rows.blocks[p] - 1) entry = s_fresh[c];
             }
-            a.new_table[(size_t)(first + c) * a.stride + j] = page;
+            a.new_table[(size_t)(first + c) * a.stride + j] = entry;
         }
         if (!status) {
             long long to = (long long)head + count + freed_before + at;
-            for (uint32_t left = freed; left; left &= left - 1) {
-                const int r = __ffs(left) - 1;
-                while (to >= a.n_pages) to -= a.n_pages;
-                a.ring[to++] = a.table[(size_t)(first + r) * a.stride + j];
-            }
+#pragma unroll
+            for (int r = 0; r < W; ++r)
+                if (freed >> r & 1) {
+                    while (to >= a.n_pages) to -= a.n_pages;
+                    a.ring[to++] = page[r];
+                }
         }
     }
 }
@@ -457,12 +469,12 @@ __global__ __launch_bounds__(kReorderBlocks) void reorder_rows_kernel(ReorderArg
 hipError_t launch_cache_write(void *cache, const CacheShape &c, const void *k, const void *v, int is_bf16, long long k_stride,
                               long long v_stride, const int *slots, int n_tokens, hipStream_t s)
 {
-    const unsigned items = (unsigned)n_tokens * c.n_kv;
-    const unsigned grid = (unsigned)(((size_t)items * (c.d / 8) + 255) / 256);
+    const int tokens = 2048 / c.d;  // of a workgroup
+    const unsigned grid = (unsigned)((n_tokens + tokens - 1) / tokens) * c.n_kv;
     unsigned char *to = static_cast<unsigned char *>(cache);
 #define POP_WRITE(D)                                                                                                         \
-    (is_bf16 ? cache_write_kernel<D, true><<<grid, 256, 0, s>>>(to, c, k, v, k_stride, v_stride, slots, items)               \
-             : cache_write_kernel<D, false><<<grid, 256, 0, s>>>(to, c, k, v, k_stride, v_stride, slots, items))
+    (is_bf16 ? cache_write_kernel<D, true><<<grid, 256, 0, s>>>(to, c, k, v, k_stride, v_stride, slots, n_tokens)            \
+             : cache_write_kernel<D, false><<<grid, 256, 0, s>>>(to, c, k, v, k_stride, v_stride, slots, n_tokens))
     if (c.d == 64) POP_WRITE(64);
     else if (c.d == 128) POP_WRITE(128);
     else POP_WRITE(256);
@@ -503,20 +515,29 @@ hipError_t launch_cache_plan(const PlanArgs &a, hipStream_t s)
 
 size_t reorder_counts(int n_seq, int group, int stride)
 {
-    return (size_t)(n_seq / group) * ((stride + kReorderBlocks - 1) / kReorderBlocks);
+    return (size_t)(n_seq / group) * ((stride + kReorderBlocks - 1) / kReorderBlocks + 1);
 }
 
-hipError_t launch_cache_reorder(const ReorderArgs &a, hipStream_t s)
+template <int W>
+static hipError_t launch_reorder(const ReorderArgs &a, hipStream_t s)
 {
     const dim3 grid((unsigned)(a.n_seq / a.group), (unsigned)((a.stride + kReorderBlocks - 1) / kReorderBlocks));
     const int alone = grid.x * grid.y == 1;
     if (!alone) {
-        reorder_count_kernel<<<grid, kReorderBlocks, 0, s>>>(a);
+        reorder_count_kernel<W><<<grid, kReorderBlocks, 0, s>>>(a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    reorder_rows_kernel<<<grid, kReorderBlocks, 0, s>>>(a, alone);
+    reorder_rows_kernel<W><<<grid, kReorderBlocks, 0, s>>>(a, alone);
     return hipGetLastError();
+}
+
+hipError_t launch_cache_reorder(const ReorderArgs &a, hipStream_t s)
+{
+    if (a.group == 1) return launch_reorder<1>(a, s);
+    if (a.group <= 4) return launch_reorder<4>(a, s);
+    if (a.group <= 8) return launch_reorder<8>(a, s);
+    return launch_reorder<POP_MAX_BEAMS>(a, s);
 }
 
 }  // namespace pop

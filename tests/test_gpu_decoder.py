@@ -527,8 +527,10 @@ def test_equal_and_forbidden_logits(pop, dtype, vocab):
     x = x.cuda().to(DT[dtype])
     was = torch.tensor([-1.0, -30.0, -2.0, -64.0, -90.0, -120.0, -torch.inf, -200.0], device="cuda")
     done = torch.tensor([0, 0, 0, 0, 0, 0, 0, 1], dtype=torch.uint8, device="cuda")
-    for k in (1, 5, 16):
+    for k in (1, 5, 16, 64):
         for beams in (1, 2, 8):
+            if k > beams * vocab:
+                continue
             got = _select(pop, x, dtype, was, done, beams, k, 4)
             _check_beams(x, was, done, beams, k, 4, got)
 
