@@ -2,7 +2,7 @@
 //
 // One pass over the logits, bound by memory where there are many rows and by latency where there are few.  A wave goes over its part of
 // a row a tile at a time, the next tile's loads under way: each lane sums exponentials against a maximum of its own and keeps the
-// maximum of each of its *segments* (its 32 values of a tile).  Then every wave ranks its lanes' maxima: the k-th largest is a lower
+// maximum of each of its *segments* (its 16 values of a tile).  Then every wave ranks its lanes' maxima: the k-th largest is a lower
 // bound of the row's k-th largest value, and the largest of the workgroup's four bounds leaves about k segments that can hold one of
 // its k best.  Only those are read again, what reaches the bound is listed in LDS, and the lists are ranked.  So a value costs
 // six operations in the pass.  The last workgroup of a request to finish joins the sums and ranks what the others found.
@@ -93,7 +93,7 @@ __device__ __attribute__((noinline)) int thin_out(unsigned long long *list, int 
     return left;
 }
 
-constexpr int kWaveTiles = 8;  // of a wave
+constexpr int kWaveTiles = 17;  // of a wave
 
 struct BeamShared {
     unsigned long long list[4][kListed];
@@ -242,7 +242,7 @@ __device__ __forceinline__ void join_request(const BeamArgs &a, BeamShared &s, i
 // Grid: (rows, stretches); `tiles` tiles of NV vectors a lane to a stretch, taken by the waves in turn.  Rows begin where they begin: a
 // stretch starts at a 16-byte boundary of memory, and the vectors that a row's ends cut are read value by value.
 template <bool BF16, int NV>
-__global__ __launch_bounds__(256, 4) void beam_select_kernel(BeamArgs a, int stretches, int tiles, unsigned long long tag)
+__global__ __launch_bounds__(256, 3) void beam_select_kernel(BeamArgs a, int stretches, int tiles, unsigned long long tag)
 {
     constexpr int V = BF16 ? 8 : 4, E = NV * V;
     __shared__ BeamShared s;
@@ -268,7 +268,7 @@ __global__ __launch_bounds__(256, 4) void beam_select_kernel(BeamArgs a, int str
             const_cast<char *>(static_cast<const char *>(a.logits)) + (row_at - skew) * size, 0, (int)min(left & ~(size_t)3, (size_t)0x7ffffffc), 0x00020000);
         auto load = [&](u32x4 (&r)[NV], int tile) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i) r[i] = __builtin_amdgcn_raw_buffer_load_b128(rows, ((tile * NV + i) * 64 + lane) * 16, 0, 2);  // (non-temporal)
+            for (int i = 0; i < NV; ++i) r[i] = __builtin_amdgcn_raw_buffer_load_b128(rows, ((tile * NV + i) * 64 + lane) * 16, 0, 0);
         };
         const auto values = [&](float *x, const u32x4 &r) {
 #pragma unroll
@@ -384,20 +384,22 @@ __global__ __launch_bounds__(256, 4) void beam_select_kernel(BeamArgs a, int str
     join_request(a, s, request, stretches, is_open);
 }
 
-// Tiles of 32 values a lane where that leaves four workgroups to a compute unit, else of one vector; a stretch has a tile for each wave
-// at least, and as many as leave about 1024 workgroups.
+// Tiles of 16 values a lane (32: 256 rows of 131071 float32 37.2 us instead of 33.6).  A stretch has a tile for each wave at least, a
+// sixteenth of the row (a request of 8 rows of 131071: 33 stretches a row 24.4 us, 17 of them 16.8), and what leaves about 512
+// workgroups: their ends, where the best values are found, cost a compute unit about 5 us each (256 rows: 1024 workgroups 44.9 us where
+// 512 take 41.2, 2048 take 65.9).
+constexpr int kLaneValues = 16;
 struct Stretches {
-    int nv, tiles, n;
+    int tiles, n;
 };
 Stretches beam_stretches(int requests, int beams, int vocab, int is_bf16)
 {
-    const long long rows = (long long)requests * beams, v = is_bf16 ? 8 : 4, values = vocab + v - 1;
+    const long long rows = (long long)requests * beams, tile = 64 * kLaneValues, n_tiles = (vocab + (is_bf16 ? 7 : 3) + tile - 1) / tile;
+    const long long of_row = min(max(512 / rows, 1ll), 16ll);
+    const long long tiles = min(max((n_tiles + of_row - 1) / of_row, 4ll), 4ll * kWaveTiles);
     Stretches s;
-    s.nv = rows * values >= 1024 * 4 * 64 * 32 ? 32 / (int)v : 1;
-    const long long tile = 64 * v * s.nv, n_tiles = (values + tile - 1) / tile;
-    const long long most = max(1024 / rows, 1ll);  // stretches of a row
-    s.tiles = (int)min(max((n_tiles + most - 1) / most, 4ll), 4ll * kWaveTiles);
-    s.n = (int)((n_tiles + s.tiles - 1) / s.tiles);
+    s.n = (int)((n_tiles + tiles - 1) / tiles);
+    s.tiles = (int)((n_tiles + s.n - 1) / s.n);  // (all alike)
     return s;
 }
 
@@ -414,13 +416,8 @@ hipError_t launch_beam_select(const BeamArgs &a, hipStream_t s)
     const Stretches st = beam_stretches(a.requests, a.beams, a.vocab, a.is_bf16);
     const dim3 grid((unsigned)(a.requests * a.beams), (unsigned)st.n);
     const unsigned long long tag = launch_tag();
-    if (a.is_bf16) {
-        if (st.nv == 1) beam_select_kernel<true, 1><<<grid, 256, 0, s>>>(a, st.n, st.tiles, tag);
-        else beam_select_kernel<true, 4><<<grid, 256, 0, s>>>(a, st.n, st.tiles, tag);
-    } else {
-        if (st.nv == 1) beam_select_kernel<false, 1><<<grid, 256, 0, s>>>(a, st.n, st.tiles, tag);
-        else beam_select_kernel<false, 8><<<grid, 256, 0, s>>>(a, st.n, st.tiles, tag);
-    }
+    if (a.is_bf16) beam_select_kernel<true, kLaneValues / 8><<<grid, 256, 0, s>>>(a, st.n, st.tiles, tag);
+    else beam_select_kernel<false, kLaneValues / 4><<<grid, 256, 0, s>>>(a, st.n, st.tiles, tag);
     return hipGetLastError();
 }
 
