@@ -612,14 +612,75 @@ __device__ __forceinline__ void convert_tile(uint32_t *to_k, uint32_t *to_v, con
     }
 }
 
+// The q-th longest of all sequences' blocks of 128 columns, by the position that its last column reaches (equal ones by sequence, then the
+// later block first): found by bisection over positions, a lane for a run of sequences.  False if there are not that many.
+__device__ __forceinline__ bool nth_longest_block(const AttentionArgs &a, int q, int share, int lane, int *seq, int *block)
+{
+    const int per_lane = (a.n_seq + 63) / 64;
+    // blocks of a sequence that reach no further than t >= 0
+    const auto up_to = [&](const Columns &c, int t) {
+        const long long reach = ((long long)t - c.first_pos + 1) * c.share;
+        return reach >= c.n ? (c.n + 127) / 128 : reach <= 0 ? 0 : (int)(reach / 128);
+    };
+    const auto columns = [&](int s, Columns *c) {
+        c->n = 0, c->first_pos = 0, c->share = share;
+        if (s < a.n_seq && !sequence_columns(a, a.start[s], a.start[s + 1], a.context[s], share, c)) c->n = 0;
+    };
+    Columns own;  // (the lane's sequence where it has one only)
+    columns(lane * per_lane, &own);
+    const auto count = [&](int t) {  // of the lane's sequences: blocks up to t
+        int n = 0;
+        for (int i = 0; i < per_lane; ++i) {
+            Columns c = own;
+            if (per_lane > 1) columns(lane * per_lane + i, &c);
+            n += up_to(c, t);
+        }
+        return n;
+    };
+    const auto total = [](int n) { return __builtin_amdgcn_readlane(wave_scan(n), 63); };
+    int top = 0;
+    for (int i = 0; i < per_lane; ++i) {
+        Columns c = own;
+        if (per_lane > 1) columns(lane * per_lane + i, &c);
+        if (c.n > 0) top = max(top, c.first_pos + (c.n - 1) / share);
+    }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) top = max(top, __shfl_xor(top, off, kWave));
+    top = __builtin_amdgcn_readfirstlane(top);
+    const int all = total(count(top));
+    if (q >= all) return false;
+    int lo = 0, hi = top;  // the least position that no more than q blocks pass
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (all - total(count(mid)) <= q) hi = mid;
+        else lo = mid + 1;
+    }
+    // blocks that reach just this position, by sequence; those at negative positions count with 0
+    int mine = count(lo), below = lo > 0 ? count(lo - 1) : 0;
+    const int left = q - (all - total(mine)), upto = wave_scan(mine - below);
+    const int owner = __ffsll((unsigned long long)__ballot(upto > left)) - 1;
+    int rest = left - __builtin_amdgcn_readlane(upto - (mine - below), owner), s = owner * per_lane;
+    for (;; ++s) {
+        Columns c;
+        columns(s, &c);
+        const int last = up_to(c, lo), n = last - (lo > 0 ? up_to(c, lo - 1) : 0);
+        if (rest < n) {
+            *seq = __builtin_amdgcn_readfirstlane(s), *block = __builtin_amdgcn_readfirstlane(last - 1 - rest);
+            return true;
+        }
+        rest -= n;
+    }
+}
+
 // Matrix-bound.  Workgroup: 4 waves, 32 columns each, of one kv head and sequence; 64 tokens at a time are converted to bf16 in LDS, a
 // tile of the cache by each wave, while the tokens before them are used.  A step is 32 tokens: S^T = K q^T (32 tokens x 32 columns),
 // softmax, O^T += V^T P^T; S^T of a step is asked for before the softmax of the one before, so that the matrix pipe has work
-// meanwhile.  Columns of the longest reach come first, since workgroups start in order.  Grid: (units, splits): where units are few the
+// meanwhile.  The longest units come first, since workgroups start in order (four chunks of 955 to 2048 tokens over 2867 to 6144: LPT us,
+// block by block from the sequences' ends 385).  Grid: (units, splits): where units are few the
 // tokens of each are split, and the last workgroup to finish a unit joins its pieces, which stand in memory as they stood in the
 // registers of each wave, in the order of the tokens.
 template <int D>
-__global__ __launch_bounds__(256, 2) void cache_prompt_kernel(AttentionArgs a, int blocks, int splits, unsigned long long tag)
+__global__ __launch_bounds__(256, 2) void cache_prompt_kernel(AttentionArgs a, int units, int splits, unsigned long long tag)
 {
     constexpr int kTile = cache_tile_bytes(D), NT = 1, kCols = 32 * NT, kBlock = 4 * kCols;
     extern __shared__ __align__(16) unsigned char s_raw[];
@@ -627,13 +688,9 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(AttentionArgs a, i
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
     const int lc = lane & 31, h = lane >> 5;
     const int share = a.n_heads / a.c.n_kv, n_kv = a.c.n_kv;
-    const int head = blockIdx.x % n_kv, seq = blockIdx.x / n_kv % a.n_seq, rank = blockIdx.x / n_kv / a.n_seq;
-    Columns cols;
-    const int row0 = a.start[seq];
-    if (!sequence_columns(a, row0, a.start[seq + 1], a.context[seq], share, &cols)) return;
+    const int head = blockIdx.x % n_kv;
     const float scale = a.scale != 0.0f ? fabsf(a.scale) * kLog2e : 1.0f;
     const TileOffsets<D> offsets(n, g);
-    const scalar_ints table = (scalar_ints)(uintptr_t)(a.table + (size_t)seq * a.stride);
     const unsigned page_bytes = n_kv * (a.c.page >> 4) * kTile;
     const unsigned char *const cache = a.cache + (size_t)(head * (a.c.page >> 4)) * kTile;
 
@@ -644,7 +701,13 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(AttentionArgs a, i
         reinterpret_cast<unsigned long long *>(reinterpret_cast<f32x4 *>(a.ws) + (size_t)gridDim.x * splits * 4 * kVectors * 64) + blockIdx.x;
     bool announced = true;  // (units that the caller did not announce have no room for pieces: one workgroup sees to each)
 
-    for (int block = (cols.n + kBlock - 1) / kBlock - 1 - rank; block >= 0; block -= blocks, announced = false) {
+    for (int rank = blockIdx.x / n_kv;; rank += units, announced = false) {
+        int seq, block;
+        if (!nth_longest_block(a, rank, share, lane, &seq, &block)) break;
+        Columns cols;
+        const int row0 = a.start[seq];
+        sequence_columns(a, row0, a.start[seq + 1], a.context[seq], share, &cols);
+        const scalar_ints table = (scalar_ints)(uintptr_t)(a.table + (size_t)seq * a.stride);
         const SeenTokens seen = seen_tokens(cols, block * kBlock, min((block + 1) * kBlock, cols.n));
         const int col0 = block * kBlock + wave * kCols;
         // positions of the wave's columns (of columns that are not there: none)
@@ -903,7 +966,7 @@ hipError_t launch_prompt(const AttentionArgs &a, hipStream_t s)
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(cache_prompt_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, kBytes);
     if (e != hipSuccess) return e;
     const PromptGrid g = prompt_grid(a.n_seq, a.n_heads, a.c.n_kv, a.max_new, a.max_context);
-    cache_prompt_kernel<D><<<dim3((unsigned)(g.blocks * a.n_seq * a.c.n_kv), (unsigned)g.splits), 256, kBytes, s>>>(a, g.blocks, g.splits, launch_tag());
+    cache_prompt_kernel<D><<<dim3((unsigned)(g.blocks * a.n_seq * a.c.n_kv), (unsigned)g.splits), 256, kBytes, s>>>(a, g.blocks * a.n_seq, g.splits, launch_tag());
     return hipGetLastError();
 }
 
