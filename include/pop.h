@@ -339,7 +339,8 @@ int pop_cache_read(const void *cache, int n_kv_heads, int head_dim, int page_tok
  * [0, n_tokens) is left out and its rows are undefined.
  * max_new, max_context: the longest that the caller expects; longer ones are right too, but may be slow.  float32 q is
  * taken in full (three bf16 terms of q and of the softmax weights), with bf16 q the weights are rounded to bf16.
- * workspace: dev, of pop_cache_attention_workspace bytes for the same sizes, any content, for this call alone.
+ * workspace: dev, of pop_cache_attention_workspace bytes for the same sizes, or for larger n_tokens, n_seq, max_new or max_context; any
+ * content, for this call alone.
  * Errors: NULL or misaligned pointers, bad dtype, a scale that is not finite -> POP_EINVAL; sizes, n_heads no multiple of
  * n_kv_heads, a workspace that is too small -> POP_ESHAPE. */
 int pop_cache_attention(const void *q, pop_dtype_t dtype, int n_tokens, const void *cache, int n_kv_heads,

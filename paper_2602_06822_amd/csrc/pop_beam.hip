@@ -8,6 +8,8 @@
 // six operations in the pass.  The last workgroup of a request to finish joins the sums and ranks what the others found.
 #include <math.h>
 
+#include <algorithm>
+
 #include "pop_cache.h"
 
 namespace pop {
@@ -395,8 +397,8 @@ struct Stretches {
 Stretches beam_stretches(int requests, int beams, int vocab, int is_bf16)
 {
     const long long rows = (long long)requests * beams, tile = 64 * kLaneValues, n_tiles = (vocab + (is_bf16 ? 7 : 3) + tile - 1) / tile;
-    const long long of_row = min(max(512 / rows, 1ll), 16ll);
-    const long long tiles = min(max((n_tiles + of_row - 1) / of_row, 4ll), 4ll * kWaveTiles);
+    const long long of_row = std::min(std::max(512 / rows, 1ll), 16ll);
+    const long long tiles = std::min(std::max((n_tiles + of_row - 1) / of_row, 4ll), 4ll * kWaveTiles);
     Stretches s;
     s.n = (int)((n_tiles + tiles - 1) / tiles);
     s.tiles = (int)((n_tiles + s.n - 1) / s.n);  // (all alike)
@@ -407,7 +409,7 @@ Stretches beam_stretches(int requests, int beams, int vocab, int is_bf16)
 
 size_t beam_ws(int requests, int beams, int vocab, int k)
 {
-    const int n = max(beam_stretches(requests, beams, vocab, 0).n, beam_stretches(requests, beams, vocab, 1).n);
+    const int n = std::max(beam_stretches(requests, beams, vocab, 0).n, beam_stretches(requests, beams, vocab, 1).n);
     return (size_t)requests * (beams * (size_t)n * (k + 1) + 1) * 8;
 }
 

@@ -133,7 +133,7 @@ struct AttentionArgs {
     int y_bf16;
     float *ws;
 };
-size_t cache_attention_ws(int n_seq, int n_heads, int n_kv, int d, int max_new, int max_context);
+size_t cache_attention_ws(int n_tokens, int n_seq, int n_heads, int n_kv, int d, int max_new, int max_context);
 hipError_t launch_cache_attention(const AttentionArgs &a, hipStream_t s);
 
 struct BeamArgs {

@@ -8,6 +8,7 @@
 // of the cache's bytes: a lane's K and V codes are loads of D/8 bytes each, a wave's loads are contiguous kilobytes.
 #include <math.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "pop_cache.h"
@@ -578,7 +579,7 @@ constexpr int kPromptTile = 64;  // tokens that the workgroup has in LDS at a ti
 // n D/16 + c writes its halves of the runs at place c 16 + n, so that neighbouring lanes write neighbouring runs.  O^T's rows are in
 // the order of those places.
 // Keys are read in the half of an iteration in front of its barrier, values behind it too: two and three tiles of them, and one
-// barrier a tile.  80 KB for D = 128: two workgroups to a compute unit.
+// barrier a tile.  80 KB for D = 128: two workgroups to a compute unit; D = 256 has one.
 template <int D>
 struct PromptTiles {
     uint32_t k[2][D / 8 * kPromptTile * 4], v[3][8 * D * 4];
@@ -675,12 +676,12 @@ __device__ __forceinline__ bool nth_longest_block(const AttentionArgs &a, int q,
 // Matrix-bound.  Workgroup: 4 waves, 32 columns each, of one kv head and sequence; 64 tokens at a time are converted to bf16 in LDS, a
 // tile of the cache by each wave, while the tokens before them are used.  A step is 32 tokens: S^T = K q^T (32 tokens x 32 columns),
 // softmax, O^T += V^T P^T; S^T of a step is asked for before the softmax of the one before, so that the matrix pipe has work
-// meanwhile.  The longest units come first, since workgroups start in order (four chunks of 955 to 2048 tokens over 2867 to 6144: LPT us,
+// meanwhile.  The longest units come first, since workgroups start in order (four chunks of 955 to 2048 tokens over 2867 to 6144: 372 us,
 // block by block from the sequences' ends 385).  Grid: (units, splits): where units are few the
 // tokens of each are split, and the last workgroup to finish a unit joins its pieces, which stand in memory as they stood in the
 // registers of each wave, in the order of the tokens.
 template <int D>
-__global__ __launch_bounds__(256, 2) void cache_prompt_kernel(AttentionArgs a, int units, int splits, unsigned long long tag)
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_prompt_kernel(AttentionArgs a, int units, int splits, unsigned long long tag)
 {
     constexpr int kTile = cache_tile_bytes(D), NT = 1, kCols = 32 * NT, kBlock = 4 * kCols;
     extern __shared__ __align__(16) unsigned char s_raw[];
@@ -927,8 +928,8 @@ __global__ __launch_bounds__(256, 2) void cache_prompt_kernel(AttentionArgs a, i
 int attention_workgroups(int n_seq, int n_heads, int n_kv, int d, int max_new, long long max_context)
 {
     const long long blocks = ((long long)max_new * (n_heads / n_kv) + 15) / 16, rounds = (max_context + kRound - 1) / kRound;
-    const long long units = max((long long)n_seq * n_kv * blocks, 1ll);
-    return (int)min(min(units * rounds, units * kPieces), units >= 128 && d < 256 ? (long long)kWorkgroups : kWorkgroups / 2ll);
+    const long long units = std::max((long long)n_seq * n_kv * blocks, 1ll);
+    return (int)std::min(units * std::min<long long>(rounds, kPieces), units >= 128 && d < 256 ? (long long)kWorkgroups : kWorkgroups / 2ll);
 }
 
 // From this many bytes of cache on (at the longest length) codes are loaded past the caches: what one layer's attention reads, other
@@ -937,45 +938,56 @@ int attention_workgroups(int n_seq, int n_heads, int n_kv, int d, int max_new, l
 // three 14.1 / 14.6, twelve 14.9 / 14.7.
 constexpr long long kPastBytes = 48ll << 20;
 
-// Blocks of 128 columns of the longest chunk, and the parts that the tokens of each are split into.
+// Blocks of 128 columns that the sequences can have (each no more than the longest chunk, all no more than the rows hold), and the parts
+// that the tokens of each are split into.  Another part costs its unit's last workgroup, which joins them one by one, about half of
+// what 64 tokens cost; so sqrt(2 x tiles of 64) of them, and either one workgroup to a compute unit or all that fit.  (Microseconds, D 128, 512
+// columns over 4 kv heads, 16000 tokens: 8 parts 65.6, 16 48.5, 22 54.5; 60000 tokens: 8 195, 16 115, 32 102; 1024 columns over 8 kv heads, 6000
+// tokens: 8 37.0, 13 40.2; 16000: 8 66.2, 16 61.6.)
 struct PromptGrid {
-    int blocks, splits;
-    long long bytes(int n_seq, int n_kv, int d) const
+    int blocks, splits, most_splits;
+    // (for these sizes and all smaller ones, which may be split into more parts)
+    long long bytes(int n_kv, int d) const
     {
-        return splits == 1 ? 0 : (long long)blocks * n_seq * n_kv * (splits * 4ll * (d / 8 + 1) * 64 * 16 + 8);
+        const long long units = std::min<long long>((long long)blocks * n_kv, kWorkgroups);
+        return most_splits == 1 ? 0 : std::min<long long>(units * most_splits, kWorkgroups) * 4 * (d / 8 + 1) * 64 * 16 + units * 8;
     }
 };
-PromptGrid prompt_grid(int n_seq, int n_heads, int n_kv, int max_new, long long max_context)
+PromptGrid prompt_grid(int n_tokens, int n_seq, int n_heads, int n_kv, int max_new, long long max_context)
 {
     PromptGrid g;
-    const long long units = (long long)n_seq * n_kv;
-    g.blocks = (int)min(((long long)max_new * (n_heads / n_kv) + 127) / 128, 0x7fffffffll / units);
-    const long long tiles = (max_context + kPromptTile - 1) / kPromptTile;
-    g.splits = (int)max(1ll, min(min(512 / (units * g.blocks), tiles / 2), 8ll));
+    const long long share = n_heads / n_kv, tiles = (max_context + kPromptTile - 1) / kPromptTile;
+    g.blocks = (int)std::min((max_new * share + 127) / 128 * n_seq, n_tokens * share / 128 + n_seq);
+    g.most_splits = (int)std::max(1ll, std::min(32ll, (long long)sqrt(2.0 * tiles)));
+    const long long fit = kWorkgroups / ((long long)g.blocks * n_kv);
+    g.splits = (int)std::max(1ll, g.most_splits >= fit ? fit : std::min<long long>(g.most_splits, fit / 2));
     return g;
 }
 
 // Columns of a kv head from which the prompt kernel takes over.  Microseconds, general / prompt kernel: 32 kv heads x 6000 tokens, one
 // sequence 16 columns 29.9 / 30.3, 32 columns 36.7 / 30.4, 128 columns 56.8 / 34.3; 8 kv heads, 32 columns 28.1 / 28.6; 700 tokens 22.5 / 13.8.
+// D = 256 has registers and LDS for one workgroup to a compute unit, so it takes whole blocks, and units for all compute units: two chunks
+// of 1024 tokens x 32 heads over 8 kv heads x 4096 tokens 433 / 290; but 36 columns of 8 kv heads over 16000 tokens 42 / 144.
 constexpr int kPromptColumns = 32;
 
 template <int D>
-hipError_t launch_prompt(const AttentionArgs &a, hipStream_t s)
+hipError_t launch_prompt(const AttentionArgs &a, const PromptGrid &g, hipStream_t s)
 {
     constexpr int kBytes = (int)sizeof(PromptTiles<D>);
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(cache_prompt_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, kBytes);
     if (e != hipSuccess) return e;
-    const PromptGrid g = prompt_grid(a.n_seq, a.n_heads, a.c.n_kv, a.max_new, a.max_context);
-    cache_prompt_kernel<D><<<dim3((unsigned)(g.blocks * a.n_seq * a.c.n_kv), (unsigned)g.splits), 256, kBytes, s>>>(a, g.blocks * a.n_seq, g.splits, launch_tag());
+    cache_prompt_kernel<D><<<dim3((unsigned)(g.blocks * a.c.n_kv), (unsigned)g.splits), 256, kBytes, s>>>(a, g.blocks, g.splits, launch_tag());
     return hipGetLastError();
 }
 
 template <int D>
 hipError_t launch_d(const AttentionArgs &a, hipStream_t s)
 {
-    if constexpr (D <= 128)
-        if (a.q_bf16 && a.y_bf16 && (long long)a.max_new * (a.n_heads / a.c.n_kv) >= kPromptColumns) return launch_prompt<D>(a, s);
-    const long long seen = a.window > 0 ? min((long long)a.max_context, (long long)a.window + a.max_new + 31) : a.max_context;
+    const long long seen = a.window > 0 ? std::min((long long)a.max_context, (long long)a.window + a.max_new + 31) : a.max_context;
+    if (const long long columns = (long long)a.max_new * (a.n_heads / a.c.n_kv); a.q_bf16 && a.y_bf16 && columns >= kPromptColumns) {
+        PromptGrid g = prompt_grid(a.n_tokens, a.n_seq, a.n_heads, a.c.n_kv, a.max_new, seen);
+        if (D == 256) g.splits = 1;
+        if (D < 256 || (columns >= 128 && g.blocks * a.c.n_kv >= 256)) return launch_prompt<D>(a, g, s);
+    }
     const unsigned grid = (unsigned)attention_workgroups(a.n_seq, a.n_heads, a.c.n_kv, D, a.max_new, seen);
     const unsigned long long tag = launch_tag();
     if (!a.q_bf16) cache_attention_kernel<D, 3, 3, false><<<grid, 256, 0, s>>>(a, tag);
@@ -987,10 +999,11 @@ hipError_t launch_d(const AttentionArgs &a, hipStream_t s)
 
 }  // namespace
 
-size_t cache_attention_ws(int n_seq, int n_heads, int n_kv, int d, int max_new, int max_context)
+size_t cache_attention_ws(int n_tokens, int n_seq, int n_heads, int n_kv, int d, int max_new, int max_context)
 {
-    const long long prompt = d <= 128 ? prompt_grid(n_seq, n_heads, n_kv, max_new, max_context).bytes(n_seq, n_kv, d) : 0;
-    return max((size_t)prompt, (size_t)attention_workgroups(n_seq, n_heads, n_kv, d, max_new, max_context) * (2 * 16 * (d + 4) * sizeof(float) + 8));
+    const bool chunks = d < 256 && (long long)max_new * (n_heads / n_kv) >= kPromptColumns;
+    const long long prompt = chunks ? prompt_grid(n_tokens, n_seq, n_heads, n_kv, max_new, max_context).bytes(n_kv, d) : 0;
+    return std::max((size_t)prompt, (size_t)attention_workgroups(n_seq, n_heads, n_kv, d, max_new, max_context) * (2 * 16 * (d + 4) * sizeof(float) + 8));
 }
 
 hipError_t launch_cache_attention(const AttentionArgs &a, hipStream_t s)

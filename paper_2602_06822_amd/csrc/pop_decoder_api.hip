@@ -121,7 +121,7 @@ int pop_cache_attention_workspace(int n_tokens, int n_seq, int n_heads, int n_kv
     if (!bytes) return POP_EINVAL;
     const int rc = attention_sizes(n_tokens, n_seq, n_heads, n_kv, d, max_new, max_context);
     if (rc != POP_OK) return rc;
-    *bytes = n_seq ? cache_attention_ws(n_seq, n_heads, n_kv, d, max_new, max_context) : 0;
+    *bytes = n_seq ? cache_attention_ws(n_tokens, n_seq, n_heads, n_kv, d, max_new, max_context) : 0;
     return POP_OK;
 }
 
@@ -142,7 +142,7 @@ int pop_cache_attention(const void *q, pop_dtype_t dtype, int n_tokens, const vo
     if (n_seq == 0 || n_tokens == 0) return POP_OK;
     if (!q || !cache || !block_table || !q_start || !context_len || !y) return POP_EINVAL;
     if (!aligned16(q) || !aligned16(cache) || !aligned16(y) || !aligned16(workspace)) return POP_EINVAL;
-    const size_t need = cache_attention_ws(n_seq, n_heads, n_kv, d, max_new, max_context);
+    const size_t need = cache_attention_ws(n_tokens, n_seq, n_heads, n_kv, d, max_new, max_context);
     if (need && !workspace) return POP_EINVAL;
     if (workspace_bytes < need) return POP_ESHAPE;
     AttentionArgs a = {q, dtype == POP_BF16, n_tokens, static_cast<const unsigned char *>(cache), c, block_table, table_stride, q_start,

@@ -185,6 +185,23 @@ def test_attention_refuses_a_small_workspace(pop):
     _refused(pop, "POP_EINVAL", "pop_cache_attention", _with(one, ws=None, ws_bytes=0))
 
 
+@pytest.mark.parametrize("heads,n_kv", [(1, 1), (32, 32), (32, 8), (71, 1)])
+def test_a_workspace_of_larger_sizes_is_enough(pop, heads, n_kv):
+    sizes = [1, 2, 3, 8, 17, 64, 130, 600, 5000, 70000]
+    for n_seq in (1, 4, 37, 256):
+        for context in sizes:
+            of_new = []
+            for new in sizes:
+                need = [pop.pop_cache_attention_workspace(n, n_seq, heads, n_kv, 128, new, context) for n in sizes]
+                assert need == sorted(need)
+                of_new.append(need)
+            assert all(a <= b for few, more in zip(of_new, of_new[1:]) for a, b in zip(few, more))
+    for new in sizes:
+        need = [[pop.pop_cache_attention_workspace(3000, n_seq, heads, n_kv, 64, new, c) for c in sizes] for n_seq in (1, 2, 5, 30, 400)]
+        assert all(row == sorted(row) for row in need)
+        assert all(a <= b for few, more in zip(need, need[1:]) for a, b in zip(few, more))
+
+
 BEAM = dict(logits=A, dtype=0, scores=A, done=None, requests=1, beams=4, vocab=100, k=4, pad=0, s=A + 64, t=A, p=A, ws=A,
             ws_bytes=1 << 30, stream=None)
 

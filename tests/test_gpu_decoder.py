@@ -431,6 +431,57 @@ def test_another_stream_and_a_replayed_graph(pop):
         assert all(torch.equal(a, b) for a, b in zip(got, (y1[:17 + i], slots, so, to, po, cache)))
 
 
+@pytest.mark.parametrize("page,window", [(16, 0), (32, 77)])
+def test_chunks_with_the_widest_heads(pop, page, window):
+    """Units for every compute unit; a page that is none, a context shorter than the chunk, an empty sequence."""
+    rng = np.random.default_rng(page)
+    c = Cached(pop, rng, [401, 130, 0, 257], 64, 256, page)
+    start = np.array([0, 129, 259, 259, 389])
+    q = _queries(rng, 389, 64, 256, BF16)
+    y = _attend(pop, c, q, start, BF16, BF16, 64, 0.06, window)
+    _check(c, y, q, start, BF16, BF16, 0.06, window)
+    table = c.table.copy()
+    table[0, 64 // page] = -1
+    there = [np.arange(n) // page != 64 // page if s == 0 else np.ones(n, dtype=bool) for s, n in enumerate(c.context)]
+    y = _attend(pop, c, q, start, BF16, BF16, 64, 0.06, window, table=table)
+    _check(c, y, q, start, BF16, BF16, 0.06, window, there)
+    short = [401, 60, 0, 257]
+    y = _attend(pop, c, q, start, BF16, BF16, 64, 0.06, window, context=short, max_new=130)
+    _check(c, y, q, start, BF16, BF16, 0.06, window, context=short)
+
+
+@pytest.mark.parametrize("new", [[1, 1], [64, 30]])
+def test_pieces_are_joined_in_a_replayed_graph(pop, new):
+    """Units that several workgroups share, captured; other work uses the workspace in between."""
+    rng = np.random.default_rng(11)
+    c = Cached(pop, rng, [2900, 300], 2, 128, 32)
+    start = np.concatenate([[0], np.cumsum(new)])
+    q, y = _queries(rng, start[-1], 8, 128, BF16), torch.zeros(start[-1], 8, 128, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(pop.pop_cache_attention_workspace(start[-1], 2, 8, 2, 128, max(new), 2900), dtype=torch.uint8, device="cuda")
+    table, starts, context = i32(c.table), i32(start), i32(c.context)
+
+    def attend(s):
+        pop.pop_cache_attention(q, BF16, start[-1], c.cache, 2, 128, 32, c.n_pages, table, c.table.shape[1], starts, context, 2, 8, max(new), 2900,
+                                0.09, 0, y, BF16, ws, stream=s)
+
+    attend(torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        attend(torch.cuda.current_stream())
+    for i in range(4):
+        q.normal_(generator=torch.Generator(device="cuda").manual_seed(i))
+        ws.fill_(255 - i)
+        y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = y.clone()
+        _check(c, got, q, start, BF16, BF16, 0.09)
+        attend(torch.cuda.current_stream())
+        torch.cuda.synchronize()
+        assert torch.equal(got, y)
+
+
 def test_offsets_beyond_32_bits(pop):
     """The last pages of a cache of more than 4 GB."""
     n_kv, d, page = 8, 128, 64
