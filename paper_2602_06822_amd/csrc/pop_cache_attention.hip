@@ -132,11 +132,11 @@ __device__ __forceinline__ void store_y2(const AttentionArgs &a, size_t at, floa
     else *reinterpret_cast<float2 *>(static_cast<float *>(a.y) + at) = {x, y};
 }
 
-// Sum over the lanes up to this one.
+// Sum over the lanes up to this one, of numbers that are not negative; no more than INT_MAX.
 template <int CTRL, int ROWS>
 __device__ __forceinline__ int dpp_add(int v)
 {
-    return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+    return __builtin_elementwise_add_sat(v, __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false));
 }
 __device__ __forceinline__ int wave_scan(int v)
 {
@@ -336,7 +336,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_kernel(
         if (s < a.n_seq) {
             my_start = a.start[s], my_next = a.start[s + 1], my_context = a.context[s];
             const SequenceWork w = sequence_work(a, my_start, my_next, my_context, share);
-            mine += w.rounds * w.blocks * n_kv;
+            mine = __builtin_elementwise_add_sat(mine, w.rounds * w.blocks * n_kv);
         }
     }
     const int upto = wave_scan(mine);
@@ -352,7 +352,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_kernel(
     const int first_round = blockIdx.x * fewest + min(blockIdx.x, longer), end = first_round + (int)fewest + (blockIdx.x < longer);
     int at = first_round;
     const int owner = __ffsll((unsigned long long)__ballot(upto > at)) - 1;
-    int seq = owner * per_lane, seq_at = __builtin_amdgcn_readlane(upto - mine, owner);  // the sequence's first round
+    int seq = owner * per_lane, seq_at = owner > 0 ? __builtin_amdgcn_readlane(upto, owner - 1) : 0;  // the sequence's first round
     unsigned long long *const counters = reinterpret_cast<unsigned long long *>(partial_of<D>(a, 2 * (int)gridDim.x));
     const unsigned page_bytes = n_kv * (a.c.page >> 4) * kTile;
 
@@ -366,7 +366,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_kernel(
         }
         const SequenceWork w = sequence_work(a, start, next, context, share);
         const int of_seq = w.rounds * w.blocks * n_kv;
-        if (at >= seq_at + of_seq) {
+        if ((unsigned)at >= (unsigned)seq_at + (unsigned)of_seq) {
             seq_at += of_seq, ++seq;
             continue;
         }
