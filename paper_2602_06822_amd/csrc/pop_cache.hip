@@ -55,7 +55,8 @@ __device__ __forceinline__ uint32_t quantise8(float (&x)[8], int *byte)
 
 // One thread: eight channels of K and of V of one token and head.  A workgroup has one head and as many tokens in a row as it holds (16
 // for D = 128): what it stores is whole lines of one or two tiles, put together in one L2.  8191 tokens of 32 heads, 128 channels, bf16:
-// 40.6 us (170 MB, 4.2 TB/s); with all heads of two tokens to a workgroup, whose lines come together from several L2s, 49.1.
+// 40.6 us, bound by memory (170 MB, 4.2 TB/s, where a copy has 4.8); with all heads of two tokens to a workgroup, whose lines come together
+// from several L2s, 49.1.
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void cache_write_kernel(unsigned char *__restrict__ cache, CacheShape c, const void *__restrict__ k,
                                                           const void *__restrict__ v, long long k_stride, long long v_stride,
@@ -65,14 +66,14 @@ __global__ __launch_bounds__(256) void cache_write_kernel(unsigned char *__restr
     const int head = blockIdx.x % (unsigned)c.n_kv, token = (int)(blockIdx.x / (unsigned)c.n_kv) * kTokens + threadIdx.x / kPer;
     const int ch = threadIdx.x % kPer * 8;
     if (token >= n_tokens) return;  // (four lanes of a block leave together: kPer is a multiple of four)
-    const int slot = slots[token];
-    const int page = slot >> c.log_page;
-    if (slot < 0 || page >= c.n_pages) return;
     float xk[8], xv[8];
     load8<BF16>(k, token * k_stride + head * D + ch, xk);
     load8<BF16>(v, token * v_stride + head * D + ch, xv);
+    const int slot = slots[token];  // (asked for together with the values)
+    const int page = slot >> c.log_page;
     int bk, bv;
     const uint32_t ck = quantise8(xk, &bk), cv = quantise8(xv, &bv);
+    if (slot < 0 || page >= c.n_pages) return;
     const int t = slot & 15;
     unsigned char *tile = cache + cache_tile_offset(page, head, slot & (c.page - 1), c.n_kv, c.log_page, cache_tile_bytes(D));
     *reinterpret_cast<uint32_t *>(tile + t * (D / 2) + ch / 2) = ck;
@@ -102,20 +103,20 @@ __device__ __forceinline__ void store8(void *p, long long at, uint32_t codes, fl
     }
 }
 
+// Dealt as the writer's threads are, so that a line of the cache comes into one L2 only: the same tokens 26.3 us (170 MB, 6.4 TB/s); with the
+// heads of a token side by side, where the cache was fetched three times over, 35.9.
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void cache_read_kernel(const unsigned char *__restrict__ cache, CacheShape c,
-                                                         const int *__restrict__ slots, unsigned n_items, void *__restrict__ k,
+                                                         const int *__restrict__ slots, int n_tokens, void *__restrict__ k,
                                                          void *__restrict__ v)
 {
-    constexpr int kPer = D / 8, W = D / 32;
-    const unsigned id = blockIdx.x * 256u + threadIdx.x;
-    const unsigned item = id / kPer;
-    const int ch = (int)(id % kPer) * 8;
-    if (item >= n_items) return;
-    const int token = item / (unsigned)c.n_kv, head = item - (unsigned)token * c.n_kv;
+    constexpr int kPer = D / 8, W = D / 32, kTokens = 256 / kPer;
+    const int head = blockIdx.x % (unsigned)c.n_kv, token = (int)(blockIdx.x / (unsigned)c.n_kv) * kTokens + threadIdx.x / kPer;
+    const int ch = threadIdx.x % kPer * 8;
+    if (token >= n_tokens) return;
     const int slot = slots[token];
     const int page = slot >> c.log_page;
-    const long long out = (long long)item * D + ch;
+    const long long out = ((long long)token * c.n_kv + head) * D + ch;
     uint32_t ck = 0, cv = 0, bk = 1, bv = 1;
     if (slot >= 0 && page < c.n_pages) {
         const int t = slot & 15;
@@ -485,12 +486,12 @@ hipError_t launch_cache_write(void *cache, const CacheShape &c, const void *k, c
 hipError_t launch_cache_read(const void *cache, const CacheShape &c, const int *slots, int n_tokens, void *k, void *v, int is_bf16,
                              hipStream_t s)
 {
-    const unsigned items = (unsigned)n_tokens * c.n_kv;
-    const unsigned grid = (unsigned)(((size_t)items * (c.d / 8) + 255) / 256);
+    const int tokens = 2048 / c.d;  // of a workgroup
+    const unsigned grid = (unsigned)((n_tokens + tokens - 1) / tokens) * c.n_kv;
     const unsigned char *from = static_cast<const unsigned char *>(cache);
 #define POP_READ(D)                                                                              \
-    (is_bf16 ? cache_read_kernel<D, true><<<grid, 256, 0, s>>>(from, c, slots, items, k, v)      \
-             : cache_read_kernel<D, false><<<grid, 256, 0, s>>>(from, c, slots, items, k, v))
+    (is_bf16 ? cache_read_kernel<D, true><<<grid, 256, 0, s>>>(from, c, slots, n_tokens, k, v)      \
+             : cache_read_kernel<D, false><<<grid, 256, 0, s>>>(from, c, slots, n_tokens, k, v))
     if (c.d == 64) POP_READ(64);
     else if (c.d == 128) POP_READ(128);
     else POP_READ(256);
