@@ -312,14 +312,23 @@ __device__ __forceinline__ void reorder_rows(const ReorderArgs &a, int g, Reorde
     __syncthreads();
 }
 
-// The pages of block j of the rows, -1 for none, and by bit the rows whose page no row keeps: a page counts at the first row that has
-// it.  A page that rows hold together stands at the same block of each (they share it since they were one row).
+// Block j's entries of the rows: asked for before it is known how many blocks a row has.
 template <int W>
-__device__ __forceinline__ unsigned freed_rows(const ReorderArgs &a, const ReorderRows &rows, int g, int j, int (&page)[W])
+__device__ __forceinline__ void load_entries(const ReorderArgs &a, int g, int j, int (&page)[W])
 {
     const int *at = a.table + (size_t)g * a.group * a.stride + j;
 #pragma unroll
-    for (int r = 0; r < W; ++r) page[r] = r < a.group && j < rows.blocks[r] ? at[(size_t)r * a.stride] : -1;
+    for (int r = 0; r < W; ++r) page[r] = r < a.group && j < a.stride ? at[(size_t)r * a.stride] : -1;
+}
+
+// Makes them the pages of block j of the rows, -1 for none, and gives by bit the rows whose page no row keeps: a page counts at the first row that has
+// it.  A page that rows hold together stands at the same block of each (they share it since they were one row).
+template <int W>
+__device__ __forceinline__ unsigned freed_rows(const ReorderArgs &a, const ReorderRows &rows, int j, int (&page)[W])
+{
+#pragma unroll
+    for (int r = 0; r < W; ++r)
+        if (r >= a.group || j >= rows.blocks[r]) page[r] = -1;
     unsigned freed = 0;
 #pragma unroll
     for (int r = 0; r < W; ++r) {
@@ -364,9 +373,10 @@ __global__ __launch_bounds__(kReorderBlocks) void reorder_count_kernel(ReorderAr
     __shared__ ReorderRows s_rows;
     __shared__ int s_wave[4];
     const int g = blockIdx.x, j = blockIdx.y * kReorderBlocks + threadIdx.x;
-    reorder_rows(a, g, s_rows);
     int page[W], before;
-    const int total = block_sum(j < a.stride ? __popc(freed_rows(a, s_rows, g, j, page)) : 0, s_wave, &before);
+    load_entries(a, g, j, page);
+    reorder_rows(a, g, s_rows);
+    const int total = block_sum(__popc(freed_rows(a, s_rows, j, page)), s_wave, &before);
     if (threadIdx.x == 0) {
         a.counts[g * gridDim.y + blockIdx.y] = total;
         if (blockIdx.y == 0) {
@@ -385,6 +395,8 @@ __global__ __launch_bounds__(kReorderBlocks) void reorder_rows_kernel(ReorderArg
     const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n_groups = gridDim.x, chunks = gridDim.y;
     const int part = g * chunks + blockIdx.y, n_parts = n_groups * chunks, j = blockIdx.y * kReorderBlocks + tid, first = g * a.group;
     const int head = a.pool[0], count = a.pool[1];
+    int page[W], at;
+    load_entries(a, g, j, page);
     // of the parts and requests in front of this one, and of all: pages given back, copies
     int freed_before = 0, freed_all = 0, copies_before = 0, copies_all = 0;
     if (!alone) {
@@ -401,8 +413,7 @@ __global__ __launch_bounds__(kReorderBlocks) void reorder_rows_kernel(ReorderArg
         if (lane == 0) s_sums[wave][0] = freed_before, s_sums[wave][1] = freed_all, s_sums[wave][2] = copies_before, s_sums[wave][3] = copies_all;
     }
     reorder_rows(a, g, s_rows);  // (its barriers stand behind the sums)
-    int page[W], at;
-    const unsigned freed = j < a.stride ? freed_rows(a, s_rows, g, j, page) : 0;
+    const unsigned freed = freed_rows(a, s_rows, j, page);
     const int mine = block_sum(__popc(freed), s_wave, &at);
     if (alone) {
         freed_all = mine;
