@@ -6,6 +6,10 @@
 // bound of the row's k-th largest value, and the largest of the workgroup's four bounds leaves about k segments that can hold one of
 // its k best.  Only those are read again, what reaches the bound is listed in LDS, and the lists are ranked.  So a value costs
 // six operations in the pass.  The last workgroup of a request to finish joins the sums and ranks what the others found.
+//
+// 32 requests of 8 rows of 131071 float32, 16 best: 30.3 us, of which the pass is 18 (134 MB, 7 TB/s) and what follows a chain of a
+// dozen latencies: bound 2.1, reading again 1.6, ranking 1.0, handing over 0.9, the last workgroup's join 3.4.  One request of 4 rows of 32000
+// bf16: 11.3 us, the same chain.  (The first tile asked for before the beams' states, which then return behind it: 32.7.)
 #include <math.h>
 
 #include <algorithm>
@@ -40,7 +44,7 @@ template <int BITS>
 __device__ __forceinline__ uint32_t kth_of_lanes(uint32_t v, int k)
 {
     uint32_t found = 0;
-#pragma unroll
+#pragma unroll 4
     for (int bit = 31; bit >= 32 - BITS; --bit) {
         const uint32_t next = found | 1u << bit;
         found = __popcll(__ballot(v >= next)) >= k ? next : found;
@@ -49,50 +53,54 @@ __device__ __forceinline__ uint32_t kth_of_lanes(uint32_t v, int k)
 }
 
 // A wave's list, of n words, all different: what cannot be among its k largest is dropped, and at most kListed - kRoom words are left.
+// The list is gone over 64 words at a time, in place; such code runs once or twice in a launch, and most of what it costs is to fetch it.
 __device__ __attribute__((noinline)) int thin_out(unsigned long long *list, int n, int k, int lane)
 {
+    const auto word = [&](int i) { return i + lane < n ? list[i + lane] : 0; };
+    const auto keep = [&](unsigned long long bound) {
+        int left = 0;
+#pragma unroll 1
+        for (int i = 0; i < n; i += 64) {
+            const unsigned long long w = word(i), m = __ballot(w != 0 && w >= bound);
+            if (w != 0 && w >= bound) list[left + __popcll(m & ((1ull << lane) - 1))] = w;
+            left += __popcll(m);
+        }
+        n = left;
+    };
+    const auto largest = [&] {  // (its upper half)
+        uint32_t most = 0;
+#pragma unroll 1
+        for (int i = 0; i < n; i += 64) most = max(most, (uint32_t)(word(i) >> 32));
+        return most;
+    };
+    keep((unsigned long long)kth_of_lanes<20>(largest(), k) << 32);
+    if (n <= kListed - kRoom) return n;
+    // a crowd of equal values: k lanes have the k-th largest value or more, and among words with just this value a place of `place` or more
+    const uint32_t value = kth_of_lanes<32>(largest(), k);
+    uint32_t place = 0;
+#pragma unroll 1
+    for (int i = 0; i < n; i += 64) {
+        const unsigned long long w = word(i);
+        const uint32_t v = (uint32_t)(w >> 32);
+        place = v >= value ? max(place, v > value ? ~0u : (uint32_t)w) : place;
+    }
+    keep((unsigned long long)value << 32 | kth_of_lanes<32>(place, k));
+    if (n <= kListed - kRoom) return n;
+    // (only where k is near 64) the k largest are counted out
     constexpr int P = kListed / 64;
     unsigned long long w[P];
 #pragma unroll
-    for (int i = 0; i < P; ++i) w[i] = i * 64 + lane < n ? list[i * 64 + lane] : 0;
-    uint32_t most = 0;
+    for (int i = 0; i < P; ++i) w[i] = word(i * 64);
+    int rank[P] = {};
+    for (int e = 0; e < n; ++e) {
+        const unsigned long long other = list[e];
 #pragma unroll
-    for (int i = 0; i < P; ++i) most = max(most, (uint32_t)(w[i] >> 32));
-    unsigned long long bound = (unsigned long long)kth_of_lanes<20>(most, k) << 32;
-    int left = 0;
-#pragma unroll 1
-    for (int turn = 0; turn < 2; ++turn) {
-        left = 0;
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-            const bool stays = w[i] != 0 && w[i] >= bound;
-            const unsigned long long m = __ballot(stays);
-            if (stays) list[left + __popcll(m & ((1ull << lane) - 1))] = w[i];
-            left += __popcll(m);
-        }
-        if (left <= kListed - kRoom) break;
-        // a crowd of equal values: k lanes have the k-th largest value or more, and among words with just this value a place of `place` or more
-        const uint32_t value = kth_of_lanes<32>(most, k);
-        uint32_t place = 0;
-#pragma unroll
-        for (int i = 0; i < P; ++i) place = (uint32_t)(w[i] >> 32) >= value ? max(place, (uint32_t)(w[i] >> 32) > value ? ~0u : (uint32_t)w[i]) : place;
-        bound = (unsigned long long)value << 32 | kth_of_lanes<32>(place, k);
+        for (int i = 0; i < P; ++i) rank[i] += other > w[i];
     }
-    if (left > kListed - kRoom) {  // (only where k is near 64) the k largest are counted out
 #pragma unroll
-        for (int i = 0; i < P; ++i) w[i] = i * 64 + lane < left ? list[i * 64 + lane] : 0;
-        int rank[P] = {};
-        for (int e = 0; e < left; ++e) {
-            const unsigned long long other = list[e];
-#pragma unroll
-            for (int i = 0; i < P; ++i) rank[i] += other > w[i];
-        }
-#pragma unroll
-        for (int i = 0; i < P; ++i)
-            if (w[i] != 0 && rank[i] < k) list[rank[i]] = w[i];
-        left = min(left, k);
-    }
-    return left;
+    for (int i = 0; i < P; ++i)
+        if (w[i] != 0 && rank[i] < k) list[rank[i]] = w[i];
+    return min(n, k);
 }
 
 constexpr int kWaveTiles = 17;  // of a wave
@@ -116,25 +124,37 @@ __device__ __forceinline__ void append(unsigned long long *list, int &n, bool li
     n += __popcll(m);
 }
 
-// The k largest words of the four waves' lists, in order to put(rank, word).  All threads; n[] has been written.
+// The k largest words of the four waves' lists, in order to put(rank, word).  All threads; n[] has been written.  Each wave counts, for
+// all words, those of its own list that come in front of them: two words a lane, eight reads under way; then the four counts are added
+// up.  (One thread to a word over all four lists: 2.1 us where this takes 1.0, of 16 words out of about 80.)
 template <class Put>
 __device__ __forceinline__ void select_listed(BeamShared &s, int k, Put put)
 {
-    const int n0 = s.n[0], n1 = n0 + s.n[1], n2 = n1 + s.n[2], n = n2 + s.n[3];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int n0 = s.n[0], n1 = n0 + s.n[1], n2 = n1 + s.n[2], n = n2 + s.n[3], own = s.n[wave];  // n <= 4 (kListed - kRoom)
+    const auto word = [&](int e) { return e < n0 ? s.list[0][e] : e < n1 ? s.list[1][e - n0] : e < n2 ? s.list[2][e - n1] : s.list[3][e - n2]; };
+    const auto counts = [&](int w) { return reinterpret_cast<int *>(s.most[w]); };  // (the maxima have been used)
+    if (lane < 8) s.list[wave][own + lane] = 0;  // (a list's end, so that eight can be read)
+#pragma unroll 1
+    for (int e = lane; e < n; e += 128) {
+        const unsigned long long a = word(e), b = e + 64 < n ? word(e + 64) : ~0ull;
+        int of_a = 0, of_b = 0;
+#pragma unroll 1
+        for (int i = 0; i < own; i += 8) {
+            unsigned long long other[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) other[j] = s.list[wave][i + j];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) of_a += other[j] > a, of_b += other[j] > b;
+        }
+        counts(wave)[e] = of_a;
+        if (e + 64 < n) counts(wave)[e + 64] = of_b;
+    }
+    __syncthreads();
+#pragma unroll 1
     for (int e = threadIdx.x; e < n; e += 256) {
-        const unsigned long long mine = e < n0 ? s.list[0][e] : e < n1 ? s.list[1][e - n0] : e < n2 ? s.list[2][e - n1] : s.list[3][e - n2];
-        int rank = 0;
-#pragma unroll 1
-        for (int w = 0; w < 4; ++w)
-#pragma unroll 1
-            for (int i = 0; i < s.n[w]; i += 8) {  // (eight reads under way; a list's room is a multiple of eight)
-                unsigned long long other[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) other[j] = s.list[w][i + j];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) rank += i + j < s.n[w] && other[j] > mine;
-            }
-        if (rank < k) put(rank, mine);
+        const int rank = counts(0)[e] + counts(1)[e] + counts(2)[e] + counts(3)[e];
+        if (rank < k) put(rank, word(e));
     }
 }
 
@@ -164,6 +184,7 @@ __device__ __forceinline__ void join_request(const BeamArgs &a, BeamShared &s, i
     constexpr int E = 4;
     const unsigned long long *words = words_of(a, stretches) + (size_t)row0 * stretches * a.k;
     const int per = stretches * a.k, total = a.beams * per;
+    const float by_per = __builtin_amdgcn_rcpf((float)per);
     unsigned long long w[E];
     const auto load = [&](int tile) {
 #pragma unroll
@@ -207,7 +228,9 @@ __device__ __forceinline__ void join_request(const BeamArgs &a, BeamShared &s, i
         if (n > kListed - kRoom) n = thin_out(s.list[wave], n, a.k, lane);
 #pragma unroll
         for (int i = 0; i < E; ++i) {
-            const int c = tile + i * 256 + threadIdx.x, b = (unsigned)c / (unsigned)per, left = c - b * per;
+            if (tile + i * 256 >= total) break;
+            // (total < 2^20, per < 2^16: half a word is far more than what the product is rounded by)
+            const int c = tile + i * 256 + threadIdx.x, b = (int)(((float)c + 0.5f) * by_per), left = c - b * per;
             uint32_t token = 0xffffffffu;
             float score = -INFINITY;
             if (c < total && !s.closed[b]) {
@@ -325,25 +348,56 @@ __global__ __launch_bounds__(256, 3) void beam_select_kernel(BeamArgs a, int str
         const float limit = ranked_value((unsigned long long)max(max(max(s.bound[0], s.bound[1]), max(s.bound[2], s.bound[3])), kMinusInfinity) << 32);
         // segments with a value that reaches the limit, and those values; minus infinities are no such value
         int n_segments = 0, n = 0;
-        for (int t = 0; t < mine; ++t) {
-            const float most = s.most[wave][t][lane];
-            const bool is = most >= limit && most > -INFINITY;
-            const unsigned long long m = __ballot(is);
-            if (is) s.segment[wave][n_segments + __popcll(m & ((1ull << lane) - 1))] = (uint16_t)(t * 64 + lane);
-            n_segments += __popcll(m);
-        }
-        for (int base = 0; base < n_segments; base += 64 / NV) {
-            if (n > kListed - kRoom) n = thin_out(s.list[wave], n, a.k, lane);
-            const int i = base + lane / NV, segment = i < n_segments ? s.segment[wave][i] : -1;
-            const int vector = ((first + 4 * (segment >> 6)) * NV + lane % NV) * 64 + (segment & 63);
-            const u32x4 r = __builtin_amdgcn_raw_buffer_load_b128(rows, segment >= 0 ? vector * 16 : 0x7ffffff0, 0, 0);
-            float x[V];
-            values(x, r);
+#pragma unroll 1
+        for (int t = 0; t < mine; t += 4) {
+            float most[4];
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const int at = vector * V - skew + j;
-                if (odd && at == a.vocab - 1) x[j] = odd_value;
-                append(s.list[wave], n, segment >= 0 && at >= 0 && at < a.vocab && x[j] >= limit && x[j] > -INFINITY, rank_word(x[j], (uint32_t)at), lane);
+            for (int j = 0; j < 4; ++j) most[j] = t + j < mine ? s.most[wave][t + j][lane] : -INFINITY;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bool is = most[j] >= limit && most[j] > -INFINITY;
+                const unsigned long long m = __ballot(is);
+                if (is) s.segment[wave][n_segments + __popcll(m & ((1ull << lane) - 1))] = (uint16_t)((t + j) * 64 + lane);
+                n_segments += __popcll(m);
+            }
+        }
+        constexpr int kRound = 64 / NV;  // segments that a load takes
+        int segment[2], vector[2];
+        u32x4 again[2];
+        const auto fetch = [&](int base) {  // two rounds
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int i = base + u * kRound + lane / NV;
+                segment[u] = i < n_segments ? s.segment[wave][i] : -1;
+                vector[u] = ((first + 4 * (segment[u] >> 6)) * NV + lane % NV) * 64 + (segment[u] & 63);
+                again[u] = __builtin_amdgcn_raw_buffer_load_b128(rows, segment[u] >= 0 ? vector[u] * 16 : 0x7ffffff0, 0, 0);
+            }
+        };
+        fetch(0);
+        // meanwhile the wave's sums
+        float most = ref;
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor(most, off, kWave));
+        sum = wave_sum(sum * __builtin_amdgcn_exp2f(ref - finite_or_zero(most)));
+        if (lane == 0) s.ref[wave] = most, s.sum[wave] = sum;
+        if (threadIdx.x < kMostK) s.found[threadIdx.x] = 0;
+#pragma unroll 1
+        for (int base = 0; base < n_segments; base += 2 * kRound) {
+            if (base > 0) fetch(base);
+#pragma unroll 1
+            for (int u = 0; u < 2; ++u) {
+                if (base + u * kRound >= n_segments) break;
+                if (n > kListed - kRoom) n = thin_out(s.list[wave], n, a.k, lane);
+                float x[V];
+                values(x, u == 0 ? again[0] : again[1]);
+                const int at0 = (u == 0 ? vector[0] : vector[1]) * V - skew;
+                const bool there = (u == 0 ? segment[0] : segment[1]) >= 0;
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const int at = at0 + j;
+                    if (odd && at == a.vocab - 1) x[j] = odd_value;
+                    append(s.list[wave], n, there && at >= 0 && at < a.vocab && x[j] >= limit && x[j] > -INFINITY, rank_word(x[j], (uint32_t)at), lane);
+                }
             }
         }
         if (n > 32) n = thin_out(s.list[wave], n, a.k, lane);
@@ -360,14 +414,8 @@ __global__ __launch_bounds__(256, 3) void beam_select_kernel(BeamArgs a, int str
             append(s.list[wave], n, lists, rank_word(-INFINITY, (uint32_t)at), lane);
             if (lane == 0) s.n[wave] = n;
         }
-        // the workgroup's sums and its k largest
-        float most = ref;
-#pragma unroll
-        for (int off = 32; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor(most, off, kWave));
-        sum = wave_sum(sum * __builtin_amdgcn_exp2f(ref - finite_or_zero(most)));
-        if (lane == 0) s.ref[wave] = most, s.sum[wave] = sum;
-        if (threadIdx.x < kMostK) s.found[threadIdx.x] = 0;
         __syncthreads();
+        // the workgroup's sums and its k largest
         select_listed(s, a.k, [&](int rank, unsigned long long word) { s.found[rank] = word; });
         const float all = fmaxf(fmaxf(s.ref[0], s.ref[1]), fmaxf(s.ref[2], s.ref[3]));
         float total = 0.0f;
@@ -386,10 +434,9 @@ __global__ __launch_bounds__(256, 3) void beam_select_kernel(BeamArgs a, int str
     join_request(a, s, request, stretches, is_open);
 }
 
-// Tiles of 16 values a lane (32: 256 rows of 131071 float32 37.2 us instead of 33.6).  A stretch has a tile for each wave at least, a
-// sixteenth of the row (a request of 8 rows of 131071: 33 stretches a row 24.4 us, 17 of them 16.8), and what leaves about 512
-// workgroups: their ends, where the best values are found, cost a compute unit about 5 us each (256 rows: 1024 workgroups 44.9 us where
-// 512 take 41.2, 2048 take 65.9).
+// Tiles of 16 values a lane (32: 256 rows of 131071 float32 3.6 us more).  A stretch has a tile for each wave at least, a
+// sixteenth of the row (a request of 8 rows of 131071: 33 stretches a row 7.6 us more than 17), and what leaves about 512
+// workgroups: more of them have more ends, where the best values are found (256 rows: 768 workgroups 6 us more, 1024 19 more).
 constexpr int kLaneValues = 16;
 struct Stretches {
     int tiles, n;
