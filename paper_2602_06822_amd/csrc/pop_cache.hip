@@ -138,6 +138,7 @@ __global__ __launch_bounds__(256) void cache_read_kernel(const unsigned char *__
 
 // ---------------------------------------------------------------- page copies
 
+// Bound by memory; a launch for few copies by its latency (2.3 us).  4 KB to a workgroup, one trip: a page of 34 KB has nine.
 __global__ __launch_bounds__(256) void cache_copy_kernel(unsigned char *__restrict__ cache, size_t page_bytes, int n_pages,
                                                          const int *__restrict__ copies)
 {
@@ -188,7 +189,8 @@ constexpr int kPlanTokens = 1024;  // slots a workgroup writes
 
 // Latency-bound integer work.  Every workgroup sums all sequences' lengths for itself (a few kilobytes, from the L2 for all
 // but the first), keeps the sequences whose new tokens meet its own 1024 slots, and writes those; nothing is handed from
-// one workgroup to another, so one launch does it.  A fresh block is entered into the table by its first token's thread.
+// one workgroup to another, so one launch does it.  A fresh block is entered into the table by its first token's thread.  8 sequences of
+// one token 3.3 us, 256 prompts of up to 2048 tokens 7.0.
 __global__ __launch_bounds__(256) void cache_plan_kernel(PlanArgs a)
 {
     __shared__ Sums wave_totals[4];
@@ -365,8 +367,8 @@ __device__ __forceinline__ int block_sum(int v, int *s_wave, int *before)
 }
 
 // Latency-bound integer work in two launches (one where a single workgroup sees to everything): what each part of the requests gives
-// back and takes has to be known before the first page finds its place in the ring.  W: rows of a request at most.  counts: pages given back, by request and part, then
-// copies by request.
+// back and takes has to be known before the first page finds its place in the ring.  W: rows of a request at most.  counts: pages given back,
+// by request and part, then copies by request.  One request of four rows 4.3 us; 64 of eight rows of 250 blocks 4.4 + 8.4.
 template <int W>
 __global__ __launch_bounds__(kReorderBlocks) void reorder_count_kernel(ReorderArgs a)
 {

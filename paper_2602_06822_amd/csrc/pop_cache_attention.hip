@@ -313,6 +313,13 @@ __device__ __forceinline__ float2 load_pair(const float *p)
 // one, in the order of the tokens.  QT, PT: bf16 terms that q and the softmax weights are split into: q one if it is bf16 (exact),
 // else three (24 bits); the weights one if the output is bf16 (rounded to 8 significant bits, as the output is), else three.  K and V
 // are exact in bf16.
+//
+// Bound by memory on long contexts (two of up to 131072 tokens, 32 heads over 8, D 128: 43 us, 224 MB at 5.2 TB/s; the instructions of the
+// conversion take 45 % of the time, waits 27), by its chain of latencies on short ones (eight of up to 4096, 32 heads: 22.3 us, of which
+// the codes' 87 MB take 11.5; lengths 1.6, q and table 1.1 a unit, the waves' sums 0.8, pieces stored and counted 1.0, joined 1.5).
+// Counting all pieces at the workgroup's end (24.2) and asking for the next unit before the last one's sums (22.7, long contexts 45) cost
+// more than they hide, as do three or four steps in registers (23.9, 25.2).  A chunk in float32 is bound by its three
+// products (two of 1024 tokens over 4096, 32 heads over 8: 262 us, 0.9 PFLOP/s).
 template <int D, int QT, int PT, bool PAST>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_kernel(AttentionArgs a, unsigned long long tag)
 {
@@ -677,7 +684,10 @@ __device__ __forceinline__ bool nth_longest_block(const AttentionArgs &a, int q,
 // tile of the cache by each wave, while the tokens before them are used.  A step is 32 tokens: S^T = K q^T (32 tokens x 32 columns),
 // softmax, O^T += V^T P^T; S^T of a step is asked for before the softmax of the one before, so that the matrix pipe has work
 // meanwhile.  The longest units come first, since workgroups start in order (four chunks of 955 to 2048 tokens over 2867 to 6144: 372 us,
-// block by block from the sequences' ends 385).  Grid: (units, splits): where units are few the
+// block by block from the sequences' ends 385).  That is 0.87 PFLOP/s, where a large product of a library has 1.18: the matrix pipe is busy
+// 40 % of the time, vector instructions (exponentials, conversions, maxima) 50, a wave waits 31, and two waves to a pipe do not interleave
+// better: products in groups with vector instructions between them (412), priorities (382), 8 waves to a workgroup (395), 64
+// columns to a wave (616), 32 tokens a barrier (414) and operands asked for earlier (368) gave no more.  Grid: (units, splits): where units are few the
 // tokens of each are split, and the last workgroup to finish a unit joins its pieces, which stand in memory as they stood in the
 // registers of each wave, in the order of the tokens.
 template <int D>
