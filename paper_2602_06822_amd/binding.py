@@ -98,13 +98,14 @@ def _check(status: int, where: str):
 def _ptr(t):
     if t is None:
         return None
-    if isinstance(t, int):
-        return t
-    if not t.is_cuda:
-        raise ValueError("device tensor expected")
-    if not t.is_contiguous():
-        raise ValueError("contiguous tensor expected")
-    return t.data_ptr()
+    try:  # (a step's calls take a dozen of them: the usual case first)
+        if t.is_cuda and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        if isinstance(t, int):
+            return t
+        raise
+    raise ValueError("contiguous tensor expected" if t.is_cuda else "device tensor expected")
 
 
 # torch's current stream without a stream object around it (0.2 us instead of 2.8)
@@ -312,7 +313,7 @@ def _rows(t, width, stride):
 
 
 def _workspace(t):
-    return (None, 0) if t is None else (_ptr(t), t.numel() * t.element_size())
+    return (None, 0) if t is None else (_ptr(t), t.nbytes)
 
 
 def pop_cache_bytes(n_kv_heads, head_dim, page_tokens, n_pages) -> int:
