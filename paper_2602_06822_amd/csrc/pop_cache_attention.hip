@@ -694,7 +694,7 @@ __device__ __forceinline__ bool nth_longest_block(const AttentionArgs &a, int q,
 template <int D>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_prompt_kernel(AttentionArgs a, int units, int splits, unsigned long long tag)
 {
-    constexpr int kTile = cache_tile_bytes(D), NT = 1, kCols = 32 * NT, kBlock = 4 * kCols;
+    constexpr int kTile = cache_tile_bytes(D), kCols = 32, kBlock = 4 * kCols;
     extern __shared__ __align__(16) unsigned char s_raw[];
     PromptTiles<D> &s_tiles = *reinterpret_cast<PromptTiles<D> *>(s_raw);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
@@ -725,33 +725,25 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_prompt_kernel(Att
         // positions of the wave's columns (of columns that are not there: none)
         const int wave_first = cols.first_pos + col0 / share;
         const int wave_last = col0 < cols.n ? cols.first_pos + (min(col0 + kCols, cols.n) - 1) / share : -1;
-        int pos[NT];
-        bf16x8 q[NT][D / 16];
+        bf16x8 q[D / 16];
         const uint32_t sign = a.scale < 0.0f ? 0x80008000u : 0u, keep = a.scale != 0.0f ? ~0u : 0u;
+        const int col = col0 + lc;
+        const bool live = col < cols.n;
+        const int pos = live ? cols.first_pos + col / share : -1;
+        const u32x4 *from = reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(a.q) +
+                                                            ((size_t)(row0 + col / share) * a.n_heads + head * share + col % share) * D);
 #pragma unroll
-        for (int c = 0; c < NT; ++c) {
-            const int col = col0 + 32 * c + lc;
-            const bool live = col < cols.n;
-            pos[c] = live ? cols.first_pos + col / share : -1;
-            const u32x4 *from = reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(a.q) +
-                                                                ((size_t)(row0 + col / share) * a.n_heads + head * share + col % share) * D);
-#pragma unroll
-            for (int s = 0; s < D / 16; ++s) {
-                u32x4 x = {0, 0, 0, 0};
-                if (live) x = from[2 * s + h];
-                q[c][s] = __builtin_bit_cast(bf16x8, (x ^ sign) & keep);
-            }
+        for (int s = 0; s < D / 16; ++s) {
+            u32x4 x = {0, 0, 0, 0};
+            if (live) x = from[2 * s + h];
+            q[s] = __builtin_bit_cast(bf16x8, (x ^ sign) & keep);
         }
-        f32x16 o[NT][D / 32], s0[NT], s1[NT];
-        float m[NT], l[NT];
+        f32x16 o[D / 32], s0, s1;
+        float m = kLowest, l = 0.0f;
 #pragma unroll
-        for (int c = 0; c < NT; ++c) {
-            m[c] = kLowest, l[c] = 0.0f;
+        for (int j = 0; j < D / 32; ++j)
 #pragma unroll
-            for (int j = 0; j < D / 32; ++j)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[c][j][i] = 0.0f;
-        }
+            for (int i = 0; i < 16; ++i) o[j][i] = 0.0f;
         // tokens in front of this one are all there: 0 if some page is none
         int full = seen.hi;
         for (int i = (seen.lo >> a.c.log_page) + lane; i << a.c.log_page < seen.hi; i += 64)
@@ -775,20 +767,17 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_prompt_kernel(Att
         auto convert = [&](int tile) {
             convert_tile<D>(s_tiles.k[tile % 2], s_tiles.v[tile % 3], regs, wave, limit - (first + tile * kPromptTile + 16 * wave), n, g);
         };
-        auto scores = [&](f32x16 (&s)[NT], int tile, int half) {
+        auto scores = [&](f32x16 &s, int tile, int half) {
             const uint32_t *const from = s_tiles.k[tile % 2];
 #pragma unroll
-            for (int c = 0; c < NT; ++c)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[c][i] = 0.0f;
+            for (int i = 0; i < 16; ++i) s[i] = 0.0f;
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {
                 const bf16x8 x = *reinterpret_cast<const bf16x8 *>(&from[((2 * k + h) * kPromptTile + 32 * half + row) * 4]);
-#pragma unroll
-                for (int c = 0; c < NT; ++c) s[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[c][k], s[c], 0, 0, 0);
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[k], s, 0, 0, 0);
             }
         };
-        auto weights = [&](f32x16 (&s)[NT], bf16x8 (&p)[NT][2], int tile, int half) {
+        auto weights = [&](f32x16 &s, bf16x8 (&p)[2], int tile, int half) {
             const int t0 = first + tile * kPromptTile + 32 * half;
             if (!(t0 + 32 <= full && t0 + 31 <= wave_first && wave_last - t0 < cols.window)) {
                 int lim0 = seen.hi, lim1 = seen.hi;
@@ -797,52 +786,46 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_prompt_kernel(Att
                     if (t0 + 16 < seen.hi && (unsigned)table[(t0 + 16) >> a.c.log_page] >= (unsigned)a.c.n_pages) lim1 = 0;
                 }
 #pragma unroll
-                for (int c = 0; c < NT; ++c)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int t = t0 + (8 * (i / 4) ^ 8 * h) + 4 * h + i % 4;
-                        if (!(t < (i < 8 ? lim0 : lim1) && t <= pos[c] && pos[c] - t < cols.window)) s[c][i] = -INFINITY;
-                    }
-            }
-#pragma unroll
-            for (int c = 0; c < NT; ++c) {
-                float top = s[c][0];
-#pragma unroll
-                for (int i = 1; i < 16; ++i) top = fmaxf(top, s[c][i]);
-                top *= scale;
-                if (__any(top > m[c] + kSlack)) {
-                    top = fmaxf(top, __shfl_xor(top, 32, kWave));
-                    const float next = fmaxf(m[c], top), factor = __builtin_amdgcn_exp2f(m[c] - next);
-                    m[c] = next;
-                    l[c] *= factor;
-#pragma unroll
-                    for (int j = 0; j < D / 32; ++j) o[c][j] *= factor;
-                }
-                float x[16];
-#pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    x[i] = __builtin_amdgcn_exp2f(fmaf(s[c][i], scale, -m[c]));
-                    l[c] += x[i];
+                    const int t = t0 + (8 * (i / 4) ^ 8 * h) + 4 * h + i % 4;
+                    if (!(t < (i < 8 ? lim0 : lim1) && t <= pos && pos - t < cols.window)) s[i] = -INFINITY;
                 }
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    p[c][j] = as_bf16x8(pack_bf16(x[8 * j], x[8 * j + 1]), pack_bf16(x[8 * j + 2], x[8 * j + 3]), pack_bf16(x[8 * j + 4], x[8 * j + 5]),
-                                        pack_bf16(x[8 * j + 6], x[8 * j + 7]));
             }
+            float top = s[0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+            top *= scale;
+            if (__any(top > m + kSlack)) {
+                top = fmaxf(top, __shfl_xor(top, 32, kWave));
+                const float next = fmaxf(m, top), factor = __builtin_amdgcn_exp2f(m - next);
+                m = next;
+                l *= factor;
+#pragma unroll
+                for (int j = 0; j < D / 32; ++j) o[j] *= factor;
+            }
+            float x[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                x[i] = __builtin_amdgcn_exp2f(fmaf(s[i], scale, -m));
+                l += x[i];
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                p[j] = as_bf16x8(pack_bf16(x[8 * j], x[8 * j + 1]), pack_bf16(x[8 * j + 2], x[8 * j + 3]), pack_bf16(x[8 * j + 4], x[8 * j + 5]),
+                                 pack_bf16(x[8 * j + 6], x[8 * j + 7]));
         };
-        auto values = [&](bf16x8 (&p)[NT][2], int tile, int half) {
+        auto values = [&](bf16x8 (&p)[2], int tile, int half) {
             const uint32_t *const from = s_tiles.v[tile % 3];
 #pragma unroll
             for (int j = 0; j < D / 32; ++j)
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const bf16x8 x = *reinterpret_cast<const bf16x8 *>(&from[((2 * (2 * half + k) + h) * D + 32 * j + lc) * 4]);
-#pragma unroll
-                    for (int c = 0; c < NT; ++c) o[c][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p[c][k], o[c][j], 0, 0, 0);
+                    o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p[k], o[j], 0, 0, 0);
                 }
         };
 
-        bf16x8 p[NT][2];
+        bf16x8 p[2];
         if (n_tiles > tile0) {
             load(tile0);
             if (parts > 1 && threadIdx.x == 0) announce(counter, counted, tag);
@@ -876,8 +859,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_prompt_kernel(Att
             for (int j = 0; j < D / 32; ++j)
 #pragma unroll
                 for (int b = 0; b < 4; ++b)
-                    store_past(mine, 4 * j + b, lane, f32x4{o[0][j][4 * b], o[0][j][4 * b + 1], o[0][j][4 * b + 2], o[0][j][4 * b + 3]});
-            store_past(mine, kVectors - 1, lane, f32x4{m[0], l[0], 0.0f, 0.0f});
+                    store_past(mine, 4 * j + b, lane, f32x4{o[j][4 * b], o[j][4 * b + 1], o[j][4 * b + 2], o[j][4 * b + 3]});
+            store_past(mine, kVectors - 1, lane, f32x4{m, l, 0.0f, 0.0f});
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's stores are acknowledged
             __syncthreads();
             int *const s_last = reinterpret_cast<int *>(s_raw);
@@ -886,31 +869,28 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_prompt_kernel(Att
             const bool last = *s_last;
             __syncthreads();  // (the next unit's tiles take its place)
             if (!last) continue;
-            m[0] = kLowest, l[0] = 0.0f;
+            m = kLowest, l = 0.0f;
 #pragma unroll
             for (int j = 0; j < D / 32; ++j)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) o[0][j][i] = 0.0f;
+                for (int i = 0; i < 16; ++i) o[j][i] = 0.0f;
 #pragma unroll 1
             for (int i = 0; i < parts; ++i) {
                 const f32x4 *from = pieces + (size_t)i * 4 * kVectors * 64;
                 f32x4 x[kVectors];
 #pragma unroll
                 for (int v = 0; v < kVectors; ++v) x[v] = load_past(from, (v * 64 + lane) * 16);
-                const float top = fmaxf(m[0], x[kVectors - 1][0]);
-                const float f = __builtin_amdgcn_exp2f(m[0] - top), e = __builtin_amdgcn_exp2f(x[kVectors - 1][0] - top);
-                m[0] = top, l[0] = f * l[0] + e * x[kVectors - 1][1];
+                const float top = fmaxf(m, x[kVectors - 1][0]);
+                const float f = __builtin_amdgcn_exp2f(m - top), e = __builtin_amdgcn_exp2f(x[kVectors - 1][0] - top);
+                m = top, l = f * l + e * x[kVectors - 1][1];
 #pragma unroll
                 for (int j = 0; j < D / 32; ++j)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) o[0][j][r] = f * o[0][j][r] + e * x[4 * j + r / 4][r % 4];
+                    for (int r = 0; r < 16; ++r) o[j][r] = f * o[j][r] + e * x[4 * j + r / 4][r % 4];
             }
         }
-#pragma unroll
-        for (int c = 0; c < NT; ++c) {
-            const int col = col0 + 32 * c + lc;
-            const float sum = l[c] + __shfl_xor(l[c], 32, kWave), by = sum > 0.0f ? 1.0f / sum : 0.0f;
-            if (col >= cols.n) continue;
+        const float sum = l + __shfl_xor(l, 32, kWave), by = sum > 0.0f ? 1.0f / sum : 0.0f;
+        if (live) {
             uint16_t *y = static_cast<uint16_t *>(a.y) + ((size_t)(row0 + col / share) * a.n_heads + head * share + col % share) * D;
             // channels r D/16 .. of the lane's eight r: the places c 16 + r of all c
 #pragma unroll
@@ -920,7 +900,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_prompt_kernel(Att
                     constexpr int C = D / 16;
                     uint32_t w[C / 2];
 #pragma unroll
-                    for (int e = 0; e < C; e += 2) w[e / 2] = pack_bf16(o[c][e / 2][4 * b + i] * by, o[c][e / 2][8 + 4 * b + i] * by);
+                    for (int e = 0; e < C; e += 2) w[e / 2] = pack_bf16(o[e / 2][4 * b + i] * by, o[e / 2][8 + 4 * b + i] * by);
                     uint32_t *to = reinterpret_cast<uint32_t *>(y + (8 * b + 4 * h + i) * C);
                     if constexpr (C == 4) *reinterpret_cast<u32x2 *>(to) = u32x2{w[0], w[1]};
                     else
