@@ -253,7 +253,6 @@ struct WaveSums {
 constexpr int kBuffers = 2;   // steps that a wave has in registers: the one it uses and the next
 constexpr int kRound = 128;   // tokens of a round: a step of each of the four waves
 constexpr int kWorkgroups = 512;
-constexpr int kPieces = 32;    // of a unit, as a rule
 
 // How the work is dealt.  A unit is one kv head's block of 16 columns of one sequence: a number of rounds over the tokens that the
 // sequence's columns see.  All units stand in one row (sequence, block, head), and every workgroup takes the same number of rounds of
@@ -913,14 +912,16 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_prompt_kernel(Att
 }
 
 // Two workgroups to a compute unit hide each other's beginnings and ends, but cost the last of a unit's workgroups more pieces to join:
-// two where there are 128 units, else one, and 32 pieces of a unit at most.  (Microseconds with 512 / 256 workgroups, D 128: 8 sequences x
-// 40 heads x 4096 tokens 26.3 / 30.6, 64 x 8 x 1000 26.8 / 31.0; 2 x 8 x 131072 47.5 / 45.6, 1 x 8 x 131072 33.6 / 29.9, 1 x 32 x 4096 10.8 /
-// 10.1; 1 x 1 x 131072 80 with 512 pieces, 46 with 256, 29 with 32.)  D = 256 has registers for one.
+// two where there are 128 units, else one, and at most twice the square root of a unit's rounds (32 at least) for its pieces.  (Microseconds
+// with 512 / 256 workgroups, D 128: 8 sequences x 40 heads x 4096 tokens 25.8 / 30.6, 64 x 8 x 1000 21.2 / 31.0; 2 x 8 x 131072 47.5 / 43,
+// 1 x 8 x 131072 33.6 / 27.9, 1 x 32 x 4096 10.8 / 9.7.  With 16, 32, 48, 64, 96 pieces: 1 x 1 x 131072 46.9, 29.2, 26.6, 23.7, 25.1; 2 x 2 x
+// 60000 23.8, 19.0, 17.2, 17.7, 17.7; 1 x 1 x 16000 14.5, 13.0, 15.5, 15.8, 19.5.)  D = 256 has registers for one.
 int attention_workgroups(int n_seq, int n_heads, int n_kv, int d, int max_new, long long max_context)
 {
     const long long blocks = ((long long)max_new * (n_heads / n_kv) + 15) / 16, rounds = (max_context + kRound - 1) / kRound;
     const long long units = std::max((long long)n_seq * n_kv * blocks, 1ll);
-    return (int)std::min(units * std::min<long long>(rounds, kPieces), units >= 128 && d < 256 ? (long long)kWorkgroups : kWorkgroups / 2ll);
+    const long long pieces = std::max(32ll, (long long)(2.0 * sqrt((double)rounds)));  // of a unit
+    return (int)std::min(units * std::min(rounds, pieces), units >= 128 && d < 256 ? (long long)kWorkgroups : kWorkgroups / 2ll);
 }
 
 // From this many bytes of cache on (at the longest length) codes are loaded past the caches: what one layer's attention reads, other
