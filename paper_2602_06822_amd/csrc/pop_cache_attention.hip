@@ -132,17 +132,20 @@ __device__ __forceinline__ void store_y2(const AttentionArgs &a, size_t at, floa
     else *reinterpret_cast<float2 *>(static_cast<float *>(a.y) + at) = {x, y};
 }
 
-// Sum over the lanes up to this one, of numbers that are not negative; no more than INT_MAX.
-template <int CTRL, int ROWS>
-__device__ __forceinline__ int dpp_add(int v)
+// Sum over the lanes up to this one, of numbers that are not negative, no more than INT_MAX; or the largest of them.
+template <bool MOST, int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_step(int v)
 {
-    return __builtin_elementwise_add_sat(v, __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false));
+    const int from = __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+    return MOST ? max(v, from) : __builtin_elementwise_add_sat(v, from);
 }
+template <bool MOST = false>
 __device__ __forceinline__ int wave_scan(int v)
 {
-    v = dpp_add<0x111, 0xf>(v), v = dpp_add<0x112, 0xf>(v), v = dpp_add<0x114, 0xf>(v), v = dpp_add<0x118, 0xf>(v);  // rows of 16
-    v = dpp_add<0x142, 0xa>(v);                                                                                      // pairs of rows
-    return dpp_add<0x143, 0xc>(v);
+    v = dpp_step<MOST, 0x111, 0xf>(v), v = dpp_step<MOST, 0x112, 0xf>(v);  // rows of 16
+    v = dpp_step<MOST, 0x114, 0xf>(v), v = dpp_step<MOST, 0x118, 0xf>(v);
+    v = dpp_step<MOST, 0x142, 0xa>(v);  // pairs of rows
+    return dpp_step<MOST, 0x143, 0xc>(v);
 }
 
 constexpr int kNoWindow = 0x7fffffff, kMostTokens = 1 << 30;  // (a sequence's table holds no more: checked by the caller)
@@ -257,7 +260,7 @@ constexpr int kWorkgroups = 512;
 // How the work is dealt.  A unit is one kv head's block of 16 columns of one sequence: a number of rounds over the tokens that the
 // sequence's columns see.  All units stand in one row (sequence, block, head), and every workgroup takes the same number of rounds of
 // it, wherever units begin and end: ragged batches and single long sequences load all compute units alike.  A piece of a unit
-// is what one workgroup has of it.
+// is what one workgroup has of it.  Where that gains less than pieces cost, workgroups take units.
 struct SequenceWork {
     int rounds;  // of a unit
     int blocks;
@@ -274,6 +277,16 @@ __device__ __forceinline__ SequenceWork sequence_work(const AttentionArgs &a, in
     w.seen = seen_tokens(w.cols, 0, w.cols.n);
     w.rounds = max((w.seen.hi - w.seen.lo + kRound - 1) / kRound, 1);
     return w;
+}
+
+// Whether whole units are dealt: pieces cost as much as about 7 rounds of a compute unit (4 where nobody has more than one round), so the
+// compute unit with the longest unit may have that many more than the even share.  Microseconds, pieces / units, D 128, 4 query heads to
+// a kv head: 64 sequences x 8 kv heads x 500 tokens 15.5 / 9.3, x 1000 19.6 / 12.5, x 4000 38.3 / 35.5; 8 x 32 x 500 13.4 / 7.1, x 2000 17.7 / 14.3, x
+// 4000 23.9 / 23.2; 8 x 8 x 1000 11.3 / 8.9, x 2000 12.1 / 13.2; 1 x 8 x 500 8.0 / 7.9, x 1000 8.1 / 9.0, x 4000 8.9 / 21.3.
+__device__ __forceinline__ bool deal_units(int units, int rounds, int longest)
+{
+    const float all = (float)rounds, on_average = all * __builtin_amdgcn_rcpf((float)max(units, 1));
+    return (float)((units - 1) >> 8) * on_average + (float)longest <= all * (1.0f / 256) + (rounds <= 256 ? 4.5f : 7.75f);
 }
 
 // What workgroups hand to each other goes past the caches (scope of the device), 16 bytes a lane at a time: the descriptor is a wave's.
@@ -333,32 +346,37 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_kernel(
     const float scale = a.scale != 0.0f ? fabsf(a.scale) * kLog2e : 1.0f;
     const TileOffsets<D> offsets(n, g);
 
-    // this workgroup's rounds, and the sequence that the first of them belongs to: every wave sums all sequences' for itself, a lane
-    // those of a run of sequences
+    // what there is: every wave sums all sequences' work for itself, a lane that of a run of sequences
     const int per_lane = (a.n_seq + 63) / 64;
-    int mine = 0, my_start = 0, my_next = 0, my_context = 0;
+    int my_rounds = 0, my_units = 0, my_longest = 0, my_start = 0, my_next = 0, my_context = 0;
     for (int i = 0; i < per_lane; ++i) {
         const int s = lane * per_lane + i;
         if (s < a.n_seq) {
             my_start = a.start[s], my_next = a.start[s + 1], my_context = a.context[s];
             const SequenceWork w = sequence_work(a, my_start, my_next, my_context, share);
-            mine = __builtin_elementwise_add_sat(mine, w.rounds * w.blocks * n_kv);
+            my_rounds = __builtin_elementwise_add_sat(my_rounds, w.rounds * w.blocks * n_kv);
+            my_units = __builtin_elementwise_add_sat(my_units, w.blocks * n_kv);
+            my_longest = max(my_longest, w.rounds);
         }
     }
-    const int upto = wave_scan(mine);
-    const unsigned total = (unsigned)__builtin_amdgcn_readlane(upto, 63);
-    const unsigned n_wg = min(gridDim.x, total);
+    const int rounds_upto = wave_scan(my_rounds), units_upto = wave_scan(my_units);
+    const int all_rounds = __builtin_amdgcn_readlane(rounds_upto, 63), all_units = __builtin_amdgcn_readlane(units_upto, 63);
+    const bool by_units =
+        __builtin_amdgcn_readfirstlane(deal_units(all_units, all_rounds, __builtin_amdgcn_readlane(wave_scan<true>(my_longest), 63)));
+    // this workgroup's share of them, and the sequence that it begins with
+    const int upto = by_units ? units_upto : rounds_upto;
+    const unsigned total = by_units ? all_units : all_rounds, n_wg = min(gridDim.x, total);
     if (blockIdx.x >= n_wg) return;
-    // the first `longer` workgroups have one round more than the others
+    // the first `longer` workgroups have one more than the others
     const unsigned fewest = total / n_wg, longer = total - fewest * n_wg;
     const auto workgroup_of = [&](unsigned round) {
         const unsigned of_longer = longer * (fewest + 1);
         return (int)(round < of_longer ? round / (fewest + 1) : longer + (round - of_longer) / fewest);
     };
-    const int first_round = blockIdx.x * fewest + min(blockIdx.x, longer), end = first_round + (int)fewest + (blockIdx.x < longer);
-    int at = first_round;
+    const int first_of_all = blockIdx.x * fewest + min(blockIdx.x, longer), end = first_of_all + (int)fewest + (blockIdx.x < longer);
+    int at = first_of_all;
     const int owner = __ffsll((unsigned long long)__ballot(upto > at)) - 1;
-    int seq = owner * per_lane, seq_at = owner > 0 ? __builtin_amdgcn_readlane(upto, owner - 1) : 0;  // the sequence's first round
+    int seq = owner * per_lane, seq_at = owner > 0 ? __builtin_amdgcn_readlane(upto, owner - 1) : 0;  // where the sequence begins
     unsigned long long *const counters = reinterpret_cast<unsigned long long *>(partial_of<D>(a, 2 * (int)gridDim.x));
     const unsigned page_bytes = n_kv * (a.c.page >> 4) * kTile;
 
@@ -371,13 +389,13 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_kernel(
             start = a.start[seq], next = a.start[seq + 1], context = a.context[seq];
         }
         const SequenceWork w = sequence_work(a, start, next, context, share);
-        const int of_seq = w.rounds * w.blocks * n_kv;
+        const int dealt = by_units ? 1 : w.rounds, of_seq = dealt * w.blocks * n_kv;  // (of a unit, of the sequence's)
         if ((unsigned)at >= (unsigned)seq_at + (unsigned)of_seq) {
             seq_at += of_seq, ++seq;
             continue;
         }
-        const int unit = (int)((unsigned)(at - seq_at) / (unsigned)w.rounds), block = (int)((unsigned)unit / (unsigned)n_kv), head = unit - block * n_kv;
-        const int unit_at = seq_at + unit * w.rounds, begin = at - unit_at, stop = min(w.rounds, end - unit_at);
+        const int unit = (int)((unsigned)(at - seq_at) / (unsigned)dealt), block = (int)((unsigned)unit / (unsigned)n_kv), head = unit - block * n_kv;
+        const int unit_at = seq_at + unit * dealt, begin = at - unit_at, stop = by_units ? w.rounds : min(w.rounds, end - unit_at);
         const Columns &cols = w.cols;
         const SeenTokens seen = seen_tokens(cols, block * 16, min(block * 16 + 16, cols.n));
         const scalar_ints table = (scalar_ints)(uintptr_t)(a.table + (size_t)seq * a.stride);
@@ -422,7 +440,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_kernel(
                 if (live) q[i] = q_from[i];
             }
             unsigned long long counted = 0;
-            const bool first_unit = at == first_round && threadIdx.x == 0;
+            const bool first_unit = at == first_of_all && !by_units && threadIdx.x == 0;
             if (first_unit) counted = coherent_load(counters + blockIdx.x);
 #pragma unroll
             for (int i = 0; i < kBuffers - 1; ++i) {
@@ -570,7 +588,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_kernel(
                 }
             }
         }
-        at = unit_at + stop;
+        at = unit_at + (by_units ? 1 : stop);
     }
 }
 
@@ -913,7 +931,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_prompt_kernel(Att
 
 // Two workgroups to a compute unit hide each other's beginnings and ends, but cost the last of a unit's workgroups more pieces to join:
 // two where there are 128 units, else one, and at most twice the square root of a unit's rounds (32 at least) for its pieces.  (Microseconds
-// with 512 / 256 workgroups, D 128: 8 sequences x 40 heads x 4096 tokens 25.8 / 30.6, 64 x 8 x 1000 21.2 / 31.0; 2 x 8 x 131072 47.5 / 43,
+// with 512 / 256 workgroups, D 128: 8 sequences x 40 heads x 4096 tokens 25.8 / 30.6, 64 x 8 x 1000, by pieces, 21.2 / 31.0; 2 x 8 x 131072 47.5 / 43,
 // 1 x 8 x 131072 33.6 / 27.9, 1 x 32 x 4096 10.8 / 9.7.  With 16, 32, 48, 64, 96 pieces: 1 x 1 x 131072 46.9, 29.2, 26.6, 23.7, 25.1; 2 x 2 x
 // 60000 23.8, 19.0, 17.2, 17.7, 17.7; 1 x 1 x 16000 14.5, 13.0, 15.5, 15.8, 19.5.)  D = 256 has registers for one.
 int attention_workgroups(int n_seq, int n_heads, int n_kv, int d, int max_new, long long max_context)

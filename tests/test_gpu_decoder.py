@@ -431,6 +431,22 @@ def test_another_stream_and_a_replayed_graph(pop):
         assert all(torch.equal(a, b) for a, b in zip(got, (y1[:17 + i], slots, so, to, po, cache)))
 
 
+@pytest.mark.parametrize("dtype,ydtype", [(BF16, BF16), (F32, F32)])
+@pytest.mark.parametrize("n_seq,longest,window", [(150, 0, 0), (150, 9000, 0), (40, 3000, 700), (70, 1100, 0), (260, 0, 31)])
+def test_many_sequences(pop, dtype, ydtype, n_seq, longest, window):
+    """Dealt by whole units and by pieces; several sequences to a lane; empty ones and ones without new tokens."""
+    rng = np.random.default_rng(n_seq + longest)
+    context = rng.integers(0, 300, n_seq)
+    context[rng.integers(0, n_seq)] = max(longest, 1)
+    new = np.minimum(rng.integers(0, 4, n_seq), context)
+    c = Cached(pop, rng, context.tolist(), 3, 64, 16)
+    start = np.concatenate([[0], np.cumsum(new)])
+    q = _queries(rng, start[-1], 9, 64, dtype)
+    y = _attend(pop, c, q, start, dtype, ydtype, 9, 0.125, window)
+    _check(c, y, q, start, dtype, ydtype, 0.125, window)
+    assert torch.equal(y, _attend(pop, c, q, start, dtype, ydtype, 9, 0.125, window))
+
+
 @pytest.mark.parametrize("page,window", [(16, 0), (32, 77)])
 def test_chunks_with_the_widest_heads(pop, page, window):
     """Units for every compute unit; a page that is none, a context shorter than the chunk, an empty sequence."""
