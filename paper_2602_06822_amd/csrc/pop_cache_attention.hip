@@ -973,11 +973,20 @@ PromptGrid prompt_grid(int n_tokens, int n_seq, int n_heads, int n_kv, int max_n
     return g;
 }
 
-// Columns of a kv head from which the prompt kernel takes over.  Microseconds, general / prompt kernel: 32 kv heads x 6000 tokens, one
-// sequence 16 columns 29.9 / 30.3, 32 columns 36.7 / 30.4, 128 columns 56.8 / 34.3; 8 kv heads, 32 columns 28.1 / 28.6; 700 tokens 22.5 / 13.8.
-// D = 256 has registers and LDS for one workgroup to a compute unit, so it takes whole blocks, and units for all compute units: two chunks
-// of 1024 tokens x 32 heads over 8 kv heads x 4096 tokens 433 / 290; but 36 columns of 8 kv heads over 16000 tokens 42 / 144.
-constexpr int kPromptColumns = 32;
+// Whether the prompt kernel takes a call: its blocks of 128 columns need half the time for each column, but it begins 11 us later, and 19 where
+// units are few and their parts have to be joined.  A round of 128 tokens for all compute units: 0.57 us for a unit of 16 columns each, 2.4 for a
+// block each.  Microseconds, general / prompt kernel, D 128, 4 query heads to each of 8 kv heads: 4 sequences x 512 new tokens 36.3 / 24.8, over 3000
+// cached ones 126 / 94; 1 x 512 17.5 / 21.3, over 1000 32.7 / 31.2, over 3000 61 / 49; 1 x 128 over 700 10.0 / 20.0, over 16000 78 / 62; 32 heads
+// of their own, 32 new tokens over 60000 91 / 121.  D = 256 has registers and LDS for one workgroup to a compute unit, so it takes whole blocks, and
+// units for all compute units (two chunks of 1024 over 4096: 433 / 290).
+constexpr int kPromptColumns = 65;  // with fewer it never does
+bool takes_prompt(const PromptGrid &g, int n_tokens, int n_seq, int n_heads, int n_kv, int d, int max_new, long long max_context)
+{
+    const long long share = n_heads / n_kv, columns = max_new * share, blocks = (long long)g.blocks * n_kv;
+    if (columns < kPromptColumns || (d == 256 && (columns < 128 || blocks < 256))) return false;
+    const double units = (double)n_kv * std::min((columns + 15) / 16 * n_seq, n_tokens * share / 16 + n_seq), rounds = (double)((max_context + kRound - 1) / kRound);
+    return rounds * (0.57 * units - 2.4 * (double)blocks) > 256.0 * (blocks < 256 ? 19.0 : 11.0);
+}
 
 template <int D>
 hipError_t launch_prompt(const AttentionArgs &a, const PromptGrid &g, hipStream_t s)
@@ -993,10 +1002,10 @@ template <int D>
 hipError_t launch_d(const AttentionArgs &a, hipStream_t s)
 {
     const long long seen = a.window > 0 ? std::min((long long)a.max_context, (long long)a.window + a.max_new + 31) : a.max_context;
-    if (const long long columns = (long long)a.max_new * (a.n_heads / a.c.n_kv); a.q_bf16 && a.y_bf16 && columns >= kPromptColumns) {
+    if (a.q_bf16 && a.y_bf16) {
         PromptGrid g = prompt_grid(a.n_tokens, a.n_seq, a.n_heads, a.c.n_kv, a.max_new, seen);
         if (D == 256) g.splits = 1;
-        if (D < 256 || (columns >= 128 && g.blocks * a.c.n_kv >= 256)) return launch_prompt<D>(a, g, s);
+        if (takes_prompt(g, a.n_tokens, a.n_seq, a.n_heads, a.c.n_kv, D, a.max_new, seen)) return launch_prompt<D>(a, g, s);
     }
     const unsigned grid = (unsigned)attention_workgroups(a.n_seq, a.n_heads, a.c.n_kv, D, a.max_new, seen);
     const unsigned long long tag = launch_tag();

@@ -431,6 +431,78 @@ def test_another_stream_and_a_replayed_graph(pop):
         assert all(torch.equal(a, b) for a, b in zip(got, (y1[:17 + i], slots, so, to, po, cache)))
 
 
+LARGE = dict(max_new=2048, max_context=1 << 19)  # sizes for which blocks of 128 columns are taken, whatever the chunks really have
+
+
+@pytest.mark.parametrize("window", [0, 60])
+@pytest.mark.parametrize("heads,n_kv,d,page,context,new", [
+    (4, 4, 128, 16, [240, 7, 400, 0], [200, 3, 380, 0]), (6, 2, 64, 64, [130, 64, 33], [70, 64, 5]), (5, 1, 128, 32, [300, 1], [150, 1]),
+    (2, 1, 128, 64, [2900, 65], [130, 65]), (3, 3, 64, 32, [1500], [97]), (16, 1, 64, 16, [63, 64, 65, 127, 129], [9, 8, 7, 33, 5])])
+def test_blocks_of_128_columns(pop, window, heads, n_kv, d, page, context, new):
+    rng = np.random.default_rng(d + window + len(context))
+    c = Cached(pop, rng, context, n_kv, d, page)
+    start = np.concatenate([[0], np.cumsum(new)])
+    q = _queries(rng, start[-1], heads, d, BF16)
+    for scale in (0.07, -0.4, 0.0):
+        y = _attend(pop, c, q, start, BF16, BF16, heads, scale, window, **LARGE)
+        _check(c, y, q, start, BF16, BF16, scale, window)
+    assert torch.equal(y, _attend(pop, c, q, start, BF16, BF16, heads, scale, window, **LARGE))
+    # pages that are none, a context shorter than its new tokens
+    table = c.table.copy()
+    table[0, ::3] = -1
+    there = [np.repeat((t >= 0) & (t < c.n_pages), page) for t in table]
+    y = _attend(pop, c, q, start, BF16, BF16, heads, 0.07, window, table=table, **LARGE)
+    _check(c, y, q, start, BF16, BF16, 0.07, window, there=there)
+    short = [new[0] // 2] + context[1:]
+    y = _attend(pop, c, q, start, BF16, BF16, heads, 0.07, window, context=short, **LARGE)
+    _check(c, y, q, start, BF16, BF16, 0.07, window, context=short)
+    assert (f64(y)[: new[0] - new[0] // 2] == 0).all()
+
+
+@pytest.mark.parametrize("page,window", [(16, 0), (32, 77)])
+def test_blocks_of_128_columns_with_the_widest_heads(pop, page, window):
+    rng = np.random.default_rng(page + 1)
+    c = Cached(pop, rng, [301, 200], 64, 256, page)
+    start = np.array([0, 250, 450])
+    q = _queries(rng, 450, 64, 256, BF16)
+    table = c.table.copy()
+    table[0, 64 // page] = -1
+    there = [np.repeat((t >= 0) & (t < c.n_pages), page) for t in table]
+    y = _attend(pop, c, q, start, BF16, BF16, 64, 0.06, window, table=table, **LARGE)
+    _check(c, y, q, start, BF16, BF16, 0.06, window, there=there)
+
+
+def test_blocks_of_128_columns_in_a_replayed_graph(pop):
+    """Units that several workgroups share; other work uses the workspace in between."""
+    rng = np.random.default_rng(13)
+    c = Cached(pop, rng, [2900, 300], 2, 128, 32)
+    start = np.array([0, 64, 94])
+    q, y = _queries(rng, 94, 8, 128, BF16), torch.zeros(94, 8, 128, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(pop.pop_cache_attention_workspace(94, 2, 8, 2, 128, *LARGE.values()), dtype=torch.uint8, device="cuda")
+    table, starts, context = i32(c.table), i32(start), i32(c.context)
+
+    def attend(s):
+        pop.pop_cache_attention(q, BF16, 94, c.cache, 2, 128, 32, c.n_pages, table, c.table.shape[1], starts, context, 2, 8, *LARGE.values(), 0.09, 0,
+                                y, BF16, ws, stream=s)
+
+    attend(torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        attend(torch.cuda.current_stream())
+    for i in range(4):
+        q.normal_(generator=torch.Generator(device="cuda").manual_seed(i))
+        ws.fill_(255 - i)
+        y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = y.clone()
+        _check(c, got, q, start, BF16, BF16, 0.09)
+        attend(torch.cuda.current_stream())
+        torch.cuda.synchronize()
+        assert torch.equal(got, y)
+
+
 @pytest.mark.parametrize("dtype,ydtype", [(BF16, BF16), (F32, F32)])
 @pytest.mark.parametrize("n_seq,longest,window", [(150, 0, 0), (150, 9000, 0), (40, 3000, 700), (70, 1100, 0), (260, 0, 31)])
 def test_many_sequences(pop, dtype, ydtype, n_seq, longest, window):
