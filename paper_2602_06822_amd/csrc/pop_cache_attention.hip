@@ -659,7 +659,7 @@ __device__ __forceinline__ bool nth_longest_block(const AttentionArgs &a, int q,
         for (int i = 0; i < per_lane; ++i) {
             Columns c = own;
             if (per_lane > 1) columns(lane * per_lane + i, &c);
-            n += up_to(c, t);
+            n = __builtin_elementwise_add_sat(n, up_to(c, t));
         }
         return n;
     };
@@ -685,8 +685,9 @@ __device__ __forceinline__ bool nth_longest_block(const AttentionArgs &a, int q,
     int mine = count(lo), below = lo > 0 ? count(lo - 1) : 0;
     const int left = q - (all - total(mine)), upto = wave_scan(mine - below);
     const int owner = __ffsll((unsigned long long)__ballot(upto > left)) - 1;
+    if (owner < 0) return false;  // (more blocks than 32 bits count: starts that do not ascend)
     int rest = left - __builtin_amdgcn_readlane(upto - (mine - below), owner), s = owner * per_lane;
-    for (;; ++s) {
+    for (; s < a.n_seq; ++s) {
         Columns c;
         columns(s, &c);
         const int last = up_to(c, lo), n = last - (lo > 0 ? up_to(c, lo - 1) : 0);
@@ -696,6 +697,7 @@ __device__ __forceinline__ bool nth_longest_block(const AttentionArgs &a, int q,
         }
         rest -= n;
     }
+    return false;
 }
 
 // Matrix-bound.  Workgroup: 4 waves, 32 columns each, of one kv head and sequence; 64 tokens at a time are converted to bf16 in LDS, a
