@@ -202,8 +202,8 @@ def beam_select(logits, scores, done, k, pad):
         x = np.where(np.isnan(x), -np.inf, x)
         if scores[b] == -np.inf or not np.isfinite(x).any():
             continue
-        lse = x.max() + np.log(np.exp(x - x.max()).sum())
-        out[b] = np.where(np.isfinite(x), float(scores[b]) + (x - lse), -np.inf)
+        down = x - x.max()  # (first, so that the sum's logarithm is not lost beside masks of a type's lowest value)
+        out[b] = np.where(np.isfinite(x), float(scores[b]) + (down - np.log(np.exp(down).sum())), -np.inf)
     flat = out.ravel()
     at = np.argsort(-flat, kind="stable")[:k]
     return flat[at], at % vocab, at // vocab

@@ -5,7 +5,7 @@
 // maximum of each of its *segments* (its 16 values of a tile).  Then every wave ranks its lanes' maxima: the k-th largest is a lower
 // bound of the row's k-th largest value, and the largest of the workgroup's four bounds leaves about k segments that can hold one of
 // its k best.  Only those are read again, what reaches the bound is listed in LDS, and the lists are ranked.  So a value costs
-// six operations in the pass.  The last workgroup of a request to finish joins the sums and ranks what the others found.
+// seven operations in the pass.  The last workgroup of a request to finish joins the sums and ranks what the others found.
 //
 // 32 requests of 8 rows of 131071 float32, 16 best: 30.3 us, of which the pass is 18 (134 MB, 7 TB/s) and what follows a chain of a
 // dozen latencies: bound 2.1, reading again 1.6, ranking 1.0, handing over 0.9, the last workgroup's join 3.4.  One request of 4 rows of 32000
@@ -38,6 +38,7 @@ __device__ __forceinline__ float ranked_value(unsigned long long w)
     return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
 }
 __device__ __forceinline__ float finite_or_zero(float x) { return x > -INFINITY ? x : 0.0f; }
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2e); }
 
 // The leading BITS bits of the k-th largest of the 64 lanes' values, k <= 64, bit by bit: k lanes at least are not below the result.
 template <int BITS>
@@ -112,7 +113,7 @@ struct BeamShared {
     uint16_t segment[4][kWaveTiles * 64];
     uint32_t bound[4];
     int n[4];
-    float ref[4], sum[4], lse[POP_MAX_BEAMS], was[POP_MAX_BEAMS];
+    float ref[4], sum[4], top[POP_MAX_BEAMS], log[POP_MAX_BEAMS], was[POP_MAX_BEAMS];
     int closed[POP_MAX_BEAMS], last;
 };
 
@@ -204,7 +205,7 @@ __device__ __forceinline__ void join_request(const BeamArgs &a, BeamShared &s, i
             for (int i = i0; i < stretches; i += 16) {
                 const unsigned long long w = coherent_load(st + i);
                 const float next = fmaxf(ref, __uint_as_float((uint32_t)w)), shift = finite_or_zero(next);
-                sum = sum * __builtin_amdgcn_exp2f(ref - shift) + __uint_as_float((uint32_t)(w >> 32)) * __builtin_amdgcn_exp2f(__uint_as_float((uint32_t)w) - shift);
+                sum = sum * exp_of(ref - shift) + __uint_as_float((uint32_t)(w >> 32)) * exp_of(__uint_as_float((uint32_t)w) - shift);
                 ref = next;
             }
         }
@@ -212,13 +213,13 @@ __device__ __forceinline__ void join_request(const BeamArgs &a, BeamShared &s, i
 #pragma unroll
         for (int off = 8; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor(most, off, kWave));
         const float shift = finite_or_zero(most);
-        sum *= __builtin_amdgcn_exp2f(ref - shift);
+        sum *= exp_of(ref - shift);
 #pragma unroll
         for (int off = 8; off > 0; off >>= 1) sum += __shfl_xor(sum, off, kWave);
         if (b < a.beams && i0 == 0) {
             s.was[b] = was;
             s.closed[b] = !open;
-            s.lse[b] = (shift + __builtin_amdgcn_logf(sum)) * kLn2;
+            s.top[b] = shift, s.log[b] = __builtin_amdgcn_logf(sum) * kLn2;
         }
     }
     __syncthreads();
@@ -237,7 +238,7 @@ __device__ __forceinline__ void join_request(const BeamArgs &a, BeamShared &s, i
                 if (w[i]) {
                     token = ~(uint32_t)w[i];
                     const float x = ranked_value(w[i]);
-                    if (x > -INFINITY) score = s.was[b] + (x - s.lse[b]);
+                    if (x > -INFINITY) score = s.was[b] + ((x - s.top[b]) - s.log[b]);
                 }
             } else if (c < total && left < a.k) {  // an ended beam goes on by the padding token; else its tokens are the last resort, in their order
                 const bool ended = a.done && a.done[row0 + b];
@@ -303,8 +304,9 @@ __global__ __launch_bounds__(256, 3) void beam_select_kernel(BeamArgs a, int str
         float odd_value = 0.0f;
         const bool odd = BF16 && (left & 2) && row == a.requests * a.beams - 1;
         if (odd) odd_value = __uint_as_float((uint32_t)static_cast<const uint16_t *>(a.logits)[row_at + a.vocab - 1] << 16);
-        // sum: of 2^(x log2 e - ref); ref is the maximum in those units as it was rounded, so that its rounding cancels
-        float top = -INFINITY, ref = -INFINITY, sum = 0.0f;
+        // sum: of e^(x - top).  The difference comes before the factor log2 e: it is exact where the weight is large, while x log2 e is
+        // rounded by more than an exponential can hold from 2^31 on, and passes float32's range where masks of its lowest value stand.
+        float top = -INFINITY, sum = 0.0f;
         const int first = stretch * tiles + wave;
         u32x4 now[NV], next[NV];
         load(now, first);
@@ -331,13 +333,12 @@ __global__ __launch_bounds__(256, 3) void beam_select_kernel(BeamArgs a, int str
             }
             s.most[wave][mine][lane] = most;
             if (most > top) {
-                const float up = most * kLog2e;
-                sum *= __builtin_amdgcn_exp2f(ref - up);
-                top = most, ref = up;
+                sum *= exp_of(top - most);
+                top = most;
             }
-            const float shift = finite_or_zero(ref);
+            const float shift = finite_or_zero(top);
 #pragma unroll
-            for (int i = 0; i < E; ++i) sum += __builtin_amdgcn_exp2f(fmaf(x[i], kLog2e, -shift));
+            for (int i = 0; i < E; ++i) sum += exp_of(x[i] - shift);
 #pragma unroll
             for (int i = 0; i < NV; ++i) now[i] = next[i];
         }
@@ -375,10 +376,10 @@ __global__ __launch_bounds__(256, 3) void beam_select_kernel(BeamArgs a, int str
         };
         fetch(0);
         // meanwhile the wave's sums
-        float most = ref;
+        float most = top;
 #pragma unroll
         for (int off = 32; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor(most, off, kWave));
-        sum = wave_sum(sum * __builtin_amdgcn_exp2f(ref - finite_or_zero(most)));
+        sum = wave_sum(sum * exp_of(top - finite_or_zero(most)));
         if (lane == 0) s.ref[wave] = most, s.sum[wave] = sum;
         if (threadIdx.x < kMostK) s.found[threadIdx.x] = 0;
 #pragma unroll 1
@@ -420,7 +421,7 @@ __global__ __launch_bounds__(256, 3) void beam_select_kernel(BeamArgs a, int str
         const float all = fmaxf(fmaxf(s.ref[0], s.ref[1]), fmaxf(s.ref[2], s.ref[3]));
         float total = 0.0f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) total += s.sum[w] * __builtin_amdgcn_exp2f(s.ref[w] - finite_or_zero(all));
+        for (int w = 0; w < 4; ++w) total += s.sum[w] * exp_of(s.ref[w] - finite_or_zero(all));
         __syncthreads();
         const size_t part = (size_t)row * stretches + stretch;
         if ((int)threadIdx.x < a.k) hand_over(words_of(a, stretches) + part * a.k + threadIdx.x, s.found[threadIdx.x]);

@@ -680,3 +680,39 @@ def test_selection_over_many_tiles_of_candidates(pop):
     x = torch.from_numpy((np.round(rng.standard_normal((16, 150000)) * 64) / 64).astype(np.float32)).cuda()
     was = torch.from_numpy((-8.3 * np.arange(16)).astype(np.float32)).cuda()
     _check_beams(x, was, None, 16, 64, 0, _select(pop, x, F32, was, None, 16, 64, 0))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("vocab", [70, 2500, 33001])
+def test_logits_of_lowest_and_largest_values(pop, dtype, vocab):
+    """Rows that are masked with finite values, whole and in part, rows far from zero, and a row of largest values."""
+    low = float(torch.finfo(DT[dtype]).min)
+    x = torch.zeros(8, vocab)
+    x[0] = low                       # masked whole: every token is as likely as the others
+    x[1] = low
+    x[1, [3, vocab // 2, vocab - 1]] = torch.tensor([1.0, 0.5, 0.25])
+    x[2] = -1e30
+    x[3] = -1e10
+    x[3, vocab // 3] = 0.0
+    x[4] = -low
+    x[5] = low / 2
+    x[5, :vocab // 2] = low
+    x[6] = -torch.inf
+    x[6, 1:9] = low
+    x[7, 5] = -low                   # the others' scores are lower than float32 goes
+    x = x.cuda().to(DT[dtype])
+    was = torch.tensor([-3.0, -9.0, -30.0, -50.0, -70.0, -90.0, -110.0, -130.0], device="cuda")
+    h = f64(was)
+    for beams in (1, 2, 8):
+        for k in (1, 4, 16):
+            so, to, po = _select(pop, x, dtype, was, None, beams, k, 0)
+            for i in range(8 // beams):
+                rows = slice(i * beams, (i + 1) * beams)
+                s, t, p = orc.beam_select(f64(x[rows]), h[rows], None, k, 0)
+                with np.errstate(over="ignore"):
+                    s = s.astype(np.float32).astype(np.float64)
+                assert np.array_equal(so[i] == -np.inf, s == -np.inf)
+                fin = np.isfinite(s)
+                # 32-bit sums of exponentials (2^-18 of the sum, as above) and roundings of the score
+                assert (np.abs(so[i][fin] - s[fin]) <= 2.0 ** -18 + 2.0 ** -21 * np.abs(s[fin])).all()
+                assert np.array_equal(to[i], t) and np.array_equal(po[i], p)
