@@ -139,11 +139,12 @@ def reorder(table, length, parents, n_beams, page_tokens, ring, pool):
                 copies[g + c] = table[old, blocks[old] - 1], fresh
                 new_table[g + c, blocks[old] - 1] = fresh
             goes_on.add(p)
-    if taken > count:
+    wrong = any(x < 0 or -(-int(x) // page_tokens) > stride for x in length)
+    if wrong or taken > count:
         same = np.full_like(table, -1)
         for r in range(n_seq):
             same[r, :blocks[r]] = table[r, :blocks[r]]
-        return same, np.array(length), np.full((n_seq, 2), -1), ring, tuple(pool), 1
+        return same, np.array(length), np.full((n_seq, 2), -1), ring, tuple(pool), 4 if wrong else 1
     freed = 0
     for g in range(0, n_seq, n_beams):
         keeps = {g + int(p) for p in parents[g:g + n_beams] if 0 <= p < n_beams}

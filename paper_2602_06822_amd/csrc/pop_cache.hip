@@ -285,6 +285,7 @@ constexpr int kReorderBlocks = 256;  // blocks of a request that a workgroup see
 struct ReorderRows {
     int parent[POP_MAX_BEAMS], length[POP_MAX_BEAMS], blocks[POP_MAX_BEAMS], copy[POP_MAX_BEAMS];
     unsigned parented;  // rows that go on, by bit
+    int wrong;          // some row has a negative length, or one that its table row has no room for
 };
 
 // What the request's rows are and which of them take a copy of their parent's last page: where it is partly filled and an earlier row
@@ -298,14 +299,15 @@ __device__ __forceinline__ void reorder_rows(const ReorderArgs &a, int g, Reorde
         r.length[c] = len;
         r.blocks[c] = (int)min(ceil_pages(max(len, 0), a.log_page), (long long)a.stride);
     }
-    if (c == 0) r.parented = 0;
+    if (c == 0) r.parented = 0, r.wrong = 0;
     __syncthreads();
     if (c < a.group) {
         const int p = r.parent[c];
         int copy = 0;
+        if (r.length[c] < 0 || ceil_pages(r.length[c], a.log_page) > a.stride) r.wrong = 1;
         if (p >= 0) {
             const int len = r.length[p];
-            if (len > 0 && (len & ((1 << a.log_page) - 1)) && ceil_pages(len, a.log_page) <= a.stride)
+            if (len > 0 && (len & ((1 << a.log_page) - 1)))
                 for (int b = 0; b < c; ++b) copy |= r.parent[b] == p;
             atomicOr(&r.parented, 1u << p);
         }
@@ -368,7 +370,7 @@ __device__ __forceinline__ int block_sum(int v, int *s_wave, int *before)
 
 // Latency-bound integer work in two launches (one where a single workgroup sees to everything): what each part of the requests gives
 // back and takes has to be known before the first page finds its place in the ring.  W: rows of a request at most.  counts: pages given back,
-// by request and part, then copies by request.  One request of four rows 4.3 us; 64 of eight rows of 250 blocks 4.4 + 8.4.
+// by request and part, then copies by request, -1 where a length is wrong.  One request of four rows 4.3 us; 64 of eight rows of 250 blocks 4.4 + 8.4.
 template <int W>
 __global__ __launch_bounds__(kReorderBlocks) void reorder_count_kernel(ReorderArgs a)
 {
@@ -384,7 +386,7 @@ __global__ __launch_bounds__(kReorderBlocks) void reorder_count_kernel(ReorderAr
         if (blockIdx.y == 0) {
             int n = 0;
             for (int c = 0; c < a.group; ++c) n += s_rows.copy[c];
-            a.counts[gridDim.x * gridDim.y + g] = n;
+            a.counts[gridDim.x * gridDim.y + g] = s_rows.wrong ? -1 : n;
         }
     }
 }
@@ -393,14 +395,14 @@ template <int W>
 __global__ __launch_bounds__(kReorderBlocks) void reorder_rows_kernel(ReorderArgs a, int alone)
 {
     __shared__ ReorderRows s_rows;
-    __shared__ int s_fresh[POP_MAX_BEAMS], s_wave[4], s_sums[4][4];
+    __shared__ int s_fresh[POP_MAX_BEAMS], s_wave[4], s_sums[4][5];
     const int g = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n_groups = gridDim.x, chunks = gridDim.y;
     const int part = g * chunks + blockIdx.y, n_parts = n_groups * chunks, j = blockIdx.y * kReorderBlocks + tid, first = g * a.group;
     const int head = a.pool[0], count = a.pool[1];
     int page[W], at;
     load_entries(a, g, j, page);
     // of the parts and requests in front of this one, and of all: pages given back, copies
-    int freed_before = 0, freed_all = 0, copies_before = 0, copies_all = 0;
+    int freed_before = 0, freed_all = 0, copies_before = 0, copies_all = 0, wrong = 0;
     if (!alone) {
         for (int i = tid; i < n_parts; i += kReorderBlocks) {
             const int n = a.counts[i];
@@ -408,25 +410,28 @@ __global__ __launch_bounds__(kReorderBlocks) void reorder_rows_kernel(ReorderArg
         }
         for (int i = tid; i < n_groups; i += kReorderBlocks) {
             const int n = a.counts[n_parts + i];
-            copies_all += n, copies_before += i < g ? n : 0;
+            copies_all += n, copies_before += i < g ? n : 0, wrong |= n < 0;
         }
         freed_before = wave_sum(freed_before), freed_all = wave_sum(freed_all);
         copies_before = wave_sum(copies_before), copies_all = wave_sum(copies_all);
-        if (lane == 0) s_sums[wave][0] = freed_before, s_sums[wave][1] = freed_all, s_sums[wave][2] = copies_before, s_sums[wave][3] = copies_all;
+        wrong = __any(wrong);
+        if (lane == 0)
+            s_sums[wave][0] = freed_before, s_sums[wave][1] = freed_all, s_sums[wave][2] = copies_before, s_sums[wave][3] = copies_all, s_sums[wave][4] = wrong;
     }
     reorder_rows(a, g, s_rows);  // (its barriers stand behind the sums)
     const unsigned freed = freed_rows(a, s_rows, j, page);
     const int mine = block_sum(__popc(freed), s_wave, &at);
     if (alone) {
-        freed_all = mine;
+        freed_all = mine, wrong = s_rows.wrong;
         for (int c = 0; c < a.group; ++c) copies_all += s_rows.copy[c];
     } else {
         freed_before = freed_all = copies_before = copies_all = 0;
 #pragma unroll
         for (int w = 0; w < 4; ++w)
-            freed_before += s_sums[w][0], freed_all += s_sums[w][1], copies_before += s_sums[w][2], copies_all += s_sums[w][3];
+            freed_before += s_sums[w][0], freed_all += s_sums[w][1], copies_before += s_sums[w][2], copies_all += s_sums[w][3], wrong |= s_sums[w][4];
     }
-    int status = copies_all > count ? POP_PLAN_PAGES : 0;
+    // (where a length is wrong, only that is said: the copies were not counted)
+    int status = wrong ? POP_PLAN_INVALID : copies_all > count ? POP_PLAN_PAGES : 0;
     if (head < 0 || head >= a.n_pages || count < 0 || count > a.n_pages ||
         (long long)count + freed_all > a.n_pages)
         status |= POP_PLAN_INVALID;  // no ring of this many pages: one stands in it and in a row as well, or in rows of two requests

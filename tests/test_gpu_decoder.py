@@ -716,3 +716,21 @@ def test_logits_of_lowest_and_largest_values(pop, dtype, vocab):
                 # 32-bit sums of exponentials (2^-18 of the sum, as above) and roundings of the score
                 assert (np.abs(so[i][fin] - s[fin]) <= 2.0 ** -18 + 2.0 ** -21 * np.abs(s[fin])).all()
                 assert np.array_equal(to[i], t) and np.array_equal(po[i], p)
+
+
+@pytest.mark.parametrize("length,page", [(-1, 16), (49, 16), (2147483647, 16), (-2147483648, 64)])
+@pytest.mark.parametrize("groups,stride", [(1, 3), (3, 3), (2, 300)])
+def test_reorder_says_which_lengths_are_wrong(pop, length, page, groups, stride):
+    """Negative lengths and those that a table's row has no room for, in a row that goes on and in one that does not."""
+    for at in (0, 2 * groups - 1):
+        n = 2 * groups
+        lengths = np.full(n, 20)
+        lengths[at] = length if length != 49 else stride * page + 1
+        table = np.arange(n * stride).reshape(n, stride)
+        n_pages = n * stride + 4
+        for parents in (np.zeros(n, int), np.ones(n, int), np.full(n, -1)):
+            args = (table, lengths, parents, 2, page, np.concatenate([np.arange(n * stride, n_pages), np.zeros(n * stride, int)]), (0, 4))
+            got = _run_reorder(pop, *args)
+            assert got[-1] == 4
+            _same(got, orc.reorder(*args))
+            assert np.array_equal(got[1], lengths) and (got[2] == -1).all() and got[4] == (0, 4) and np.array_equal(got[3], args[5])
