@@ -133,7 +133,7 @@ def reorder(table, length, parents, n_beams, page_tokens, ring, pool):
             old = g + p
             new_len[g + c] = length[old]
             new_table[g + c, :blocks[old]] = table[old, :blocks[old]]
-            if length[old] > 0 and length[old] % page_tokens and p in goes_on:
+            if length[old] > 0 and length[old] % page_tokens and p in goes_on and 0 <= table[old, blocks[old] - 1] < n_pages:
                 fresh = ring[(head + taken) % n_pages]
                 taken += 1
                 copies[g + c] = table[old, blocks[old] - 1], fresh

@@ -284,12 +284,13 @@ constexpr int kReorderBlocks = 256;  // blocks of a request that a workgroup see
 // A request's rows, in LDS.
 struct ReorderRows {
     int parent[POP_MAX_BEAMS], length[POP_MAX_BEAMS], blocks[POP_MAX_BEAMS], copy[POP_MAX_BEAMS];
+    int last[POP_MAX_BEAMS];  // of a row that takes a copy: the page that is copied
     unsigned parented;  // rows that go on, by bit
     int wrong;          // some row has a negative length, or one that its table row has no room for
 };
 
 // What the request's rows are and which of them take a copy of their parent's last page: where it is partly filled and an earlier row
-// goes on in it.  All threads call it; the rows can be read when it returns.
+// goes on in it, and is a page.  All threads call it; the rows can be read when it returns.
 __device__ __forceinline__ void reorder_rows(const ReorderArgs &a, int g, ReorderRows &r)
 {
     const int c = threadIdx.x, row = g * a.group + c;
@@ -309,6 +310,11 @@ __device__ __forceinline__ void reorder_rows(const ReorderArgs &a, int g, Reorde
             const int len = r.length[p];
             if (len > 0 && (len & ((1 << a.log_page) - 1)))
                 for (int b = 0; b < c; ++b) copy |= r.parent[b] == p;
+            if (copy) {
+                const int last = a.table[(size_t)(g * a.group + p) * a.stride + r.blocks[p] - 1];
+                copy = last >= 0 && last < a.n_pages;
+                r.last[c] = last;
+            }
             atomicOr(&r.parented, 1u << p);
         }
         r.copy[c] = copy;
@@ -443,9 +449,10 @@ __global__ __launch_bounds__(kReorderBlocks) void reorder_rows_kernel(ReorderArg
         a.pool_out[1] = status ? count : count - copies_all + freed_all;
     }
     // the copies of this request
+    const auto copied = [&](int c) { return !status && s_rows.copy[c]; };
     if (tid < a.group) {
         int fresh = -1;
-        if (!status && s_rows.copy[tid]) {
+        if (copied(tid)) {
             long long r = (long long)head + copies_before;
             for (int c = 0; c < tid; ++c) r += s_rows.copy[c];
             if (r >= a.n_pages) r -= a.n_pages;
@@ -454,7 +461,7 @@ __global__ __launch_bounds__(kReorderBlocks) void reorder_rows_kernel(ReorderArg
         s_fresh[tid] = fresh;
         if (blockIdx.y == 0) {
             const int row = first + tid, p = s_rows.parent[tid];
-            a.copies[2 * row] = fresh >= 0 ? a.table[(size_t)(first + p) * a.stride + s_rows.blocks[p] - 1] : -1;
+            a.copies[2 * row] = copied(tid) ? s_rows.last[tid] : -1;
             a.copies[2 * row + 1] = fresh;
             a.new_length[row] = status ? a.length[row] : p < 0 ? 0 : s_rows.length[p];
         }
@@ -467,7 +474,7 @@ __global__ __launch_bounds__(kReorderBlocks) void reorder_rows_kernel(ReorderArg
             if (p >= 0) {
 #pragma unroll
                 for (int r = 0; r < W; ++r) entry = r == p ? page[r] : entry;  // (-1 behind a row's last block)
-                if (s_fresh[c] >= 0 && j == s_rows.blocks[p] - 1) entry = s_fresh[c];
+                if (copied(c) && j == s_rows.blocks[p] - 1) entry = s_fresh[c];  // (whatever the ring holds)
             }
             a.new_table[(size_t)(first + c) * a.stride + j] = entry;
         }

@@ -734,3 +734,17 @@ def test_reorder_says_which_lengths_are_wrong(pop, length, page, groups, stride)
             assert got[-1] == 4
             _same(got, orc.reorder(*args))
             assert np.array_equal(got[1], lengths) and (got[2] == -1).all() and got[4] == (0, 4) and np.array_equal(got[3], args[5])
+
+
+def test_reorder_of_last_pages_that_are_none(pop):
+    """What a row did not see its children do not see: no page is taken to copy one that there is not."""
+    table = np.array([[1, -1, -1], [1, 77, -1], [4, 5, 6], [4, 5, 7]])
+    args = (table, np.array([20, 20, 40, 40]), np.array([0, 0, 1, 1]), 2, 16, np.array([0, 8, 2, 3, 0, 0, 0, 0, 0]), (0, 4))
+    got = _run_reorder(pop, *args)
+    _same(got, orc.reorder(*args))
+    assert got[2].tolist() == [[-1, -1], [-1, -1], [-1, -1], [7, 0]] and got[0][1].tolist() == [1, -1, -1]
+    # a ring that holds what is no page: the child has none either, and does not write to its parent's
+    args = args[:5] + (np.array([-5, 8, 2, 3, 0, 0, 0, 0, 0]), (0, 4))
+    got = _run_reorder(pop, *args)
+    _same(got, orc.reorder(*args))
+    assert got[0][3].tolist() == [4, 5, -5]
