@@ -335,7 +335,8 @@ int pop_cache_read(const void *cache, int n_kv_heads, int head_dim, int page_tok
  * q_start[s + 1] - 1 and the last of them is at position context_len[s] - 1; all of them
  * have been written.  A token sees the positions up to its own, with window > 0 only the last `window` of them; query head h reads kv
  * head h / (n_heads / n_kv_heads).  A token that sees nothing (pages that are none, a context shorter than the new tokens)
- * gives zeros.  y: dev [n_tokens][n_heads][head_dim] of ydtype; rows of no sequence are not written.  A sequence whose rows leave
+ * gives zeros.  Scores (scale * q k) stay within +-2.3e38, and the values that a token sees add up to less than 1e26 a channel; beyond that
+ * sums overflow.  y: dev [n_tokens][n_heads][head_dim] of ydtype; rows of no sequence are not written.  A sequence whose rows leave
  * [0, n_tokens) is left out and its rows are undefined.
  * max_new, max_context: the longest that the caller expects; longer ones are right too, but may be slow.  float32 q is
  * taken in full (three bf16 terms of q and of the softmax weights), with bf16 q the weights are rounded to bf16.

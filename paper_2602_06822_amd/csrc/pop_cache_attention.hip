@@ -24,11 +24,27 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef const __attribute__((address_space(4))) int *scalar_ints;  // read by scalar loads
 
 constexpr float kLog2e = 1.44269504088896340736f;
-// A column's maximum starts here: below every finite score, and a difference with it is no NaN.
-constexpr float kLowest = -1.0e37f;
+// A column's maximum starts here: below every score times log2 e down to a score of -2.3e38, and a difference with it is no NaN.
+constexpr float kLowest = -3.40282347e38f;
 // A new maximum is taken only where it exceeds the old one by this many powers of two: until then the weights are at most
 // 2^8, which 32 bits hold as exactly, and O is not rescaled.
 constexpr float kSlack = 8.0f;
+// Weights are 2^(s scale - m), relative to a maximum m that is a rounded product itself: what the rounding takes off stays in all weights of the
+// column and cancels, but from 2^32 on it is more than an exponential can hold.  Beyond kFar a column goes by the power of two below the
+// scale instead, with which the product of its maximum is exact: scores of that size that differ at all (float32 has 24 bits) differ by 2^6
+// or more there, so weights are 1 or nothing by either factor.  (A factor to a lane instead of one for all: four chunks of 955 to 2048 tokens over 2867 to 6144 358 -> 361 us, single
+// tokens as before; rounding the products of such steps alone, in a branch, 368 to 372.)
+constexpr float kFar = 1073741824.0f;
+
+// The column's factor and its maximum in that unit, where the maximum has just become `raw` (a score without the scale) or stays as it is.
+__device__ __forceinline__ void choose_unit(float &by, float &m, float raw, float scale)
+{
+    const float size = fabsf(m * (scale / by));  // (by the scale, whichever unit it is in: a power of two goes in and out without rounding)
+    const float next = m != kLowest && size > kFar ? __uint_as_float(__float_as_uint(scale) & 0x7f800000u) : scale;
+    if (next != by) by = next, m = raw * next;
+}
+// A maximum by the scale, to be compared with those of others.
+__device__ __forceinline__ float by_scale(float m, float by, float scale) { return by == scale ? m : m * (scale / by); }
 
 __device__ __forceinline__ bf16x8 as_bf16x8(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
 {
@@ -182,6 +198,7 @@ struct WaveSums {
     bf16x8 q[D / 32][QT];  // the lane's part of q: channels [g D/4, (g + 1) D/4) of column n
     f32x4 o[D / 16];       // O^T: channel (4 g + i) D/16 + j of column n in o[j][i]
     float m, l;            // maximum that the weights are relative to; the lane's part of their sum
+    float by;              // the factor of the column's scores: the scale, or see choose_unit
 
     // limit[u]: tokens of tile u from this position on are not there; masked: some of the 32 are not seen by some column.
     __device__ __forceinline__ void step(const TileRegs<D> (&r)[2], const int (&limit)[2], bool masked, int t0, int pos, int window, int g,
@@ -212,12 +229,12 @@ struct WaveSums {
             }
         }
         float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-        top *= scale;  // (scale > 0)
-        if (__any(top > m + kSlack)) {
+        if (__any(top * by > m + kSlack)) {  // (by > 0)
             top = fmaxf(top, __shfl_xor(top, 16, kWave));
             top = fmaxf(top, __shfl_xor(top, 32, kWave));
-            const float next = fmaxf(m, top), factor = __builtin_amdgcn_exp2f(m - next);
+            const float next = fmaxf(m, top * by), factor = __builtin_amdgcn_exp2f(m - next);
             m = next;
+            choose_unit(by, m, top, scale);
             l *= factor;
 #pragma unroll
             for (int j = 0; j < D / 16; ++j) o[j] *= factor;
@@ -225,7 +242,7 @@ struct WaveSums {
         float p[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            p[i] = __builtin_amdgcn_exp2f(fmaf(s[i / 4][i % 4], scale, -m));
+            p[i] = __builtin_amdgcn_exp2f(fmaf(s[i / 4][i % 4], by, -m));
             l += p[i];
         }
         bf16x8 w[PT];
@@ -464,7 +481,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_kernel(
             }
 #pragma unroll
             for (int j = 0; j < D / 16; ++j) sums.o[j] = f32x4{0, 0, 0, 0};
-            sums.m = kLowest, sums.l = 0.0f;
+            sums.m = kLowest, sums.l = 0.0f, sums.by = scale;
             for (int t0 = first; t0 < t1;) {
 #pragma unroll
                 for (int i = 0; i < kBuffers; ++i) {
@@ -505,7 +522,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_kernel(
                 }
             }
         };
-        if (g == 0) s_m[wave][n] = sums.m, s_l[wave][n] = sums.l;
+        if (g == 0) s_m[wave][n] = by_scale(sums.m, sums.by, scale), s_l[wave][n] = sums.l;
         float *const part = partial_of<D>(a, 2 * blockIdx.x + (begin == 0));
 #pragma unroll
         for (int pass = 0; pass < D / kPass; ++pass) {
@@ -759,6 +776,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_prompt_kernel(Att
         }
         f32x16 o[D / 32], s0, s1;
         float m = kLowest, l = 0.0f;
+        float by = scale;  // (see choose_unit)
 #pragma unroll
         for (int j = 0; j < D / 32; ++j)
 #pragma unroll
@@ -813,11 +831,11 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_prompt_kernel(Att
             float top = s[0];
 #pragma unroll
             for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
-            top *= scale;
-            if (__any(top > m + kSlack)) {
+            if (__any(top * by > m + kSlack)) {
                 top = fmaxf(top, __shfl_xor(top, 32, kWave));
-                const float next = fmaxf(m, top), factor = __builtin_amdgcn_exp2f(m - next);
+                const float next = fmaxf(m, top * by), factor = __builtin_amdgcn_exp2f(m - next);
                 m = next;
+                choose_unit(by, m, top, scale);
                 l *= factor;
 #pragma unroll
                 for (int j = 0; j < D / 32; ++j) o[j] *= factor;
@@ -825,7 +843,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_prompt_kernel(Att
             float x[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                x[i] = __builtin_amdgcn_exp2f(fmaf(s[i], scale, -m));
+                x[i] = __builtin_amdgcn_exp2f(fmaf(s[i], by, -m));
                 l += x[i];
             }
 #pragma unroll
@@ -879,7 +897,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_prompt_kernel(Att
 #pragma unroll
                 for (int b = 0; b < 4; ++b)
                     store_past(mine, 4 * j + b, lane, f32x4{o[j][4 * b], o[j][4 * b + 1], o[j][4 * b + 2], o[j][4 * b + 3]});
-            store_past(mine, kVectors - 1, lane, f32x4{m, l, 0.0f, 0.0f});
+            store_past(mine, kVectors - 1, lane, f32x4{by_scale(m, by, scale), l, 0.0f, 0.0f});
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's stores are acknowledged
             __syncthreads();
             int *const s_last = reinterpret_cast<int *>(s_raw);
@@ -908,7 +926,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_prompt_kernel(Att
                     for (int r = 0; r < 16; ++r) o[j][r] = f * o[j][r] + e * x[4 * j + r / 4][r % 4];
             }
         }
-        const float sum = l + __shfl_xor(l, 32, kWave), by = sum > 0.0f ? 1.0f / sum : 0.0f;
+        const float sum = l + __shfl_xor(l, 32, kWave), per = sum > 0.0f ? 1.0f / sum : 0.0f;
         if (live) {
             uint16_t *y = static_cast<uint16_t *>(a.y) + ((size_t)(row0 + col / share) * a.n_heads + head * share + col % share) * D;
             // channels r D/16 .. of the lane's eight r: the places c 16 + r of all c
@@ -919,7 +937,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_prompt_kernel(Att
                     constexpr int C = D / 16;
                     uint32_t w[C / 2];
 #pragma unroll
-                    for (int e = 0; e < C; e += 2) w[e / 2] = pack_bf16(o[e / 2][4 * b + i] * by, o[e / 2][8 + 4 * b + i] * by);
+                    for (int e = 0; e < C; e += 2) w[e / 2] = pack_bf16(o[e / 2][4 * b + i] * per, o[e / 2][8 + 4 * b + i] * per);
                     uint32_t *to = reinterpret_cast<uint32_t *>(y + (8 * b + 4 * h + i) * C);
                     if constexpr (C == 4) *reinterpret_cast<u32x2 *>(to) = u32x2{w[0], w[1]};
                     else

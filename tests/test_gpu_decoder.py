@@ -748,3 +748,36 @@ def test_reorder_of_last_pages_that_are_none(pop):
     got = _run_reorder(pop, *args)
     _same(got, orc.reorder(*args))
     assert got[0][3].tolist() == [4, 5, -5]
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("dtype,ydtype", TYPES)
+def test_scores_far_from_zero(pop, d, dtype, ydtype):
+    """Keys of up to 1.5 x 2^116 in all tokens, or in one beside zeros: scores of 2^29 to 2^125, of either sign.  Products and their sums
+    are exact in 32 bits, so that scores have no error (and stored values are written again as they are)."""
+    rng = np.random.default_rng(d + 1)
+    for heads, n_kv, new, kw in ((2, 1, 1, {}), (4, 2, 3, {}), (8, 1, 40, dict(max_new=2048, max_context=1 << 19))):
+        c = Cached(pop, rng, [300, 2000], n_kv, d, 16)
+        start = np.array([0, new, 2 * new])
+        q = torch.ones(2 * new, heads, d, device="cuda", dtype=DT[dtype])
+        for size in (1.5 * 2.0 ** 23, 1.5 * 2.0 ** 60, 1.5 * 2.0 ** 116):
+            for alike in (False, True):
+                for s, length in enumerate(c.context):
+                    k = np.full((length, n_kv, d), size if alike else 0.0, dtype=np.float32)
+                    if not alike:
+                        k[length // 3], k[length // 2] = size, -size
+                    t = np.arange(length)
+                    slots = c.table[s, t // c.page] * c.page + t % c.page
+                    kd, vd = (torch.from_numpy(x.astype(np.float32)).cuda() for x in (k, c.v[s]))
+                    pop.pop_cache_write(c.cache, n_kv, d, c.page, c.n_pages, kd, vd, F32, i32(slots), length)
+                    c.k[s] = k
+                for scale in (1.0, -0.75):
+                    h = f64(_attend(pop, c, q, start, dtype, ydtype, heads, scale, **kw))
+                    for s, length in enumerate(c.context):
+                        sizes = []
+                        a, b = start[s], start[s + 1]
+                        want = orc.attention(f64(q[a:b]), c.k[s], c.v[s], scale, length - new, 0, None, sizes)
+                        bound = sizes[0] * ((length + 32) * 2.0 ** -24 + 2.0 ** -21) + 2.0 ** -23 * np.abs(want)  # (as in _check, of exact scores)
+                        if ydtype == BF16:
+                            bound = bound + 2.0 ** -8 * sizes[0] + 2.0 ** -8 * np.abs(want)
+                        assert (np.abs(h[a:b] - want) <= bound + 1e-30).all(), (heads, size, alike, scale, s)
