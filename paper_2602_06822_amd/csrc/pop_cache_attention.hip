@@ -395,7 +395,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_kernel(
     const int owner = __ffsll((unsigned long long)__ballot(upto > at)) - 1;
     int seq = owner * per_lane, seq_at = owner > 0 ? __builtin_amdgcn_readlane(upto, owner - 1) : 0;  // where the sequence begins
     unsigned long long *const counters = reinterpret_cast<unsigned long long *>(partial_of<D>(a, 2 * (int)gridDim.x));
-    const unsigned page_bytes = n_kv * (a.c.page >> 4) * kTile;
+    const size_t page_bytes = cache_page_bytes(a.c);
 
     while (at < end) {
         int start, next, context;
@@ -739,7 +739,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_prompt_kernel(Att
     const int head = blockIdx.x % n_kv;
     const float scale = a.scale != 0.0f ? fabsf(a.scale) * kLog2e : 1.0f;
     const TileOffsets<D> offsets(n, g);
-    const unsigned page_bytes = n_kv * (a.c.page >> 4) * kTile;
+    const size_t page_bytes = cache_page_bytes(a.c);
     const unsigned char *const cache = a.cache + (size_t)(head * (a.c.page >> 4)) * kTile;
 
     // a unit's pieces, and behind all of them the units' counters

@@ -781,3 +781,26 @@ def test_scores_far_from_zero(pop, d, dtype, ydtype):
                         if ydtype == BF16:
                             bound = bound + 2.0 ** -8 * sizes[0] + 2.0 ** -8 * np.abs(want)
                         assert (np.abs(h[a:b] - want) <= bound + 1e-30).all(), (heads, size, alike, scale, s)
+
+
+def test_pages_of_more_than_32_bits(pop):
+    """Two pages of 4.3 GB, of which the second holds the tokens of three heads and zeros for the others."""
+    n_kv, d, page = 62000, 256, 256
+    rng = np.random.default_rng(14)
+    cache = torch.zeros(pop.pop_cache_bytes(n_kv, d, page, 2), dtype=torch.uint8, device="cuda")
+    assert cache.numel() > 2 << 32
+    heads = [0, 30000, n_kv - 1]
+    kh, vh = (rng.standard_normal((2, 3, d)).astype(np.float32) for _ in range(2))
+    k, v = torch.zeros(2, n_kv, d, device="cuda"), torch.zeros(2, n_kv, d, device="cuda")
+    k[:, heads], v[:, heads] = torch.from_numpy(kh).cuda(), torch.from_numpy(vh).cuda()
+    pop.pop_cache_write(cache, n_kv, d, page, 2, k, v, F32, i32([page, page + 1]), 2)
+    q = torch.zeros(1, n_kv, d, device="cuda")
+    q[0, heads] = torch.from_numpy(rng.standard_normal((3, d)).astype(np.float32)).cuda()
+    y = torch.full_like(q, 7.0)
+    ws = torch.empty(pop.pop_cache_attention_workspace(1, 1, n_kv, n_kv, d, 1, 2), dtype=torch.uint8, device="cuda")
+    pop.pop_cache_attention(q, F32, 1, cache, n_kv, d, page, 2, i32([[1]]), 1, i32([0, 1]), i32([2]), 1, n_kv, 1, 2, 0.1, 0, y, F32, ws)
+    want = orc.attention(f64(q[:, heads]), orc.decode(*orc.encode(kh)), orc.decode(*orc.encode(vh)), 0.1, 1)
+    # 32-bit sums of 256 products below 4 x 4, and two weights
+    assert np.abs(f64(y[:, heads]) - want).max() < 1e-5
+    y[:, heads] = 0
+    assert not y.any()
