@@ -362,7 +362,7 @@ int pop_cache_attention_workspace(int n_tokens, int n_seq, int n_heads, int n_kv
  * NaN logits count as -inf; with +inf ones results are unspecified.
  * workspace: dev, of pop_beam_workspace bytes for the same sizes, any content.
  * Errors: NULL or misaligned pointers, bad dtype -> POP_EINVAL; sizes, pad_token outside the vocabulary, a workspace that is
- * too small -> POP_ESHAPE; beyond the limits above, vocab > 2^24 -> POP_EUNSUPPORTED. */
+ * too small -> POP_ESHAPE; beyond the limits above, vocab > 2^24, 2^24 rows or more -> POP_EUNSUPPORTED. */
 int pop_beam_select(const void *logits, pop_dtype_t dtype, const float *scores, const unsigned char *done,
                     int n_requests, int n_beams, int vocab, int k, int pad_token, float *out_scores, int *out_tokens,
                     int *out_parents, void *workspace, size_t workspace_bytes, void *stream);
@@ -378,7 +378,7 @@ int pop_beam_workspace(int n_requests, int n_beams, int vocab, int k, size_t *by
  * Outputs (dev): new_table [n_seq][table_stride] (-1 behind a row's last page), new_len [n_seq], copies, pool_out, status, and
  * the ring's free places.  workspace: dev, of pop_cache_reorder_workspace bytes, any content.
  * Errors: NULL pointers, outputs that are their inputs -> POP_EINVAL; sizes, n_seq no multiple of n_beams, a workspace
- * that is too small -> POP_ESHAPE; n_beams > POP_MAX_BEAMS -> POP_EUNSUPPORTED. */
+ * that is too small -> POP_ESHAPE; n_beams > POP_MAX_BEAMS, 2^24 groups or more -> POP_EUNSUPPORTED. */
 int pop_cache_reorder(const int *block_table, const int *len, const int *parents, int n_seq, int n_beams,
                       int page_tokens, int table_stride, int *new_table, int *new_len, int *copies, int *ring,
                       int n_pages, const int *pool, int *pool_out, void *workspace, size_t workspace_bytes, int *status,
@@ -387,7 +387,8 @@ int pop_cache_reorder(const int *block_table, const int *len, const int *parents
 int pop_cache_reorder_workspace(int n_seq, int n_beams, int table_stride, size_t *bytes);
 
 /* Page copies {from, to} of one layer's cache: copies dev [n_copies][2]; pairs with a number that is no page do nothing.  No page
- * may be copied to twice, or from and to.  Errors: NULL or misaligned pointers -> POP_EINVAL; sizes -> POP_ESHAPE. */
+ * may be copied to twice, or from and to.  Errors: NULL or misaligned pointers -> POP_EINVAL; sizes -> POP_ESHAPE; 2^24 copies or
+ * more -> POP_EUNSUPPORTED. */
 int pop_cache_copy_pages(void *cache, int n_kv_heads, int head_dim, int page_tokens, int n_pages, const int *copies,
                          int n_copies, void *stream);
 

@@ -22,6 +22,9 @@ inline hipStream_t as_stream(void *s) { return reinterpret_cast<hipStream_t>(s);
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline bool is_dtype(int t) { return t == POP_F32 || t == POP_BF16; }
 
+// An axis of a grid counts its threads in 32 bits: workgroups of 256.
+constexpr int kMostWorkgroups = (1 << 24) - 1;
+
 int log_of_page(int page)
 {
     for (int l = 4; l <= 8; ++l)
@@ -155,7 +158,7 @@ int pop_cache_attention(const void *q, pop_dtype_t dtype, int n_tokens, const vo
 static int beam_sizes(int n_requests, int n_beams, int vocab, int k)
 {
     if (n_requests < 0 || n_beams < 1 || vocab < 1 || k < 1 || (long long)n_beams * vocab < k) return POP_ESHAPE;
-    if (n_beams > POP_MAX_BEAMS || k > 64 || vocab > 1 << 24 || n_requests > INT_MAX / POP_MAX_BEAMS / 64) return POP_EUNSUPPORTED;
+    if (n_beams > POP_MAX_BEAMS || k > 64 || vocab > 1 << 24 || n_requests > kMostWorkgroups / n_beams) return POP_EUNSUPPORTED;
     return POP_OK;
 }
 
@@ -188,7 +191,7 @@ int pop_beam_select(const void *logits, pop_dtype_t dtype, const float *scores, 
 static int reorder_sizes(int n_seq, int n_beams, int table_stride)
 {
     if (n_seq < 1 || n_beams < 1 || n_seq % n_beams || table_stride < 1) return POP_ESHAPE;
-    if (n_beams > POP_MAX_BEAMS) return POP_EUNSUPPORTED;
+    if (n_beams > POP_MAX_BEAMS || n_seq / n_beams > kMostWorkgroups) return POP_EUNSUPPORTED;
     return POP_OK;
 }
 
@@ -226,6 +229,7 @@ int pop_cache_copy_pages(void *cache, int n_kv, int d, int page, int n_pages, co
     const int rc = cache_shape(n_kv, d, page, n_pages, &c);
     if (rc != POP_OK) return rc;
     if (n_copies < 0) return POP_ESHAPE;
+    if (n_copies > kMostWorkgroups) return POP_EUNSUPPORTED;
     if (n_copies == 0) return POP_OK;
     if (!cache || !copies || !aligned16(cache)) return POP_EINVAL;
     POP_HIP(launch_cache_copy_pages(cache, c, copies, n_copies, as_stream(stream)));

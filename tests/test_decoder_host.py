@@ -243,3 +243,21 @@ def test_binding_takes_device_tensors_only(pop):
         pop.pop_cache_plan(x, x, 4, 16, x, 1, x, 4, x, x, 0, x, x, x, x, x)
     with pytest.raises(ValueError):
         pop.pop_cache_write(0, 1, 64, 16, 1, torch.zeros(1, 64), torch.zeros(1, 64), 0, 0, 1)
+
+
+@pytest.mark.parametrize("rows", [1 << 24, (1 << 24) + 16, 1 << 30])
+def test_more_rows_than_a_grid_holds_are_refused(pop, rows):
+    """A grid's axis counts threads in 32 bits: 2^24 workgroups of 256 would begin anew at zero."""
+    _refused(pop, "POP_EUNSUPPORTED", "pop_beam_select", _with(BEAM, requests=rows // 4, beams=4, vocab=1, k=1))
+    with pytest.raises(pop.PopError) as e:
+        pop.pop_beam_workspace(rows // 4, 4, 1, 1)
+    assert e.value.status == pop.POP_EUNSUPPORTED
+    _refused(pop, "POP_EUNSUPPORTED", "pop_cache_reorder", _with(REORDER, n_seq=rows, beams=1, ws_bytes=1 << 40))
+    with pytest.raises(pop.PopError) as e:
+        pop.pop_cache_reorder_workspace(rows, 1, 8)
+    assert e.value.status == pop.POP_EUNSUPPORTED
+    _refused(pop, "POP_EUNSUPPORTED", "pop_cache_copy_pages", [A, 2, 64, 16, 8, A, rows, None])
+
+
+def test_the_most_rows_have_a_workspace(pop):
+    assert pop.pop_beam_workspace((1 << 20) - 1, 16, 1, 1) > 0 and pop.pop_cache_reorder_workspace((1 << 24) - 1, 1, 1) > 0
