@@ -295,14 +295,24 @@ def _size(fn, name, *args) -> int:
     return n.value
 
 
-def _rows(t, width, stride):
-    """(address, elements from row to row) of token rows that may be part of longer ones; a raw address needs `stride`."""
+def _rows(t, width, stride, n):
+    """(address, elements from row to row) of n token rows that may be part of longer ones; a raw address needs `stride`."""
     if t is None or isinstance(t, int):
         return t, width if stride is None else stride
     if not t.is_cuda:
         raise ValueError("device tensor expected")
     if t.is_contiguous():
-        return t.data_ptr(), width if stride is None else stride
+        if stride is None:
+            stride = width
+            if t.numel() != n * width:  # rows are the least run of last axes that holds one, where there are n of them
+                row = 1
+                for size in reversed(t.shape):
+                    row *= size
+                    if row >= width:
+                        break
+                if (n - 1) * row + width <= t.numel():
+                    stride = max(row, width)
+        return t.data_ptr(), stride
     steps, sizes = t.stride(), t.shape
     inner = 1
     for step, size in zip(steps[:0:-1], sizes[:0:-1]):
@@ -329,8 +339,8 @@ def pop_cache_plan(cached_len, new_len, n_seq, page_tokens, block_table, table_s
 
 def pop_cache_write(cache, n_kv_heads, head_dim, page_tokens, n_pages, k, v, dtype, slots, n_tokens, k_stride=None,
                     v_stride=None, stream=None):
-    k, k_stride = _rows(k, n_kv_heads * head_dim, k_stride)
-    v, v_stride = _rows(v, n_kv_heads * head_dim, v_stride)
+    k, k_stride = _rows(k, n_kv_heads * head_dim, k_stride, n_tokens)
+    v, v_stride = _rows(v, n_kv_heads * head_dim, v_stride, n_tokens)
     _check(_lib.pop_cache_write(_ptr(cache), n_kv_heads, head_dim, page_tokens, n_pages, k, v, dtype, k_stride, v_stride,
                                 _ptr(slots), n_tokens, _stream(stream)), "pop_cache_write")
 

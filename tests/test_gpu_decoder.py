@@ -804,3 +804,17 @@ def test_pages_of_more_than_32_bits(pop):
     assert np.abs(f64(y[:, heads]) - want).max() < 1e-5
     y[:, heads] = 0
     assert not y.any()
+
+
+@pytest.mark.parametrize("shape", [(5, 192), (5, 3, 64), (7, 192), (5, 128), (5, 2, 64), (10, 64), (1, 5, 2, 64), (1, 640), (640,), (9, 2, 64), (1, 5, 192)])
+def test_write_takes_rows_as_a_tensor_has_them(pop, shape):
+    """Contiguous tensors of 5 tokens of 2 heads of 64, some with longer rows or more of them, or with axes of their own."""
+    x = torch.arange(int(np.prod(shape)), device="cuda").remainder(5).float().sub_(2.0).view(shape)  # (-2 .. 2: kept as they are)
+    width = shape[-1] if shape[-1] == 192 else 192 if shape[1:] == (3, 64) else 128
+    want = f64(x).reshape(-1, width)[:5, :128]
+    cache = torch.zeros(pop.pop_cache_bytes(2, 64, 16, 1), dtype=torch.uint8, device="cuda")
+    ko, vo = torch.zeros(5, 2, 64, device="cuda"), torch.zeros(5, 2, 64, device="cuda")
+    slots = i32(np.arange(5))
+    pop.pop_cache_write(cache, 2, 64, 16, 1, x, x, F32, slots, 5)
+    pop.pop_cache_read(cache, 2, 64, 16, 1, slots, 5, ko, vo, F32)
+    assert np.array_equal(f64(ko).reshape(5, 128), want) and np.array_equal(f64(vo).reshape(5, 128), want)
