@@ -352,6 +352,11 @@ int pop_cache_attention(const void *q, pop_dtype_t dtype, int n_tokens, const vo
 /* Host only. */
 int pop_cache_attention_workspace(int n_tokens, int n_seq, int n_heads, int n_kv_heads, int head_dim, int max_new,
                                   int max_context, size_t *bytes);
+/* Host only.  Which implementation a call of these sizes runs: 0 = none (nothing to do), 1 = units of 16 columns (new tokens x query heads
+ * of a kv head), 2 = blocks of 128.  If parts != NULL it receives the parts that a block's tokens may be split into (0 for 0 and 1).
+ * Errors: as pop_cache_attention. */
+int pop_cache_attention_kind(pop_dtype_t dtype, pop_dtype_t ydtype, int n_tokens, int n_seq, int n_heads, int n_kv_heads,
+                             int head_dim, int max_new, int max_context, int window, int *parts);
 
 /* Beam search's selection.  logits: dev [n_requests * n_beams][vocab] (float32 or bf16), scores: dev [n_requests * n_beams]
  * float32, the beams' sums of log-probabilities (-inf: not alive), done: dev, a byte for each beam (may be NULL).

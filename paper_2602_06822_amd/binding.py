@@ -67,6 +67,7 @@ _SIGS = {
     "pop_cache_attention": (_i, [_vp, _i, _i, _vp, _i, _i, _i, _i, _vp, _i, _vp, _vp, _i, _i, _i, _i, C.c_float, _i, _vp, _i,
                                  _vp, C.c_size_t, _vp]),
     "pop_cache_attention_workspace": (_i, [_i, _i, _i, _i, _i, _i, _i, _szp]),
+    "pop_cache_attention_kind": (_i, [_i, _i, _i, _i, _i, _i, _i, _i, _i, _i, _ip]),
     "pop_beam_select": (_i, [_vp, _i, _vp, _vp, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp, C.c_size_t, _vp]),
     "pop_beam_workspace": (_i, [_i, _i, _i, _i, _szp]),
     "pop_cache_reorder": (_i, [_vp, _vp, _vp, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp, _vp, _vp, C.c_size_t, _vp, _vp]),
@@ -363,6 +364,16 @@ def pop_cache_attention(q, dtype, n_tokens, cache, n_kv_heads, head_dim, page_to
 def pop_cache_attention_workspace(n_tokens, n_seq, n_heads, n_kv_heads, head_dim, max_new, max_context) -> int:
     return _size(_lib.pop_cache_attention_workspace, "pop_cache_attention_workspace", n_tokens, n_seq, n_heads, n_kv_heads,
                  head_dim, max_new, max_context)
+
+
+def pop_cache_attention_kind(dtype, ydtype, n_tokens, n_seq, n_heads, n_kv_heads, head_dim, max_new, max_context, window=0):
+    """(kind, parts): kind 0 nothing to do, 1 units of 16 columns, 2 blocks of 128, whose tokens may be split into `parts`."""
+    parts = C.c_int()
+    kind = _lib.pop_cache_attention_kind(dtype, ydtype, n_tokens, n_seq, n_heads, n_kv_heads, head_dim, max_new, max_context, window,
+                                         C.byref(parts))
+    if kind < 0:
+        raise PopError(kind, "pop_cache_attention_kind")
+    return kind, parts.value
 
 
 def pop_beam_select(logits, dtype, scores, done, n_requests, n_beams, vocab, k, pad_token, out_scores, out_tokens,

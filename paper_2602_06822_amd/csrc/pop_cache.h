@@ -134,6 +134,8 @@ struct AttentionArgs {
     float *ws;
 };
 size_t cache_attention_ws(int n_tokens, int n_seq, int n_heads, int n_kv, int d, int max_new, int max_context);
+// Parts that the prompt kernel splits the tokens of a block of 128 columns into, 0 where the general kernel takes the call.
+int cache_attention_parts(int n_tokens, int n_seq, int n_heads, int n_kv, int d, int max_new, int max_context, int window, int all_bf16);
 hipError_t launch_cache_attention(const AttentionArgs &a, hipStream_t s);
 
 struct BeamArgs {

@@ -1008,6 +1008,22 @@ bool takes_prompt(const PromptGrid &g, int n_tokens, int n_seq, int n_heads, int
     return rounds * (0.57 * units - 2.4 * (double)blocks) > 256.0 * (blocks < 256 ? 19.0 : 11.0);
 }
 
+// Positions that a row can see, at most, as far as the caller says.
+long long longest_seen(int max_new, int max_context, int window)
+{
+    return window > 0 ? std::min((long long)max_context, (long long)window + max_new + 31) : max_context;
+}
+
+// The prompt kernel's grid for a call that it takes, else one without blocks.
+PromptGrid prompt_of(int n_tokens, int n_seq, int n_heads, int n_kv, int d, int max_new, long long seen, bool all_bf16)
+{
+    PromptGrid none = {0, 1, 1};
+    if (!all_bf16) return none;
+    PromptGrid g = prompt_grid(n_tokens, n_seq, n_heads, n_kv, max_new, seen);
+    if (d == 256) g.splits = 1;
+    return takes_prompt(g, n_tokens, n_seq, n_heads, n_kv, d, max_new, seen) ? g : none;
+}
+
 template <int D>
 hipError_t launch_prompt(const AttentionArgs &a, const PromptGrid &g, hipStream_t s)
 {
@@ -1021,12 +1037,9 @@ hipError_t launch_prompt(const AttentionArgs &a, const PromptGrid &g, hipStream_
 template <int D>
 hipError_t launch_d(const AttentionArgs &a, hipStream_t s)
 {
-    const long long seen = a.window > 0 ? std::min((long long)a.max_context, (long long)a.window + a.max_new + 31) : a.max_context;
-    if (a.q_bf16 && a.y_bf16) {
-        PromptGrid g = prompt_grid(a.n_tokens, a.n_seq, a.n_heads, a.c.n_kv, a.max_new, seen);
-        if (D == 256) g.splits = 1;
-        if (takes_prompt(g, a.n_tokens, a.n_seq, a.n_heads, a.c.n_kv, D, a.max_new, seen)) return launch_prompt<D>(a, g, s);
-    }
+    const long long seen = longest_seen(a.max_new, a.max_context, a.window);
+    const PromptGrid g = prompt_of(a.n_tokens, a.n_seq, a.n_heads, a.c.n_kv, D, a.max_new, seen, a.q_bf16 && a.y_bf16);
+    if (g.blocks > 0) return launch_prompt<D>(a, g, s);
     const unsigned grid = (unsigned)attention_workgroups(a.n_seq, a.n_heads, a.c.n_kv, D, a.max_new, seen);
     const unsigned long long tag = launch_tag();
     if (!a.q_bf16) cache_attention_kernel<D, 3, 3, false><<<grid, 256, 0, s>>>(a, tag);
@@ -1043,6 +1056,12 @@ size_t cache_attention_ws(int n_tokens, int n_seq, int n_heads, int n_kv, int d,
     const bool chunks = d < 256 && (long long)max_new * (n_heads / n_kv) >= kPromptColumns;
     const long long prompt = chunks ? prompt_grid(n_tokens, n_seq, n_heads, n_kv, max_new, max_context).bytes(n_kv, d) : 0;
     return std::max((size_t)prompt, (size_t)attention_workgroups(n_seq, n_heads, n_kv, d, max_new, max_context) * (2 * 16 * (d + 4) * sizeof(float) + 8));
+}
+
+int cache_attention_parts(int n_tokens, int n_seq, int n_heads, int n_kv, int d, int max_new, int max_context, int window, int all_bf16)
+{
+    const PromptGrid g = prompt_of(n_tokens, n_seq, n_heads, n_kv, d, max_new, longest_seen(max_new, max_context, window), all_bf16 != 0);
+    return g.blocks > 0 ? g.splits : 0;
 }
 
 hipError_t launch_cache_attention(const AttentionArgs &a, hipStream_t s)

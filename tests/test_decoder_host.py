@@ -261,3 +261,25 @@ def test_more_rows_than_a_grid_holds_are_refused(pop, rows):
 
 def test_the_most_rows_have_a_workspace(pop):
     assert pop.pop_beam_workspace((1 << 20) - 1, 16, 1, 1) > 0 and pop.pop_cache_reorder_workspace((1 << 24) - 1, 1, 1) > 0
+
+
+KIND = dict(dtype=1, ydtype=1, n_tokens=4096, n_seq=2, n_heads=32, n_kv=8, d=128, max_new=2048, max_context=6144, window=0, parts=None)
+
+
+@pytest.mark.parametrize("status,change", [
+    ("POP_EINVAL", dict(dtype=7)), ("POP_EINVAL", dict(ydtype=-1)), ("POP_ESHAPE", dict(n_heads=33)), ("POP_ESHAPE", dict(window=-1)),
+    ("POP_ESHAPE", dict(max_new=0)), ("POP_EUNSUPPORTED", dict(d=96))])
+def test_attention_kind_refuses(pop, status, change):
+    _refused(pop, status, "pop_cache_attention_kind", _with(KIND, **change))
+
+
+def test_attention_kinds(pop):
+    def kind(**change):
+        return pop.pop_cache_attention_kind(*_with(KIND, **change)[:-1])
+
+    assert kind(n_seq=0) == (0, 0) and kind(n_tokens=0) == (0, 0)
+    assert kind()[0] == 2
+    for general in (dict(dtype=0), dict(ydtype=0), dict(n_tokens=2, max_new=1), dict(n_tokens=32, max_new=16), dict(d=256, n_tokens=128, max_new=64)):
+        assert kind(**general) == (1, 0)
+    few = dict(n_tokens=128, n_seq=1, n_heads=16, n_kv=4, max_new=128, max_context=60000)
+    assert kind(**few)[1] > 1 and kind(**few, window=50) == (1, 0)

@@ -818,3 +818,66 @@ def test_write_takes_rows_as_a_tensor_has_them(pop, shape):
     pop.pop_cache_write(cache, 2, 64, 16, 1, x, x, F32, slots, 5)
     pop.pop_cache_read(cache, 2, 64, 16, 1, slots, 5, ko, vo, F32)
     assert np.array_equal(f64(ko).reshape(5, 128), want) and np.array_equal(f64(vo).reshape(5, 128), want)
+
+
+def _attend_in_blocks(pop, c, q, start, heads, scale, window=0, max_new=1 << 19, max_context=1 << 19, parts=None, **kw):
+    """_attend with sizes that take blocks of 128 columns, which is asked of the library: a rule that changes does not take the test with it."""
+    kind, got = pop.pop_cache_attention_kind(BF16, BF16, q.shape[0], len(c.context), heads, c.n_kv, c.d, max_new, max_context, window)
+    assert kind == 2 and (parts is None or (got > 1) == parts), (kind, got)
+    return _attend(pop, c, q, start, BF16, BF16, heads, scale, window, max_new=max_new, max_context=max_context, **kw)
+
+
+@pytest.mark.parametrize("window", [1, 60, 333])
+@pytest.mark.parametrize("heads,n_kv,d,page,context,new", [
+    (4, 4, 128, 16, [240, 7, 400, 0], [200, 3, 380, 0]), (6, 2, 64, 64, [130, 64, 33], [70, 64, 5]), (5, 1, 128, 32, [300, 1], [150, 1]),
+    (2, 1, 128, 64, [2900, 65], [130, 65]), (3, 3, 64, 32, [1500], [97]), (16, 1, 64, 16, [63, 64, 65, 127, 129], [9, 8, 7, 33, 5]),
+    (4, 2, 128, 256, [2100, 900, 130], [130, 65, 130])])
+def test_windows_in_blocks_of_128_columns(pop, window, heads, n_kv, d, page, context, new):
+    """Blocks that begin behind the first token, whole and in parts; pages that are none; a context shorter than its new tokens."""
+    rng = np.random.default_rng(d + window + len(context))
+    c = Cached(pop, rng, context, n_kv, d, page)
+    start = np.concatenate([[0], np.cumsum(new)])
+    q = _queries(rng, start[-1], heads, d, BF16)
+    for scale in (0.07, -0.4):
+        y = _attend_in_blocks(pop, c, q, start, heads, scale, window, parts=True)
+        _check(c, y, q, start, BF16, BF16, scale, window)
+    assert torch.equal(y, _attend_in_blocks(pop, c, q, start, heads, -0.4, window))
+    table = c.table.copy()
+    table[0, ::3] = -1
+    there = [np.repeat((t >= 0) & (t < c.n_pages), page) for t in table]
+    y = _attend_in_blocks(pop, c, q, start, heads, 0.07, window, table=table)
+    _check(c, y, q, start, BF16, BF16, 0.07, window, there=there)
+    short = [new[0] // 2] + context[1:]
+    y = _attend_in_blocks(pop, c, q, start, heads, 0.07, window, context=short)
+    _check(c, y, q, start, BF16, BF16, 0.07, window, context=short)
+
+
+@pytest.mark.parametrize("window", [0, 90])
+@pytest.mark.parametrize("n_seq,heads,n_kv,d", [(65, 4, 1, 64), (150, 8, 2, 64), (129, 16, 4, 128)])
+def test_many_sequences_in_blocks_of_128_columns(pop, n_seq, heads, n_kv, d, window):
+    """Several sequences to a lane; empty ones, ones without new tokens, many of one length."""
+    rng = np.random.default_rng(n_seq + window)
+    context = rng.integers(0, 300, n_seq)
+    context[rng.integers(0, n_seq, n_seq // 3)] = 200
+    context[5] = 900
+    new = np.minimum(rng.integers(0, 120, n_seq), context)
+    new[context == 200] = 70
+    c = Cached(pop, rng, context.tolist(), n_kv, d, 16)
+    start = np.concatenate([[0], np.cumsum(new)])
+    q = _queries(rng, start[-1], heads, d, BF16)
+    y = _attend_in_blocks(pop, c, q, start, heads, 0.11, window)
+    _check(c, y, q, start, BF16, BF16, 0.11, window)
+    assert torch.equal(y, _attend_in_blocks(pop, c, q, start, heads, 0.11, window))
+
+
+@pytest.mark.parametrize("page,window", [(16, 0), (32, 77)])
+def test_widest_heads_in_blocks_of_128_columns(pop, page, window):
+    rng = np.random.default_rng(page + 2)
+    c = Cached(pop, rng, [401, 0, 257], 64, 256, page)
+    start = np.array([0, 250, 250, 450])
+    q = _queries(rng, 450, 64, 256, BF16)
+    y = _attend_in_blocks(pop, c, q, start, 64, 0.06, window, parts=False)
+    _check(c, y, q, start, BF16, BF16, 0.06, window)
+    short = [401, 0, 150]
+    y = _attend_in_blocks(pop, c, q, start, 64, 0.06, window, context=short)
+    _check(c, y, q, start, BF16, BF16, 0.06, window, context=short)
