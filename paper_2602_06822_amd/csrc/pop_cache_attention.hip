@@ -169,14 +169,15 @@ constexpr int kNoWindow = 0x7fffffff, kMostTokens = 1 << 30;  // (a sequence's t
 // Sequences' rows of q and y: rows outside the tensors are not touched.
 __device__ __forceinline__ bool sequence_columns(const AttentionArgs &a, int start, int next, int context, int share, Columns *c)
 {
-    const int fresh = next - start;
+    const bool there = start >= 0 && next > start && next <= a.n_tokens;
+    const int fresh = there ? next - start : 0;
     context = min(max(context, 0), kMostTokens);
     c->length = min(context, a.stride << a.c.log_page);
     c->first_pos = context - fresh;
     c->share = share;
     c->n = fresh * share;
     c->window = a.window > 0 ? min(a.window, kMostTokens) : kNoWindow;
-    return start >= 0 && fresh > 0 && fresh <= a.n_tokens - start;
+    return there;
 }
 
 // Tokens [lo, hi) that some of the columns [begin, end) see, lo a multiple of 32, and the first and the last of the columns' positions.

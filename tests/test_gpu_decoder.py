@@ -881,3 +881,29 @@ def test_widest_heads_in_blocks_of_128_columns(pop, page, window):
     short = [401, 0, 150]
     y = _attend_in_blocks(pop, c, q, start, 64, 0.06, window, context=short)
     _check(c, y, q, start, BF16, BF16, 0.06, window, context=short)
+
+
+@pytest.mark.parametrize("dtype,blocks", [(F32, False), (BF16, False), (BF16, True)])
+def test_starts_that_do_not_ascend(pop, dtype, blocks):
+    """Sequences whose rows are none or leave the tensors are left out; the others' rows, wherever they stand, are right."""
+    rng = np.random.default_rng(15)
+    c = Cached(pop, rng, [300, 200, 90, 64, 500, 7], 2, 64, 16)
+    n = 150
+    q = _queries(rng, n, 8, 64, dtype)
+    for starts, kept in (([100, 140, 20, 60, 5000, 7000, -3], [0, 2]), ([150, 80, 149, 90, 2 ** 31 - 1, -2 ** 31, 0], [1]), ([-5, -1, 140, 3, 3, 10, 9], [4])):
+        if blocks:
+            h = f64(_attend_in_blocks(pop, c, q, starts, 8, 0.1, max_context=1 << 22))
+        else:
+            h = f64(_attend(pop, c, q, starts, dtype, dtype, 8, 0.1, max_new=40, max_context=500))
+        written = np.zeros(n, bool)
+        for s in kept:
+            a, b = starts[s], starts[s + 1]
+            written[a:b] = True
+            sizes = []
+            want = orc.attention(f64(q[a:b]), c.k[s], c.v[s], 0.1, c.context[s] - (b - a), 0, None, sizes)
+            scores = (c.d + 8) * 2.0 ** -24 * sizes[1]
+            bound = sizes[0] * (2 * scores + (c.context[s] + 32) * 2.0 ** -24 + 2.0 ** -21) + 2.0 ** -23 * np.abs(want)  # (as in _check)
+            if dtype == BF16:
+                bound = bound + 2.0 ** -8 * sizes[0] + 2.0 ** -8 * np.abs(want)
+            assert (np.abs(h[a:b] - want) <= bound + 1e-30).all(), (starts, s)
+        assert (h[~written] == 7.0).all()
