@@ -287,8 +287,8 @@ int pop_probe_step_read(pop_layer_t *layer, int k, int workgroups, unsigned int 
  *     K scales [16 tokens][D/32], V scales [4 groups][D/32][4 tokens];  the lower channel of a byte is its low nibble.
  * A token's *slot* is page * page_tokens + its place in the page.  A row of `block_table` (dev [n_seq][table_stride]) names
  * the pages of a sequence in order; entries outside [0, n_pages) are no page.  All layers of a model can share the tables.
- * head_dim is 64, 128 or 256, page_tokens 16, 32, 64, 128 or 256, else POP_EUNSUPPORTED; n_pages * page_tokens stays
- * below 2^31 and table_stride * page_tokens does not pass 2^30, else POP_EUNSUPPORTED.  cache, q, k, v, y, logits, workspaces: 16-byte aligned.
+ * head_dim is 64, 128 or 256, page_tokens 16, 32, 64, 128 or 256, n_kv_heads at most 65535, else POP_EUNSUPPORTED; n_pages * page_tokens
+ * stays below 2^31 and table_stride * page_tokens does not pass 2^30, else POP_EUNSUPPORTED.  cache, q, k, v, y, logits, workspaces: 16-byte aligned.
  *
  * Free pages stand in a ring: `ring` (dev [n_pages]) and `pool` (dev, two ints): the place of the first free page, and how many
  * are free.  Pages are taken at the front and given back at the end, so a call's inputs stay as they are and its outputs
@@ -321,7 +321,8 @@ int pop_cache_plan(const int *cached_len, const int *new_len, int n_seq, int pag
  * beyond the cache are left out.  A block's scale is 2^(e - 2), e the exponent of its largest magnitude, and twice that from a
  * significand of 1.75 on; values go to the nearest code, halves to the even one, magnitudes above 6 to 6.  An infinity is stored
  * as the largest float32, a NaN as zero: nothing that the format holds is infinite or no number.
- * Errors: NULL or misaligned pointers, bad dtype -> POP_EINVAL; sizes, strides -> POP_ESHAPE. */
+ * Errors: NULL or misaligned pointers, bad dtype -> POP_EINVAL; sizes, strides -> POP_ESHAPE; n_tokens * n_kv_heads * head_dim of 2^34 or
+ * more -> POP_EUNSUPPORTED. */
 int pop_cache_write(void *cache, int n_kv_heads, int head_dim, int page_tokens, int n_pages, const void *k,
                     const void *v, pop_dtype_t dtype, long long k_stride, long long v_stride, const int *slots,
                     int n_tokens, void *stream);
@@ -339,11 +340,14 @@ int pop_cache_read(const void *cache, int n_kv_heads, int head_dim, int page_tok
  * sums overflow.  y: dev [n_tokens][n_heads][head_dim] of ydtype; rows of no sequence are not written.  A sequence whose rows leave
  * [0, n_tokens) is left out and its rows are undefined.
  * max_new, max_context: the longest that the caller expects; longer ones are right too, but may be slow.  float32 q is
- * taken in full (three bf16 terms of q and of the softmax weights), with bf16 q the weights are rounded to bf16.
+ * taken in full (three bf16 terms).  The softmax weights are rounded to bf16 where q and y are both bf16, else taken in full too; their
+ * sum is of the unrounded ones, in float32.
  * workspace: dev, of pop_cache_attention_workspace bytes for the same sizes, or for larger n_tokens, n_seq, max_new or max_context; any
  * content, for this call alone.
  * Errors: NULL or misaligned pointers, bad dtype, a scale that is not finite -> POP_EINVAL; sizes, n_heads no multiple of
- * n_kv_heads, a workspace that is too small -> POP_ESHAPE. */
+ * n_kv_heads, a workspace that is too small -> POP_ESHAPE; n_seq * n_kv_heads > 65535, n_tokens * n_heads >= 2^30, or more rounds than
+ * 32 bits count, (n_tokens * n_heads / n_kv_heads / 16 + n_seq) * n_kv_heads * (table_stride * page_tokens / 128 + 1) >= 2^31 (of the
+ * table's width, whatever the contexts are) -> POP_EUNSUPPORTED. */
 int pop_cache_attention(const void *q, pop_dtype_t dtype, int n_tokens, const void *cache, int n_kv_heads,
                         int head_dim, int page_tokens, int n_pages, const int *block_table, int table_stride,
                         const int *q_start, const int *context_len, int n_seq, int n_heads, int max_new,

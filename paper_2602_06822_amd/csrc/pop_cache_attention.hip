@@ -277,7 +277,9 @@ constexpr int kWorkgroups = 512;
 
 // How the work is dealt.  A unit is one kv head's block of 16 columns of one sequence: a number of rounds over the tokens that the
 // sequence's columns see.  All units stand in one row (sequence, block, head), and every workgroup takes the same number of rounds of
-// it, wherever units begin and end: ragged batches and single long sequences load all compute units alike.  A piece of a unit
+// it, wherever units begin and end: ragged batches and single long sequences of single tokens load all compute units alike.  (Chunks less so: a
+// unit has the rounds of its whole sequence's columns, of which its own block may see few, under a window or where little is cached;
+// rounds behind what a block sees cost nothing, those in front of it, under a window, are gone over masked.)  A piece of a unit
 // is what one workgroup has of it.  Where that gains less than pieces cost, workgroups take units.
 struct SequenceWork {
     int rounds;  // of a unit
@@ -341,7 +343,8 @@ __device__ __forceinline__ float2 load_pair(const float *p)
 // Workgroup: 4 waves.  In a round wave w takes tokens 32 w .. 32 w + 31 and asks for the next round's codes before it uses this one's.
 // Units that end and begin with a workgroup are written to y; the pieces of others are joined by the last workgroup that finishes
 // one, in the order of the tokens.  QT, PT: bf16 terms that q and the softmax weights are split into: q one if it is bf16 (exact),
-// else three (24 bits); the weights one if the output is bf16 (rounded to 8 significant bits, as the output is), else three.  K and V
+// else three (24 bits); the weights one if q and the output are bf16 (rounded to 8 significant bits, as the output is, which adds about as
+// much error again: 2.2e-3 of the result where the output's own rounding makes 1.65e-3), else three.  K and V
 // are exact in bf16.
 //
 // Bound by memory on long contexts (two of up to 131072 tokens, 32 heads over 8, D 128: 43 us, 224 MB at 5.2 TB/s; the instructions of the
@@ -999,7 +1002,8 @@ PromptGrid prompt_grid(int n_tokens, int n_seq, int n_heads, int n_kv, int max_n
 // block each.  Microseconds, general / prompt kernel, D 128, 4 query heads to each of 8 kv heads: 4 sequences x 512 new tokens 36.3 / 24.8, over 3000
 // cached ones 126 / 94; 1 x 512 17.5 / 21.3, over 1000 32.7 / 31.2, over 3000 61 / 49; 1 x 128 over 700 10.0 / 20.0, over 16000 78 / 62; 32 heads
 // of their own, 32 new tokens over 60000 91 / 121.  D = 256 has registers and LDS for one workgroup to a compute unit, so it takes whole blocks, and
-// units for all compute units (two chunks of 1024 over 4096: 433 / 290).
+// units for all compute units (two chunks of 1024 over 4096: 433 / 290).  (Every unit is counted with the longest context's rounds, and D = 64
+// like D = 128: near the border, and for windows, which leave the prompt kernel's blocks less than that, either kernel may be the faster.)
 constexpr int kPromptColumns = 65;  // with fewer it never does
 bool takes_prompt(const PromptGrid &g, int n_tokens, int n_seq, int n_heads, int n_kv, int d, int max_new, long long max_context)
 {

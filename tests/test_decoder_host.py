@@ -283,3 +283,15 @@ def test_attention_kinds(pop):
         assert kind(**general) == (1, 0)
     few = dict(n_tokens=128, n_seq=1, n_heads=16, n_kv=4, max_new=128, max_context=60000)
     assert kind(**few)[1] > 1 and kind(**few, window=50) == (1, 0)
+
+
+@pytest.mark.parametrize("change", [
+    dict(n_seq=32768), dict(n_kv=65536, n_heads=65536, n_seq=1), dict(n_tokens=1 << 28), dict(n_tokens=1 << 26, stride=1 << 22),
+    dict(n_tokens=1 << 20, n_seq=16, n_heads=64, n_kv=64, stride=1 << 26)])
+def test_attention_refuses_what_it_does_not_count(pop, change):
+    _refused(pop, "POP_EUNSUPPORTED", "pop_cache_attention", _with(ATTENTION, **change))
+
+
+def test_write_and_read_refuse_what_a_grid_does_not_count(pop):
+    _refused(pop, "POP_EUNSUPPORTED", "pop_cache_write", _with(WRITE, n=1 << 26))
+    _refused(pop, "POP_EUNSUPPORTED", "pop_cache_read", _with(READ, n=1 << 26))
