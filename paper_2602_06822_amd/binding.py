@@ -305,7 +305,7 @@ def _rows(t, width, stride, n):
     if t.is_contiguous():
         if stride is None:
             stride = width
-            if t.numel() != n * width:  # rows are the least run of last axes that holds one, where there are n of them
+            if n > 1 and t.numel() != n * width:  # rows are the least run of last axes that holds one, where there are n of them
                 row = 1
                 for size in reversed(t.shape):
                     row *= size

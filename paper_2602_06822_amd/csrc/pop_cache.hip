@@ -376,7 +376,8 @@ __device__ __forceinline__ int block_sum(int v, int *s_wave, int *before)
 
 // Latency-bound integer work in two launches (one where a single workgroup sees to everything): what each part of the requests gives
 // back and takes has to be known before the first page finds its place in the ring.  W: rows of a request at most.  counts: pages given back,
-// by request and part, then copies by request, -1 where a length is wrong.  One request of four rows 4.5 us; 64 of eight rows of 250 blocks 4.4 + 9.0.
+// by request and part, then copies by request, -1 where a length is wrong.  One request of four rows 4.5 us; 64 of eight rows of 250 blocks
+// 4.4 + 9.0.
 template <int W>
 __global__ __launch_bounds__(kReorderBlocks) void reorder_count_kernel(ReorderArgs a)
 {

@@ -32,8 +32,8 @@ constexpr float kSlack = 8.0f;
 // Weights are 2^(s scale - m), relative to a maximum m that is a rounded product itself: what the rounding takes off stays in all weights of the
 // column and cancels, but from 2^32 on it is more than an exponential can hold.  Beyond kFar a column goes by the power of two below the
 // scale instead, with which the product of its maximum is exact: scores of that size that differ at all (float32 has 24 bits) differ by 2^6
-// or more there, so weights are 1 or nothing by either factor.  (A factor to a lane instead of one for all: four chunks of 955 to 2048 tokens over 2867 to 6144 358 -> 361 us, single
-// tokens as before; rounding the products of such steps alone, in a branch, 368 to 372.)
+// or more there, so weights are 1 or nothing by either factor.  (A factor to a lane instead of one for all: four chunks of 955 to 2048 tokens
+// over 2867 to 6144 358 -> 361 us, single tokens as before; rounding the products of such steps alone, in a branch, 368 to 372.)
 constexpr float kFar = 1073741824.0f;
 
 // The column's factor and its maximum in that unit, where the maximum has just become `raw` (a score without the scale) or stays as it is.

@@ -907,3 +907,15 @@ def test_starts_that_do_not_ascend(pop, dtype, blocks):
                 bound = bound + 2.0 ** -8 * sizes[0] + 2.0 ** -8 * np.abs(want)
             assert (np.abs(h[a:b] - want) <= bound + 1e-30).all(), (starts, s)
         assert (h[~written] == 7.0).all()
+
+
+def test_write_of_one_token_or_none_from_rows_of_any_length(pop):
+    """Where there is no second row its distance says nothing, whatever 16 bytes make of it."""
+    x = torch.arange(5 * 130, device="cuda").remainder(5).float().sub_(2.0).view(5, 130)
+    cache = torch.zeros(pop.pop_cache_bytes(2, 64, 16, 1), dtype=torch.uint8, device="cuda")
+    pop.pop_cache_write(cache, 2, 64, 16, 1, x, x, BF16, i32([0]), 0)
+    assert not cache.any()
+    pop.pop_cache_write(cache, 2, 64, 16, 1, x, x, F32, i32([3]), 1)
+    ko, vo = torch.zeros(1, 2, 64, device="cuda"), torch.zeros(1, 2, 64, device="cuda")
+    pop.pop_cache_read(cache, 2, 64, 16, 1, i32([3]), 1, ko, vo, F32)
+    assert np.array_equal(f64(ko).ravel(), f64(x)[0, :128]) and np.array_equal(f64(vo).ravel(), f64(x)[0, :128])
