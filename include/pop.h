@@ -401,6 +401,58 @@ int pop_cache_reorder_workspace(int n_seq, int n_beams, int table_stride, size_t
 int pop_cache_copy_pages(void *cache, int n_kv_heads, int head_dim, int page_tokens, int n_pages, const int *copies,
                          int n_copies, void *stream);
 
+/* ---- between a layer's blocks ----
+ *
+ * Residual sums with the norms around a block, and rotary positions, on rows of any length and alignment (of their elements); rows whose length,
+ * distance and address are multiples of 16 bytes are faster.  Strides are in elements, from row to row. */
+
+/* The residual stream after a block, and the next block's input, in one pass:
+ *     u' = u r(u) (w_post + weight_offset)  if post_norm, else u;       r(v) = 1 / sqrt(sum of squares of v / d + eps)
+ *     x' = x_scale x + u_scale gate u';
+ *     z  = x' r(x') (w_pre + weight_offset).
+ * x: dev, n_tokens rows of d of xdtype.  u: dev, rows of dtype, NULL for none (x' = x_scale x; no gate, no post_norm then).  gate: dev, gate_rows
+ * = 1 (for all tokens) or n_tokens rows of d of dtype, NULL (and 0) for none.  w_post, w_pre: dev [d] of dtype, NULL for a factor of 1 (without
+ * the offset).  Outputs (dev): x_out of xdtype, z of dtype; either may be NULL.  z is formed from x' before that is rounded to xdtype.
+ * An output may be x or u itself where type and stride are the same; otherwise outputs lie apart from inputs and from each other.
+ * Sums of squares are float32.
+ * Errors: NULL x, no output, outputs that are inputs in another way, misaligned pointers, bad dtype, eps not above 0, numbers that are not
+ * finite -> POP_EINVAL; sizes, strides below d, other gate_rows -> POP_ESHAPE; d > 65536, 2^22 tokens or more -> POP_EUNSUPPORTED. */
+int pop_block_norm(const void *x, pop_dtype_t xdtype, long long x_stride, const void *u, pop_dtype_t dtype, long long u_stride, const void *gate,
+                   int gate_rows, long long gate_stride, int n_tokens, int d, const void *w_post, const void *w_pre, int post_norm,
+                   float weight_offset, float eps, float x_scale, float u_scale, void *x_out, long long x_out_stride, void *z,
+                   long long z_stride, void *stream);
+
+/* Which channels of a head are turned together: i and i + rotary_dim / 2, or 2 i and 2 i + 1. */
+enum { POP_ROTARY_HALVES = 0, POP_ROTARY_PAIRS = 1 };
+/* How the frequencies base^(-2 i / rotary_dim) are scaled for contexts longer than the trained one, by a factor >= 1:
+ *   POP_ROTARY_PLAIN   not at all (factor is not looked at);
+ *   POP_ROTARY_LINEAR  divided by the factor;
+ *   POP_ROTARY_BASE    base times factor^(R / (R - 2)), R = rotary_dim >= 4: the slowest are divided by the factor, the fastest stay;
+ *   POP_ROTARY_BANDS   by the rotations r that a frequency makes over `context` tokens: divided up to `low` of them, as they are from `high` on, and
+ *                      in between (1 - s) f / factor + s f with s = (r - low) / (high - low);
+ *   POP_ROTARY_RAMP    the same with s falling linearly over i, from the floor of the place where a frequency makes `high` rotations to
+ *                      the ceiling of that of `low` (both within 0 .. R - 1); sines and cosines times 1 + ln(factor) / 10. */
+enum { POP_ROTARY_PLAIN = 0, POP_ROTARY_LINEAR = 1, POP_ROTARY_BASE = 2, POP_ROTARY_BANDS = 3, POP_ROTARY_RAMP = 4 };
+/* Host only.  turns: host [rotary_dim / 2], the frequencies in revolutions a token (f / 2 pi), 64 bits; amplitude (may be NULL): the factor of sines and
+ * cosines, 1 but for POP_ROTARY_RAMP.  context, low and high are looked at by the last two only.
+ * Errors: NULL turns, an unknown scaling, base not above 1, factor below 1, context or low not above 0, high not above low, numbers that are not
+ * finite -> POP_EINVAL; rotary_dim odd, below 2 (4) or above 1024 -> POP_ESHAPE. */
+int pop_rotary_frequencies(int rotary_dim, double base, int scaling, double factor, double context, double low, double high, double *turns,
+                           float *amplitude);
+/* Turns the heads of tokens by their positions: of channels a and b that go together, at an angle t = 2 pi position turns[i],
+ *     a' = amplitude (a cos t - b sin t),  b' = amplitude (a sin t + b cos t).
+ * The first rotary_dim channels of each head are turned, the others copied.  q, k: dev, rows of [n_heads][head_dim] and [n_kv_heads][head_dim] of
+ * dtype, q_stride and k_stride elements apart (so both may be parts of one projection's rows); k may be NULL (with k_out).
+ * positions: dev [n_tokens]; rows whose position is negative are not read and not written.  turns: dev [rotary_dim / 2], 64 bits.  q_out, k_out:
+ * dev, may be q and k themselves (with the same strides), otherwise apart from them.
+ * Angles are products in 64 bits, sines and cosines float32.
+ * Errors: NULL or misaligned pointers, bad dtype or layout, an amplitude that is not finite, outputs that are inputs with another stride
+ * -> POP_EINVAL; sizes, rotary_dim odd or above head_dim, strides below a row -> POP_ESHAPE; rotary_dim > 1024, (n_heads + n_kv_heads) * head_dim
+ * >= 2^30, 2^22 tokens or more -> POP_EUNSUPPORTED. */
+int pop_rotary(const void *q, const void *k, pop_dtype_t dtype, int n_tokens, int n_heads, int n_kv_heads, int head_dim, int rotary_dim, int layout,
+               long long q_stride, long long k_stride, const int *positions, const double *turns, float amplitude, void *q_out, void *k_out,
+               long long q_out_stride, long long k_out_stride, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

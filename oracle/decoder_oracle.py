@@ -208,3 +208,55 @@ def beam_select(logits, scores, done, k, pad):
     flat = out.ravel()
     at = np.argsort(-flat, kind="stable")[:k]
     return flat[at], at % vocab, at // vocab
+
+
+# ---------------------------------------------------------------- norms and rotary positions
+
+def block_norm(x, u, *, gate=None, w_post=None, w_pre=None, post=False, offset=0.0, eps=1e-6, x_scale=1.0, u_scale=1.0):
+    """x, u [tokens][d] (u may be None).  Returns (x', z) of the row after the block and of the next block's input."""
+    def normed(v, w):
+        r = 1.0 / np.sqrt((v * v).mean(-1, keepdims=True) + eps)
+        return v * r * (1.0 if w is None else w.astype(np.float64) + offset)
+
+    x = x_scale * x.astype(np.float64)
+    if u is not None:
+        u = u.astype(np.float64)
+        if post:
+            u = normed(u, w_post)
+        x = x + u_scale * (u if gate is None else u * gate.astype(np.float64))
+    return x, normed(x, w_pre)
+
+
+def rotary_frequencies(r, base, scaling, factor=1.0, context=0.0, low=0.0, high=0.0):
+    """Frequencies (radians a token) of the r/2 pairs and the amplitude; scaling by name."""
+    i = np.arange(r // 2)
+    if scaling == "base":
+        base = base * factor ** (r / (r - 2.0))
+    f = base ** (-2.0 * i / r)
+    if scaling == "linear":
+        return f / factor, 1.0
+    if scaling == "bands":
+        s = np.clip((context * f / (2 * np.pi) - low) / (high - low), 0, 1)
+        return (1 - s) * f / factor + s * f, 1.0
+    if scaling == "ramp":
+        def place(rotations):
+            return r * np.log(context / (rotations * 2 * np.pi)) / (2 * np.log(base))
+        begin, end = np.clip([np.floor(place(high)), np.ceil(place(low))], 0, r - 1)
+        s = 1 - np.clip((i - begin) / (end - begin if end > begin else 1e-3), 0, 1)
+        return (1 - s) * f / factor + s * f, 1 + 0.1 * np.log(factor)
+    return f, 1.0
+
+
+def rotary(x, positions, turns, amplitude, pairs):
+    """x [tokens][heads][d], turns [R/2] in revolutions a token.  Tokens at negative positions come back as they are."""
+    y, r = x.astype(np.float64).copy(), 2 * len(turns)
+    a, b = (slice(0, r, 2), slice(1, r, 2)) if pairs else (slice(0, r // 2), slice(r // 2, r))
+    for t, p in enumerate(positions):
+        if p < 0:
+            continue
+        turn = np.longdouble(int(p)) * turns.astype(np.longdouble)
+        angle = (2 * np.pi * (turn - np.rint(turn))).astype(np.float64)
+        c, s = amplitude * np.cos(angle), amplitude * np.sin(angle)
+        u, v = y[t][:, a].copy(), y[t][:, b].copy()
+        y[t][:, a], y[t][:, b] = u * c - v * s, u * s + v * c
+    return y

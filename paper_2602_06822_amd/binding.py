@@ -26,7 +26,7 @@ POP_EDEVICE = -7
 POP_REGION_RETAINED, POP_REGION_CANDIDATE, POP_REGION_PRUNED = 0, 1, 2
 POP_MAX_BATCH = 8
 
-_vp, _i, _dbl = C.c_void_p, C.c_int, C.c_double
+_vp, _i, _dbl, _f, _ll = C.c_void_p, C.c_int, C.c_double, C.c_float, C.c_longlong
 _ip = C.POINTER(C.c_int)
 _szp = C.POINTER(C.c_size_t)
 
@@ -73,6 +73,9 @@ _SIGS = {
     "pop_cache_reorder": (_i, [_vp, _vp, _vp, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp, _vp, _vp, C.c_size_t, _vp, _vp]),
     "pop_cache_reorder_workspace": (_i, [_i, _i, _i, _szp]),
     "pop_cache_copy_pages": (_i, [_vp, _i, _i, _i, _i, _vp, _i, _vp]),
+    "pop_block_norm": (_i, [_vp, _i, _ll, _vp, _i, _ll, _vp, _i, _ll, _i, _i, _vp, _vp, _i, _f, _f, _f, _f, _vp, _ll, _vp, _ll, _vp]),
+    "pop_rotary_frequencies": (_i, [_i, _dbl, _i, _dbl, _dbl, _dbl, _dbl, C.POINTER(C.c_double), C.POINTER(_f)]),
+    "pop_rotary": (_i, [_vp, _vp, _i, _i, _i, _i, _i, _i, _i, _ll, _ll, _vp, _vp, _f, _vp, _vp, _ll, _ll, _vp]),
 }
 for _name, (_res, _args) in _SIGS.items():
     _fn = getattr(_lib, _name)
@@ -403,6 +406,41 @@ def pop_cache_reorder_workspace(n_seq, n_beams, table_stride) -> int:
 def pop_cache_copy_pages(cache, n_kv_heads, head_dim, page_tokens, n_pages, copies, n_copies, stream=None):
     _check(_lib.pop_cache_copy_pages(_ptr(cache), n_kv_heads, head_dim, page_tokens, n_pages, _ptr(copies), n_copies,
                                      _stream(stream)), "pop_cache_copy_pages")
+
+
+def pop_block_norm(x, xdtype, u, dtype, n_tokens, d, x_out, z, w_pre=None, *, post_norm=False, w_post=None, gate=None, gate_rows=0,
+                   weight_offset=0.0, eps=1e-6, x_scale=1.0, u_scale=1.0, x_stride=None, u_stride=None, gate_stride=None,
+                   x_out_stride=None, z_stride=None, stream=None):
+    x, x_stride = _rows(x, d, x_stride, n_tokens)
+    u, u_stride = _rows(u, d, u_stride, n_tokens)
+    gate, gate_stride = _rows(gate, d, gate_stride, gate_rows)
+    x_out, x_out_stride = _rows(x_out, d, x_out_stride, n_tokens)
+    z, z_stride = _rows(z, d, z_stride, n_tokens)
+    _check(_lib.pop_block_norm(x, xdtype, x_stride, u, dtype, u_stride, gate, gate_rows, gate_stride, n_tokens, d, _ptr(w_post), _ptr(w_pre),
+                               1 if post_norm else 0, weight_offset, eps, x_scale, u_scale, x_out, x_out_stride, z, z_stride,
+                               _stream(stream)), "pop_block_norm")
+
+
+POP_ROTARY_HALVES, POP_ROTARY_PAIRS = 0, 1
+POP_ROTARY_PLAIN, POP_ROTARY_LINEAR, POP_ROTARY_BASE, POP_ROTARY_BANDS, POP_ROTARY_RAMP = 0, 1, 2, 3, 4
+
+
+def pop_rotary_frequencies(rotary_dim, base=10000.0, scaling=POP_ROTARY_PLAIN, factor=1.0, context=0.0, low=0.0, high=0.0):
+    """(list of rotary_dim / 2 frequencies in revolutions a token, amplitude)."""
+    turns, amplitude = (C.c_double * max(rotary_dim // 2, 1))(), C.c_float()
+    _check(_lib.pop_rotary_frequencies(rotary_dim, base, scaling, factor, context, low, high, turns, C.byref(amplitude)),
+           "pop_rotary_frequencies")
+    return list(turns), amplitude.value
+
+
+def pop_rotary(q, k, dtype, n_tokens, n_heads, n_kv_heads, head_dim, rotary_dim, layout, positions, turns, amplitude, q_out, k_out,
+               q_stride=None, k_stride=None, q_out_stride=None, k_out_stride=None, stream=None):
+    q, q_stride = _rows(q, n_heads * head_dim, q_stride, n_tokens)
+    k, k_stride = _rows(k, n_kv_heads * head_dim, k_stride, n_tokens)
+    q_out, q_out_stride = _rows(q_out, n_heads * head_dim, q_out_stride, n_tokens)
+    k_out, k_out_stride = _rows(k_out, n_kv_heads * head_dim, k_out_stride, n_tokens)
+    _check(_lib.pop_rotary(q, k, dtype, n_tokens, n_heads, n_kv_heads, head_dim, rotary_dim, layout, q_stride, k_stride, _ptr(positions),
+                           _ptr(turns), amplitude, q_out, k_out, q_out_stride, k_out_stride, _stream(stream)), "pop_rotary")
 
 
 def raw():

@@ -1,0 +1,249 @@
+// What stands between a decoder layer's blocks: residual sums with the norms around a block, rotary positions.
+#include <algorithm>
+
+#include "pop_block.h"
+
+namespace pop {
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b)
+{
+    const bf16x2 v = {(__bf16)a, (__bf16)b};
+    return __builtin_bit_cast(uint32_t, v);
+}
+
+// Eight channels of a row from `at` on: 16-byte loads.
+template <bool BF16>
+struct Eight {
+    u32x4 raw[BF16 ? 1 : 2];
+    __device__ __forceinline__ void load(const void *p, long long at)
+    {
+        const u32x4 *from = reinterpret_cast<const u32x4 *>(static_cast<const char *>(p) + at * (BF16 ? 2 : 4));
+#pragma unroll
+        for (int i = 0; i < (BF16 ? 1 : 2); ++i) raw[i] = from[i];
+    }
+    __device__ __forceinline__ float operator[](int i) const
+    {
+        if constexpr (BF16) return i % 2 ? bf16_hi(raw[0][i / 2]) : bf16_lo(raw[0][i / 2]);
+        else return __uint_as_float(raw[i / 4][i % 4]);
+    }
+};
+
+template <bool BF16>
+__device__ __forceinline__ void store_eight(void *p, long long at, const float (&x)[8])
+{
+    u32x4 *to = reinterpret_cast<u32x4 *>(static_cast<char *>(p) + at * (BF16 ? 2 : 4));
+    if constexpr (BF16) {
+        to[0] = u32x4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
+    } else {
+        const f32x4 a = {x[0], x[1], x[2], x[3]}, b = {x[4], x[5], x[6], x[7]};
+        to[0] = __builtin_bit_cast(u32x4, a), to[1] = __builtin_bit_cast(u32x4, b);
+    }
+}
+
+template <bool BF16>
+__device__ __forceinline__ float load_one(const void *p, long long at)
+{
+    if constexpr (BF16) return __uint_as_float((uint32_t)static_cast<const uint16_t *>(p)[at] << 16);
+    else return static_cast<const float *>(p)[at];
+}
+template <bool BF16>
+__device__ __forceinline__ void store_one(void *p, long long at, float x)
+{
+    if constexpr (BF16) static_cast<__bf16 *>(p)[at] = (__bf16)x;
+    else static_cast<float *>(p)[at] = x;
+}
+
+// ---------------------------------------------------------------- residual sums and norms
+
+// Sum over the workgroup, the same in every thread.
+__device__ __forceinline__ float workgroup_sum(float v, float *s_sums)
+{
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, kWave);
+    const int waves = blockDim.x / kWave;
+    if (waves == 1) return v;
+    if (threadIdx.x % kWave == 0) s_sums[threadIdx.x / kWave] = v;
+    __syncthreads();
+    v = 0.0f;
+    for (int i = 0; i < waves; ++i) v += s_sums[i];
+    return v;
+}
+
+// Eight of a row's channels: those from `at` on (V8), or every blockDim-th one.
+template <bool BF16, bool V8>
+__device__ __forceinline__ void row_load(const void *p, long long row, int at, int d, float (&x)[8])
+{
+    if constexpr (V8) {
+        Eight<BF16> e;
+        e.load(p, row + at);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = e[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int c = at + i * (int)blockDim.x;
+            x[i] = c < d ? load_one<BF16>(p, row + c) : 0.0f;
+        }
+    }
+}
+template <bool BF16, bool V8>
+__device__ __forceinline__ void row_store(void *p, long long row, int at, int d, const float (&x)[8])
+{
+    if constexpr (V8) {
+        store_eight<BF16>(p, row + at, x);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int c = at + i * (int)blockDim.x;
+            if (c < d) store_one<BF16>(p, row + c, x[i]);
+        }
+    }
+}
+
+// A workgroup has a row, a thread N eights of its channels in registers: everything is read once and written once.  The sums of squares
+// are float32: a thread's up to 8 N terms one by one, the rest a tree.
+template <bool XBF16, bool BF16, bool V8, int N>
+__global__ __launch_bounds__(1024) void block_norm_kernel(BlockNormArgs a)
+{
+    __shared__ float s_sums[2][16];
+    const long long row = blockIdx.x;
+    const int step = V8 ? (int)blockDim.x * 8 : (int)blockDim.x * 8, first = V8 ? (int)threadIdx.x * 8 : (int)threadIdx.x;
+    float v[N][8];
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[j][i] = 0.0f;
+        if (a.u && first + j * step < a.d) row_load<BF16, V8>(a.u, row * a.u_stride, first + j * step, a.d, v[j]);
+    }
+    if (a.post) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum = fmaf(v[j][i], v[j][i], sum);
+        const float by = 1.0f / sqrtf(workgroup_sum(sum, s_sums[0]) / (float)a.d + a.eps);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            if (first + j * step >= a.d) continue;
+            float w[8] = {1, 1, 1, 1, 1, 1, 1, 1};
+            if (a.w_post) row_load<BF16, V8>(a.w_post, 0, first + j * step, a.d, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[j][i] = v[j][i] * by * (a.w_post ? w[i] + a.offset : 1.0f);
+        }
+    }
+    float sum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        if (first + j * step >= a.d) continue;
+        float x[8];
+        row_load<XBF16, V8>(a.x, row * a.x_stride, first + j * step, a.d, x);
+        if (a.gate) {
+            float g[8];
+            row_load<BF16, V8>(a.gate, row * a.gate_stride, first + j * step, a.d, g);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[j][i] *= g[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            v[j][i] = a.u ? fmaf(a.x_scale, x[i], a.u_scale * v[j][i]) : a.x_scale * x[i];
+            sum = fmaf(v[j][i], v[j][i], sum);
+        }
+        if (a.x_out) row_store<XBF16, V8>(a.x_out, row * a.x_out_stride, first + j * step, a.d, v[j]);
+    }
+    if (!a.z) return;
+    const float by = 1.0f / sqrtf(workgroup_sum(sum, s_sums[1]) / (float)a.d + a.eps);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        if (first + j * step >= a.d) continue;
+        float w[8] = {1, 1, 1, 1, 1, 1, 1, 1};
+        if (a.w_pre) row_load<BF16, V8>(a.w_pre, 0, first + j * step, a.d, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[j][i] = v[j][i] * by * (a.w_pre ? w[i] + a.offset : 1.0f);
+        row_store<BF16, V8>(a.z, row * a.z_stride, first + j * step, a.d, v[j]);
+    }
+}
+
+inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+template <bool XBF16, bool BF16, bool V8>
+hipError_t launch_norm(const BlockNormArgs &a, hipStream_t s)
+{
+    const int eights = (a.d + 7) / 8;
+    const int n = eights <= 1024 ? 1 : eights <= 2048 ? 2 : eights <= 4096 ? 4 : 8;
+    const unsigned threads = (unsigned)(((eights + n - 1) / n + 63) / 64 * 64);
+    switch (n) {
+        case 1: block_norm_kernel<XBF16, BF16, V8, 1><<<a.n, threads, 0, s>>>(a); break;
+        case 2: block_norm_kernel<XBF16, BF16, V8, 2><<<a.n, threads, 0, s>>>(a); break;
+        case 4: block_norm_kernel<XBF16, BF16, V8, 4><<<a.n, threads, 0, s>>>(a); break;
+        default: block_norm_kernel<XBF16, BF16, V8, 8><<<a.n, threads, 0, s>>>(a); break;
+    }
+    return hipGetLastError();
+}
+
+// ---------------------------------------------------------------- rotary positions
+
+// A workgroup has a token and some of its heads: the token's sines and cosines stand in LDS, one thread computes each.  Angles are products
+// of 64 bits in revolutions, of which the whole ones are taken off before they are rounded to 32.
+template <bool BF16>
+__global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a)
+{
+    __shared__ float2 s_turn[kMostRotary / 2];
+    const int token = blockIdx.x, position = a.positions[token];
+    if (position < 0) return;
+    for (int i = threadIdx.x; i < a.r / 2; i += 256) {
+        const double t = (double)position * a.turns[i];
+        float sn, cs;
+        sincospif(2.0f * (float)(t - rint(t)), &sn, &cs);
+        s_turn[i] = {a.amplitude * cs, a.amplitude * sn};
+    }
+    __syncthreads();
+    const int per = a.r / 2 + (a.d - a.r), heads = a.n_heads + (a.k ? a.n_kv : 0);
+    for (int e = threadIdx.x; e < heads * per; e += 256) {
+        const int head = e / per, i = e % per;
+        const bool of_k = head >= a.n_heads;
+        const void *from = of_k ? a.k : a.q;
+        void *to = of_k ? a.k_out : a.q_out;
+        const int h = of_k ? head - a.n_heads : head;
+        const long long in = token * (of_k ? a.k_stride : a.q_stride) + (long long)h * a.d;
+        const long long out = token * (of_k ? a.k_out_stride : a.q_out_stride) + (long long)h * a.d;
+        if (i < a.r / 2) {
+            const int c0 = a.pairs ? 2 * i : i, c1 = a.pairs ? 2 * i + 1 : i + a.r / 2;
+            const float x = load_one<BF16>(from, in + c0), y = load_one<BF16>(from, in + c1);
+            const float2 t = s_turn[i];
+            store_one<BF16>(to, out + c0, x * t.x - y * t.y);
+            store_one<BF16>(to, out + c1, x * t.y + y * t.x);
+        } else {
+            const int c = a.r + i - a.r / 2;
+            store_one<BF16>(to, out + c, load_one<BF16>(from, in + c));
+        }
+    }
+}
+
+}  // namespace
+
+hipError_t launch_block_norm(const BlockNormArgs &a, hipStream_t s)
+{
+    const bool v8 = a.d % 8 == 0 && (a.x_stride | a.u_stride | a.gate_stride | a.x_out_stride | a.z_stride) % 8 == 0 && aligned16(a.x) && aligned16(a.u) &&
+                    aligned16(a.gate) && aligned16(a.w_post) && aligned16(a.w_pre) && aligned16(a.x_out) && aligned16(a.z);
+    if (a.x_bf16) {
+        if (a.bf16) return v8 ? launch_norm<true, true, true>(a, s) : launch_norm<true, true, false>(a, s);
+        return v8 ? launch_norm<true, false, true>(a, s) : launch_norm<true, false, false>(a, s);
+    }
+    if (a.bf16) return v8 ? launch_norm<false, true, true>(a, s) : launch_norm<false, true, false>(a, s);
+    return v8 ? launch_norm<false, false, true>(a, s) : launch_norm<false, false, false>(a, s);
+}
+
+hipError_t launch_rotary(const RotaryArgs &a, hipStream_t s)
+{
+    if (a.bf16) rotary_kernel<true><<<a.n, 256, 0, s>>>(a);
+    else rotary_kernel<false><<<a.n, 256, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace pop

@@ -1,4 +1,4 @@
-// C ABI of the calls around the FFN (cache, attention, beams): argument checks; the kernels stand in the files named below.
+// C ABI of the calls around the FFN (cache, attention, beams, norms, rotary positions): argument checks; the kernels stand in the files named below.
 #include <limits.h>
 #include <math.h>
 #include <stdint.h>
@@ -6,6 +6,7 @@
 #include <atomic>
 #include <chrono>
 
+#include "pop_block.h"  // pop_block.hip
 #include "pop_cache.h"  // pop_cache.hip, pop_cache_attention.hip, pop_beam.hip
 
 using namespace pop;
@@ -24,6 +25,11 @@ inline bool is_dtype(int t) { return t == POP_F32 || t == POP_BF16; }
 
 // An axis of a grid counts its threads in 32 bits: workgroups of 256.
 constexpr int kMostWorkgroups = (1 << 24) - 1;
+
+inline bool aligned_to(const void *p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) == 0; }
+inline int size_of(pop_dtype_t t) { return t == POP_BF16 ? 2 : 4; }
+// A workgroup of up to 1024 threads for each token.
+constexpr int kMostTokenRows = 1 << 22;
 
 int log_of_page(int page)
 {
@@ -247,6 +253,92 @@ int pop_cache_copy_pages(void *cache, int n_kv, int d, int page, int n_pages, co
     if (n_copies == 0) return POP_OK;
     if (!cache || !copies || !aligned16(cache)) return POP_EINVAL;
     POP_HIP(launch_cache_copy_pages(cache, c, copies, n_copies, as_stream(stream)));
+    return POP_OK;
+}
+
+int pop_block_norm(const void *x, pop_dtype_t xdtype, long long x_stride, const void *u, pop_dtype_t dtype, long long u_stride, const void *gate,
+                   int gate_rows, long long gate_stride, int n_tokens, int d, const void *w_post, const void *w_pre, int post_norm,
+                   float weight_offset, float eps, float x_scale, float u_scale, void *x_out, long long x_out_stride, void *z,
+                   long long z_stride, void *stream)
+{
+    if (n_tokens < 0 || d < 1) return POP_ESHAPE;
+    if (d > kMostNormWidth || n_tokens >= kMostTokenRows) return POP_EUNSUPPORTED;
+    if (!is_dtype(xdtype) || !is_dtype(dtype)) return POP_EINVAL;
+    if (!(eps > 0.0f) || !isfinite(eps) || !isfinite(weight_offset) || !isfinite(x_scale) || !isfinite(u_scale)) return POP_EINVAL;
+    if (x_stride < d || (u && u_stride < d) || (x_out && x_out_stride < d) || (z && z_stride < d)) return POP_ESHAPE;
+    if (gate ? (gate_rows != 1 && gate_rows != n_tokens) || (gate_rows > 1 && gate_stride < d) : gate_rows != 0) return POP_ESHAPE;
+    if (n_tokens == 0) return POP_OK;
+    if (!x || (!x_out && !z) || (!u && (gate || post_norm))) return POP_EINVAL;
+    const int xs = size_of(xdtype), us = size_of(dtype);
+    if (!aligned_to(x, xs) || !aligned_to(x_out, xs) || !aligned_to(u, us) || !aligned_to(gate, us) || !aligned_to(w_post, us) ||
+        !aligned_to(w_pre, us) || !aligned_to(z, us))
+        return POP_EINVAL;
+    // a thread reads the channels that it writes before it writes them: an output may take an input's place, channel by channel
+    const auto takes = [](const void *out, int os, long long of, const void *in, int is, long long from) { return out && out == in && (os != is || of != from); };
+    if (takes(x_out, xs, x_out_stride, x, xs, x_stride) || takes(x_out, xs, x_out_stride, u, us, u_stride) || takes(z, us, z_stride, x, xs, x_stride) ||
+        takes(z, us, z_stride, u, us, u_stride))
+        return POP_EINVAL;
+    if ((x_out && x_out == z) || (gate && (gate == x_out || gate == z)) || (w_pre && (w_pre == x_out || w_pre == z)) || (w_post && (w_post == x_out || w_post == z)))
+        return POP_EINVAL;
+    BlockNormArgs a = {x, xdtype == POP_BF16, x_stride, u, dtype == POP_BF16, u ? u_stride : 0, gate, gate && gate_rows > 1 ? gate_stride : 0, w_post, w_pre,
+                       n_tokens, d, post_norm != 0, weight_offset, eps, x_scale, u_scale, x_out, x_out ? x_out_stride : 0, z, z ? z_stride : 0};
+    POP_HIP(launch_block_norm(a, as_stream(stream)));
+    return POP_OK;
+}
+
+int pop_rotary_frequencies(int rotary_dim, double base, int scaling, double factor, double context, double low, double high, double *turns,
+                           float *amplitude)
+{
+    if (!turns || scaling < POP_ROTARY_PLAIN || scaling > POP_ROTARY_RAMP) return POP_EINVAL;
+    if (rotary_dim < (scaling == POP_ROTARY_BASE ? 4 : 2) || rotary_dim % 2 || rotary_dim > kMostRotary) return POP_ESHAPE;
+    if (!(base > 1.0) || !isfinite(base)) return POP_EINVAL;
+    if (scaling != POP_ROTARY_PLAIN && (!(factor >= 1.0) || !isfinite(factor))) return POP_EINVAL;
+    const bool banded = scaling >= POP_ROTARY_BANDS;
+    if (banded && (!(context > 0.0) || !isfinite(context) || !(low > 0.0) || !(high > low) || !isfinite(high))) return POP_EINVAL;
+    const double r = rotary_dim, whole = 2.0 * M_PI;
+    if (scaling == POP_ROTARY_BASE) base *= pow(factor, r / (r - 2.0));
+    if (!isfinite(base)) return POP_EINVAL;
+    // the place i (no whole number) of the frequency that makes so many rotations over the context
+    const auto place = [&](double rotations) { return r * log(context / (whole * rotations)) / (2.0 * log(base)); };
+    double begin = 0.0, end = 0.0;
+    if (scaling == POP_ROTARY_RAMP) {
+        begin = fmin(fmax(floor(place(high)), 0.0), r - 1.0), end = fmin(fmax(ceil(place(low)), 0.0), r - 1.0);
+        if (end == begin) end += 1e-3;
+    }
+    for (int i = 0; i < rotary_dim / 2; ++i) {
+        const double f = pow(base, -2.0 * i / r) / whole;
+        double kept = 1.0;  // how much of the frequency is not divided
+        if (scaling == POP_ROTARY_LINEAR) kept = 0.0;
+        if (scaling == POP_ROTARY_BANDS) kept = (context * f - low) / (high - low);
+        if (scaling == POP_ROTARY_RAMP) kept = 1.0 - (i - begin) / (end - begin);
+        kept = fmin(fmax(kept, 0.0), 1.0);
+        turns[i] = kept == 1.0 ? f : (1.0 - kept) * f / factor + kept * f;
+    }
+    if (amplitude) *amplitude = scaling == POP_ROTARY_RAMP ? (float)(1.0 + 0.1 * log(factor)) : 1.0f;
+    return POP_OK;
+}
+
+int pop_rotary(const void *q, const void *k, pop_dtype_t dtype, int n_tokens, int n_heads, int n_kv, int d, int rotary_dim, int layout,
+               long long q_stride, long long k_stride, const int *positions, const double *turns, float amplitude, void *q_out, void *k_out,
+               long long q_out_stride, long long k_out_stride, void *stream)
+{
+    if (n_tokens < 0 || n_heads < 1 || (k && n_kv < 1) || d < 1 || rotary_dim < 2 || rotary_dim % 2 || rotary_dim > d) return POP_ESHAPE;
+    const int of_k = k ? n_kv : 0;
+    if (rotary_dim > kMostRotary || ((long long)n_heads + of_k) * d >= 1 << 30 || n_tokens >= kMostTokenRows) return POP_EUNSUPPORTED;
+    if (!is_dtype(dtype) || (layout != POP_ROTARY_HALVES && layout != POP_ROTARY_PAIRS) || !isfinite(amplitude)) return POP_EINVAL;
+    if (q_stride < (long long)n_heads * d || q_out_stride < (long long)n_heads * d) return POP_ESHAPE;
+    if (k && (k_stride < (long long)n_kv * d || k_out_stride < (long long)n_kv * d)) return POP_ESHAPE;
+    if (n_tokens == 0) return POP_OK;
+    if (!q || !q_out || !k != !k_out || !positions || !turns) return POP_EINVAL;
+    const int size = size_of(dtype);
+    if (!aligned_to(q, size) || !aligned_to(k, size) || !aligned_to(q_out, size) || !aligned_to(k_out, size) || !aligned_to(positions, 4) ||
+        !aligned_to(turns, 8))
+        return POP_EINVAL;
+    if ((q_out == q && q_out_stride != q_stride) || (k && k_out == k && k_out_stride != k_stride) || q_out == k || q_out == k_out || k_out == q)
+        return POP_EINVAL;
+    RotaryArgs a = {q, k, dtype == POP_BF16, n_tokens, n_heads, of_k, d, rotary_dim, layout == POP_ROTARY_PAIRS, q_stride, k ? k_stride : 0, positions, turns,
+                    amplitude, q_out, k_out, q_out_stride, k ? k_out_stride : 0};
+    POP_HIP(launch_rotary(a, as_stream(stream)));
     return POP_OK;
 }
 

@@ -1,0 +1,134 @@
+"""Norms around a block and rotary positions on the host: frequencies, refusals, pins of their 64-bit oracle."""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import decoder_oracle as orc
+
+
+@pytest.fixture(scope="module")
+def pop():
+    from paper_2602_06822_amd import binding
+    return binding
+
+
+A = 1 << 20  # an address that is never looked at
+F = 0.25
+
+
+def _with(base, /, **change):
+    assert set(change) <= set(base)
+    return [{**base, **change}[k] for k in base]
+
+
+def _refused(pop, status, name, args):
+    assert getattr(pop.raw(), name)(*args) == getattr(pop, status), (name, args)
+
+
+NORM = dict(x=A, xdtype=0, x_stride=512, u=2 * A, dtype=1, u_stride=512, gate=3 * A, gate_rows=4, gate_stride=512, n=4, d=512, w_post=4 * A, w_pre=5 * A,
+            post=1, offset=0.0, eps=1e-6, x_scale=1.0, u_scale=1.0, x_out=6 * A, x_out_stride=512, z=7 * A, z_stride=512, stream=None)
+INF, NAN = math.inf, math.nan
+
+
+@pytest.mark.parametrize("status,change", [
+    ("POP_EINVAL", dict(x=None)), ("POP_EINVAL", dict(x_out=None, z=None)), ("POP_EINVAL", dict(xdtype=2)), ("POP_EINVAL", dict(dtype=-1)),
+    ("POP_EINVAL", dict(eps=0.0)), ("POP_EINVAL", dict(eps=-1.0)), ("POP_EINVAL", dict(eps=NAN)), ("POP_EINVAL", dict(eps=INF)),
+    ("POP_EINVAL", dict(offset=NAN)), ("POP_EINVAL", dict(x_scale=INF)), ("POP_EINVAL", dict(u_scale=NAN)),
+    ("POP_EINVAL", dict(u=None)), ("POP_EINVAL", dict(u=None, post=0)), ("POP_EINVAL", dict(u=None, gate=None, gate_rows=0)),
+    ("POP_EINVAL", dict(x=A + 2)), ("POP_EINVAL", dict(u=A + 1)), ("POP_EINVAL", dict(z=A + 1)), ("POP_EINVAL", dict(x_out=A + 2)),
+    ("POP_EINVAL", dict(gate=A + 1)), ("POP_EINVAL", dict(w_pre=A + 1)), ("POP_EINVAL", dict(w_post=A + 1)),
+    ("POP_EINVAL", dict(x_out=A, x_out_stride=1024)), ("POP_EINVAL", dict(z=A)), ("POP_EINVAL", dict(z=2 * A, z_stride=520)),
+    ("POP_EINVAL", dict(x_out=2 * A)), ("POP_EINVAL", dict(x_out=7 * A)), ("POP_EINVAL", dict(z=3 * A)), ("POP_EINVAL", dict(z=5 * A)),
+    ("POP_EINVAL", dict(x_out=4 * A)),
+    ("POP_ESHAPE", dict(n=-1)), ("POP_ESHAPE", dict(d=0)), ("POP_ESHAPE", dict(x_stride=511)), ("POP_ESHAPE", dict(u_stride=0)),
+    ("POP_ESHAPE", dict(x_out_stride=511)), ("POP_ESHAPE", dict(z_stride=-512)), ("POP_ESHAPE", dict(gate_rows=2)), ("POP_ESHAPE", dict(gate_rows=0)),
+    ("POP_ESHAPE", dict(gate=None)), ("POP_ESHAPE", dict(gate_stride=511)),
+    ("POP_EUNSUPPORTED", dict(d=65537)), ("POP_EUNSUPPORTED", dict(n=1 << 22)),
+    ("POP_OK", dict(n=0, gate_rows=1)), ("POP_OK", dict(n=0, gate=None, gate_rows=0, x=None))])
+def test_block_norm_refuses(pop, status, change):
+    _refused(pop, status, "pop_block_norm", _with(NORM, **change))
+
+
+ROTARY = dict(q=A, k=2 * A, dtype=1, n=4, n_heads=8, n_kv=2, d=64, r=64, layout=0, q_stride=512, k_stride=128, positions=A, turns=A, amplitude=1.0,
+              q_out=3 * A, k_out=4 * A, q_out_stride=512, k_out_stride=128, stream=None)
+
+
+@pytest.mark.parametrize("status,change", [
+    ("POP_EINVAL", dict(q=None)), ("POP_EINVAL", dict(q_out=None)), ("POP_EINVAL", dict(k=None)), ("POP_EINVAL", dict(k_out=None)),
+    ("POP_EINVAL", dict(positions=None)), ("POP_EINVAL", dict(turns=None)), ("POP_EINVAL", dict(dtype=3)), ("POP_EINVAL", dict(layout=2)),
+    ("POP_EINVAL", dict(amplitude=NAN)), ("POP_EINVAL", dict(q=A + 1)), ("POP_EINVAL", dict(turns=A + 4)), ("POP_EINVAL", dict(positions=A + 2)),
+    ("POP_EINVAL", dict(q_out=A, q_out_stride=640)), ("POP_EINVAL", dict(k_out=2 * A, k_out_stride=130)), ("POP_EINVAL", dict(k_out=A)),
+    ("POP_EINVAL", dict(q_out=2 * A)), ("POP_EINVAL", dict(k_out=3 * A)),
+    ("POP_ESHAPE", dict(n=-1)), ("POP_ESHAPE", dict(n_heads=0)), ("POP_ESHAPE", dict(n_kv=0)), ("POP_ESHAPE", dict(r=63)), ("POP_ESHAPE", dict(r=0)),
+    ("POP_ESHAPE", dict(r=66)), ("POP_ESHAPE", dict(q_stride=511)), ("POP_ESHAPE", dict(k_stride=127)), ("POP_ESHAPE", dict(q_out_stride=0)),
+    ("POP_ESHAPE", dict(k_out_stride=-128)),
+    ("POP_EUNSUPPORTED", dict(d=2048, r=1026, q_stride=1 << 20, k_stride=1 << 20)), ("POP_EUNSUPPORTED", dict(n=1 << 22)),
+    ("POP_EUNSUPPORTED", dict(n_heads=1 << 24, q_stride=1 << 30)), ("POP_OK", dict(n=0)), ("POP_OK", dict(n=0, k=None, n_kv=0))])
+def test_rotary_refuses(pop, status, change):
+    _refused(pop, status, "pop_rotary", _with(ROTARY, **change))
+
+
+SCALINGS = ["plain", "linear", "base", "bands", "ramp"]
+
+
+@pytest.mark.parametrize("scaling", SCALINGS)
+@pytest.mark.parametrize("r,base,factor,context,low,high", [(64, 1e4, 4.0, 4096, 1, 32), (128, 5e5, 8.0, 8192, 1, 4), (20, 1e4, 1.0, 2048, 1, 32),
+                                                            (4, 100.0, 2.5, 7, 0.5, 0.6), (1024, 1e6, 32.0, 1e6, 1, 32), (64, 1e4, 4.0, 3, 1, 32)])
+def test_frequencies(pop, scaling, r, base, factor, context, low, high):
+    got, amplitude = pop.pop_rotary_frequencies(r, base, SCALINGS.index(scaling), factor, context, low, high)
+    want, amp = orc.rotary_frequencies(r, base, scaling, factor, context, low, high)
+    # powers, logarithms and a blend in 64 bits on either side; the exponent of a power times ln(base) <= 41 may lose that many steps
+    assert np.allclose(got, want / (2 * np.pi), rtol=1e-13, atol=0)
+    assert abs(amplitude - amp) <= 2.0 ** -24 * amp
+
+
+def test_frequencies_by_hand(pop):
+    assert pop.pop_rotary_frequencies(4, 100.0)[0] == pytest.approx([1 / (2 * math.pi), 0.1 / (2 * math.pi)], rel=1e-15)
+    # the slowest is divided by the factor, the fastest stays
+    got, _ = pop.pop_rotary_frequencies(64, 1e4, pop.POP_ROTARY_BASE, 8.0)
+    plain, _ = pop.pop_rotary_frequencies(64, 1e4)
+    assert got[0] == plain[0] and got[-1] == pytest.approx(plain[-1] / 8, rel=1e-12)
+    got, amp = pop.pop_rotary_frequencies(64, 1e4, pop.POP_ROTARY_RAMP, 8.0, 4096, 1, 32)
+    assert got[0] == plain[0] and got[-1] == pytest.approx(plain[-1] / 8, rel=1e-15) and amp == pytest.approx(1.2079442, rel=1e-6)
+
+
+FREQUENCIES = dict(r=64, base=1e4, scaling=4, factor=2.0, context=4096.0, low=1.0, high=32.0)
+
+
+@pytest.mark.parametrize("status,change", [
+    ("POP_ESHAPE", dict(r=63)), ("POP_ESHAPE", dict(r=0)), ("POP_ESHAPE", dict(r=1026)), ("POP_ESHAPE", dict(r=2, scaling=2)),
+    ("POP_EINVAL", dict(scaling=5)), ("POP_EINVAL", dict(scaling=-1)), ("POP_EINVAL", dict(base=1.0)), ("POP_EINVAL", dict(base=INF)),
+    ("POP_EINVAL", dict(base=NAN)), ("POP_EINVAL", dict(factor=0.5)), ("POP_EINVAL", dict(factor=NAN)), ("POP_EINVAL", dict(context=0.0)),
+    ("POP_EINVAL", dict(low=0.0)), ("POP_EINVAL", dict(low=32.0)), ("POP_EINVAL", dict(high=INF)), ("POP_EINVAL", dict(scaling=2, base=1e300, factor=1e300)),
+    ("POP_EINVAL", dict(scaling=1, factor=0.0))])
+def test_frequencies_refuse(pop, status, change):
+    with pytest.raises(pop.PopError) as e:
+        pop.pop_rotary_frequencies(*_with(FREQUENCIES, **change))
+    assert e.value.status == getattr(pop, status)
+
+
+def test_frequencies_refuse_no_place(pop):
+    _refused(pop, "POP_EINVAL", "pop_rotary_frequencies", [64, 1e4, 0, 1.0, 0.0, 0.0, 0.0, None, None])
+
+
+# ---------------------------------------------------------------- the oracle, pinned by hand
+
+def test_oracle_norm_by_hand():
+    x, u = np.array([[3.0, 0.0]]), np.array([[1.0, 4.0]])
+    got, z = orc.block_norm(x, u, eps=0.0)
+    assert np.array_equal(got, [[4.0, 4.0]]) and np.allclose(z, 1.0, rtol=1e-15)
+    got, z = orc.block_norm(x, np.array([[5.0, 5.0]]), post=True, w_post=np.array([1.0, 3.0]), gate=np.array([[0.5, 1.0]]), offset=1.0, u_scale=2.0, eps=0.0)
+    assert np.allclose(got, [[3 + 2 * 0.5 * 2, 2 * 4]], rtol=1e-15)
+    assert np.allclose(z, got / np.sqrt((25 + 64) / 2), rtol=1e-15)
+
+
+def test_oracle_rotary_by_hand():
+    x = np.arange(1.0, 6.0).reshape(1, 1, 5)
+    quarter = orc.rotary(x, [1], np.array([0.25, 0.5]), 2.0, True)  # a quarter and half a turn
+    assert np.allclose(quarter, [[[-4, 2, -6, -8, 5]]], atol=1e-14)
+    quarter = orc.rotary(x, [1], np.array([0.25, 0.5]), 1.0, False)  # pairs (0, 2) and (1, 3)
+    assert np.allclose(quarter, [[[-3, -2, 1, -4, 5]]], atol=1e-14)
+    assert np.array_equal(orc.rotary(x, [-1], np.array([0.25, 0.5]), 2.0, True), x)
+    back = orc.rotary(orc.rotary(x, [12345], np.array([0.1, 0.37]), 1.0, True), [12345], np.array([-0.1, -0.37]), 1.0, True)
+    assert np.allclose(back, x, rtol=1e-12)
