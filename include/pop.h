@@ -362,6 +362,33 @@ int pop_cache_attention_workspace(int n_tokens, int n_seq, int n_heads, int n_kv
 int pop_cache_attention_kind(pop_dtype_t dtype, pop_dtype_t ydtype, int n_tokens, int n_seq, int n_heads, int n_kv_heads,
                              int head_dim, int max_new, int max_context, int window, int *parts);
 
+/* The same with first tokens that stay visible: with window > 0 a token at position p sees token t <= p if p - t < window or t < sinks.  Without a
+ * window, or with sinks = 0, it is pop_cache_attention.  Pages that no token sees may be none (given back to the pool).
+ * workspace: as for pop_cache_attention.  Errors: as pop_cache_attention; sinks < 0 -> POP_ESHAPE. */
+int pop_cache_attention_sinks(const void *q, pop_dtype_t dtype, int n_tokens, const void *cache, int n_kv_heads,
+                              int head_dim, int page_tokens, int n_pages, const int *block_table, int table_stride,
+                              const int *q_start, const int *context_len, int n_seq, int n_heads, int max_new,
+                              int max_context, float scale, int window, int sinks, void *y, pop_dtype_t ydtype,
+                              void *workspace, size_t workspace_bytes, void *stream);
+
+/* pop_cache_attention (without a window) for sequences that share a prefix: n_seq rows in groups of `group` sequences (beams of a prompt, or questions
+ * about one document), whose first prefix_len[g] tokens (dev [n_seq / group]) are the same in all rows of group g.  The caller sees to that: up to
+ * the shorter of prefix_len and its context, each row's table names pages that hold the same keys and values there, the same pages or copies, as
+ * pop_cache_reorder leaves them.  Tokens of the prefix are read from any of the rows that have new tokens, once for all of them; rows may be
+ * shorter than the prefix, and new tokens may stand in it.  prefix_len that is negative or 0 shares nothing.
+ * Short prefixes, and chunks for which pop_cache_attention_kind gives 2, are read by each row for itself.
+ * Rows, types, limits and errors otherwise as pop_cache_attention (of the rounds: < 2^30); group < 1 or n_seq no multiple of it -> POP_ESHAPE.
+ * workspace: dev, of pop_cache_attention_shared_workspace bytes for the same group and the same or larger other sizes; any content, for this call
+ * alone. */
+int pop_cache_attention_shared(const void *q, pop_dtype_t dtype, int n_tokens, const void *cache, int n_kv_heads,
+                               int head_dim, int page_tokens, int n_pages, const int *block_table, int table_stride,
+                               const int *q_start, const int *context_len, int n_seq, int group, const int *prefix_len,
+                               int n_heads, int max_new, int max_context, float scale, void *y, pop_dtype_t ydtype,
+                               void *workspace, size_t workspace_bytes, void *stream);
+/* Host only. */
+int pop_cache_attention_shared_workspace(int n_tokens, int n_seq, int group, int n_heads, int n_kv_heads, int head_dim,
+                                         int max_new, int max_context, size_t *bytes);
+
 /* Beam search's selection.  logits: dev [n_requests * n_beams][vocab] (float32 or bf16), scores: dev [n_requests * n_beams]
  * float32, the beams' sums of log-probabilities (-inf: not alive), done: dev, a byte for each beam (may be NULL).
  * A beam proposes scores + logit - logsumexp(logits) for every token; one that is done proposes pad_token at its own score

@@ -160,8 +160,9 @@ def reorder(table, length, parents, n_beams, page_tokens, ring, pool):
 
 # ---------------------------------------------------------------- attention
 
-def attention(q, k, v, scale, first_pos, window=0, there=None, sizes=None):
-    """One sequence: q [new][heads][D]; k, v [context][kv heads][D]; there [context]: tokens whose page exists.
+def attention(q, k, v, scale, first_pos, window=0, there=None, sizes=None, sinks=0):
+    """One sequence: q [new][heads][D]; k, v [context][kv heads][D]; there [context]: tokens whose page exists; with a window, the first `sinks`
+    tokens stay visible.
     sizes: a list that gets (sum of weight |v|, largest sum |scale q k|), both [new][heads].., for error bounds."""
     new, heads, d = q.shape
     context, n_kv, _ = k.shape
@@ -173,7 +174,7 @@ def attention(q, k, v, scale, first_pos, window=0, there=None, sizes=None):
         pos = first_pos + i
         sees = key <= pos
         if window:
-            sees &= key > pos - window
+            sees &= (key > pos - window) | (key < sinks)
         if there is not None:
             sees &= there
         if not sees.any():

@@ -66,6 +66,11 @@ _SIGS = {
     "pop_cache_read": (_i, [_vp, _i, _i, _i, _i, _vp, _i, _vp, _vp, _i, _vp]),
     "pop_cache_attention": (_i, [_vp, _i, _i, _vp, _i, _i, _i, _i, _vp, _i, _vp, _vp, _i, _i, _i, _i, C.c_float, _i, _vp, _i,
                                  _vp, C.c_size_t, _vp]),
+    "pop_cache_attention_sinks": (_i, [_vp, _i, _i, _vp, _i, _i, _i, _i, _vp, _i, _vp, _vp, _i, _i, _i, _i, C.c_float, _i, _i, _vp, _i,
+                                       _vp, C.c_size_t, _vp]),
+    "pop_cache_attention_shared": (_i, [_vp, _i, _i, _vp, _i, _i, _i, _i, _vp, _i, _vp, _vp, _i, _i, _vp, _i, _i, _i, C.c_float, _vp, _i,
+                                        _vp, C.c_size_t, _vp]),
+    "pop_cache_attention_shared_workspace": (_i, [_i, _i, _i, _i, _i, _i, _i, _i, _szp]),
     "pop_cache_attention_workspace": (_i, [_i, _i, _i, _i, _i, _i, _i, _szp]),
     "pop_cache_attention_kind": (_i, [_i, _i, _i, _i, _i, _i, _i, _i, _i, _i, _ip]),
     "pop_beam_select": (_i, [_vp, _i, _vp, _vp, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp, C.c_size_t, _vp]),
@@ -362,6 +367,31 @@ def pop_cache_attention(q, dtype, n_tokens, cache, n_kv_heads, head_dim, page_to
                                     _ptr(block_table), table_stride, _ptr(q_start), _ptr(context_len), n_seq, n_heads,
                                     max_new, max_context, scale, window, _ptr(y), ydtype, ws, ws_bytes, _stream(stream)),
            "pop_cache_attention")
+
+
+def pop_cache_attention_sinks(q, dtype, n_tokens, cache, n_kv_heads, head_dim, page_tokens, n_pages, block_table, table_stride,
+                              q_start, context_len, n_seq, n_heads, max_new, max_context, scale, window, sinks, y, ydtype, workspace,
+                              stream=None):
+    ws, ws_bytes = _workspace(workspace)
+    _check(_lib.pop_cache_attention_sinks(_ptr(q), dtype, n_tokens, _ptr(cache), n_kv_heads, head_dim, page_tokens, n_pages,
+                                          _ptr(block_table), table_stride, _ptr(q_start), _ptr(context_len), n_seq, n_heads,
+                                          max_new, max_context, scale, window, sinks, _ptr(y), ydtype, ws, ws_bytes,
+                                          _stream(stream)), "pop_cache_attention_sinks")
+
+
+def pop_cache_attention_shared(q, dtype, n_tokens, cache, n_kv_heads, head_dim, page_tokens, n_pages, block_table, table_stride,
+                               q_start, context_len, n_seq, group, prefix_len, n_heads, max_new, max_context, scale, y, ydtype, workspace,
+                               stream=None):
+    ws, ws_bytes = _workspace(workspace)
+    _check(_lib.pop_cache_attention_shared(_ptr(q), dtype, n_tokens, _ptr(cache), n_kv_heads, head_dim, page_tokens, n_pages,
+                                           _ptr(block_table), table_stride, _ptr(q_start), _ptr(context_len), n_seq, group,
+                                           _ptr(prefix_len), n_heads, max_new, max_context, scale, _ptr(y), ydtype, ws, ws_bytes,
+                                           _stream(stream)), "pop_cache_attention_shared")
+
+
+def pop_cache_attention_shared_workspace(n_tokens, n_seq, group, n_heads, n_kv_heads, head_dim, max_new, max_context) -> int:
+    return _size(_lib.pop_cache_attention_shared_workspace, "pop_cache_attention_shared_workspace", n_tokens, n_seq, group, n_heads,
+                 n_kv_heads, head_dim, max_new, max_context)
 
 
 def pop_cache_attention_workspace(n_tokens, n_seq, n_heads, n_kv_heads, head_dim, max_new, max_context) -> int:

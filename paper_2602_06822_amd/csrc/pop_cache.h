@@ -132,11 +132,28 @@ struct AttentionArgs {
     void *y;
     int y_bf16;
     float *ws;
+    int sinks;  // first tokens that stay visible next to a window
 };
+// What a call runs: blocks of 128 columns and the parts of their tokens, or (no blocks) so many workgroups of the general kernel, which load
+// codes past the caches or not.
+struct AttentionLaunch {
+    int blocks, splits, workgroups;
+    bool past;
+};
+hipError_t launch_attention_sinks(const AttentionArgs &a, const AttentionLaunch &l, hipStream_t s);  // (pop_cache_attention_sinks.hip)
 size_t cache_attention_ws(int n_tokens, int n_seq, int n_heads, int n_kv, int d, int max_new, int max_context);
 // Parts that the prompt kernel splits the tokens of a block of 128 columns into, 0 where the general kernel takes the call.
 int cache_attention_parts(int n_tokens, int n_seq, int n_heads, int n_kv, int d, int max_new, int max_context, int window, int all_bf16);
 hipError_t launch_cache_attention(const AttentionArgs &a, hipStream_t s);
+
+struct SharedArgs {
+    AttentionArgs a;
+    int group;          // sequences of a group
+    const int *prefix;  // [n_seq / group] tokens that a group's sequences share
+    float *states;      // set by the launcher
+};
+size_t cache_attention_shared_ws(int n_tokens, int n_seq, int group, int n_heads, int n_kv, int d, int max_new, int max_context);
+hipError_t launch_cache_attention_shared(SharedArgs h, hipStream_t s);  // (pop_cache_attention_shared.hip)
 
 struct BeamArgs {
     const void *logits;

@@ -1,0 +1,555 @@
+// Attention over the 4-bit paged cache for groups of sequences that share a prefix: y = softmax(scale q k^T + mask) v, the prefix's keys and
+// values read and converted once for a block of the columns of all sequences of a group.
+//
+// With m, l and O the maximum, the sum of weights and the weighted sum of values over a set of tokens, two sets join as
+//     m = max(m1, m2),  l = 2^(m1 - m) l1 + 2^(m2 - m) l2,  O = 2^(m1 - m) O1 + 2^(m2 - m) O2,   y = O / l.
+// The first kernel leaves m, l and O of the prefix and of the tokens behind it, the second joins the two for every column.
+#include <math.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "pop_cache_attention_dev.h"
+
+namespace pop {
+
+namespace {
+
+constexpr int kRound = 128;  // tokens of a round: a step of each of the four waves
+constexpr int kWorkgroups = 512;
+// A prefix shorter than this is read by each sequence for itself.
+constexpr int kLeastPrefix = 256;
+
+// One step of a wave: 32 tokens of one kv head against NC blocks of 16 columns, whose keys and values are converted once.
+template <int D, int QT, int PT, int NC>
+struct WideSums {
+    bf16x8 q[NC][D / 32][QT];
+    f32x4 o[NC][D / 16];
+    float m[NC], l[NC], by[NC];  // (as in WaveSums, by block)
+
+    // LIVE: blocks that have columns.
+    template <int LIVE>
+    __device__ __forceinline__ void step(const TileRegs<D> (&r)[2], const int (&limit)[2], bool masked, int t0, const int (&pos)[NC], int g, float scale)
+    {
+        f32x4 s[2][LIVE];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+            for (int x = 0; x < LIVE; ++x) s[u][x] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) {
+                const bf16x8 k = k_operand<D>(r[u], c);
+#pragma unroll
+                for (int t = QT - 1; t >= 0; --t)
+#pragma unroll
+                    for (int x = 0; x < LIVE; ++x) s[u][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[x][c][t], s[u][x], 0, 0, 0);
+            }
+        }
+        uint32_t vs[2] = {r[0].vs, r[1].vs};
+        if (masked) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int t = t0 + 16 * u + 4 * g;
+#pragma unroll
+                for (int x = 0; x < LIVE; ++x)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (!(t + i < limit[u] && t + i <= pos[x])) s[u][x][i] = -INFINITY;
+                // scale bytes of tokens that are not there become 2^-127, so that whatever stands in their place is finite
+                const int left = limit[u] - t;
+                vs[u] = left >= 4 ? vs[u] : left <= 0 ? 0u : vs[u] & ((1u << (8 * left)) - 1);
+            }
+        }
+        bf16x8 w[LIVE][PT];
+#pragma unroll
+        for (int x = 0; x < LIVE; ++x) {
+            const f32x4 &a = s[0][x], &b = s[1][x];
+            float top = fmaxf(fmaxf(fmaxf(a[0], a[1]), fmaxf(a[2], a[3])), fmaxf(fmaxf(b[0], b[1]), fmaxf(b[2], b[3])));
+            if (__any(top * by[x] > m[x] + kSlack)) {  // (by > 0)
+                top = fmaxf(top, __shfl_xor(top, 16, kWave));
+                top = fmaxf(top, __shfl_xor(top, 32, kWave));
+                const float next = fmaxf(m[x], top * by[x]), factor = __builtin_amdgcn_exp2f(m[x] - next);
+                m[x] = next;
+                choose_unit(by[x], m[x], top, scale);
+                l[x] *= factor;
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) o[x][j] *= factor;
+            }
+            float p[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                p[i] = __builtin_amdgcn_exp2f(fmaf(i < 4 ? a[i % 4] : b[i % 4], by[x], -m[x]));
+                l[x] += p[i];
+            }
+            split_terms<PT>(p, w[x]);
+        }
+        float sv[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sv[i] = cache_scale((vs[i / 4] >> (8 * (i % 4))) & 255u);
+        constexpr int W = D / 32;  // bytes of a token: channels 2 b and 2 b + 1 of the lane's D/16 in byte b
+#pragma unroll
+        for (int b = 0; b < W; ++b) {
+            uint32_t c[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int at = (i % 4) * W + b;
+                c[i] = cache_pair_at(r[i / 4].v[at / 4], sv[i], at % 4);
+            }
+            const bf16x8 even = as_bf16x8(low_halves(c[0], c[1]), low_halves(c[2], c[3]), low_halves(c[4], c[5]), low_halves(c[6], c[7]));
+            const bf16x8 odd = as_bf16x8(high_halves(c[0], c[1]), high_halves(c[2], c[3]), high_halves(c[4], c[5]), high_halves(c[6], c[7]));
+#pragma unroll
+            for (int t = PT - 1; t >= 0; --t)
+#pragma unroll
+                for (int x = 0; x < LIVE; ++x) {
+                    o[x][2 * b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, w[x][t], o[x][2 * b], 0, 0, 0);
+                    o[x][2 * b + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, w[x][t], o[x][2 * b + 1], 0, 0, 0);
+                }
+        }
+    }
+};
+
+// Sequences in packs: a group, or 64 sequences of a larger one (and what is left of it).  A wave looks at as many whole packs at a time as 64
+// lanes hold, a lane for a sequence.
+struct Packs {
+    int group, per_group, at_once;  // parts of a group; sequences that a wave looks at where a group is a pack
+    __device__ __forceinline__ Packs(int n_beams) : group(n_beams), per_group((n_beams + 63) / 64), at_once(n_beams >= 64 ? 64 : 64 / n_beams * n_beams) {}
+    __device__ __forceinline__ int looks(int n_seq) const { return per_group > 1 ? n_seq / group * per_group : (n_seq + at_once - 1) / at_once; }
+    // The look's first sequence and how many there are.
+    __device__ __forceinline__ int first(int look) const { return per_group > 1 ? look / per_group * group + look % per_group * 64 : look * at_once; }
+    __device__ __forceinline__ int count(int look, int n_seq) const
+    {
+        return per_group > 1 ? min(64, group - look % per_group * 64) : min(at_once, n_seq - look * at_once);
+    }
+};
+
+// What a lane knows of its sequence, and of its pack.  Units of a sequence: if it is its pack's first, those of the prefix (blocks of the columns of all
+// its sequences); then its own (blocks of its columns over the tokens behind the prefix).
+struct Sequence {
+    int start, fresh, context;  // rows, new tokens (0: left out), tokens in the cache
+    int fresh_upto;             // new tokens of the look's sequences up to this one
+    int pack0, pack_n;          // lanes of the pack
+    int prefix;                 // shared tokens that are read once: a multiple of 32, 0 for none
+    int prefix_rounds, prefix_blocks, rounds, blocks;
+};
+
+// (sequences whose rows overlap may have more than 32 bits count: they stop there)
+__device__ __forceinline__ int columns_of(int tokens, int share) { return (int)min((long long)tokens * share, 0x7fff0000ll); }
+__device__ __forceinline__ int saturated(long long v) { return (int)min(v, 0x7fffffffll); }
+
+template <int COLUMNS>
+__device__ __forceinline__ Sequence look_at(const SharedArgs &h, const Packs &packs, int look, int lane)
+{
+    const AttentionArgs &a = h.a;
+    const int first = packs.first(look), count = packs.count(look, a.n_seq), share = a.n_heads / a.c.n_kv, s = first + lane;
+    Sequence q;
+    q.start = 0, q.fresh = 0, q.context = 0;
+    int prefix = 0;
+    if (lane < count) {
+        const int next = a.start[s + 1];
+        q.start = a.start[s], q.context = min(max(a.context[s], 0), kMostTokens);
+        prefix = h.prefix[s / packs.group];
+        if (q.start >= 0 && next > q.start && next <= a.n_tokens) q.fresh = next - q.start;
+    }
+    q.fresh_upto = wave_scan(q.fresh);
+    q.pack0 = packs.per_group > 1 ? 0 : lane / packs.group * packs.group;
+    q.pack_n = packs.per_group > 1 ? count : packs.group;
+    // the longest of the pack's sequences, whose row of the table the prefix is read from; one alone shares nothing
+    const unsigned long long live = __ballot(q.fresh > 0);
+    const unsigned long long members = (q.pack_n >= 64 ? ~0ull : (1ull << q.pack_n) - 1) << q.pack0;
+    int longest = q.fresh > 0 ? q.context : 0;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const int other = __shfl_down(longest, off, kWave);
+        if (lane + off < q.pack0 + q.pack_n) longest = max(longest, other);
+    }
+    longest = __shfl(longest, q.pack0, kWave);
+    const int table = a.stride << a.c.log_page;
+    prefix = min(min(prefix, longest), table) & ~31;
+    q.prefix = prefix >= kLeastPrefix && __popcll(live & members) > 1 ? prefix : 0;
+    const int in_front = __shfl(q.fresh_upto, max(q.pack0 - 1, 0), kWave);
+    const int in_pack = __shfl(q.fresh_upto, min(q.pack0 + q.pack_n, 64) - 1, kWave) - (q.pack0 > 0 ? in_front : 0);
+    const bool heads_pack = lane == q.pack0 && q.prefix > 0;
+    q.prefix_rounds = heads_pack ? (q.prefix + kRound - 1) / kRound : 0;
+    q.prefix_blocks = heads_pack ? (columns_of(in_pack, share) + COLUMNS - 1) / COLUMNS : 0;
+    q.blocks = (columns_of(q.fresh, share) + COLUMNS - 1) / COLUMNS;
+    q.rounds = q.fresh > 0 ? max((min(q.context, table) - q.prefix + kRound - 1) / kRound, 1) : 0;
+    return q;
+}
+
+// Rows of the workspace: pieces of units that several workgroups have, two places each; their counters; O, m and l of every (token, head)
+// over the prefix and over its own tokens, and behind them whether there is a prefix.
+template <int D, int COLUMNS>
+__device__ __forceinline__ float *piece_of(const SharedArgs &h, int place)
+{
+    return h.a.ws + (size_t)place * COLUMNS * (D + 4);
+}
+template <int D>
+__device__ __forceinline__ float *state_of(const SharedArgs &h, int own, size_t row)
+{
+    return h.states + ((size_t)own * h.a.n_tokens * h.a.n_heads + row) * (D + 4);
+}
+
+// Workgroup: 4 waves; dealt in equal numbers of rounds, as the kernel for sequences that share nothing.
+template <int D, int QT, int PT, int NC>
+__global__ __launch_bounds__(256, D == 256 || NC > 2 ? 1 : 2) void shared_attention_kernel(SharedArgs h, unsigned long long tag)
+{
+    constexpr int kTile = cache_tile_bytes(D), kColumns = 16 * NC;
+    constexpr int kPass = D > 128 ? 128 : D;
+    __shared__ float s_o[4][16][kPass + 4];
+    __shared__ float s_m[4][16], s_l[4][16];
+    __shared__ int s_last, s_row[kColumns];
+    const AttentionArgs &a = h.a;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
+    const int share = a.n_heads / a.c.n_kv, n_kv = a.c.n_kv;
+    const float scale = a.scale != 0.0f ? fabsf(a.scale) * kLog2e : 1.0f;
+    const TileOffsets<D> offsets(n, g);
+    const Packs packs(h.group);
+    const int looks = packs.looks(a.n_seq);
+
+    Sequence own;
+    int upto = 0, all = 0;  // rounds of the look's sequences up to the lane's; of all looks
+    const auto rounds_in = [&](int rounds, int blocks) { return saturated((long long)saturated((long long)rounds * blocks) * n_kv); };
+    const auto rounds_of = [&](const Sequence &q) {
+        return __builtin_elementwise_add_sat(rounds_in(q.prefix_rounds, q.prefix_blocks), rounds_in(q.rounds, q.blocks));
+    };
+    for (int look = 0; look < looks; ++look) {
+        own = look_at<kColumns>(h, packs, look, lane);
+        upto = wave_scan(rounds_of(own));
+        all = __builtin_elementwise_add_sat(all, __builtin_amdgcn_readlane(upto, 63));
+    }
+    const unsigned total = all, n_wg = min(gridDim.x, total);
+    if (blockIdx.x >= n_wg) return;
+    const unsigned fewest = total / n_wg, longer = total - fewest * n_wg;
+    const auto workgroup_of = [&](unsigned round) {
+        const unsigned of_longer = longer * (fewest + 1);
+        return (int)(round < of_longer ? round / (fewest + 1) : longer + (round - of_longer) / fewest);
+    };
+    int at = blockIdx.x * fewest + min(blockIdx.x, longer);
+    const int end = at + (int)fewest + (blockIdx.x < longer);
+    int look = 0, look_at_round = 0;  // the look that `own` is of, and the rounds in front of it
+    if (looks > 1) {
+        own = look_at<kColumns>(h, packs, 0, lane);
+        upto = wave_scan(rounds_of(own));
+    }
+    unsigned long long *const counters = reinterpret_cast<unsigned long long *>(piece_of<D, kColumns>(h, 2 * (int)gridDim.x));
+    const size_t page_bytes = cache_page_bytes(a.c);
+
+    while (at < end) {
+        const int of_look = __builtin_amdgcn_readlane(upto, 63);
+        if ((unsigned)at >= (unsigned)look_at_round + (unsigned)of_look) {
+            look_at_round += of_look;
+            if (++look >= looks) break;  // (never, but for sums that saturate)
+            own = look_at<kColumns>(h, packs, look, lane);
+            upto = wave_scan(rounds_of(own));
+            continue;
+        }
+        const int owner = __ffsll((unsigned long long)__ballot(upto > at - look_at_round)) - 1;
+        const int seq_at = look_at_round + (owner > 0 ? __builtin_amdgcn_readlane(upto, owner - 1) : 0);
+        const int prefix = __builtin_amdgcn_readlane(own.prefix, owner);
+        const int prefix_rounds = __builtin_amdgcn_readlane(own.prefix_rounds, owner), prefix_blocks = __builtin_amdgcn_readlane(own.prefix_blocks, owner);
+        const int of_prefix = rounds_in(prefix_rounds, prefix_blocks);
+        const bool shared = at - seq_at < of_prefix;
+        const int rounds = shared ? prefix_rounds : __builtin_amdgcn_readlane(own.rounds, owner);
+        const int first_at = shared ? seq_at : seq_at + of_prefix;
+        const int unit = (int)((unsigned)(at - first_at) / (unsigned)rounds), block = (int)((unsigned)unit / (unsigned)n_kv), head = unit - block * n_kv;
+        const int unit_at = first_at + unit * rounds, begin = at - unit_at, stop = min(rounds, end - unit_at);
+
+        // columns: of the pack's sequences one after another, or of this one
+        const int pack0 = __builtin_amdgcn_readlane(own.pack0, owner), pack_n = __builtin_amdgcn_readlane(own.pack_n, owner);
+        const int before = shared ? (pack0 > 0 ? __builtin_amdgcn_readlane(own.fresh_upto, pack0 - 1) : 0) : 0;
+        const int tokens = shared ? __builtin_amdgcn_readlane(own.fresh_upto, pack0 + pack_n - 1) - before : __builtin_amdgcn_readlane(own.fresh, owner);
+        const int n_columns = columns_of(tokens, share), n_live = min(kColumns, n_columns - block * kColumns);
+        int row[NC], pos[NC];
+        int lowest = kMostTokens, highest = -1;  // of the live columns' positions
+#pragma unroll
+        for (int x = 0; x < NC; ++x) {
+            const int col = block * kColumns + 16 * x + n, token = min(col, n_columns - 1) / share;
+            int of = owner, local = token;
+            if (shared) {
+                int lo = 0;  // sequences whose tokens all stand in front of this one
+#pragma unroll
+                for (int half = 32; half > 0; half >>= 1)
+                    if (__shfl(own.fresh_upto, lo + half - 1, kWave) <= before + token) lo += half;
+                of = lo;
+                local = before + token - (__shfl(own.fresh_upto, max(lo - 1, 0), kWave) & (lo > 0 ? -1 : 0));
+            }
+            row[x] = __shfl(own.start, of, kWave) + local;
+            pos[x] = __shfl(own.context, of, kWave) - __shfl(own.fresh, of, kWave) + local;
+            if (col < n_columns) lowest = min(lowest, pos[x]), highest = max(highest, pos[x]);
+            else pos[x] = -1, row[x] = -1;  // a column that is not there sees nothing
+            if (wave == 0 && g == 0) s_row[16 * x + n] = row[x];
+        }
+#pragma unroll
+        for (int off = 1; off < 16; off <<= 1)
+            lowest = min(lowest, __shfl_xor(lowest, off, kWave)), highest = max(highest, __shfl_xor(highest, off, kWave));
+        lowest = __builtin_amdgcn_readfirstlane(lowest), highest = __builtin_amdgcn_readfirstlane(highest);
+        // tokens, and the row of the table that names their pages: for the prefix that of the longest sequence
+        const int context = __builtin_amdgcn_readlane(own.context, owner);
+        int source = owner, lo = prefix, hi = max(min(context, a.stride << a.c.log_page), prefix);
+        if (shared) {
+            const bool member = lane >= pack0 && lane < pack0 + pack_n && own.fresh > 0;
+            const int most = __builtin_amdgcn_readlane(wave_scan<true>(member ? own.context : 0), 63);
+            source = __ffsll((unsigned long long)__ballot(member && own.context == most)) - 1;
+            lo = 0, hi = prefix;
+        }
+        const int seq = packs.first(look) + source;
+        const scalar_ints table = (scalar_ints)(uintptr_t)(a.table + (size_t)seq * a.stride);
+        const int tiles = (n_live + 15) / 16;
+
+        WideSums<D, QT, PT, NC> sums;
+        {
+            const int t1 = min(min(hi, highest + 1), lo + stop * kRound), first = lo + begin * kRound + wave * 32;
+            const unsigned char *const cache = a.cache + (size_t)(head * (a.c.page >> 4)) * kTile;
+            TileRegs<D> r[2][2];
+            int limit[2][2], page[2];
+            // the pages of a step's tiles; past the last step that of the last token again, of which nothing is loaded
+            auto look_up = [&](int t0) {
+                if (a.c.page == 16) {
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) page[u] = table[min(t0 + 16 * u, t1 - 1) >> 4];
+                } else {  // one page holds both
+                    page[0] = page[1] = table[min(t0, t1 - 1) >> a.c.log_page];
+                }
+            };
+            auto load = [&](TileRegs<D> (&to)[2], int (&lim)[2], int t0) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int t = t0 + 16 * u;
+                    lim[u] = (unsigned)page[u] < (unsigned)a.c.n_pages ? t1 : 0;
+                    const unsigned char *tile = cache + (size_t)(lim[u] ? (unsigned)page[u] : 0u) * page_bytes + ((t & (a.c.page - 1)) >> 4) * kTile;
+                    load_tile<D, false>(to[u], tile, t < lim[u], offsets);
+                }
+            };
+            if (first < t1) look_up(first);
+            else page[0] = page[1] = -1;
+            load(r[0], limit[0], first);
+            if (first < t1) look_up(first + kRound);
+            const uint32_t sign = a.scale < 0.0f ? (QT == 1 ? 0x80008000u : 0x80000000u) : 0u, keep = a.scale != 0.0f ? ~0u : 0u;
+#pragma unroll
+            for (int x = 0; x < NC; ++x) {
+                const int col = block * kColumns + 16 * x + n, qh = head * share + col % share;
+                constexpr int kQ = QT == 1 ? D / 32 : D / 16;
+                const size_t q_at = ((size_t)max(row[x], 0) * a.n_heads + qh) * D + g * (D / 4);
+                const u32x4 *q_from = QT == 1 ? reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(a.q) + q_at)
+                                              : reinterpret_cast<const u32x4 *>(static_cast<const float *>(a.q) + q_at);
+                u32x4 q[kQ];
+#pragma unroll
+                for (int i = 0; i < kQ; ++i) {
+                    q[i] = u32x4{0, 0, 0, 0};
+                    if (row[x] >= 0) q[i] = q_from[i];
+                    q[i] = (q[i] ^ sign) & keep;
+                }
+#pragma unroll
+                for (int s = 0; s < D / 32; ++s) {
+                    if constexpr (QT == 1) {
+                        sums.q[x][s][0] = __builtin_bit_cast(bf16x8, q[s]);
+                    } else {
+                        float v[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(q[2 * s + i / 4][i % 4]);
+                        split_terms<QT>(v, sums.q[x][s]);
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < D / 16; ++j) sums.o[x][j] = f32x4{0, 0, 0, 0};
+                sums.m[x] = kLowest, sums.l[x] = 0.0f, sums.by[x] = scale;
+            }
+            const auto all_steps = [&](auto live) {
+                for (int t0 = first; t0 < t1;) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        load(r[1 - i], limit[1 - i], t0 + kRound);
+                        look_up(t0 + 2 * kRound);
+                        const bool whole = t0 + 32 <= min(limit[i][0], limit[i][1]) && t0 + 31 <= lowest;
+                        if (t0 < t1) sums.template step<decltype(live)::value>(r[i], limit[i], !whole, t0, pos, g, scale);
+                        t0 += kRound;
+                    }
+                }
+            };
+            if (NC > 1 && tiles == 1) all_steps(std::integral_constant<int, 1>());
+            else all_steps(std::integral_constant<int, NC>());
+        }
+
+        const bool whole = begin == 0 && stop == rounds;
+        float *const part = piece_of<D, kColumns>(h, 2 * blockIdx.x + (begin == 0));
+        // what the four waves left in LDS of 16 columns, each relative to its own maximum: a piece, or all there is of the unit's tokens
+        const auto merge = [&](int x, int live, int pass, bool all_there) {
+            for (int e = threadIdx.x; e < live * (kPass / 2); e += 256) {
+                const int c = e / (kPass / 2), ch = e % (kPass / 2) * 2;
+                float most = kLowest, sum = 0.0f, u = 0.0f, v = 0.0f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) most = fmaxf(most, s_m[i][c]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float f = __builtin_amdgcn_exp2f(s_m[i][c] - most);
+                    sum += f * s_l[i][c], u += f * s_o[i][c][ch], v += f * s_o[i][c][ch + 1];
+                }
+                if (!all_there) {
+                    float *const to = part + (16 * x + c) * (D + 4);
+                    store_pair(to + pass * kPass + ch, u, v);
+                    if (ch == 0 && pass == 0) store_pair(to + D, most, sum);
+                    continue;
+                }
+                const size_t of = (size_t)s_row[16 * x + c] * a.n_heads + head * share + (block * kColumns + 16 * x + c) % share;
+                float *const to = state_of<D>(h, !shared, of);
+                if (shared || prefix > 0) {
+                    *reinterpret_cast<float2 *>(to + pass * kPass + ch) = {u, v};
+                } else {
+                    const float by = sum > 0.0f ? 1.0f / sum : 0.0f;
+                    store_y2(a, of * D + pass * kPass + ch, u * by, v * by);
+                }
+                if (ch == 0 && pass == 0) *reinterpret_cast<float4 *>(to + D) = {most, sum, prefix > 0 ? 1.0f : 0.0f, 0.0f};
+            }
+        };
+#pragma unroll
+        for (int x = 0; x < NC; ++x) {
+            if (x >= tiles) break;
+            sums.l[x] += __shfl_xor(sums.l[x], 16, kWave);
+            sums.l[x] += __shfl_xor(sums.l[x], 32, kWave);
+            if (g == 0) s_m[wave][n] = by_scale(sums.m[x], sums.by[x], scale), s_l[wave][n] = sums.l[x];
+#pragma unroll
+            for (int pass = 0; pass < D / kPass; ++pass) {
+                // a lane has channels [g D/4, (g + 1) D/4) of column n, D/16 at a time; a pass takes those of some of the groups
+                constexpr int kPer = kPass / (D / 4);
+                if (g / kPer == pass) {
+                    float *to = &s_o[wave][n][(g % kPer) * (D / 4)];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int j = 0; j < D / 16; j += 4)
+                            *reinterpret_cast<float4 *>(to + i * (D / 16) + j) = {sums.o[x][j][i], sums.o[x][j + 1][i], sums.o[x][j + 2][i], sums.o[x][j + 3][i]};
+                }
+                __syncthreads();
+                merge(x, min(16, n_live - 16 * x), pass, whole);
+                __syncthreads();
+            }
+        }
+        if (!whole) {
+            // pieces of the unit: one for each of the workgroups that its first and its last round fall to and those between them
+            const int wg0 = workgroup_of(unit_at), pieces = workgroup_of(unit_at + rounds - 1) - wg0 + 1;
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's stores are acknowledged
+            __syncthreads();
+            if (threadIdx.x == 0) s_last = arrive_last(counters + wg0, tag, pieces);
+            __syncthreads();
+            if (s_last) {
+#pragma unroll 1
+                for (int x = 0; x < tiles; ++x) {
+                    const int live = min(16, n_live - 16 * x);
+                    const auto place = [&](int piece) { return piece_of<D, kColumns>(h, piece == 0 ? 2 * wg0 + 1 : 2 * (wg0 + piece)) + 16 * x * (D + 4); };
+#pragma unroll 1
+                    for (int pass = 0; pass < D / kPass; ++pass) {
+                        if (pieces <= 8) join_pieces<D, kPass, 8, 2>(a.ws, place, pieces, live, wave, lane, pass, s_o, s_m, s_l);
+                        else join_pieces<D, kPass, 2, 8>(a.ws, place, pieces, live, wave, lane, pass, s_o, s_m, s_l);
+                        __syncthreads();
+                        merge(x, live, pass, true);
+                        __syncthreads();
+                    }
+                }
+            }
+            __syncthreads();
+        }
+        at = unit_at + stop;
+    }
+}
+
+// y of the columns that have a prefix: one wave for a (token, head).
+template <int D>
+__global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs h)
+{
+    const AttentionArgs &a = h.a;
+    const int start = a.start[blockIdx.x], next = a.start[blockIdx.x + 1], lane = threadIdx.x & 63;
+    if (!(start >= 0 && next > start && next <= a.n_tokens)) return;
+    const size_t end = (size_t)next * a.n_heads;
+    for (size_t row = (size_t)start * a.n_heads + blockIdx.y * 4 + threadIdx.x / 64; row < end; row += gridDim.y * 4) {
+        const float *p = state_of<D>(h, 0, row), *own = state_of<D>(h, 1, row);
+        const float4 e = *reinterpret_cast<const float4 *>(own + D), b = *reinterpret_cast<const float4 *>(p + D);
+        if (e.z == 0.0f) continue;  // (no prefix: y is there)
+        const float most = fmaxf(b.x, e.x), f1 = __builtin_amdgcn_exp2f(b.x - most), f2 = __builtin_amdgcn_exp2f(e.x - most);
+        const float sum = f1 * b.y + f2 * e.y, by = sum > 0.0f ? 1.0f / sum : 0.0f;
+        for (int ch = 2 * lane; ch < D; ch += 128) {
+            const float2 u = *reinterpret_cast<const float2 *>(p + ch), v = *reinterpret_cast<const float2 *>(own + ch);
+            store_y2(a, row * D + ch, (f1 * u.x + f2 * v.x) * by, (f1 * u.y + f2 * v.y) * by);
+        }
+    }
+}
+
+// Blocks of 16 columns that share a conversion: as many as a pack's columns fill, up to what the registers hold.
+int column_blocks(int n_tokens, int group, int n_heads, int n_kv, int d, int max_new, int terms)
+{
+    const long long columns = std::min<long long>(n_tokens, (long long)std::min(group, 64) * max_new) * (n_heads / n_kv);
+    const int most = d == 256 ? (terms == 1 ? 2 : 1) : (terms == 1 ? 4 : 2);
+    return std::min(most, columns <= 16 ? 1 : columns <= 32 ? 2 : 4);
+}
+
+struct SharedGrid {
+    int blocks, workgroups;
+    size_t pieces, states;  // bytes
+    size_t bytes() const { return pieces + states; }
+};
+SharedGrid shared_grid(int n_tokens, int n_seq, int group, int n_heads, int n_kv, int d, int max_new, int max_context, int terms)
+{
+    SharedGrid g = {column_blocks(n_tokens, group, n_heads, n_kv, d, max_new, terms), 0, 0, 0};
+    const long long share = n_heads / n_kv, rounds = (max_context + (long long)kRound - 1) / kRound;
+    // (for these sizes and all smaller ones, whose blocks may be fewer)
+    for (int nc = 1; nc <= g.blocks; nc *= 2) {
+        const long long most = d == 256 || nc > 2 ? kWorkgroups / 2 : kWorkgroups, packs = (long long)n_seq / group * ((group + 63) / 64);
+        const long long units = n_kv * (n_seq * ((max_new * share + 16 * nc - 1) / (16 * nc)) + packs * ((std::min(group, 64) * max_new * share + 16 * nc - 1) / (16 * nc)));
+        const long long per_unit = std::min(rounds, std::max(32ll, (long long)(2.0 * sqrt((double)rounds))));
+        g.workgroups = (int)std::min(units * per_unit, units >= 128 ? most : kWorkgroups / 2ll);
+        g.pieces = std::max(g.pieces, ((size_t)g.workgroups * (2 * 16 * nc * (d + 4) * sizeof(float) + 8) + 255) / 256 * 256);
+    }
+    g.states = 2 * (size_t)n_tokens * n_heads * (d + 4) * sizeof(float);
+    return g;
+}
+
+template <int D, int QT, int PT, int NC>
+hipError_t launch_nc(const SharedArgs &h, const SharedGrid &g, hipStream_t s)
+{
+    shared_attention_kernel<D, QT, PT, NC><<<(unsigned)g.workgroups, 256, 0, s>>>(h, launch_tag());
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    const long long rows = (long long)h.a.max_new * h.a.n_heads;  // of a sequence
+    shared_join_kernel<D><<<dim3((unsigned)h.a.n_seq, (unsigned)std::min((rows + 3) / 4, 64ll)), 256, 0, s>>>(h);
+    return hipGetLastError();
+}
+template <int D, int QT, int PT>
+hipError_t launch_types(const SharedArgs &h, const SharedGrid &g, hipStream_t s)
+{
+    if (g.blocks == 1) return launch_nc<D, QT, PT, 1>(h, g, s);
+    if constexpr (QT == 1 || D < 256) {
+        if (g.blocks == 2) return launch_nc<D, QT, PT, 2>(h, g, s);
+        if constexpr (QT == 1 && D < 256) return launch_nc<D, QT, PT, 4>(h, g, s);
+    }
+    return hipErrorInvalidValue;
+}
+template <int D>
+hipError_t launch_shared_d(const SharedArgs &h, const SharedGrid &g, hipStream_t s)
+{
+    if (!h.a.q_bf16) return launch_types<D, 3, 3>(h, g, s);
+    if (!h.a.y_bf16) return launch_types<D, 1, 3>(h, g, s);
+    return launch_types<D, 1, 1>(h, g, s);
+}
+
+}  // namespace
+
+size_t cache_attention_shared_ws(int n_tokens, int n_seq, int group, int n_heads, int n_kv, int d, int max_new, int max_context)
+{
+    if (group == 1) return 0;
+    return std::max(shared_grid(n_tokens, n_seq, group, n_heads, n_kv, d, max_new, max_context, 1).bytes(),
+                    shared_grid(n_tokens, n_seq, group, n_heads, n_kv, d, max_new, max_context, 3).bytes());
+}
+
+hipError_t launch_cache_attention_shared(SharedArgs h, hipStream_t s)
+{
+    const AttentionArgs &a = h.a;
+    // chunks for which the kernel for blocks of 128 columns pays are bound by their products: they gain nothing from a prefix that is read once
+    const int parts = cache_attention_parts(a.n_tokens, a.n_seq, a.n_heads, a.c.n_kv, a.c.d, a.max_new, a.max_context, 0, a.q_bf16 && a.y_bf16);
+    if (h.group == 1 || parts > 0) return launch_cache_attention(a, s);
+    const SharedGrid g = shared_grid(a.n_tokens, a.n_seq, h.group, a.n_heads, a.c.n_kv, a.c.d, a.max_new, a.max_context, a.q_bf16 ? 1 : 3);
+    h.states = reinterpret_cast<float *>(reinterpret_cast<char *>(a.ws) + g.pieces);
+    if (a.c.d == 64) return launch_shared_d<64>(h, g, s);
+    if (a.c.d == 128) return launch_shared_d<128>(h, g, s);
+    return launch_shared_d<256>(h, g, s);
+}
+
+}  // namespace pop

@@ -3,6 +3,7 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <atomic>
 #include <chrono>
 
@@ -148,16 +149,16 @@ int pop_cache_attention_kind(pop_dtype_t dtype, pop_dtype_t ydtype, int n_tokens
     return none ? 0 : of_blocks > 0 ? 2 : 1;
 }
 
-int pop_cache_attention(const void *q, pop_dtype_t dtype, int n_tokens, const void *cache, int n_kv, int d, int page, int n_pages,
-                        const int *block_table, int table_stride, const int *q_start, const int *context_len, int n_seq, int n_heads,
-                        int max_new, int max_context, float scale, int window, void *y, pop_dtype_t ydtype, void *workspace,
-                        size_t workspace_bytes, void *stream)
+int pop_cache_attention_sinks(const void *q, pop_dtype_t dtype, int n_tokens, const void *cache, int n_kv, int d, int page, int n_pages,
+                              const int *block_table, int table_stride, const int *q_start, const int *context_len, int n_seq, int n_heads,
+                              int max_new, int max_context, float scale, int window, int sinks, void *y, pop_dtype_t ydtype, void *workspace,
+                              size_t workspace_bytes, void *stream)
 {
     CacheShape c;
     int rc = cache_shape(n_kv, d, page, n_pages, &c);
     if (rc == POP_OK) rc = attention_sizes(n_tokens, n_seq, n_heads, n_kv, d, max_new, max_context);
     if (rc != POP_OK) return rc;
-    if (table_stride < 1 || window < 0) return POP_ESHAPE;
+    if (table_stride < 1 || window < 0 || sinks < 0) return POP_ESHAPE;
     if ((long long)table_stride * page > 1 << 30) return POP_EUNSUPPORTED;
     if (!is_dtype(dtype) || !is_dtype(ydtype) || !isfinite(scale)) return POP_EINVAL;
     // rounds of 128 tokens are counted in 32 bits
@@ -170,8 +171,63 @@ int pop_cache_attention(const void *q, pop_dtype_t dtype, int n_tokens, const vo
     if (workspace_bytes < need) return POP_ESHAPE;
     AttentionArgs a = {q, dtype == POP_BF16, n_tokens, static_cast<const unsigned char *>(cache), c, block_table, table_stride, q_start,
                        context_len, n_seq, n_heads, max_new, max_context, scale, window, y, ydtype == POP_BF16,
-                       static_cast<float *>(workspace)};
+                       static_cast<float *>(workspace), sinks};
     POP_HIP(launch_cache_attention(a, as_stream(stream)));
+    return POP_OK;
+}
+
+int pop_cache_attention(const void *q, pop_dtype_t dtype, int n_tokens, const void *cache, int n_kv, int d, int page, int n_pages,
+                        const int *block_table, int table_stride, const int *q_start, const int *context_len, int n_seq, int n_heads,
+                        int max_new, int max_context, float scale, int window, void *y, pop_dtype_t ydtype, void *workspace,
+                        size_t workspace_bytes, void *stream)
+{
+    return pop_cache_attention_sinks(q, dtype, n_tokens, cache, n_kv, d, page, n_pages, block_table, table_stride, q_start, context_len, n_seq, n_heads,
+                                     max_new, max_context, scale, window, 0, y, ydtype, workspace, workspace_bytes, stream);
+}
+
+static int shared_sizes(int n_tokens, int n_seq, int group, int n_heads, int n_kv, int d, int max_new, int max_context)
+{
+    const int rc = attention_sizes(n_tokens, n_seq, n_heads, n_kv, d, max_new, max_context);
+    if (rc != POP_OK) return rc;
+    return group < 1 || n_seq % group ? POP_ESHAPE : POP_OK;
+}
+
+int pop_cache_attention_shared_workspace(int n_tokens, int n_seq, int group, int n_heads, int n_kv, int d, int max_new, int max_context, size_t *bytes)
+{
+    if (!bytes) return POP_EINVAL;
+    const int rc = shared_sizes(n_tokens, n_seq, group, n_heads, n_kv, d, max_new, max_context);
+    if (rc != POP_OK) return rc;
+    *bytes = n_seq ? std::max(cache_attention_ws(n_tokens, n_seq, n_heads, n_kv, d, max_new, max_context),
+                              cache_attention_shared_ws(n_tokens, n_seq, group, n_heads, n_kv, d, max_new, max_context))
+                   : 0;
+    return POP_OK;
+}
+
+int pop_cache_attention_shared(const void *q, pop_dtype_t dtype, int n_tokens, const void *cache, int n_kv, int d, int page, int n_pages,
+                               const int *block_table, int table_stride, const int *q_start, const int *context_len, int n_seq, int group,
+                               const int *prefix_len, int n_heads, int max_new, int max_context, float scale, void *y, pop_dtype_t ydtype,
+                               void *workspace, size_t workspace_bytes, void *stream)
+{
+    CacheShape c;
+    int rc = cache_shape(n_kv, d, page, n_pages, &c);
+    if (rc == POP_OK) rc = shared_sizes(n_tokens, n_seq, group, n_heads, n_kv, d, max_new, max_context);
+    if (rc != POP_OK) return rc;
+    if (table_stride < 1) return POP_ESHAPE;
+    if ((long long)table_stride * page > 1 << 30) return POP_EUNSUPPORTED;
+    if (!is_dtype(dtype) || !is_dtype(ydtype) || !isfinite(scale)) return POP_EINVAL;
+    // rounds of 128 tokens, of prefixes and of what stands behind them, are counted in 32 bits
+    if (((long long)n_tokens * (n_heads / n_kv) / 16 + n_seq) * n_kv * ((long long)table_stride * page / 128 + 1) > INT_MAX / 2) return POP_EUNSUPPORTED;
+    if (n_seq == 0 || n_tokens == 0) return POP_OK;
+    if (!q || !cache || !block_table || !q_start || !context_len || !prefix_len || !y) return POP_EINVAL;
+    if (!aligned16(q) || !aligned16(cache) || !aligned16(y) || !aligned16(workspace)) return POP_EINVAL;
+    const size_t need = std::max(cache_attention_ws(n_tokens, n_seq, n_heads, n_kv, d, max_new, max_context),
+                                 cache_attention_shared_ws(n_tokens, n_seq, group, n_heads, n_kv, d, max_new, max_context));
+    if (need && !workspace) return POP_EINVAL;
+    if (workspace_bytes < need) return POP_ESHAPE;
+    SharedArgs h = {{q, dtype == POP_BF16, n_tokens, static_cast<const unsigned char *>(cache), c, block_table, table_stride, q_start, context_len, n_seq,
+                     n_heads, max_new, max_context, scale, 0, y, ydtype == POP_BF16, static_cast<float *>(workspace), 0},
+                    group, prefix_len, nullptr};
+    POP_HIP(launch_cache_attention_shared(h, as_stream(stream)));
     return POP_OK;
 }
 

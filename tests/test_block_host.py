@@ -1,4 +1,5 @@
-"""Norms around a block and rotary positions on the host: frequencies, refusals, pins of their 64-bit oracle."""
+"""What stands around the FFN and its cache on the host: norms, rotary positions (frequencies), attention with first tokens and with a shared prefix;
+refusals, pins of the 64-bit oracle."""
 import math
 
 import numpy as np
@@ -132,3 +133,64 @@ def test_oracle_rotary_by_hand():
     assert np.array_equal(orc.rotary(x, [-1], np.array([0.25, 0.5]), 2.0, True), x)
     back = orc.rotary(orc.rotary(x, [12345], np.array([0.1, 0.37]), 1.0, True), [12345], np.array([-0.1, -0.37]), 1.0, True)
     assert np.allclose(back, x, rtol=1e-12)
+
+
+# ---------------------------------------------------------------- attention with first tokens, and with a shared prefix
+
+SINKS = dict(q=A, dtype=1, n=8, cache=A, n_kv=2, d=64, page=16, n_pages=100, table=A, stride=8, start=A, context=A, n_seq=4, heads=4, max_new=2, max_context=128,
+             scale=0.1, window=20, sinks=4, y=A, ydtype=1, ws=A, ws_bytes=1 << 30, stream=None)
+
+
+@pytest.mark.parametrize("status,change", [
+    ("POP_EINVAL", dict(q=None)), ("POP_EINVAL", dict(y=None)), ("POP_EINVAL", dict(cache=A + 8)), ("POP_EINVAL", dict(scale=INF)), ("POP_EINVAL", dict(ws=None)),
+    ("POP_ESHAPE", dict(sinks=-1)), ("POP_ESHAPE", dict(window=-1)), ("POP_ESHAPE", dict(heads=5)), ("POP_ESHAPE", dict(ws_bytes=0)),
+    ("POP_EUNSUPPORTED", dict(d=96)), ("POP_EUNSUPPORTED", dict(page=17)), ("POP_OK", dict(n_seq=0)), ("POP_OK", dict(n=0))])
+def test_sinks_refuse(pop, status, change):
+    _refused(pop, status, "pop_cache_attention_sinks", _with(SINKS, **change))
+
+
+SHARED = dict(q=A, dtype=1, n=8, cache=A, n_kv=2, d=64, page=16, n_pages=100, table=A, stride=8, start=A, context=A, n_seq=4, group=2, prefix=A, heads=4, max_new=2,
+              max_context=128, scale=0.1, y=A, ydtype=1, ws=A, ws_bytes=1 << 30, stream=None)
+
+
+@pytest.mark.parametrize("status,change", [
+    ("POP_EINVAL", dict(q=None)), ("POP_EINVAL", dict(y=None)), ("POP_EINVAL", dict(prefix=None)), ("POP_EINVAL", dict(table=None)), ("POP_EINVAL", dict(start=None)),
+    ("POP_EINVAL", dict(context=None)), ("POP_EINVAL", dict(cache=None)), ("POP_EINVAL", dict(cache=A + 8)), ("POP_EINVAL", dict(q=A + 8)), ("POP_EINVAL", dict(y=A + 2)),
+    ("POP_EINVAL", dict(ws=A + 4)), ("POP_EINVAL", dict(scale=NAN)), ("POP_EINVAL", dict(ws=None)), ("POP_EINVAL", dict(dtype=2)), ("POP_EINVAL", dict(ydtype=-1)),
+    ("POP_ESHAPE", dict(group=0)), ("POP_ESHAPE", dict(group=3)), ("POP_ESHAPE", dict(group=8)), ("POP_ESHAPE", dict(n_seq=-2)), ("POP_ESHAPE", dict(heads=5)),
+    ("POP_ESHAPE", dict(ws_bytes=1000)), ("POP_ESHAPE", dict(stride=0)), ("POP_ESHAPE", dict(max_new=0)), ("POP_ESHAPE", dict(max_context=0)),
+    ("POP_EUNSUPPORTED", dict(d=96)), ("POP_EUNSUPPORTED", dict(page=17)), ("POP_EUNSUPPORTED", dict(stride=1 << 27)), ("POP_EUNSUPPORTED", dict(n_seq=32768)),
+    ("POP_EUNSUPPORTED", dict(n=1 << 27, stride=1 << 12)), ("POP_OK", dict(n_seq=0)), ("POP_OK", dict(n=0))])
+def test_shared_refuses(pop, status, change):
+    _refused(pop, status, "pop_cache_attention_shared", _with(SHARED, **change))
+
+
+def test_shared_workspace(pop):
+    sizes = dict(n=64, n_seq=64, group=8, heads=32, n_kv=8, d=128, max_new=1, max_context=40000)
+    need = pop.pop_cache_attention_shared_workspace(*_with(sizes))
+    _refused(pop, "POP_ESHAPE", "pop_cache_attention_shared", _with(dict(SHARED, n=64, n_seq=64, group=8, heads=32, n_kv=8, d=128, max_new=1, max_context=40000, page=64, stride=700),
+                                                                    ws_bytes=need - 1))
+    # of larger sizes it is enough for smaller ones
+    for change in (dict(n=8, n_seq=8), dict(n=63), dict(max_context=1), dict(max_context=300), dict(n_seq=32, n=64), dict(n=1)):
+        assert pop.pop_cache_attention_shared_workspace(*_with(sizes, **change)) <= need
+    chunks = dict(sizes, n=2000, max_new=40)
+    need = pop.pop_cache_attention_shared_workspace(*_with(chunks))
+    for change in (dict(max_new=1), dict(max_new=3), dict(max_new=39), dict(n=64, max_new=1), dict(n=1999), dict(n_seq=8), dict(max_context=70)):
+        assert pop.pop_cache_attention_shared_workspace(*_with(chunks, **change)) <= need
+    with pytest.raises(pop.PopError) as e:
+        pop.pop_cache_attention_shared_workspace(*_with(sizes, group=5))
+    assert e.value.status == pop.POP_ESHAPE
+    assert pop.pop_cache_attention_shared_workspace(*_with(sizes, n_seq=0)) == 0
+
+
+def test_oracle_attention_with_first_tokens():
+    g = np.random.default_rng(2)
+    q, k, v = g.standard_normal((3, 2, 8)), g.standard_normal((20, 1, 8)), g.standard_normal((20, 1, 8))
+    y = orc.attention(q, k, v, 0.3, 17, 4, sinks=2)
+    for i in range(3):
+        seen = [0, 1] + list(range(14 + i, 18 + i))
+        z = 0.3 * k[seen, 0] @ q[i, 1]
+        w = np.exp(z - z.max())
+        assert np.allclose(y[i, 1], (w / w.sum()) @ v[seen, 0], rtol=1e-13)
+    assert np.array_equal(orc.attention(q, k, v, 0.3, 17, 0, sinks=2), orc.attention(q, k, v, 0.3, 17))
+    assert np.array_equal(orc.attention(q, k, v, 0.3, 17, 4, sinks=30), orc.attention(q, k, v, 0.3, 17))
