@@ -470,7 +470,7 @@ int pop_rotary_frequencies(int rotary_dim, double base, int scaling, double fact
  *     a' = amplitude (a cos t - b sin t),  b' = amplitude (a sin t + b cos t).
  * The first rotary_dim channels of each head are turned, the others copied.  q, k: dev, rows of [n_heads][head_dim] and [n_kv_heads][head_dim] of
  * dtype, q_stride and k_stride elements apart (so both may be parts of one projection's rows); k may be NULL (with k_out).
- * positions: dev [n_tokens]; rows whose position is negative are not read and not written.  turns: dev [rotary_dim / 2], 64 bits.  q_out, k_out:
+ * positions: dev [n_tokens]; rows whose position is negative are left as they were.  turns: dev [rotary_dim / 2], 64 bits.  q_out, k_out:
  * dev, may be q and k themselves (with the same strides), otherwise apart from them.
  * Angles are products in 64 bits, sines and cosines float32.
  * Errors: NULL or misaligned pointers, bad dtype or layout, an amplitude that is not finite, outputs that are inputs with another stride

@@ -188,22 +188,113 @@ hipError_t launch_norm(const BlockNormArgs &a, hipStream_t s)
 
 // ---------------------------------------------------------------- rotary positions
 
-// A workgroup has a token and some of its heads: the token's sines and cosines stand in LDS, one thread computes each.  Angles are products
-// of 64 bits in revolutions, of which the whole ones are taken off before they are rounded to 32.
+// A token's sines and cosines: angles are products of 64 bits in revolutions, of which the whole ones are taken off before they are rounded
+// to 32.  Times the amplitude.
+__device__ __forceinline__ float2 turn_of(int position, double per_token, float amplitude)
+{
+    const double t = (double)position * per_token;
+    float sn, cs;
+    sincospif(2.0f * (float)(t - rint(t)), &sn, &cs);
+    return {amplitude * cs, amplitude * sn};
+}
+
+// A workgroup has a run of tokens (`tokens`) and of each the same part of its heads' eights of channels; sines and cosines stand in LDS, a thread
+// computes some and all heads use them.  Halves: an eight and the one it is turned with together; pairs: an eight by itself; eights behind the
+// turned part are copied.  A thread asks for kTogether of them before it waits, the first ones before the angles are computed.
+constexpr int kTogether = 4, kMostTurns = 1024;
+template <bool BF16, bool PAIRS>
+__global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, int tokens, int part)
+{
+    __shared__ float2 s_turn[kMostTurns];
+    __shared__ int s_position[kMostTurns];
+    const int token0 = blockIdx.x * tokens, here = min(tokens, a.n - token0), half = a.r / 2;
+    const int turned = PAIRS ? a.r / 8 : a.r / 16, per_head = turned + (a.d - a.r) / 8, per_token = (a.n_heads + a.n_kv) * per_head;
+    const int first = blockIdx.y * part, mine = min(part, per_token - first), total = here * mine;
+    struct Place {
+        const void *from;
+        void *to;
+        long long in, out;
+        int token, chunk;
+    };
+    const auto place = [&](int e) {
+        Place p;
+        p.token = e / mine;
+        const int i = first + e - p.token * mine, head = i / per_head;
+        p.chunk = i - head * per_head;
+        const bool of_k = head >= a.n_heads;
+        const long long row = token0 + p.token, h = of_k ? head - a.n_heads : head;
+        const int ch = p.chunk < turned ? 8 * p.chunk : a.r + 8 * (p.chunk - turned);
+        p.from = of_k ? a.k : a.q, p.to = of_k ? a.k_out : a.q_out;
+        p.in = row * (of_k ? a.k_stride : a.q_stride) + h * a.d + ch;
+        p.out = row * (of_k ? a.k_out_stride : a.q_out_stride) + h * a.d + ch;
+        return p;
+    };
+    Eight<BF16> x[kTogether], y[kTogether];
+    const auto ask = [&](int e0) {
+#pragma unroll
+        for (int u = 0; u < kTogether; ++u) {
+            const int e = e0 + 256 * u;
+            if (e < total) {
+                const Place p = place(e);
+                x[u].load(p.from, p.in);
+                if (!PAIRS && p.chunk < turned) y[u].load(p.from, p.in + half);
+            }
+        }
+    };
+    ask(threadIdx.x);
+    for (int i = threadIdx.x; i < here * half; i += 256) {
+        const int token = i / half;
+        s_turn[i] = turn_of(a.positions[token0 + token], a.turns[i - token * half], a.amplitude);
+    }
+    if (threadIdx.x < here) s_position[threadIdx.x] = a.positions[token0 + threadIdx.x];
+    __syncthreads();
+    for (int e0 = threadIdx.x; e0 < total; e0 += 256 * kTogether) {
+#pragma unroll
+        for (int u = 0; u < kTogether; ++u) {
+            const int e = e0 + 256 * u;
+            if (e >= total) break;
+            const Place p = place(e);
+            if (s_position[p.token] < 0) continue;
+            if (p.chunk >= turned) {
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = x[u][i];
+                store_eight<BF16>(p.to, p.out, v);
+            } else if constexpr (PAIRS) {
+                const float2 *const t = s_turn + p.token * half + 4 * p.chunk;
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    v[2 * i] = x[u][2 * i] * t[i].x - x[u][2 * i + 1] * t[i].y;
+                    v[2 * i + 1] = x[u][2 * i] * t[i].y + x[u][2 * i + 1] * t[i].x;
+                }
+                store_eight<BF16>(p.to, p.out, v);
+            } else {
+                const float2 *const t = s_turn + p.token * half + 8 * p.chunk;
+                float v[8], w[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    v[i] = x[u][i] * t[i].x - y[u][i] * t[i].y;
+                    w[i] = x[u][i] * t[i].y + y[u][i] * t[i].x;
+                }
+                store_eight<BF16>(p.to, p.out, v);
+                store_eight<BF16>(p.to, p.out + half, w);
+            }
+        }
+        ask(e0 + 256 * kTogether);
+    }
+}
+
+// Rows and heads of any alignment: channels one by one, a token to a workgroup.
 template <bool BF16>
-__global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a)
+__global__ __launch_bounds__(256) void rotary_any_kernel(RotaryArgs a)
 {
     __shared__ float2 s_turn[kMostRotary / 2];
-    const int token = blockIdx.x, position = a.positions[token];
+    const int token = blockIdx.x, position = a.positions[token], half = a.r / 2;
     if (position < 0) return;
-    for (int i = threadIdx.x; i < a.r / 2; i += 256) {
-        const double t = (double)position * a.turns[i];
-        float sn, cs;
-        sincospif(2.0f * (float)(t - rint(t)), &sn, &cs);
-        s_turn[i] = {a.amplitude * cs, a.amplitude * sn};
-    }
+    for (int i = threadIdx.x; i < half; i += 256) s_turn[i] = turn_of(position, a.turns[i], a.amplitude);
     __syncthreads();
-    const int per = a.r / 2 + (a.d - a.r), heads = a.n_heads + (a.k ? a.n_kv : 0);
+    const int per = half + (a.d - a.r), heads = a.n_heads + a.n_kv;
     for (int e = threadIdx.x; e < heads * per; e += 256) {
         const int head = e / per, i = e % per;
         const bool of_k = head >= a.n_heads;
@@ -212,17 +303,36 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a)
         const int h = of_k ? head - a.n_heads : head;
         const long long in = token * (of_k ? a.k_stride : a.q_stride) + (long long)h * a.d;
         const long long out = token * (of_k ? a.k_out_stride : a.q_out_stride) + (long long)h * a.d;
-        if (i < a.r / 2) {
-            const int c0 = a.pairs ? 2 * i : i, c1 = a.pairs ? 2 * i + 1 : i + a.r / 2;
+        if (i < half) {
+            const int c0 = a.pairs ? 2 * i : i, c1 = a.pairs ? 2 * i + 1 : i + half;
             const float x = load_one<BF16>(from, in + c0), y = load_one<BF16>(from, in + c1);
             const float2 t = s_turn[i];
             store_one<BF16>(to, out + c0, x * t.x - y * t.y);
             store_one<BF16>(to, out + c1, x * t.y + y * t.x);
         } else {
-            const int c = a.r + i - a.r / 2;
+            const int c = a.r + i - half;
             store_one<BF16>(to, out + c, load_one<BF16>(from, in + c));
         }
     }
+}
+
+template <bool BF16>
+hipError_t launch_rotary_as(const RotaryArgs &a, hipStream_t s)
+{
+    const bool v8 = a.d % 8 == 0 && a.r % (a.pairs ? 8 : 16) == 0 && (a.q_stride | a.k_stride | a.q_out_stride | a.k_out_stride) % 8 == 0 && aligned16(a.q) &&
+                    aligned16(a.k) && aligned16(a.q_out) && aligned16(a.k_out);
+    if (!v8) {
+        rotary_any_kernel<BF16><<<a.n, 256, 0, s>>>(a);
+        return hipGetLastError();
+    }
+    const int per_token = (a.n_heads + a.n_kv) * (a.r / (a.pairs ? 8 : 16) + (a.d - a.r) / 8);
+    // full threads where there is work for all compute units, else as many workgroups as there are eights for
+    const int at_once = 256 * ((long long)a.n * per_token >= 512ll * 256 * kTogether ? kTogether : 1);
+    const int tokens = std::max(1, std::min({at_once / per_token, kMostTurns / (a.r / 2), 64})), part = std::min(per_token, at_once);
+    const dim3 grid((unsigned)((a.n + tokens - 1) / tokens), (unsigned)((per_token + part - 1) / part));
+    if (a.pairs) rotary_kernel<BF16, true><<<grid, 256, 0, s>>>(a, tokens, part);
+    else rotary_kernel<BF16, false><<<grid, 256, 0, s>>>(a, tokens, part);
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -239,11 +349,6 @@ hipError_t launch_block_norm(const BlockNormArgs &a, hipStream_t s)
     return v8 ? launch_norm<false, false, true>(a, s) : launch_norm<false, false, false>(a, s);
 }
 
-hipError_t launch_rotary(const RotaryArgs &a, hipStream_t s)
-{
-    if (a.bf16) rotary_kernel<true><<<a.n, 256, 0, s>>>(a);
-    else rotary_kernel<false><<<a.n, 256, 0, s>>>(a);
-    return hipGetLastError();
-}
+hipError_t launch_rotary(const RotaryArgs &a, hipStream_t s) { return a.bf16 ? launch_rotary_as<true>(a, s) : launch_rotary_as<false>(a, s); }
 
 }  // namespace pop
