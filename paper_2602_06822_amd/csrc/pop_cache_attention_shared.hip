@@ -3,7 +3,7 @@
 //
 // With m, l and O the maximum, the sum of weights and the weighted sum of values over a set of tokens, two sets join as
 //     m = max(m1, m2),  l = 2^(m1 - m) l1 + 2^(m2 - m) l2,  O = 2^(m1 - m) O1 + 2^(m2 - m) O2,   y = O / l.
-// The first kernel leaves m, l and O of the prefix and of the tokens behind it, the second joins the two for every column.
+// The first kernel leaves m, l and O of runs of tokens of the prefix and of the tokens behind it, the second joins them for every column.
 #include <math.h>
 
 #include <algorithm>
@@ -17,6 +17,8 @@ namespace {
 
 constexpr int kRound = 128;  // tokens of a round: a step of each of the four waves
 constexpr int kWorkgroups = 512;
+// What a unit costs its workgroup beside its rounds (its columns, q and table, the waves' sums), in rounds: work is dealt with that on top.
+constexpr int kUnitCost = 4;
 // A prefix shorter than this is read by each sequence for itself.
 constexpr int kLeastPrefix = 256;
 
@@ -176,28 +178,35 @@ __device__ __forceinline__ Sequence look_at(const SharedArgs &h, const Packs &pa
     return q;
 }
 
-// Rows of the workspace: pieces of units that several workgroups have, two places each; their counters; O, m and l of every (token, head)
-// over the prefix and over its own tokens, and behind them whether there is a prefix.
+// The workspace: results of units that several workgroups have, two places of COLUMNS rows to a workgroup; and results of every (token, head) over the
+// prefix and over its own tokens.  A row is O, m and l (D + 2 floats) and two more; in the latter's last four stand
+//     m, l, kWhole, 0         of a unit that one workgroup has,
+//     first, n, kPieces, c    where n workgroups from `first` on have one: row c of their places (integers),
+//     -, -, kDone, -          of own tokens without a prefix that one workgroup has: y is there.
+// The last of the four, of own tokens, has its sign set where there is no prefix.
+enum { kDone = 0, kWhole = 1, kPieces = 2 };
 template <int D, int COLUMNS>
 __device__ __forceinline__ float *piece_of(const SharedArgs &h, int place)
 {
     return h.a.ws + (size_t)place * COLUMNS * (D + 4);
 }
+// The places of a unit's pieces: the last one of the workgroup that it begins in, then the first ones of those it goes on in.
+__device__ __forceinline__ int place_of(int wg0, int piece) { return piece == 0 ? 2 * wg0 + 1 : 2 * (wg0 + piece); }
 template <int D>
 __device__ __forceinline__ float *state_of(const SharedArgs &h, int own, size_t row)
 {
     return h.states + ((size_t)own * h.a.n_tokens * h.a.n_heads + row) * (D + 4);
 }
 
-// Workgroup: 4 waves; dealt in equal numbers of rounds, as the kernel for sequences that share nothing.
+// Workgroup: 4 waves; dealt in equal numbers of rounds and units' costs.  A piece of a unit is what one workgroup has of its rounds.
 template <int D, int QT, int PT, int NC>
-__global__ __launch_bounds__(256, D == 256 || NC > 2 ? 1 : 2) void shared_attention_kernel(SharedArgs h, unsigned long long tag)
+__global__ __launch_bounds__(256, D == 256 || NC > 2 ? 1 : 2) void shared_attention_kernel(SharedArgs h)
 {
     constexpr int kTile = cache_tile_bytes(D), kColumns = 16 * NC;
     constexpr int kPass = D > 128 ? 128 : D;
     __shared__ float s_o[4][16][kPass + 4];
     __shared__ float s_m[4][16], s_l[4][16];
-    __shared__ int s_last, s_row[kColumns];
+    __shared__ int s_row[kColumns];
     const AttentionArgs &a = h.a;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 15, g = lane >> 4;
     const int share = a.n_heads / a.c.n_kv, n_kv = a.c.n_kv;
@@ -210,7 +219,7 @@ __global__ __launch_bounds__(256, D == 256 || NC > 2 ? 1 : 2) void shared_attent
     int upto = 0, all = 0;  // rounds of the look's sequences up to the lane's; of all looks
     const auto rounds_in = [&](int rounds, int blocks) { return saturated((long long)saturated((long long)rounds * blocks) * n_kv); };
     const auto rounds_of = [&](const Sequence &q) {
-        return __builtin_elementwise_add_sat(rounds_in(q.prefix_rounds, q.prefix_blocks), rounds_in(q.rounds, q.blocks));
+        return __builtin_elementwise_add_sat(rounds_in(q.prefix_rounds + kUnitCost, q.prefix_blocks), rounds_in(q.rounds + kUnitCost, q.blocks));
     };
     for (int look = 0; look < looks; ++look) {
         own = look_at<kColumns>(h, packs, look, lane);
@@ -231,7 +240,6 @@ __global__ __launch_bounds__(256, D == 256 || NC > 2 ? 1 : 2) void shared_attent
         own = look_at<kColumns>(h, packs, 0, lane);
         upto = wave_scan(rounds_of(own));
     }
-    unsigned long long *const counters = reinterpret_cast<unsigned long long *>(piece_of<D, kColumns>(h, 2 * (int)gridDim.x));
     const size_t page_bytes = cache_page_bytes(a.c);
 
     while (at < end) {
@@ -247,12 +255,15 @@ __global__ __launch_bounds__(256, D == 256 || NC > 2 ? 1 : 2) void shared_attent
         const int seq_at = look_at_round + (owner > 0 ? __builtin_amdgcn_readlane(upto, owner - 1) : 0);
         const int prefix = __builtin_amdgcn_readlane(own.prefix, owner);
         const int prefix_rounds = __builtin_amdgcn_readlane(own.prefix_rounds, owner), prefix_blocks = __builtin_amdgcn_readlane(own.prefix_blocks, owner);
-        const int of_prefix = rounds_in(prefix_rounds, prefix_blocks);
+        const int of_prefix = rounds_in(prefix_rounds + kUnitCost, prefix_blocks);
         const bool shared = at - seq_at < of_prefix;
-        const int rounds = shared ? prefix_rounds : __builtin_amdgcn_readlane(own.rounds, owner);
+        const int rounds = shared ? prefix_rounds : __builtin_amdgcn_readlane(own.rounds, owner), dealt = rounds + kUnitCost;
         const int first_at = shared ? seq_at : seq_at + of_prefix;
-        const int unit = (int)((unsigned)(at - first_at) / (unsigned)rounds), block = (int)((unsigned)unit / (unsigned)n_kv), head = unit - block * n_kv;
-        const int unit_at = first_at + unit * rounds, begin = at - unit_at, stop = min(rounds, end - unit_at);
+        const int unit = (int)((unsigned)(at - first_at) / (unsigned)dealt), block = (int)((unsigned)unit / (unsigned)n_kv), head = unit - block * n_kv;
+        // rounds [begin, stop) of the unit; the cost stands in front of them
+        const int unit_at = first_at + unit * dealt, begin = max(at - unit_at - kUnitCost, 0), stop = min(rounds, end - unit_at - kUnitCost);
+        at = unit_at + min(dealt, end - unit_at);
+        if (stop <= begin) continue;
 
         // columns: of the pack's sequences one after another, or of this one
         const int pack0 = __builtin_amdgcn_readlane(own.pack0, owner), pack_n = __builtin_amdgcn_readlane(own.pack_n, owner);
@@ -371,9 +382,11 @@ __global__ __launch_bounds__(256, D == 256 || NC > 2 ? 1 : 2) void shared_attent
         }
 
         const bool whole = begin == 0 && stop == rounds;
+        // pieces: one for each of the workgroups that the unit's first and its last round fall to and those between them
+        const int wg0 = workgroup_of(unit_at + kUnitCost), pieces = workgroup_of(unit_at + dealt - 1) - wg0 + 1;
         float *const part = piece_of<D, kColumns>(h, 2 * blockIdx.x + (begin == 0));
         // what the four waves left in LDS of 16 columns, each relative to its own maximum: a piece, or all there is of the unit's tokens
-        const auto merge = [&](int x, int live, int pass, bool all_there) {
+        const auto merge = [&](int x, int live, int pass) {
             for (int e = threadIdx.x; e < live * (kPass / 2); e += 256) {
                 const int c = e / (kPass / 2), ch = e % (kPass / 2) * 2;
                 float most = kLowest, sum = 0.0f, u = 0.0f, v = 0.0f;
@@ -384,21 +397,20 @@ __global__ __launch_bounds__(256, D == 256 || NC > 2 ? 1 : 2) void shared_attent
                     const float f = __builtin_amdgcn_exp2f(s_m[i][c] - most);
                     sum += f * s_l[i][c], u += f * s_o[i][c][ch], v += f * s_o[i][c][ch + 1];
                 }
-                if (!all_there) {
-                    float *const to = part + (16 * x + c) * (D + 4);
-                    store_pair(to + pass * kPass + ch, u, v);
-                    if (ch == 0 && pass == 0) store_pair(to + D, most, sum);
-                    continue;
-                }
                 const size_t of = (size_t)s_row[16 * x + c] * a.n_heads + head * share + (block * kColumns + 16 * x + c) % share;
-                float *const to = state_of<D>(h, !shared, of);
-                if (shared || prefix > 0) {
-                    *reinterpret_cast<float2 *>(to + pass * kPass + ch) = {u, v};
-                } else {
+                float *const state = state_of<D>(h, !shared, of), *const to = whole ? state : part + (16 * x + c) * (D + 4);
+                const bool done = whole && !shared && prefix == 0;
+                if (done) {
                     const float by = sum > 0.0f ? 1.0f / sum : 0.0f;
                     store_y2(a, of * D + pass * kPass + ch, u * by, v * by);
+                } else {
+                    *reinterpret_cast<float2 *>(to + pass * kPass + ch) = {u, v};
                 }
-                if (ch == 0 && pass == 0) *reinterpret_cast<float4 *>(to + D) = {most, sum, prefix > 0 ? 1.0f : 0.0f, 0.0f};
+                if (ch == 0 && pass == 0) {
+                    if (!whole) *reinterpret_cast<float2 *>(to + D) = {most, sum};
+                    if (whole) *reinterpret_cast<float4 *>(state + D) = {most, sum, __int_as_float(done ? kDone : kWhole), 0.0f};
+                    else if (begin == 0) *reinterpret_cast<int4 *>(state + D) = {wg0, pieces, kPieces, (16 * x + c) | (!shared && prefix == 0 ? (int)0x80000000 : 0)};
+                }
             }
         };
 #pragma unroll
@@ -420,56 +432,73 @@ __global__ __launch_bounds__(256, D == 256 || NC > 2 ? 1 : 2) void shared_attent
                             *reinterpret_cast<float4 *>(to + i * (D / 16) + j) = {sums.o[x][j][i], sums.o[x][j + 1][i], sums.o[x][j + 2][i], sums.o[x][j + 3][i]};
                 }
                 __syncthreads();
-                merge(x, min(16, n_live - 16 * x), pass, whole);
+                merge(x, min(16, n_live - 16 * x), pass);
                 __syncthreads();
             }
         }
-        if (!whole) {
-            // pieces of the unit: one for each of the workgroups that its first and its last round fall to and those between them
-            const int wg0 = workgroup_of(unit_at), pieces = workgroup_of(unit_at + rounds - 1) - wg0 + 1;
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's stores are acknowledged
-            __syncthreads();
-            if (threadIdx.x == 0) s_last = arrive_last(counters + wg0, tag, pieces);
-            __syncthreads();
-            if (s_last) {
-#pragma unroll 1
-                for (int x = 0; x < tiles; ++x) {
-                    const int live = min(16, n_live - 16 * x);
-                    const auto place = [&](int piece) { return piece_of<D, kColumns>(h, piece == 0 ? 2 * wg0 + 1 : 2 * (wg0 + piece)) + 16 * x * (D + 4); };
-#pragma unroll 1
-                    for (int pass = 0; pass < D / kPass; ++pass) {
-                        if (pieces <= 8) join_pieces<D, kPass, 8, 2>(a.ws, place, pieces, live, wave, lane, pass, s_o, s_m, s_l);
-                        else join_pieces<D, kPass, 2, 8>(a.ws, place, pieces, live, wave, lane, pass, s_o, s_m, s_l);
-                        __syncthreads();
-                        merge(x, live, pass, true);
-                        __syncthreads();
-                    }
-                }
-            }
-            __syncthreads();
-        }
-        at = unit_at + stop;
     }
 }
 
-// y of the columns that have a prefix: one wave for a (token, head).
-template <int D>
+// y of the columns whose results stand in the workspace.  Workgroup: one (token, head); a group of D/4 lanes for a row of results, four channels to
+// a lane, rows in the order of the tokens.
+template <int D, int COLUMNS>
 __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs h)
 {
+    constexpr int kLanes = D / 4, kGroups = 256 / kLanes, kTogether = 4;
+    __shared__ f32x4 s_o[kGroups][kLanes];
+    __shared__ float s_m[kGroups], s_l[kGroups];
     const AttentionArgs &a = h.a;
-    const int start = a.start[blockIdx.x], next = a.start[blockIdx.x + 1], lane = threadIdx.x & 63;
+    const int start = a.start[blockIdx.x], next = a.start[blockIdx.x + 1];
     if (!(start >= 0 && next > start && next <= a.n_tokens)) return;
+    const int group = threadIdx.x / kLanes, ch = threadIdx.x % kLanes * 4;
     const size_t end = (size_t)next * a.n_heads;
-    for (size_t row = (size_t)start * a.n_heads + blockIdx.y * 4 + threadIdx.x / 64; row < end; row += gridDim.y * 4) {
-        const float *p = state_of<D>(h, 0, row), *own = state_of<D>(h, 1, row);
-        const float4 e = *reinterpret_cast<const float4 *>(own + D), b = *reinterpret_cast<const float4 *>(p + D);
-        if (e.z == 0.0f) continue;  // (no prefix: y is there)
-        const float most = fmaxf(b.x, e.x), f1 = __builtin_amdgcn_exp2f(b.x - most), f2 = __builtin_amdgcn_exp2f(e.x - most);
-        const float sum = f1 * b.y + f2 * e.y, by = sum > 0.0f ? 1.0f / sum : 0.0f;
-        for (int ch = 2 * lane; ch < D; ch += 128) {
-            const float2 u = *reinterpret_cast<const float2 *>(p + ch), v = *reinterpret_cast<const float2 *>(own + ch);
-            store_y2(a, row * D + ch, (f1 * u.x + f2 * v.x) * by, (f1 * u.y + f2 * v.y) * by);
+    for (size_t row = (size_t)start * a.n_heads + blockIdx.y; row < end; row += gridDim.y) {
+        const float *const of_own = state_of<D>(h, 1, row), *const of_prefix = state_of<D>(h, 0, row);
+        const int4 own = *reinterpret_cast<const int4 *>(of_own + D), prefix = *reinterpret_cast<const int4 *>(of_prefix + D);
+        if (own.z == kDone) continue;
+        // (a sequence with a prefix leaves kWhole or kPieces of its own tokens, and so does one whose own unit several workgroups have)
+        const bool shares = own.w >= 0;
+        const int n1 = !shares ? 0 : prefix.z == kPieces ? prefix.y : 1, n = n1 + (own.z == kPieces ? own.y : 1);
+        f32x4 o = {0, 0, 0, 0};
+        float m = kLowest, l = 0.0f;
+        for (int i0 = group; i0 < n; i0 += kGroups * kTogether) {
+            f32x4 v[kTogether];
+            float2 ml[kTogether];
+#pragma unroll
+            for (int k = 0; k < kTogether; ++k) {
+                const int i = i0 + kGroups * k;
+                v[k] = f32x4{0, 0, 0, 0}, ml[k] = {kLowest, 0.0f};
+                if (i < n) {
+                    const int4 e = i < n1 ? prefix : own;
+                    const float *p = i < n1 ? of_prefix : of_own;
+                    if (e.z == kPieces) p = piece_of<D, COLUMNS>(h, place_of(e.x, i < n1 ? i : i - n1)) + (e.w & 255) * (D + 4);
+                    ml[k] = *reinterpret_cast<const float2 *>(p + D);
+                    v[k] = *reinterpret_cast<const f32x4 *>(p + ch);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < kTogether; ++k) {
+                const float top = fmaxf(m, ml[k].x), f = __builtin_amdgcn_exp2f(m - top), e = __builtin_amdgcn_exp2f(ml[k].x - top);
+                m = top, l = f * l + e * ml[k].y, o = f * o + e * v[k];
+            }
         }
+        s_o[group][ch / 4] = o;
+        if (ch == 0) s_m[group] = m, s_l[group] = l;
+        __syncthreads();
+        if (threadIdx.x < D / 2) {
+            const int c = threadIdx.x * 2;
+            float most = kLowest, sum = 0.0f, x = 0.0f, y = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kGroups; ++i) most = fmaxf(most, s_m[i]);
+#pragma unroll
+            for (int i = 0; i < kGroups; ++i) {
+                const float f = __builtin_amdgcn_exp2f(s_m[i] - most);
+                sum += f * s_l[i], x += f * s_o[i][c / 4][c % 4], y += f * s_o[i][c / 4][c % 4 + 1];
+            }
+            const float by = sum > 0.0f ? 1.0f / sum : 0.0f;
+            store_y2(a, row * D + c, x * by, y * by);
+        }
+        __syncthreads();
     }
 }
 
@@ -496,7 +525,7 @@ SharedGrid shared_grid(int n_tokens, int n_seq, int group, int n_heads, int n_kv
         const long long units = n_kv * (n_seq * ((max_new * share + 16 * nc - 1) / (16 * nc)) + packs * ((std::min(group, 64) * max_new * share + 16 * nc - 1) / (16 * nc)));
         const long long per_unit = std::min(rounds, std::max(32ll, (long long)(2.0 * sqrt((double)rounds))));
         g.workgroups = (int)std::min(units * per_unit, units >= 128 ? most : kWorkgroups / 2ll);
-        g.pieces = std::max(g.pieces, ((size_t)g.workgroups * (2 * 16 * nc * (d + 4) * sizeof(float) + 8) + 255) / 256 * 256);
+g.pieces = std::max(g.pieces, (size_t)g.workgroups * 2 * 16 * nc * (d + 4) * sizeof(float));
     }
     g.states = 2 * (size_t)n_tokens * n_heads * (d + 4) * sizeof(float);
     return g;
@@ -505,11 +534,11 @@ SharedGrid shared_grid(int n_tokens, int n_seq, int group, int n_heads, int n_kv
 template <int D, int QT, int PT, int NC>
 hipError_t launch_nc(const SharedArgs &h, const SharedGrid &g, hipStream_t s)
 {
-    shared_attention_kernel<D, QT, PT, NC><<<(unsigned)g.workgroups, 256, 0, s>>>(h, launch_tag());
+    shared_attention_kernel<D, QT, PT, NC><<<(unsigned)g.workgroups, 256, 0, s>>>(h);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const long long rows = (long long)h.a.max_new * h.a.n_heads;  // of a sequence
-    shared_join_kernel<D><<<dim3((unsigned)h.a.n_seq, (unsigned)std::min((rows + 3) / 4, 64ll)), 256, 0, s>>>(h);
+    shared_join_kernel<D, 16 * NC><<<dim3((unsigned)h.a.n_seq, (unsigned)std::min(rows, 4096ll)), 256, 0, s>>>(h);
     return hipGetLastError();
 }
 template <int D, int QT, int PT>
