@@ -150,7 +150,9 @@ struct SharedArgs {
     AttentionArgs a;
     int group;          // sequences of a group
     const int *prefix;  // [n_seq / group] tokens that a group's sequences share
-    float *states;      // set by the launcher
+    // set by the launcher
+    float *prefix_pieces, *own_pieces, *states;
+    int prefix_columns, own_columns;
 };
 size_t cache_attention_shared_ws(int n_tokens, int n_seq, int group, int n_heads, int n_kv, int d, int max_new, int max_context);
 hipError_t launch_cache_attention_shared(SharedArgs h, hipStream_t s);  // (pop_cache_attention_shared.hip)

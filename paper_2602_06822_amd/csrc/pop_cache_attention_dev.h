@@ -304,6 +304,54 @@ __device__ __forceinline__ float2 load_pair(const float *p)
     return {__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))};
 }
 
+// ---- blocks of 128 columns
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int kPromptTile = 64;  // tokens that the workgroup has in LDS at a time: a tile of the cache for each wave
+
+// Where a tile's keys and values stand in LDS, as operands of 32 x 32 x 16 products.  K: 16-byte runs of 8 channels, [D/8][64 tokens].
+// V: for 16 tokens and each half of a wave, 16-byte runs of that half's 8 tokens, [4 x 2][D]; a lane that converts four tokens of channels
+// n D/16 + c writes its halves of the runs at place c 16 + n, so that neighbouring lanes write neighbouring runs.  O^T's rows are in
+// the order of those places.  The second half of a wave has its two fours of tokens in the other order, in V as in S^T's rows: the lanes that
+// write at the same time then meet in no bank (D 64, two chunks of 1024 tokens over 4096, 32 heads over 8: 86 -> 77 us; D 128 is not bound by LDS).
+// Keys are read in the half of an iteration in front of its barrier, values behind it too: two and three tiles of them, and one
+// barrier a tile.  80 KB for D = 128: two workgroups to a compute unit; D = 256 has one.
+template <int D>
+struct PromptTiles {
+    uint32_t k[2][D / 8 * kPromptTile * 4], v[3][8 * D * 4];
+};
+
+// One wave's tile of the cache, converted into LDS.
+template <int D>
+__device__ __forceinline__ void convert_tile(uint32_t *to_k, uint32_t *to_v, const TileRegs<D> &r, int j, int left, int n, int g)
+{
+    constexpr int W = D / 32;
+#pragma unroll
+    for (int q = 0; q < W; ++q)
+        *reinterpret_cast<bf16x8 *>(&to_k[((g * W + q) * kPromptTile + 16 * j + n) * 4]) = k_operand<D>(r, q);
+    // scale bytes of tokens that are not there become 2^-127, so that whatever stands in their place is finite
+    left -= 4 * g;
+    const uint32_t vs = left >= 4 ? r.vs : left <= 0 ? 0u : r.vs & ((1u << (8 * left)) - 1);
+    float sv[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sv[i] = cache_scale((vs >> (8 * i)) & 255u);
+#pragma unroll
+    for (int b = 0; b < W; ++b) {
+        uint32_t c[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int at = i * W + b;
+            c[i] = cache_pair_at(r.v[at / 4], sv[i], at % 4);
+        }
+        uint32_t *run = &to_v[((2 * j + (g & 1)) * D + 2 * b * 16 + n) * 4 + ((g >> 1) ^ (g & 1)) * 2];
+        *reinterpret_cast<u32x2 *>(run) = u32x2{low_halves(c[0], c[1]), low_halves(c[2], c[3])};
+        *reinterpret_cast<u32x2 *>(run + 16 * 4) = u32x2{high_halves(c[0], c[1]), high_halves(c[2], c[3])};
+    }
+}
+
+// ---- joining
+
 // The pieces of a unit's columns (channels [pass kPass, (pass + 1) kPass) of them), joined into four sums that the waves leave in LDS: wave w takes
 // pieces w, w + 4, ..; four channels to a lane, so several columns to a load; G such groups of columns and P pieces under way together.
 // place(i): piece i, n_live rows of D channels, the column's maximum and sum, and two floats more.

@@ -110,6 +110,9 @@ struct WideSums {
     }
 };
 
+// v of lane `from` (modulo 64).
+__device__ __forceinline__ int lane_value(int v, int from) { return __builtin_amdgcn_ds_bpermute(from * 4, v); }
+
 // Sequences in packs: a group, or 64 sequences of a larger one (and what is left of it).  A wave looks at as many whole packs at a time as 64
 // lanes hold, a lane for a sequence.
 struct Packs {
@@ -132,13 +135,38 @@ struct Sequence {
     int pack0, pack_n;          // lanes of the pack
     int prefix;                 // shared tokens that are read once: a multiple of 32, 0 for none
     int prefix_rounds, prefix_blocks, rounds, blocks;
+
+    // Row and position of a token: of the pack's sequences one after another, which begin behind `before` tokens of the look, or of lane `owner`'s.
+    __device__ __forceinline__ void column(bool of_pack, int owner, int before, int token, int *row, int *pos) const
+    {
+        int of = owner, local = token;
+        if (of_pack) {
+            int lo = 0;  // sequences whose tokens all stand in front of this one
+#pragma unroll
+            for (int half = 32; half > 0; half >>= 1)
+                if (lane_value(fresh_upto, lo + half - 1) <= before + token) lo += half;
+            of = lo;
+            local = before + token - (lane_value(fresh_upto, max(lo - 1, 0)) & (lo > 0 ? -1 : 0));
+        }
+        *row = lane_value(start, of) + local;
+        *pos = lane_value(context, of) - lane_value(fresh, of) + local;
+    }
+    // The lane of the longest of the pack's sequences, whose row of the table the prefix is read from.
+    __device__ __forceinline__ int source(int pack0, int pack_n, int lane) const
+    {
+        const bool member = lane >= pack0 && lane < pack0 + pack_n && fresh > 0;
+        const int most = __builtin_amdgcn_readlane(wave_scan<true>(member ? context : 0), 63);
+        return __ffsll((unsigned long long)__ballot(member && context == most)) - 1;
+    }
 };
 
 // (sequences whose rows overlap may have more than 32 bits count: they stop there)
 __device__ __forceinline__ int columns_of(int tokens, int share) { return (int)min((long long)tokens * share, 0x7fff0000ll); }
 __device__ __forceinline__ int saturated(long long v) { return (int)min(v, 0x7fffffffll); }
 
-template <int COLUMNS>
+// UNITS: both kinds, or one of them.
+enum { kBoth = 0, kOfPrefix = 1, kOwn = 2 };
+template <int COLUMNS, int UNITS>
 __device__ __forceinline__ Sequence look_at(const SharedArgs &h, const Packs &packs, int look, int lane)
 {
     const AttentionArgs &a = h.a;
@@ -161,34 +189,52 @@ __device__ __forceinline__ Sequence look_at(const SharedArgs &h, const Packs &pa
     int longest = q.fresh > 0 ? q.context : 0;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
-        const int other = __shfl_down(longest, off, kWave);
+        const int other = lane_value(longest, lane + off);
         if (lane + off < q.pack0 + q.pack_n) longest = max(longest, other);
     }
-    longest = __shfl(longest, q.pack0, kWave);
+    longest = lane_value(longest, q.pack0);
     const int table = a.stride << a.c.log_page;
     prefix = min(min(prefix, longest), table) & ~31;
     q.prefix = prefix >= kLeastPrefix && __popcll(live & members) > 1 ? prefix : 0;
-    const int in_front = __shfl(q.fresh_upto, max(q.pack0 - 1, 0), kWave);
-    const int in_pack = __shfl(q.fresh_upto, min(q.pack0 + q.pack_n, 64) - 1, kWave) - (q.pack0 > 0 ? in_front : 0);
+    const int in_front = lane_value(q.fresh_upto, max(q.pack0 - 1, 0));
+    const int in_pack = lane_value(q.fresh_upto, min(q.pack0 + q.pack_n, 64) - 1) - (q.pack0 > 0 ? in_front : 0);
     const bool heads_pack = lane == q.pack0 && q.prefix > 0;
     q.prefix_rounds = heads_pack ? (q.prefix + kRound - 1) / kRound : 0;
-    q.prefix_blocks = heads_pack ? (columns_of(in_pack, share) + COLUMNS - 1) / COLUMNS : 0;
-    q.blocks = (columns_of(q.fresh, share) + COLUMNS - 1) / COLUMNS;
+    q.prefix_blocks = heads_pack && UNITS != kOwn ? (columns_of(in_pack, share) + COLUMNS - 1) / COLUMNS : 0;
+    q.blocks = UNITS == kOfPrefix ? 0 : (columns_of(q.fresh, share) + COLUMNS - 1) / COLUMNS;
     q.rounds = q.fresh > 0 ? max((min(q.context, table) - q.prefix + kRound - 1) / kRound, 1) : 0;
     return q;
 }
 
-// The workspace: results of units that several workgroups have, two places of COLUMNS rows to a workgroup; and results of every (token, head) over the
-// prefix and over its own tokens.  A row is O, m and l (D + 2 floats) and two more; in the latter's last four stand
+// Equal shares of `all` rounds for the workgroups; the first `longer` ones have one more than the others.
+struct Shares {
+    unsigned n, fewest, longer;
+    __device__ __forceinline__ Shares(int all)
+    {
+        n = min(gridDim.x, (unsigned)all);
+        fewest = n ? (unsigned)all / n : 0, longer = (unsigned)all - fewest * n;
+    }
+    __device__ __forceinline__ int first() const { return blockIdx.x * fewest + min(blockIdx.x, longer); }
+    __device__ __forceinline__ int end() const { return first() + (int)fewest + (blockIdx.x < longer); }
+    __device__ __forceinline__ int workgroup_of(unsigned round) const
+    {
+        const unsigned of_longer = longer * (fewest + 1);
+        return (int)(round < of_longer ? round / (fewest + 1) : longer + (round - of_longer) / fewest);
+    }
+};
+__device__ __forceinline__ int rounds_in(int rounds, int blocks, int n_kv) { return saturated((long long)saturated((long long)rounds * blocks) * n_kv); }
+
+// The workspace: results of units that several workgroups have, two places to a workgroup, a row for each of a unit's columns; and results of every
+// (token, head) over the prefix and over its own tokens.  A row is O, m and l (D + 2 floats) and two more; in the latter's last four stand
 //     m, l, kWhole, 0         of a unit that one workgroup has,
 //     first, n, kPieces, c    where n workgroups from `first` on have one: row c of their places (integers),
 //     -, -, kDone, -          of own tokens without a prefix that one workgroup has: y is there.
 // The last of the four, of own tokens, has its sign set where there is no prefix.
 enum { kDone = 0, kWhole = 1, kPieces = 2 };
-template <int D, int COLUMNS>
-__device__ __forceinline__ float *piece_of(const SharedArgs &h, int place)
+template <int D>
+__device__ __forceinline__ float *piece_of(float *pieces, int columns, int place)
 {
-    return h.a.ws + (size_t)place * COLUMNS * (D + 4);
+    return pieces + (size_t)place * columns * (D + 4);
 }
 // The places of a unit's pieces: the last one of the workgroup that it begins in, then the first ones of those it goes on in.
 __device__ __forceinline__ int place_of(int wg0, int piece) { return piece == 0 ? 2 * wg0 + 1 : 2 * (wg0 + piece); }
@@ -199,8 +245,8 @@ __device__ __forceinline__ float *state_of(const SharedArgs &h, int own, size_t 
 }
 
 // Workgroup: 4 waves; dealt in equal numbers of rounds and units' costs.  A piece of a unit is what one workgroup has of its rounds.
-template <int D, int QT, int PT, int NC>
-__global__ __launch_bounds__(256, D == 256 || NC > 2 ? 1 : 2) void shared_attention_kernel(SharedArgs h)
+template <int D, int QT, int PT, int NC, int UNITS>
+__global__ __launch_bounds__(256, D == 256 || (D == 128 && NC == 2 && QT == 3) ? 1 : 2) void shared_attention_kernel(SharedArgs h)
 {
     constexpr int kTile = cache_tile_bytes(D), kColumns = 16 * NC;
     constexpr int kPass = D > 128 ? 128 : D;
@@ -217,27 +263,21 @@ __global__ __launch_bounds__(256, D == 256 || NC > 2 ? 1 : 2) void shared_attent
 
     Sequence own;
     int upto = 0, all = 0;  // rounds of the look's sequences up to the lane's; of all looks
-    const auto rounds_in = [&](int rounds, int blocks) { return saturated((long long)saturated((long long)rounds * blocks) * n_kv); };
     const auto rounds_of = [&](const Sequence &q) {
-        return __builtin_elementwise_add_sat(rounds_in(q.prefix_rounds + kUnitCost, q.prefix_blocks), rounds_in(q.rounds + kUnitCost, q.blocks));
+        return __builtin_elementwise_add_sat(rounds_in(q.prefix_rounds + kUnitCost, q.prefix_blocks, n_kv), rounds_in(q.rounds + kUnitCost, q.blocks, n_kv));
     };
     for (int look = 0; look < looks; ++look) {
-        own = look_at<kColumns>(h, packs, look, lane);
+        own = look_at<kColumns, UNITS>(h, packs, look, lane);
         upto = wave_scan(rounds_of(own));
         all = __builtin_elementwise_add_sat(all, __builtin_amdgcn_readlane(upto, 63));
     }
-    const unsigned total = all, n_wg = min(gridDim.x, total);
-    if (blockIdx.x >= n_wg) return;
-    const unsigned fewest = total / n_wg, longer = total - fewest * n_wg;
-    const auto workgroup_of = [&](unsigned round) {
-        const unsigned of_longer = longer * (fewest + 1);
-        return (int)(round < of_longer ? round / (fewest + 1) : longer + (round - of_longer) / fewest);
-    };
-    int at = blockIdx.x * fewest + min(blockIdx.x, longer);
-    const int end = at + (int)fewest + (blockIdx.x < longer);
+    const Shares shares(all);
+    if (blockIdx.x >= shares.n) return;
+    int at = shares.first();
+    const int end = shares.end();
     int look = 0, look_at_round = 0;  // the look that `own` is of, and the rounds in front of it
     if (looks > 1) {
-        own = look_at<kColumns>(h, packs, 0, lane);
+        own = look_at<kColumns, UNITS>(h, packs, 0, lane);
         upto = wave_scan(rounds_of(own));
     }
     const size_t page_bytes = cache_page_bytes(a.c);
@@ -247,7 +287,7 @@ __global__ __launch_bounds__(256, D == 256 || NC > 2 ? 1 : 2) void shared_attent
         if ((unsigned)at >= (unsigned)look_at_round + (unsigned)of_look) {
             look_at_round += of_look;
             if (++look >= looks) break;  // (never, but for sums that saturate)
-            own = look_at<kColumns>(h, packs, look, lane);
+            own = look_at<kColumns, UNITS>(h, packs, look, lane);
             upto = wave_scan(rounds_of(own));
             continue;
         }
@@ -255,7 +295,7 @@ __global__ __launch_bounds__(256, D == 256 || NC > 2 ? 1 : 2) void shared_attent
         const int seq_at = look_at_round + (owner > 0 ? __builtin_amdgcn_readlane(upto, owner - 1) : 0);
         const int prefix = __builtin_amdgcn_readlane(own.prefix, owner);
         const int prefix_rounds = __builtin_amdgcn_readlane(own.prefix_rounds, owner), prefix_blocks = __builtin_amdgcn_readlane(own.prefix_blocks, owner);
-        const int of_prefix = rounds_in(prefix_rounds + kUnitCost, prefix_blocks);
+        const int of_prefix = rounds_in(prefix_rounds + kUnitCost, prefix_blocks, n_kv);
         const bool shared = at - seq_at < of_prefix;
         const int rounds = shared ? prefix_rounds : __builtin_amdgcn_readlane(own.rounds, owner), dealt = rounds + kUnitCost;
         const int first_at = shared ? seq_at : seq_at + of_prefix;
@@ -274,18 +314,8 @@ __global__ __launch_bounds__(256, D == 256 || NC > 2 ? 1 : 2) void shared_attent
         int lowest = kMostTokens, highest = -1;  // of the live columns' positions
 #pragma unroll
         for (int x = 0; x < NC; ++x) {
-            const int col = block * kColumns + 16 * x + n, token = min(col, n_columns - 1) / share;
-            int of = owner, local = token;
-            if (shared) {
-                int lo = 0;  // sequences whose tokens all stand in front of this one
-#pragma unroll
-                for (int half = 32; half > 0; half >>= 1)
-                    if (__shfl(own.fresh_upto, lo + half - 1, kWave) <= before + token) lo += half;
-                of = lo;
-                local = before + token - (__shfl(own.fresh_upto, max(lo - 1, 0), kWave) & (lo > 0 ? -1 : 0));
-            }
-            row[x] = __shfl(own.start, of, kWave) + local;
-            pos[x] = __shfl(own.context, of, kWave) - __shfl(own.fresh, of, kWave) + local;
+            const int col = block * kColumns + 16 * x + n;
+            own.column(shared, owner, before, min(col, n_columns - 1) / share, &row[x], &pos[x]);
             if (col < n_columns) lowest = min(lowest, pos[x]), highest = max(highest, pos[x]);
             else pos[x] = -1, row[x] = -1;  // a column that is not there sees nothing
             if (wave == 0 && g == 0) s_row[16 * x + n] = row[x];
@@ -298,9 +328,7 @@ __global__ __launch_bounds__(256, D == 256 || NC > 2 ? 1 : 2) void shared_attent
         const int context = __builtin_amdgcn_readlane(own.context, owner);
         int source = owner, lo = prefix, hi = max(min(context, a.stride << a.c.log_page), prefix);
         if (shared) {
-            const bool member = lane >= pack0 && lane < pack0 + pack_n && own.fresh > 0;
-            const int most = __builtin_amdgcn_readlane(wave_scan<true>(member ? own.context : 0), 63);
-            source = __ffsll((unsigned long long)__ballot(member && own.context == most)) - 1;
+            source = own.source(pack0, pack_n, lane);
             lo = 0, hi = prefix;
         }
         const int seq = packs.first(look) + source;
@@ -383,8 +411,8 @@ __global__ __launch_bounds__(256, D == 256 || NC > 2 ? 1 : 2) void shared_attent
 
         const bool whole = begin == 0 && stop == rounds;
         // pieces: one for each of the workgroups that the unit's first and its last round fall to and those between them
-        const int wg0 = workgroup_of(unit_at + kUnitCost), pieces = workgroup_of(unit_at + dealt - 1) - wg0 + 1;
-        float *const part = piece_of<D, kColumns>(h, 2 * blockIdx.x + (begin == 0));
+        const int wg0 = shares.workgroup_of(unit_at + kUnitCost), pieces = shares.workgroup_of(unit_at + dealt - 1) - wg0 + 1;
+        float *const part = piece_of<D>(h.own_pieces, kColumns, 2 * blockIdx.x + (begin == 0));
         // what the four waves left in LDS of 16 columns, each relative to its own maximum: a piece, or all there is of the unit's tokens
         const auto merge = [&](int x, int live, int pass) {
             for (int e = threadIdx.x; e < live * (kPass / 2); e += 256) {
@@ -439,9 +467,236 @@ __global__ __launch_bounds__(256, D == 256 || NC > 2 ? 1 : 2) void shared_attent
     }
 }
 
+// The prefix where a pack has many columns: matrix-bound, in blocks of 128 columns (as cache_prompt_kernel).  Workgroup: 4 waves, 32 columns each; 64
+// tokens at a time are converted to bf16 in LDS, a tile of the cache by each wave, while the tokens before them are used.  Dealt in equal numbers of
+// tiles of 64 tokens and units' costs.
+constexpr int kBlockColumns = 128, kBlockCost = 4;
+template <int D>
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void shared_blocks_kernel(SharedArgs h)
+{
+    constexpr int kTile = cache_tile_bytes(D), kCols = 32;
+    extern __shared__ __align__(16) unsigned char s_raw[];
+    PromptTiles<D> &s_tiles = *reinterpret_cast<PromptTiles<D> *>(s_raw);
+    const AttentionArgs &a = h.a;
+    const int lane_of_block = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane_of_block & 15, g = lane_of_block >> 4;
+    const int lc = lane_of_block & 31, half_of = lane_of_block >> 5, token_row = lc ^ (lc & 4) << 1;  // (token_row: the token of S^T's row lc)
+    const int share = a.n_heads / a.c.n_kv, n_kv = a.c.n_kv;
+    const float scale = a.scale != 0.0f ? fabsf(a.scale) * kLog2e : 1.0f;
+    const TileOffsets<D> offsets(n, g);
+    const size_t page_bytes = cache_page_bytes(a.c);
+    const Packs packs(h.group);
+    const int looks = packs.looks(a.n_seq);
+
+    const auto tiles_of = [&](int prefix) { return (prefix + kPromptTile - 1) / kPromptTile; };
+    const auto units_of = [&](const Sequence &q) { return rounds_in(tiles_of(q.prefix) + kBlockCost, q.prefix_blocks, n_kv); };
+    Shares shares(0);
+    int at = -1, end = 0;
+    // (what the lanes know of the sequences is looked up anew for every piece: it does not fit next to a block's registers, and nor does what
+    // could be computed of the lane's number ahead of the loop)
+    for (;;) {
+        int lane = lane_of_block;
+        asm volatile("" : "+v"(lane));
+        int look = 0, look_at_tile = 0;  // the look that `own` is of, and the tiles in front of it
+        Sequence own = look_at<kBlockColumns, kOfPrefix>(h, packs, 0, lane);
+        int upto = wave_scan(units_of(own)), of_look = __builtin_amdgcn_readlane(upto, 63);
+        if (at < 0) {
+            int all = of_look;
+            for (int i = 1; i < looks; ++i)
+                all = __builtin_elementwise_add_sat(
+                    all, __builtin_amdgcn_readlane(wave_scan(units_of(look_at<kBlockColumns, kOfPrefix>(h, packs, i, lane))), 63));
+            shares = Shares(all);
+            if (blockIdx.x >= shares.n) return;
+            at = shares.first(), end = shares.end();
+        }
+        if (at >= end) return;
+        while ((unsigned)at >= (unsigned)look_at_tile + (unsigned)of_look) {
+            look_at_tile += of_look;
+            if (++look >= looks) return;  // (never, but for sums that saturate)
+            own = look_at<kBlockColumns, kOfPrefix>(h, packs, look, lane);
+            upto = wave_scan(units_of(own)), of_look = __builtin_amdgcn_readlane(upto, 63);
+        }
+        const int owner = __ffsll((unsigned long long)__ballot(upto > at - look_at_tile)) - 1;
+        const int seq_at = look_at_tile + (owner > 0 ? __builtin_amdgcn_readlane(upto, owner - 1) : 0);
+        const int prefix = __builtin_amdgcn_readlane(own.prefix, owner);
+        const int tiles = tiles_of(prefix), dealt = tiles + kBlockCost;
+        const int unit = (int)((unsigned)(at - seq_at) / (unsigned)dealt), block = (int)((unsigned)unit / (unsigned)n_kv), head = unit - block * n_kv;
+        const int unit_at = seq_at + unit * dealt, tile0 = max(at - unit_at - kBlockCost, 0), stop = min(tiles, end - unit_at - kBlockCost);
+        at = unit_at + min(dealt, end - unit_at);
+        if (stop <= tile0) continue;
+
+        const int pack0 = __builtin_amdgcn_readlane(own.pack0, owner), pack_n = __builtin_amdgcn_readlane(own.pack_n, owner);
+        const int before = pack0 > 0 ? __builtin_amdgcn_readlane(own.fresh_upto, pack0 - 1) : 0;
+        const int n_columns = columns_of(__builtin_amdgcn_readlane(own.fresh_upto, pack0 + pack_n - 1) - before, share);
+        const int seq = packs.first(look) + own.source(pack0, pack_n, lane);
+        const scalar_ints table = (scalar_ints)(uintptr_t)(a.table + (size_t)seq * a.stride);
+        const unsigned char *const cache = a.cache + (size_t)(head * (a.c.page >> 4)) * kTile;
+        const int col = block * kBlockColumns + wave * kCols + lc;
+        const bool live = col < n_columns;
+        int row, pos;
+        own.column(true, owner, before, min(col, n_columns - 1) / share, &row, &pos);
+        if (!live) pos = -1;  // a column that is not there sees nothing
+        // positions of the wave's columns (of columns that are not there: none)
+        int lowest = live ? pos : kMostTokens, highest = pos;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1)
+            lowest = min(lowest, __shfl_xor(lowest, off, kWave)), highest = max(highest, __shfl_xor(highest, off, kWave));
+        lowest = __builtin_amdgcn_readfirstlane(lowest), highest = __builtin_amdgcn_readfirstlane(highest);
+        const int y_row = row * a.n_heads + head * share + min(col, n_columns - 1) % share;
+        bf16x8 q[D / 16];
+        const uint32_t sign = a.scale < 0.0f ? 0x80008000u : 0u, keep = a.scale != 0.0f ? ~0u : 0u;
+        const u32x4 *from = reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(a.q) + (size_t)y_row * D);
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) {
+            u32x4 x = {0, 0, 0, 0};
+            if (live) x = from[2 * s + half_of];
+            q[s] = __builtin_bit_cast(bf16x8, (x ^ sign) & keep);
+        }
+        f32x16 o[D / 32], s0, s1;
+        float m = kLowest, l = 0.0f;
+        float by = scale;  // (see choose_unit)
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[j][i] = 0.0f;
+        const int lo = tile0 * kPromptTile, hi = min(prefix, stop * kPromptTile);
+        // tokens in front of this one are all there: 0 if some page is none
+        int full = hi;
+        for (int i = (lo >> a.c.log_page) + lane; i << a.c.log_page < hi; i += 64)
+            if ((unsigned)table[i] >= (unsigned)a.c.n_pages) full = 0;
+        full = __any(full == 0) ? 0 : full;
+
+        TileRegs<D> regs;
+        int limit = 0;
+        auto load = [&](int tile) {  // this wave's 16 tokens
+            const int t = tile * kPromptTile + 16 * wave;
+            const int page = t < hi ? table[t >> a.c.log_page] : -1;
+            limit = (unsigned)page < (unsigned)a.c.n_pages ? hi : 0;
+            load_tile<D, false>(regs, cache + (size_t)(limit ? (unsigned)page : 0u) * page_bytes + ((t & (a.c.page - 1)) >> 4) * kTile, t < limit, offsets);
+        };
+        auto convert = [&](int tile) {
+            convert_tile<D>(s_tiles.k[tile % 2], s_tiles.v[tile % 3], regs, wave, limit - (tile * kPromptTile + 16 * wave), n, g);
+        };
+        auto scores = [&](f32x16 &s, int tile, int half) {
+            const uint32_t *const k_from = s_tiles.k[tile % 2];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) {
+                const bf16x8 x = *reinterpret_cast<const bf16x8 *>(&k_from[((2 * k + half_of) * kPromptTile + 32 * half + token_row) * 4]);
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, q[k], s, 0, 0, 0);
+            }
+        };
+        auto weights = [&](f32x16 &s, bf16x8 (&p)[2], int tile, int half) {
+            const int t0 = tile * kPromptTile + 32 * half;
+            if (!(t0 + 32 <= full && t0 + 31 <= lowest)) {
+                int lim0 = hi, lim1 = hi;
+                if (full == 0) {
+                    if (t0 < hi && (unsigned)table[t0 >> a.c.log_page] >= (unsigned)a.c.n_pages) lim0 = 0;
+                    if (t0 + 16 < hi && (unsigned)table[(t0 + 16) >> a.c.log_page] >= (unsigned)a.c.n_pages) lim1 = 0;
+                }
+                int of_half = half_of;  // (opaque: else the sixteen places within a step are computed ahead of the loop, and stay in registers)
+                asm volatile("" : "+v"(of_half));
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int t = t0 + (8 * (i / 4) ^ 8 * of_half) + 4 * of_half + i % 4;
+                    if (!(t < (i < 8 ? lim0 : lim1) && t <= pos)) s[i] = -INFINITY;
+                }
+            }
+            float top = s[0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+            if (__any(top * by > m + kSlack)) {
+                top = fmaxf(top, __shfl_xor(top, 32, kWave));
+                const float next = fmaxf(m, top * by), factor = __builtin_amdgcn_exp2f(m - next);
+                m = next;
+                choose_unit(by, m, top, scale);
+                l *= factor;
+#pragma unroll
+                for (int j = 0; j < D / 32; ++j) o[j] *= factor;
+            }
+            float x[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                x[i] = __builtin_amdgcn_exp2f(fmaf(s[i], by, -m));
+                l += x[i];
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                p[j] = as_bf16x8(pack_bf16(x[8 * j], x[8 * j + 1]), pack_bf16(x[8 * j + 2], x[8 * j + 3]), pack_bf16(x[8 * j + 4], x[8 * j + 5]),
+                                 pack_bf16(x[8 * j + 6], x[8 * j + 7]));
+        };
+        auto values = [&](bf16x8 (&p)[2], int tile, int half) {
+            const uint32_t *const v_from = s_tiles.v[tile % 3];
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const bf16x8 x = *reinterpret_cast<const bf16x8 *>(&v_from[((2 * (2 * half + k) + half_of) * D + 32 * j + lc) * 4]);
+                    o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, p[k], o[j], 0, 0, 0);
+                }
+        };
+        bf16x8 p[2];
+        load(tile0);
+        convert(tile0);
+        if (tile0 + 1 < stop) load(tile0 + 1);
+        __syncthreads();
+        // (a wave whose columns see none of the piece only converts: with that as a branch within the loop registers do not suffice)
+        if (highest < lo) {
+            for (int tile = tile0; tile < stop; ++tile) {
+                if (tile + 1 < stop) {
+                    convert(tile + 1);
+                    if (tile + 2 < stop) load(tile + 2);
+                }
+                __syncthreads();
+            }
+        } else {
+            scores(s0, tile0, 0);
+            for (int tile = tile0; tile < stop; ++tile) {
+                const bool more = tile + 1 < stop;
+                scores(s1, tile, 1);
+                weights(s0, p, tile, 0);
+                values(p, tile, 0);
+                if (more) {
+                    convert(tile + 1);
+                    if (tile + 2 < stop) load(tile + 2);
+                }
+                __syncthreads();
+                if (more) scores(s0, tile + 1, 0);
+                weights(s1, p, tile, 1);
+                values(p, tile, 1);
+            }
+        }
+        l += __shfl_xor(l, 32, kWave);
+        const bool whole = tile0 == 0 && stop == tiles;
+        const int wg0 = shares.workgroup_of(unit_at + kBlockCost), pieces = shares.workgroup_of(unit_at + dealt - 1) - wg0 + 1;
+        if (live) {
+            float *const state = state_of<D>(h, 0, y_row);
+            float *const to = whole ? state : piece_of<D>(h.prefix_pieces, kBlockColumns, 2 * blockIdx.x + (tile0 == 0)) + (wave * kCols + lc) * (D + 4);
+            // channels r D/16 .. of the lane's eight r: the places c 16 + r of all c
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    constexpr int C = D / 16;
+#pragma unroll
+                    for (int e = 0; e < C; e += 4)
+                        *reinterpret_cast<f32x4 *>(to + (8 * b + 4 * half_of + i) * C + e) =
+                            f32x4{o[e / 2][4 * b + i], o[e / 2][8 + 4 * b + i], o[e / 2 + 1][4 * b + i], o[e / 2 + 1][8 + 4 * b + i]};
+                }
+            if (half_of == 0) {
+                const float most = by_scale(m, by, scale);
+                if (whole) *reinterpret_cast<float4 *>(state + D) = {most, l, __int_as_float(kWhole), 0.0f};
+                else *reinterpret_cast<float2 *>(to + D) = {most, l};
+                if (!whole && tile0 == 0) *reinterpret_cast<int4 *>(state + D) = {wg0, pieces, kPieces, wave * kCols + lc};
+            }
+        }
+        __syncthreads();  // (the next unit's tiles take these buffers)
+    }
+}
+
 // y of the columns whose results stand in the workspace.  Workgroup: one (token, head); a group of D/4 lanes for a row of results, four channels to
 // a lane, rows in the order of the tokens.
-template <int D, int COLUMNS>
+template <int D>
 __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs h)
 {
     constexpr int kLanes = D / 4, kGroups = 256 / kLanes, kTogether = 4;
@@ -471,7 +726,9 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs h)
                 if (i < n) {
                     const int4 e = i < n1 ? prefix : own;
                     const float *p = i < n1 ? of_prefix : of_own;
-                    if (e.z == kPieces) p = piece_of<D, COLUMNS>(h, place_of(e.x, i < n1 ? i : i - n1)) + (e.w & 255) * (D + 4);
+                    if (e.z == kPieces)
+                        p = (i < n1 ? piece_of<D>(h.prefix_pieces, h.prefix_columns, place_of(e.x, i)) : piece_of<D>(h.own_pieces, h.own_columns, place_of(e.x, i - n1))) +
+                            (e.w & 255) * (D + 4);
                     ml[k] = *reinterpret_cast<const float2 *>(p + D);
                     v[k] = *reinterpret_cast<const f32x4 *>(p + ch);
                 }
@@ -502,54 +759,60 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs h)
     }
 }
 
-// Blocks of 16 columns that share a conversion: as many as a pack's columns fill, up to what the registers hold.
-int column_blocks(int n_tokens, int group, int n_heads, int n_kv, int d, int max_new, int terms)
-{
-    const long long columns = std::min<long long>(n_tokens, (long long)std::min(group, 64) * max_new) * (n_heads / n_kv);
-    const int most = d == 256 ? (terms == 1 ? 2 : 1) : (terms == 1 ? 4 : 2);
-    return std::min(most, columns <= 16 ? 1 : columns <= 32 ? 2 : 4);
-}
-
+// How a call is launched.  Columns of a pack (new tokens x query heads to a kv head) in blocks of 128 from kMostNarrow on, where all is bf16; else in one or two blocks
+// of 16 that share a conversion, as many as they fill, as far as registers go.
+constexpr int kMostNarrow = 64;
 struct SharedGrid {
-    int blocks, workgroups;
-    size_t pieces, states;  // bytes
-    size_t bytes() const { return pieces + states; }
+    int prefix_wg, own_wg;  // workgroups of the kernel for blocks of 128 (0: the other one has all units), and of the other one
+    int nc;
+    size_t prefix_pieces, own_pieces, states;  // bytes
+    size_t bytes() const { return prefix_pieces + own_pieces + states; }
 };
-SharedGrid shared_grid(int n_tokens, int n_seq, int group, int n_heads, int n_kv, int d, int max_new, int max_context, int terms)
+SharedGrid shared_grid(int n_tokens, int n_seq, int group, int n_heads, int n_kv, int d, int max_new, int max_context, bool all_bf16)
 {
-    SharedGrid g = {column_blocks(n_tokens, group, n_heads, n_kv, d, max_new, terms), 0, 0, 0};
-    const long long share = n_heads / n_kv, rounds = (max_context + (long long)kRound - 1) / kRound;
-    // (for these sizes and all smaller ones, whose blocks may be fewer)
-    for (int nc = 1; nc <= g.blocks; nc *= 2) {
-        const long long most = d == 256 || nc > 2 ? kWorkgroups / 2 : kWorkgroups, packs = (long long)n_seq / group * ((group + 63) / 64);
-        const long long units = n_kv * (n_seq * ((max_new * share + 16 * nc - 1) / (16 * nc)) + packs * ((std::min(group, 64) * max_new * share + 16 * nc - 1) / (16 * nc)));
-        const long long per_unit = std::min(rounds, std::max(32ll, (long long)(2.0 * sqrt((double)rounds))));
-        g.workgroups = (int)std::min(units * per_unit, units >= 128 ? most : kWorkgroups / 2ll);
-g.pieces = std::max(g.pieces, (size_t)g.workgroups * 2 * 16 * nc * (d + 4) * sizeof(float));
+    const long long share = n_heads / n_kv, rounds = (max_context + (long long)kRound - 1) / kRound, packs = (long long)n_seq / group * ((group + 63) / 64);
+    const long long of_pack = std::min<long long>(n_tokens, (long long)std::min(group, 64) * max_new) * share, of_seq = std::min(n_tokens, max_new) * share;
+    SharedGrid g = {0, 0, 1, 0, 0, 0};
+    const bool in_blocks = all_bf16 && of_pack > kMostNarrow;
+    if (in_blocks) {
+        const long long units = packs * n_kv * ((of_pack + kBlockColumns - 1) / kBlockColumns);
+        g.prefix_wg = (int)std::min<long long>(units * 2 * rounds, d == 256 ? kWorkgroups / 2 : kWorkgroups);
+        g.prefix_pieces = (size_t)g.prefix_wg * 2 * kBlockColumns * (d + 4) * sizeof(float);
     }
+    if (d < 256 && (in_blocks ? of_seq : of_pack) > 16) g.nc = 2;
+    const long long columns = 16 * g.nc, units = n_kv * (n_seq * ((of_seq + columns - 1) / columns) + (in_blocks ? 0 : packs * ((of_pack + columns - 1) / columns)));
+    const long long per_unit = std::min(rounds + kUnitCost, std::max(32ll, (long long)(2.0 * sqrt((double)rounds))));
+    g.own_wg = (int)std::min(units * per_unit, units >= 128 && d < 256 ? (long long)kWorkgroups : kWorkgroups / 2ll);
+    g.own_pieces = (size_t)g.own_wg * 2 * columns * (d + 4) * sizeof(float);
     g.states = 2 * (size_t)n_tokens * n_heads * (d + 4) * sizeof(float);
     return g;
 }
 
 template <int D, int QT, int PT, int NC>
-hipError_t launch_nc(const SharedArgs &h, const SharedGrid &g, hipStream_t s)
+hipError_t launch_units(const SharedArgs &h, const SharedGrid &g, hipStream_t s)
 {
-    shared_attention_kernel<D, QT, PT, NC><<<(unsigned)g.workgroups, 256, 0, s>>>(h);
+    if (g.prefix_wg == 0) {
+        shared_attention_kernel<D, QT, PT, NC, kBoth><<<(unsigned)g.own_wg, 256, 0, s>>>(h);
+    } else if constexpr (QT == 1 && PT == 1) {
+        constexpr int kBytes = (int)sizeof(PromptTiles<D>);
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(shared_blocks_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+        if (e != hipSuccess) return e;
+        shared_blocks_kernel<D><<<(unsigned)g.prefix_wg, 256, kBytes, s>>>(h);
+        shared_attention_kernel<D, QT, PT, NC, kOwn><<<(unsigned)g.own_wg, 256, 0, s>>>(h);
+    }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const long long rows = (long long)h.a.max_new * h.a.n_heads;  // of a sequence
-    shared_join_kernel<D, 16 * NC><<<dim3((unsigned)h.a.n_seq, (unsigned)std::min(rows, 4096ll)), 256, 0, s>>>(h);
+    shared_join_kernel<D><<<dim3((unsigned)h.a.n_seq, (unsigned)std::min(rows, 4096ll)), 256, 0, s>>>(h);
     return hipGetLastError();
 }
 template <int D, int QT, int PT>
 hipError_t launch_types(const SharedArgs &h, const SharedGrid &g, hipStream_t s)
 {
-    if (g.blocks == 1) return launch_nc<D, QT, PT, 1>(h, g, s);
-    if constexpr (QT == 1 || D < 256) {
-        if (g.blocks == 2) return launch_nc<D, QT, PT, 2>(h, g, s);
-        if constexpr (QT == 1 && D < 256) return launch_nc<D, QT, PT, 4>(h, g, s);
+    if constexpr (D < 256) {
+        if (g.nc == 2) return launch_units<D, QT, PT, 2>(h, g, s);
     }
-    return hipErrorInvalidValue;
+    return launch_units<D, QT, PT, 1>(h, g, s);
 }
 template <int D>
 hipError_t launch_shared_d(const SharedArgs &h, const SharedGrid &g, hipStream_t s)
@@ -564,18 +827,25 @@ hipError_t launch_shared_d(const SharedArgs &h, const SharedGrid &g, hipStream_t
 size_t cache_attention_shared_ws(int n_tokens, int n_seq, int group, int n_heads, int n_kv, int d, int max_new, int max_context)
 {
     if (group == 1) return 0;
-    return std::max(shared_grid(n_tokens, n_seq, group, n_heads, n_kv, d, max_new, max_context, 1).bytes(),
-                    shared_grid(n_tokens, n_seq, group, n_heads, n_kv, d, max_new, max_context, 3).bytes());
+    // for either type, and for all smaller sizes: the most workgroups that any of them has, of the widest units
+    const SharedGrid g = shared_grid(n_tokens, n_seq, group, n_heads, n_kv, d, max_new, max_context, true);
+    const size_t own = (size_t)kWorkgroups * 2 * 32 * (d + 4) * sizeof(float);
+    return g.prefix_pieces + own + g.states;
 }
 
 hipError_t launch_cache_attention_shared(SharedArgs h, hipStream_t s)
 {
     const AttentionArgs &a = h.a;
+    const bool all_bf16 = a.q_bf16 && a.y_bf16;
     // chunks for which the kernel for blocks of 128 columns pays are bound by their products: they gain nothing from a prefix that is read once
-    const int parts = cache_attention_parts(a.n_tokens, a.n_seq, a.n_heads, a.c.n_kv, a.c.d, a.max_new, a.max_context, 0, a.q_bf16 && a.y_bf16);
+    const int parts = cache_attention_parts(a.n_tokens, a.n_seq, a.n_heads, a.c.n_kv, a.c.d, a.max_new, a.max_context, 0, all_bf16);
     if (h.group == 1 || parts > 0) return launch_cache_attention(a, s);
-    const SharedGrid g = shared_grid(a.n_tokens, a.n_seq, h.group, a.n_heads, a.c.n_kv, a.c.d, a.max_new, a.max_context, a.q_bf16 ? 1 : 3);
-    h.states = reinterpret_cast<float *>(reinterpret_cast<char *>(a.ws) + g.pieces);
+    const SharedGrid g = shared_grid(a.n_tokens, a.n_seq, h.group, a.n_heads, a.c.n_kv, a.c.d, a.max_new, a.max_context, all_bf16);
+    char *const ws = reinterpret_cast<char *>(a.ws);
+    h.prefix_pieces = reinterpret_cast<float *>(ws), h.own_pieces = reinterpret_cast<float *>(ws + g.prefix_pieces);
+    h.states = reinterpret_cast<float *>(ws + g.prefix_pieces + g.own_pieces);
+    h.own_columns = 16 * g.nc, h.prefix_columns = g.prefix_wg ? kBlockColumns : h.own_columns;
+    if (!g.prefix_wg) h.prefix_pieces = h.own_pieces;
     if (a.c.d == 64) return launch_shared_d<64>(h, g, s);
     if (a.c.d == 128) return launch_shared_d<128>(h, g, s);
     return launch_shared_d<256>(h, g, s);
