@@ -70,6 +70,7 @@ _SIGS = {
                                        _vp, C.c_size_t, _vp]),
     "pop_cache_attention_shared": (_i, [_vp, _i, _i, _vp, _i, _i, _i, _i, _vp, _i, _vp, _vp, _i, _i, _vp, _i, _i, _i, C.c_float, _vp, _i,
                                         _vp, C.c_size_t, _vp]),
+    "pop_cache_attention_shared_kind": (_i, [_i] * 10),
     "pop_cache_attention_shared_workspace": (_i, [_i, _i, _i, _i, _i, _i, _i, _i, _szp]),
     "pop_cache_attention_workspace": (_i, [_i, _i, _i, _i, _i, _i, _i, _szp]),
     "pop_cache_attention_kind": (_i, [_i, _i, _i, _i, _i, _i, _i, _i, _i, _i, _ip]),
@@ -387,6 +388,14 @@ def pop_cache_attention_shared(q, dtype, n_tokens, cache, n_kv_heads, head_dim, 
                                            _ptr(block_table), table_stride, _ptr(q_start), _ptr(context_len), n_seq, group,
                                            _ptr(prefix_len), n_heads, max_new, max_context, scale, _ptr(y), ydtype, ws, ws_bytes,
                                            _stream(stream)), "pop_cache_attention_shared")
+
+
+def pop_cache_attention_shared_kind(dtype, ydtype, n_tokens, n_seq, group, n_heads, n_kv_heads, head_dim, max_new, max_context) -> int:
+    """0 nothing to do, 1 each row for itself, 2 prefixes by blocks of 16 or 32 columns, 3 by blocks of 128."""
+    kind = _lib.pop_cache_attention_shared_kind(dtype, ydtype, n_tokens, n_seq, group, n_heads, n_kv_heads, head_dim, max_new, max_context)
+    if kind < 0:
+        raise PopError(kind, "pop_cache_attention_shared_kind")
+    return kind
 
 
 def pop_cache_attention_shared_workspace(n_tokens, n_seq, group, n_heads, n_kv_heads, head_dim, max_new, max_context) -> int:

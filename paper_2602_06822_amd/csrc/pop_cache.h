@@ -146,14 +146,28 @@ size_t cache_attention_ws(int n_tokens, int n_seq, int n_heads, int n_kv, int d,
 int cache_attention_parts(int n_tokens, int n_seq, int n_heads, int n_kv, int d, int max_new, int max_context, int window, int all_bf16);
 hipError_t launch_cache_attention(const AttentionArgs &a, hipStream_t s);
 
+// Division of numbers below 2^31 by one that the host knows: ceil(2^(31 + l) / d) with 2^l >= d is off by less than 2^l / d parts of a quotient.
+struct Divisor {
+    unsigned factor, shift;
+    explicit Divisor(int d) : shift(31)
+    {
+        while (1ull << (shift - 31) < (unsigned)d) ++shift;
+        factor = (unsigned)(((1ull << shift) + d - 1) / d);
+    }
+    __device__ __forceinline__ int of(int x) const { return (int)(((unsigned long long)(unsigned)x * factor) >> shift); }
+};
+
 struct SharedArgs {
     AttentionArgs a;
+    Divisor by_share, by_kv, by_group;  // query heads to a kv head, kv heads, sequences of a group
     int group;          // sequences of a group
     const int *prefix;  // [n_seq / group] tokens that a group's sequences share
     // set by the launcher
     float *prefix_pieces, *own_pieces, *states;
     int prefix_columns, own_columns;
 };
+// 0: nothing to do, 1: each sequence for itself (launch_cache_attention), 2: the prefix by blocks of 16 or 32 columns of a group, 3: by blocks of 128.
+int cache_attention_shared_kind(int n_tokens, int n_seq, int group, int n_heads, int n_kv, int d, int max_new, int max_context, int all_bf16);
 size_t cache_attention_shared_ws(int n_tokens, int n_seq, int group, int n_heads, int n_kv, int d, int max_new, int max_context);
 hipError_t launch_cache_attention_shared(SharedArgs h, hipStream_t s);  // (pop_cache_attention_shared.hip)
 

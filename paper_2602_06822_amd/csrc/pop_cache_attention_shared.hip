@@ -17,7 +17,7 @@ namespace {
 
 constexpr int kRound = 128;  // tokens of a round: a step of each of the four waves
 constexpr int kWorkgroups = 512;
-// What a unit costs its workgroup beside its rounds (its columns, q and table, the waves' sums), in rounds: work is dealt with that on top.
+// What a unit costs its workgroup beside its rounds (its columns, q and table, the waves' sums), in rounds.
 constexpr int kUnitCost = 4;
 // A prefix shorter than this is read by each sequence for itself.
 constexpr int kLeastPrefix = 256;
@@ -110,14 +110,28 @@ struct WideSums {
     }
 };
 
+// The least and the largest of a row of 16 lanes, in all of them.
+template <int ROR>
+__device__ __forceinline__ int turned_row(int v) { return __builtin_amdgcn_update_dpp(0, v, 0x120 + ROR, 0xf, 0xf, false); }
+__device__ __forceinline__ int row_min(int v)
+{
+    v = min(v, turned_row<8>(v)), v = min(v, turned_row<4>(v)), v = min(v, turned_row<2>(v));
+    return min(v, turned_row<1>(v));
+}
+__device__ __forceinline__ int row_max(int v)
+{
+    v = max(v, turned_row<8>(v)), v = max(v, turned_row<4>(v)), v = max(v, turned_row<2>(v));
+    return max(v, turned_row<1>(v));
+}
+
 // v of lane `from` (modulo 64).
 __device__ __forceinline__ int lane_value(int v, int from) { return __builtin_amdgcn_ds_bpermute(from * 4, v); }
 
 // Sequences in packs: a group, or 64 sequences of a larger one (and what is left of it).  A wave looks at as many whole packs at a time as 64
 // lanes hold, a lane for a sequence.
 struct Packs {
-    int group, per_group, at_once;  // parts of a group; sequences that a wave looks at where a group is a pack
-    __device__ __forceinline__ Packs(int n_beams) : group(n_beams), per_group((n_beams + 63) / 64), at_once(n_beams >= 64 ? 64 : 64 / n_beams * n_beams) {}
+    int group, per_group, at_once;  // sequences of a group, parts of one; sequences that a wave looks at where a group is a pack
+    __device__ __forceinline__ explicit Packs(const SharedArgs &h) : group(h.group), per_group((h.group + 63) / 64), at_once(h.group >= 64 ? 64 : h.by_group.of(64) * h.group) {}
     __device__ __forceinline__ int looks(int n_seq) const { return per_group > 1 ? n_seq / group * per_group : (n_seq + at_once - 1) / at_once; }
     // The look's first sequence and how many there are.
     __device__ __forceinline__ int first(int look) const { return per_group > 1 ? look / per_group * group + look % per_group * 64 : look * at_once; }
@@ -137,16 +151,22 @@ struct Sequence {
     int prefix_rounds, prefix_blocks, rounds, blocks;
 
     // Row and position of a token: of the pack's sequences one after another, which begin behind `before` tokens of the look, or of lane `owner`'s.
-    __device__ __forceinline__ void column(bool of_pack, int owner, int before, int token, int *row, int *pos) const
+    __device__ __forceinline__ void column(bool of_pack, int owner, int before, int token, int lane, int *row, int *pos) const
     {
+        const int pack0_of = __builtin_amdgcn_readlane(pack0, owner);
+        const bool lane_outside = lane < pack0_of || lane >= pack0_of + pack_n;
         int of = owner, local = token;
         if (of_pack) {
-            int lo = 0;  // sequences whose tokens all stand in front of this one
+            if (__all(fresh == 1 || lane_outside)) {  // a token each
+                of = pack0_of + token, local = 0;
+            } else {
+                int lo = 0;  // sequences whose tokens all stand in front of this one
 #pragma unroll
-            for (int half = 32; half > 0; half >>= 1)
-                if (lane_value(fresh_upto, lo + half - 1) <= before + token) lo += half;
-            of = lo;
-            local = before + token - (lane_value(fresh_upto, max(lo - 1, 0)) & (lo > 0 ? -1 : 0));
+                for (int half = 32; half > 0; half >>= 1)
+                    if (lane_value(fresh_upto, lo + half - 1) <= before + token) lo += half;
+                of = lo;
+                local = before + token - (lane_value(fresh_upto, max(lo - 1, 0)) & (lo > 0 ? -1 : 0));
+            }
         }
         *row = lane_value(start, of) + local;
         *pos = lane_value(context, of) - lane_value(fresh, of) + local;
@@ -177,22 +197,26 @@ __device__ __forceinline__ Sequence look_at(const SharedArgs &h, const Packs &pa
     if (lane < count) {
         const int next = a.start[s + 1];
         q.start = a.start[s], q.context = min(max(a.context[s], 0), kMostTokens);
-        prefix = h.prefix[s / packs.group];
+        prefix = h.prefix[h.by_group.of(s)];
         if (q.start >= 0 && next > q.start && next <= a.n_tokens) q.fresh = next - q.start;
     }
     q.fresh_upto = wave_scan(q.fresh);
-    q.pack0 = packs.per_group > 1 ? 0 : lane / packs.group * packs.group;
-    q.pack_n = packs.per_group > 1 ? count : packs.group;
+    q.pack0 = packs.per_group > 1 ? 0 : h.by_group.of(lane) * packs.group;
+    q.pack_n = packs.per_group > 1 ? count : packs.group;  // (the same for all lanes)
     // the longest of the pack's sequences, whose row of the table the prefix is read from; one alone shares nothing
     const unsigned long long live = __ballot(q.fresh > 0);
     const unsigned long long members = (q.pack_n >= 64 ? ~0ull : (1ull << q.pack_n) - 1) << q.pack0;
     int longest = q.fresh > 0 ? q.context : 0;
+    if (q.pack_n >= count) {  // (one pack)
+        longest = __builtin_amdgcn_readlane(wave_scan<true>(longest), 63);
+    } else {
 #pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const int other = lane_value(longest, lane + off);
-        if (lane + off < q.pack0 + q.pack_n) longest = max(longest, other);
+        for (int off = 1; off < 64; off <<= 1) {
+            const int other = lane_value(longest, lane + off);
+            if (lane + off < q.pack0 + q.pack_n) longest = max(longest, other);
+        }
+        longest = lane_value(longest, q.pack0);
     }
-    longest = lane_value(longest, q.pack0);
     const int table = a.stride << a.c.log_page;
     prefix = min(min(prefix, longest), table) & ~31;
     q.prefix = prefix >= kLeastPrefix && __popcll(live & members) > 1 ? prefix : 0;
@@ -206,29 +230,48 @@ __device__ __forceinline__ Sequence look_at(const SharedArgs &h, const Packs &pa
     return q;
 }
 
-// Equal shares of `all` rounds for the workgroups; the first `longer` ones have one more than the others.
-struct Shares {
-    unsigned n, fewest, longer;
-    __device__ __forceinline__ Shares(int all)
+__device__ __forceinline__ int times(int a, int b) { return saturated((long long)a * b); }
+
+// How the work is dealt.  A unit is one kv head's block of columns over the prefix (of a pack) or over its own tokens (of a sequence), so many rounds; with what
+// it costs beside them all units make up `all`, and a unit is split into as many parts as it has of that, in workgroups, but at least one.  A part is an item; workgroup
+// w has items w, w + gridDim.x, ..: most have one.  (What had parts of several units a workgroup, in equal numbers of rounds: 8 sequences x 32 heads, 4000 tokens and 200 of
+// their own, 11.6 us; 64 sequences x 8 heads, 700 of their own, 13.6.)  Parts of units that have several have a place for their results each; there
+// are no more of those than workgroups.
+struct Dealing {
+    int all;
+    float per_round;  // parts
+    __device__ __forceinline__ explicit Dealing(int all_) : all(max(all_, 1)), per_round((float)gridDim.x / (float)max(all_, 1)) {}
+    __device__ __forceinline__ int parts(int rounds) const
     {
-        n = min(gridDim.x, (unsigned)all);
-        fewest = n ? (unsigned)all / n : 0, longer = (unsigned)all - fewest * n;
-    }
-    __device__ __forceinline__ int first() const { return blockIdx.x * fewest + min(blockIdx.x, longer); }
-    __device__ __forceinline__ int end() const { return first() + (int)fewest + (blockIdx.x < longer); }
-    __device__ __forceinline__ int workgroup_of(unsigned round) const
-    {
-        const unsigned of_longer = longer * (fewest + 1);
-        return (int)(round < of_longer ? round / (fewest + 1) : longer + (round - of_longer) / fewest);
+        // the whole number in rounds gridDim.x / all, so that all units' together are no more than gridDim.x (sums that have saturated: one each)
+        const long long share = (long long)rounds * gridDim.x;
+        int n = all == 0x7fffffff ? 0 : (int)((float)rounds * per_round);
+        if ((long long)(n + 1) * all <= share) ++n;
+        if ((long long)n * all > share) --n;
+        return min(max(n, 1), max(rounds, 1));
     }
 };
-__device__ __forceinline__ int rounds_in(int rounds, int blocks, int n_kv) { return saturated((long long)saturated((long long)rounds * blocks) * n_kv); }
 
-// The workspace: results of units that several workgroups have, two places to a workgroup, a row for each of a unit's columns; and results of every
-// (token, head) over the prefix and over its own tokens.  A row is O, m and l (D + 2 floats) and two more; in the latter's last four stand
-//     m, l, kWhole, 0         of a unit that one workgroup has,
-//     first, n, kPieces, c    where n workgroups from `first` on have one: row c of their places (integers),
-//     -, -, kDone, -          of own tokens without a prefix that one workgroup has: y is there.
+// Item `at` of units of so many rounds: its unit, and which part of it, rounds [begin, stop).
+struct PartOf {
+    int unit, part, begin, stop;
+};
+__device__ __forceinline__ PartOf part_of(int at, int rounds, int parts)
+{
+    PartOf p = {at, 0, 0, rounds};
+    if (parts > 1) {
+        p.unit = (int)((unsigned)at / (unsigned)parts), p.part = at - p.unit * parts;
+        const int each = (int)((unsigned)rounds / (unsigned)parts), more = rounds - each * parts;
+        p.begin = p.part * each + min(p.part, more), p.stop = p.begin + each + (p.part < more);
+    }
+    return p;
+}
+
+// The workspace: places for results of parts, a row for each of a unit's columns; and results of every (token, head) over the prefix and over its own
+// tokens.  A row is O, m and l (D + 2 floats) and two more; in the latter's last four stand
+//     m, l, kWhole, 0         of a unit that is one part,
+//     first, n, kPieces, c    where it is n: row c of the n places from `first` on (integers),
+//     -, -, kDone, -          of own tokens without a prefix in one part: y is there.
 // The last of the four, of own tokens, has its sign set where there is no prefix.
 enum { kDone = 0, kWhole = 1, kPieces = 2 };
 template <int D>
@@ -236,15 +279,13 @@ __device__ __forceinline__ float *piece_of(float *pieces, int columns, int place
 {
     return pieces + (size_t)place * columns * (D + 4);
 }
-// The places of a unit's pieces: the last one of the workgroup that it begins in, then the first ones of those it goes on in.
-__device__ __forceinline__ int place_of(int wg0, int piece) { return piece == 0 ? 2 * wg0 + 1 : 2 * (wg0 + piece); }
 template <int D>
 __device__ __forceinline__ float *state_of(const SharedArgs &h, int own, size_t row)
 {
     return h.states + ((size_t)own * h.a.n_tokens * h.a.n_heads + row) * (D + 4);
 }
 
-// Workgroup: 4 waves; dealt in equal numbers of rounds and units' costs.  A piece of a unit is what one workgroup has of its rounds.
+// Workgroup: 4 waves; in a round of 128 tokens each has 32.
 template <int D, int QT, int PT, int NC, int UNITS>
 __global__ __launch_bounds__(256, D == 256 || (D == 128 && NC == 2 && QT == 3) ? 1 : 2) void shared_attention_kernel(SharedArgs h)
 {
@@ -258,73 +299,58 @@ __global__ __launch_bounds__(256, D == 256 || (D == 128 && NC == 2 && QT == 3) ?
     const int share = a.n_heads / a.c.n_kv, n_kv = a.c.n_kv;
     const float scale = a.scale != 0.0f ? fabsf(a.scale) * kLog2e : 1.0f;
     const TileOffsets<D> offsets(n, g);
-    const Packs packs(h.group);
+    const Packs packs(h);
     const int looks = packs.looks(a.n_seq);
 
     Sequence own;
-    int upto = 0, all = 0;  // rounds of the look's sequences up to the lane's; of all looks
-    const auto rounds_of = [&](const Sequence &q) {
-        return __builtin_elementwise_add_sat(rounds_in(q.prefix_rounds + kUnitCost, q.prefix_blocks, n_kv), rounds_in(q.rounds + kUnitCost, q.blocks, n_kv));
-    };
+    int all = 0;
     for (int look = 0; look < looks; ++look) {
         own = look_at<kColumns, UNITS>(h, packs, look, lane);
-        upto = wave_scan(rounds_of(own));
-        all = __builtin_elementwise_add_sat(all, __builtin_amdgcn_readlane(upto, 63));
+        const int cost = __builtin_elementwise_add_sat(times(times(own.prefix_rounds + kUnitCost, own.prefix_blocks), n_kv),
+                                                       times(times(own.rounds + kUnitCost, own.blocks), n_kv));
+        all = __builtin_elementwise_add_sat(all, __builtin_amdgcn_readlane(wave_scan(cost), 63));
     }
-    const Shares shares(all);
-    if (blockIdx.x >= shares.n) return;
-    int at = shares.first();
-    const int end = shares.end();
-    int look = 0, look_at_round = 0;  // the look that `own` is of, and the rounds in front of it
-    if (looks > 1) {
-        own = look_at<kColumns, UNITS>(h, packs, 0, lane);
-        upto = wave_scan(rounds_of(own));
-    }
+    const Dealing dealing(all);
+    int upto = 0, places_upto = 0;  // items and places of the look's sequences up to the lane's
+    int look = 0, items_before = 0, places_before = 0;  // the look that `own` is of, and items and places in front of it
+    int parts1 = 1, parts2 = 1, items1 = 0;  // parts of a unit of the prefix and of an own one, items of the former
+    const auto deal = [&]() {
+        parts1 = dealing.parts(own.prefix_rounds), parts2 = dealing.parts(own.rounds);
+        items1 = times(times(own.prefix_blocks, n_kv), parts1);
+        const int items2 = times(times(own.blocks, n_kv), parts2);
+        upto = wave_scan(__builtin_elementwise_add_sat(items1, items2));
+        places_upto = wave_scan((parts1 > 1 ? items1 : 0) + (parts2 > 1 ? items2 : 0));
+    };
+    if (looks > 1) own = look_at<kColumns, UNITS>(h, packs, 0, lane);
+    deal();
     const size_t page_bytes = cache_page_bytes(a.c);
 
-    while (at < end) {
+    for (int item = blockIdx.x;;) {
         const int of_look = __builtin_amdgcn_readlane(upto, 63);
-        if ((unsigned)at >= (unsigned)look_at_round + (unsigned)of_look) {
-            look_at_round += of_look;
-            if (++look >= looks) break;  // (never, but for sums that saturate)
+        if ((unsigned)item >= (unsigned)items_before + (unsigned)of_look) {
+            if (++look >= looks) break;
+            items_before += of_look, places_before += __builtin_amdgcn_readlane(places_upto, 63);
             own = look_at<kColumns, UNITS>(h, packs, look, lane);
-            upto = wave_scan(rounds_of(own));
+            deal();
             continue;
         }
-        const int owner = __ffsll((unsigned long long)__ballot(upto > at - look_at_round)) - 1;
-        const int seq_at = look_at_round + (owner > 0 ? __builtin_amdgcn_readlane(upto, owner - 1) : 0);
-        const int prefix = __builtin_amdgcn_readlane(own.prefix, owner);
-        const int prefix_rounds = __builtin_amdgcn_readlane(own.prefix_rounds, owner), prefix_blocks = __builtin_amdgcn_readlane(own.prefix_blocks, owner);
-        const int of_prefix = rounds_in(prefix_rounds + kUnitCost, prefix_blocks, n_kv);
-        const bool shared = at - seq_at < of_prefix;
-        const int rounds = shared ? prefix_rounds : __builtin_amdgcn_readlane(own.rounds, owner), dealt = rounds + kUnitCost;
-        const int first_at = shared ? seq_at : seq_at + of_prefix;
-        const int unit = (int)((unsigned)(at - first_at) / (unsigned)dealt), block = (int)((unsigned)unit / (unsigned)n_kv), head = unit - block * n_kv;
-        // rounds [begin, stop) of the unit; the cost stands in front of them
-        const int unit_at = first_at + unit * dealt, begin = max(at - unit_at - kUnitCost, 0), stop = min(rounds, end - unit_at - kUnitCost);
-        at = unit_at + min(dealt, end - unit_at);
-        if (stop <= begin) continue;
+        const int owner = __ffsll((unsigned long long)__ballot(upto > item - items_before)) - 1;
+        const int prefix = __builtin_amdgcn_readlane(own.prefix, owner), prefix_rounds = __builtin_amdgcn_readlane(own.prefix_rounds, owner);
+        const int of_prefix = __builtin_amdgcn_readlane(items1, owner);
+        int at = item - items_before - (owner > 0 ? __builtin_amdgcn_readlane(upto, owner - 1) : 0);
+        int place0 = places_before + (owner > 0 ? __builtin_amdgcn_readlane(places_upto, owner - 1) : 0);
+        const bool shared = at < of_prefix;
+        const int rounds = shared ? prefix_rounds : __builtin_amdgcn_readlane(own.rounds, owner);
+        const int parts = __builtin_amdgcn_readlane(shared ? parts1 : parts2, owner);
+        if (!shared) at -= of_prefix, place0 += __builtin_amdgcn_readlane(parts1, owner) > 1 ? of_prefix : 0;
+        const PartOf of = part_of(at, rounds, parts);
+        const int unit = of.unit, part = of.part, begin = of.begin, stop = of.stop;
+        const int block = h.by_kv.of(unit), head = unit - block * n_kv;
+        place0 += unit * parts;  // (of parts that have places)
+        item += gridDim.x;
 
-        // columns: of the pack's sequences one after another, or of this one
-        const int pack0 = __builtin_amdgcn_readlane(own.pack0, owner), pack_n = __builtin_amdgcn_readlane(own.pack_n, owner);
-        const int before = shared ? (pack0 > 0 ? __builtin_amdgcn_readlane(own.fresh_upto, pack0 - 1) : 0) : 0;
-        const int tokens = shared ? __builtin_amdgcn_readlane(own.fresh_upto, pack0 + pack_n - 1) - before : __builtin_amdgcn_readlane(own.fresh, owner);
-        const int n_columns = columns_of(tokens, share), n_live = min(kColumns, n_columns - block * kColumns);
-        int row[NC], pos[NC];
-        int lowest = kMostTokens, highest = -1;  // of the live columns' positions
-#pragma unroll
-        for (int x = 0; x < NC; ++x) {
-            const int col = block * kColumns + 16 * x + n;
-            own.column(shared, owner, before, min(col, n_columns - 1) / share, &row[x], &pos[x]);
-            if (col < n_columns) lowest = min(lowest, pos[x]), highest = max(highest, pos[x]);
-            else pos[x] = -1, row[x] = -1;  // a column that is not there sees nothing
-            if (wave == 0 && g == 0) s_row[16 * x + n] = row[x];
-        }
-#pragma unroll
-        for (int off = 1; off < 16; off <<= 1)
-            lowest = min(lowest, __shfl_xor(lowest, off, kWave)), highest = max(highest, __shfl_xor(highest, off, kWave));
-        lowest = __builtin_amdgcn_readfirstlane(lowest), highest = __builtin_amdgcn_readfirstlane(highest);
         // tokens, and the row of the table that names their pages: for the prefix that of the longest sequence
+        const int pack0 = __builtin_amdgcn_readlane(own.pack0, owner), pack_n = __builtin_amdgcn_readlane(own.pack_n, owner);
         const int context = __builtin_amdgcn_readlane(own.context, owner);
         int source = owner, lo = prefix, hi = max(min(context, a.stride << a.c.log_page), prefix);
         if (shared) {
@@ -333,42 +359,60 @@ __global__ __launch_bounds__(256, D == 256 || (D == 128 && NC == 2 && QT == 3) ?
         }
         const int seq = packs.first(look) + source;
         const scalar_ints table = (scalar_ints)(uintptr_t)(a.table + (size_t)seq * a.stride);
-        const int tiles = (n_live + 15) / 16;
+        const int first = lo + begin * kRound + wave * 32;
+        int t1 = min(hi, lo + stop * kRound);
 
         WideSums<D, QT, PT, NC> sums;
+        const unsigned char *const cache = a.cache + (size_t)(head * (a.c.page >> 4)) * kTile;
+        TileRegs<D> r[2][2];
+        int limit[2][2], page[2];
+        // the pages of a step's tiles; past the last step that of the last token again, of which nothing is loaded
+        const auto look_up = [&](int t0) {
+            if (a.c.page == 16) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u) page[u] = table[min(t0 + 16 * u, t1 - 1) >> 4];
+            } else {  // one page holds both
+                page[0] = page[1] = table[min(t0, t1 - 1) >> a.c.log_page];
+            }
+        };
+        const auto load = [&](TileRegs<D> (&to)[2], int (&lim)[2], int t0) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int t = t0 + 16 * u;
+                lim[u] = (unsigned)page[u] < (unsigned)a.c.n_pages ? t1 : 0;
+                const unsigned char *tile = cache + (size_t)(lim[u] ? (unsigned)page[u] : 0u) * page_bytes + ((t & (a.c.page - 1)) >> 4) * kTile;
+                load_tile<D, false>(to[u], tile, t < lim[u], offsets);
+            }
+        };
+        if (first < t1) look_up(first);  // (asked for ahead of all that the columns need)
+        else page[0] = page[1] = -1;
+
+        // columns: of the pack's sequences one after another, or of this one
+        const int before = shared ? (pack0 > 0 ? __builtin_amdgcn_readlane(own.fresh_upto, pack0 - 1) : 0) : 0;
+        const int tokens = shared ? __builtin_amdgcn_readlane(own.fresh_upto, pack0 + pack_n - 1) - before : __builtin_amdgcn_readlane(own.fresh, owner);
+        const int n_columns = columns_of(tokens, share), n_live = min(kColumns, n_columns - block * kColumns);
+        int row[NC], pos[NC], qh[NC];
+        int lowest = kMostTokens, highest = -1;  // of the live columns' positions
+#pragma unroll
+        for (int x = 0; x < NC; ++x) {
+            const int col = block * kColumns + 16 * x + n, there = min(col, n_columns - 1), token = h.by_share.of(there);
+            qh[x] = head * share + there - token * share;
+            own.column(shared, owner, before, token, lane, &row[x], &pos[x]);
+            if (col < n_columns) lowest = min(lowest, pos[x]), highest = max(highest, pos[x]);
+            else pos[x] = -1, row[x] = -1;  // a column that is not there sees nothing
+            if (wave == 0 && g == 0) s_row[16 * x + n] = row[x] * a.n_heads + qh[x];
+        }
+        lowest = __builtin_amdgcn_readfirstlane(row_min(lowest)), highest = __builtin_amdgcn_readfirstlane(row_max(highest));
+        const int tiles = (n_live + 15) / 16;
+        load(r[0], limit[0], first);
+        t1 = min(t1, highest + 1);  // (behind that nothing is seen)
         {
-            const int t1 = min(min(hi, highest + 1), lo + stop * kRound), first = lo + begin * kRound + wave * 32;
-            const unsigned char *const cache = a.cache + (size_t)(head * (a.c.page >> 4)) * kTile;
-            TileRegs<D> r[2][2];
-            int limit[2][2], page[2];
-            // the pages of a step's tiles; past the last step that of the last token again, of which nothing is loaded
-            auto look_up = [&](int t0) {
-                if (a.c.page == 16) {
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) page[u] = table[min(t0 + 16 * u, t1 - 1) >> 4];
-                } else {  // one page holds both
-                    page[0] = page[1] = table[min(t0, t1 - 1) >> a.c.log_page];
-                }
-            };
-            auto load = [&](TileRegs<D> (&to)[2], int (&lim)[2], int t0) {
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const int t = t0 + 16 * u;
-                    lim[u] = (unsigned)page[u] < (unsigned)a.c.n_pages ? t1 : 0;
-                    const unsigned char *tile = cache + (size_t)(lim[u] ? (unsigned)page[u] : 0u) * page_bytes + ((t & (a.c.page - 1)) >> 4) * kTile;
-                    load_tile<D, false>(to[u], tile, t < lim[u], offsets);
-                }
-            };
-            if (first < t1) look_up(first);
-            else page[0] = page[1] = -1;
-            load(r[0], limit[0], first);
             if (first < t1) look_up(first + kRound);
             const uint32_t sign = a.scale < 0.0f ? (QT == 1 ? 0x80008000u : 0x80000000u) : 0u, keep = a.scale != 0.0f ? ~0u : 0u;
 #pragma unroll
             for (int x = 0; x < NC; ++x) {
-                const int col = block * kColumns + 16 * x + n, qh = head * share + col % share;
                 constexpr int kQ = QT == 1 ? D / 32 : D / 16;
-                const size_t q_at = ((size_t)max(row[x], 0) * a.n_heads + qh) * D + g * (D / 4);
+                const size_t q_at = ((size_t)max(row[x], 0) * a.n_heads + qh[x]) * D + g * (D / 4);
                 const u32x4 *q_from = QT == 1 ? reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(a.q) + q_at)
                                               : reinterpret_cast<const u32x4 *>(static_cast<const float *>(a.q) + q_at);
                 u32x4 q[kQ];
@@ -409,10 +453,7 @@ __global__ __launch_bounds__(256, D == 256 || (D == 128 && NC == 2 && QT == 3) ?
             else all_steps(std::integral_constant<int, NC>());
         }
 
-        const bool whole = begin == 0 && stop == rounds;
-        // pieces: one for each of the workgroups that the unit's first and its last round fall to and those between them
-        const int wg0 = shares.workgroup_of(unit_at + kUnitCost), pieces = shares.workgroup_of(unit_at + dealt - 1) - wg0 + 1;
-        float *const part = piece_of<D>(h.own_pieces, kColumns, 2 * blockIdx.x + (begin == 0));
+        const bool whole = parts == 1;
         // what the four waves left in LDS of 16 columns, each relative to its own maximum: a piece, or all there is of the unit's tokens
         const auto merge = [&](int x, int live, int pass) {
             for (int e = threadIdx.x; e < live * (kPass / 2); e += 256) {
@@ -425,8 +466,8 @@ __global__ __launch_bounds__(256, D == 256 || (D == 128 && NC == 2 && QT == 3) ?
                     const float f = __builtin_amdgcn_exp2f(s_m[i][c] - most);
                     sum += f * s_l[i][c], u += f * s_o[i][c][ch], v += f * s_o[i][c][ch + 1];
                 }
-                const size_t of = (size_t)s_row[16 * x + c] * a.n_heads + head * share + (block * kColumns + 16 * x + c) % share;
-                float *const state = state_of<D>(h, !shared, of), *const to = whole ? state : part + (16 * x + c) * (D + 4);
+                const size_t of = s_row[16 * x + c];
+                float *const state = state_of<D>(h, !shared, of), *const to = whole ? state : piece_of<D>(h.own_pieces, kColumns, place0 + part) + (16 * x + c) * (D + 4);
                 const bool done = whole && !shared && prefix == 0;
                 if (done) {
                     const float by = sum > 0.0f ? 1.0f / sum : 0.0f;
@@ -437,7 +478,7 @@ __global__ __launch_bounds__(256, D == 256 || (D == 128 && NC == 2 && QT == 3) ?
                 if (ch == 0 && pass == 0) {
                     if (!whole) *reinterpret_cast<float2 *>(to + D) = {most, sum};
                     if (whole) *reinterpret_cast<float4 *>(state + D) = {most, sum, __int_as_float(done ? kDone : kWhole), 0.0f};
-                    else if (begin == 0) *reinterpret_cast<int4 *>(state + D) = {wg0, pieces, kPieces, (16 * x + c) | (!shared && prefix == 0 ? (int)0x80000000 : 0)};
+                    else if (part == 0) *reinterpret_cast<int4 *>(state + D) = {place0, parts, kPieces, (16 * x + c) | (!shared && prefix == 0 ? (int)0x80000000 : 0)};
                 }
             }
         };
@@ -468,9 +509,8 @@ __global__ __launch_bounds__(256, D == 256 || (D == 128 && NC == 2 && QT == 3) ?
 }
 
 // The prefix where a pack has many columns: matrix-bound, in blocks of 128 columns (as cache_prompt_kernel).  Workgroup: 4 waves, 32 columns each; 64
-// tokens at a time are converted to bf16 in LDS, a tile of the cache by each wave, while the tokens before them are used.  Dealt in equal numbers of
-// tiles of 64 tokens and units' costs.
-constexpr int kBlockColumns = 128, kBlockCost = 4;
+// tokens at a time are converted to bf16 in LDS, a tile of the cache by each wave, while the tokens before them are used.
+constexpr int kBlockColumns = 128;
 template <int D>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void shared_blocks_kernel(SharedArgs h)
 {
@@ -484,45 +524,46 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void shared_blocks_kernel(Sh
     const float scale = a.scale != 0.0f ? fabsf(a.scale) * kLog2e : 1.0f;
     const TileOffsets<D> offsets(n, g);
     const size_t page_bytes = cache_page_bytes(a.c);
-    const Packs packs(h.group);
+    const Packs packs(h);
     const int looks = packs.looks(a.n_seq);
 
     const auto tiles_of = [&](int prefix) { return (prefix + kPromptTile - 1) / kPromptTile; };
-    const auto units_of = [&](const Sequence &q) { return rounds_in(tiles_of(q.prefix) + kBlockCost, q.prefix_blocks, n_kv); };
-    Shares shares(0);
-    int at = -1, end = 0;
-    // (what the lanes know of the sequences is looked up anew for every piece: it does not fit next to a block's registers, and nor does what
+    const auto look_up = [&](int look, int lane) { return look_at<kBlockColumns, kOfPrefix>(h, packs, look, lane); };
+    Dealing dealing(0);
+    bool dealt = false;
+    // (what the lanes know of the sequences is looked up anew for every item: it does not fit next to a block's registers, and nor does what
     // could be computed of the lane's number ahead of the loop)
-    for (;;) {
+    for (int item = blockIdx.x;; item += gridDim.x) {
         int lane = lane_of_block;
         asm volatile("" : "+v"(lane));
-        int look = 0, look_at_tile = 0;  // the look that `own` is of, and the tiles in front of it
-        Sequence own = look_at<kBlockColumns, kOfPrefix>(h, packs, 0, lane);
-        int upto = wave_scan(units_of(own)), of_look = __builtin_amdgcn_readlane(upto, 63);
-        if (at < 0) {
-            int all = of_look;
-            for (int i = 1; i < looks; ++i)
-                all = __builtin_elementwise_add_sat(
-                    all, __builtin_amdgcn_readlane(wave_scan(units_of(look_at<kBlockColumns, kOfPrefix>(h, packs, i, lane))), 63));
-            shares = Shares(all);
-            if (blockIdx.x >= shares.n) return;
-            at = shares.first(), end = shares.end();
+        int look = 0, items_before = 0, place0 = 0;  // the look that `own` is of, and items and places in front of it
+        Sequence own = look_up(0, lane);
+        if (!dealt) {
+            int all = 0;
+            for (int i = 0; i < looks; ++i) {
+                const Sequence q = i == 0 ? own : look_up(i, lane);
+                all = __builtin_elementwise_add_sat(all, __builtin_amdgcn_readlane(wave_scan(times(times(tiles_of(q.prefix), q.prefix_blocks), n_kv)), 63));
+            }
+            dealing = Dealing(all), dealt = true;
         }
-        if (at >= end) return;
-        while ((unsigned)at >= (unsigned)look_at_tile + (unsigned)of_look) {
-            look_at_tile += of_look;
-            if (++look >= looks) return;  // (never, but for sums that saturate)
-            own = look_at<kBlockColumns, kOfPrefix>(h, packs, look, lane);
-            upto = wave_scan(units_of(own)), of_look = __builtin_amdgcn_readlane(upto, 63);
+        int items, upto, places_upto;
+        const auto deal = [&]() {
+            const int parts = dealing.parts(tiles_of(own.prefix));
+            items = times(times(own.prefix_blocks, n_kv), parts);
+            upto = wave_scan(items), places_upto = wave_scan(parts > 1 ? items : 0);
+        };
+        deal();
+        while ((unsigned)item >= (unsigned)items_before + (unsigned)__builtin_amdgcn_readlane(upto, 63)) {
+            if (++look >= looks) return;
+            items_before += __builtin_amdgcn_readlane(upto, 63), place0 += __builtin_amdgcn_readlane(places_upto, 63);
+            own = look_up(look, lane);
+            deal();
         }
-        const int owner = __ffsll((unsigned long long)__ballot(upto > at - look_at_tile)) - 1;
-        const int seq_at = look_at_tile + (owner > 0 ? __builtin_amdgcn_readlane(upto, owner - 1) : 0);
-        const int prefix = __builtin_amdgcn_readlane(own.prefix, owner);
-        const int tiles = tiles_of(prefix), dealt = tiles + kBlockCost;
-        const int unit = (int)((unsigned)(at - seq_at) / (unsigned)dealt), block = (int)((unsigned)unit / (unsigned)n_kv), head = unit - block * n_kv;
-        const int unit_at = seq_at + unit * dealt, tile0 = max(at - unit_at - kBlockCost, 0), stop = min(tiles, end - unit_at - kBlockCost);
-        at = unit_at + min(dealt, end - unit_at);
-        if (stop <= tile0) continue;
+        const int owner = __ffsll((unsigned long long)__ballot(upto > item - items_before)) - 1;
+        const int prefix = __builtin_amdgcn_readlane(own.prefix, owner), tiles = tiles_of(prefix), parts = dealing.parts(tiles);
+        const PartOf of = part_of(item - items_before - (owner > 0 ? __builtin_amdgcn_readlane(upto, owner - 1) : 0), tiles, parts);
+        const int part = of.part, tile0 = of.begin, stop = of.stop, block = h.by_kv.of(of.unit), head = of.unit - block * n_kv;
+        place0 += (owner > 0 ? __builtin_amdgcn_readlane(places_upto, owner - 1) : 0) + of.unit * parts;
 
         const int pack0 = __builtin_amdgcn_readlane(own.pack0, owner), pack_n = __builtin_amdgcn_readlane(own.pack_n, owner);
         const int before = pack0 > 0 ? __builtin_amdgcn_readlane(own.fresh_upto, pack0 - 1) : 0;
@@ -533,7 +574,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void shared_blocks_kernel(Sh
         const int col = block * kBlockColumns + wave * kCols + lc;
         const bool live = col < n_columns;
         int row, pos;
-        own.column(true, owner, before, min(col, n_columns - 1) / share, &row, &pos);
+        const int there = min(col, n_columns - 1), token = h.by_share.of(there);
+        own.column(true, owner, before, token, lane, &row, &pos);
         if (!live) pos = -1;  // a column that is not there sees nothing
         // positions of the wave's columns (of columns that are not there: none)
         int lowest = live ? pos : kMostTokens, highest = pos;
@@ -541,7 +583,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void shared_blocks_kernel(Sh
         for (int off = 1; off < 32; off <<= 1)
             lowest = min(lowest, __shfl_xor(lowest, off, kWave)), highest = max(highest, __shfl_xor(highest, off, kWave));
         lowest = __builtin_amdgcn_readfirstlane(lowest), highest = __builtin_amdgcn_readfirstlane(highest);
-        const int y_row = row * a.n_heads + head * share + min(col, n_columns - 1) % share;
+        const int y_row = row * a.n_heads + head * share + there - token * share;
         bf16x8 q[D / 16];
         const uint32_t sign = a.scale < 0.0f ? 0x80008000u : 0u, keep = a.scale != 0.0f ? ~0u : 0u;
         const u32x4 *from = reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(a.q) + (size_t)y_row * D);
@@ -667,11 +709,10 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void shared_blocks_kernel(Sh
             }
         }
         l += __shfl_xor(l, 32, kWave);
-        const bool whole = tile0 == 0 && stop == tiles;
-        const int wg0 = shares.workgroup_of(unit_at + kBlockCost), pieces = shares.workgroup_of(unit_at + dealt - 1) - wg0 + 1;
+        const bool whole = parts == 1;
         if (live) {
             float *const state = state_of<D>(h, 0, y_row);
-            float *const to = whole ? state : piece_of<D>(h.prefix_pieces, kBlockColumns, 2 * blockIdx.x + (tile0 == 0)) + (wave * kCols + lc) * (D + 4);
+            float *const to = whole ? state : piece_of<D>(h.prefix_pieces, kBlockColumns, place0 + part) + (wave * kCols + lc) * (D + 4);
             // channels r D/16 .. of the lane's eight r: the places c 16 + r of all c
 #pragma unroll
             for (int b = 0; b < 2; ++b)
@@ -687,7 +728,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void shared_blocks_kernel(Sh
                 const float most = by_scale(m, by, scale);
                 if (whole) *reinterpret_cast<float4 *>(state + D) = {most, l, __int_as_float(kWhole), 0.0f};
                 else *reinterpret_cast<float2 *>(to + D) = {most, l};
-                if (!whole && tile0 == 0) *reinterpret_cast<int4 *>(state + D) = {wg0, pieces, kPieces, wave * kCols + lc};
+                if (!whole && part == 0) *reinterpret_cast<int4 *>(state + D) = {place0, parts, kPieces, wave * kCols + lc};
             }
         }
         __syncthreads();  // (the next unit's tiles take these buffers)
@@ -703,14 +744,19 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs h)
     __shared__ f32x4 s_o[kGroups][kLanes];
     __shared__ float s_m[kGroups], s_l[kGroups];
     const AttentionArgs &a = h.a;
-    const int start = a.start[blockIdx.x], next = a.start[blockIdx.x + 1];
-    if (!(start >= 0 && next > start && next <= a.n_tokens)) return;
     const int group = threadIdx.x / kLanes, ch = threadIdx.x % kLanes * 4;
-    const size_t end = (size_t)next * a.n_heads;
-    for (size_t row = (size_t)start * a.n_heads + blockIdx.y; row < end; row += gridDim.y) {
+    const size_t rows = (size_t)a.n_tokens * a.n_heads;
+    for (size_t row = blockIdx.x; row < rows; row += gridDim.x) {
         const float *const of_own = state_of<D>(h, 1, row), *const of_prefix = state_of<D>(h, 0, row);
         const int4 own = *reinterpret_cast<const int4 *>(of_own + D), prefix = *reinterpret_cast<const int4 *>(of_prefix + D);
-        if (own.z == kDone) continue;
+        // is it some sequence's row? (of one that is not, the workspace says nothing)
+        const int token = (int)(row / a.n_heads);
+        bool found = false;
+        for (int i = threadIdx.x; i < a.n_seq; i += 256) {
+            const int start = a.start[i], next = a.start[i + 1];
+            found |= start >= 0 && start <= token && token < next && next <= a.n_tokens;
+        }
+        if (!__syncthreads_or(found) || own.z == kDone) continue;
         // (a sequence with a prefix leaves kWhole or kPieces of its own tokens, and so does one whose own unit several workgroups have)
         const bool shares = own.w >= 0;
         const int n1 = !shares ? 0 : prefix.z == kPieces ? prefix.y : 1, n = n1 + (own.z == kPieces ? own.y : 1);
@@ -727,7 +773,7 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs h)
                     const int4 e = i < n1 ? prefix : own;
                     const float *p = i < n1 ? of_prefix : of_own;
                     if (e.z == kPieces)
-                        p = (i < n1 ? piece_of<D>(h.prefix_pieces, h.prefix_columns, place_of(e.x, i)) : piece_of<D>(h.own_pieces, h.own_columns, place_of(e.x, i - n1))) +
+                        p = (i < n1 ? piece_of<D>(h.prefix_pieces, h.prefix_columns, e.x + i) : piece_of<D>(h.own_pieces, h.own_columns, e.x + i - n1)) +
                             (e.w & 255) * (D + 4);
                     ml[k] = *reinterpret_cast<const float2 *>(p + D);
                     v[k] = *reinterpret_cast<const f32x4 *>(p + ch);
@@ -777,15 +823,24 @@ SharedGrid shared_grid(int n_tokens, int n_seq, int group, int n_heads, int n_kv
     if (in_blocks) {
         const long long units = packs * n_kv * ((of_pack + kBlockColumns - 1) / kBlockColumns);
         g.prefix_wg = (int)std::min<long long>(units * 2 * rounds, d == 256 ? kWorkgroups / 2 : kWorkgroups);
-        g.prefix_pieces = (size_t)g.prefix_wg * 2 * kBlockColumns * (d + 4) * sizeof(float);
+        g.prefix_pieces = (size_t)g.prefix_wg * kBlockColumns * (d + 4) * sizeof(float);
     }
     if (d < 256 && (in_blocks ? of_seq : of_pack) > 16) g.nc = 2;
     const long long columns = 16 * g.nc, units = n_kv * (n_seq * ((of_seq + columns - 1) / columns) + (in_blocks ? 0 : packs * ((of_pack + columns - 1) / columns)));
     const long long per_unit = std::min(rounds + kUnitCost, std::max(32ll, (long long)(2.0 * sqrt((double)rounds))));
     g.own_wg = (int)std::min(units * per_unit, units >= 128 && d < 256 ? (long long)kWorkgroups : kWorkgroups / 2ll);
-    g.own_pieces = (size_t)g.own_wg * 2 * columns * (d + 4) * sizeof(float);
+    g.own_pieces = (size_t)g.own_wg * columns * (d + 4) * sizeof(float);
     g.states = 2 * (size_t)n_tokens * n_heads * (d + 4) * sizeof(float);
     return g;
+}
+
+// Whether reading the prefix once can save more than the second launch and its joining cost: with rounds of 128 tokens for 256 compute units at 0.57 us as in
+// cache_attention_kernel, where the prefix is most of the context.
+bool pays(int n_tokens, int n_seq, int group, int n_heads, int n_kv, int max_new, int max_context)
+{
+    const long long columns = std::min<long long>(n_tokens, max_new) * (n_heads / n_kv);
+    const double rounds = (double)((max_context + (long long)kRound - 1) / kRound) * n_seq * n_kv * (double)((columns + 15) / 16);
+    return rounds * (1.0 - 1.0 / group) * 0.57 / 256 > 5.0;
 }
 
 template <int D, int QT, int PT, int NC>
@@ -802,8 +857,7 @@ hipError_t launch_units(const SharedArgs &h, const SharedGrid &g, hipStream_t s)
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const long long rows = (long long)h.a.max_new * h.a.n_heads;  // of a sequence
-    shared_join_kernel<D><<<dim3((unsigned)h.a.n_seq, (unsigned)std::min(rows, 4096ll)), 256, 0, s>>>(h);
+    shared_join_kernel<D><<<(unsigned)std::min((long long)h.a.n_tokens * h.a.n_heads, 1ll << 16), 256, 0, s>>>(h);
     return hipGetLastError();
 }
 template <int D, int QT, int PT>
@@ -824,12 +878,21 @@ hipError_t launch_shared_d(const SharedArgs &h, const SharedGrid &g, hipStream_t
 
 }  // namespace
 
+int cache_attention_shared_kind(int n_tokens, int n_seq, int group, int n_heads, int n_kv, int d, int max_new, int max_context, int all_bf16)
+{
+    if (n_seq == 0 || n_tokens == 0) return 0;
+    // chunks for which the kernel for blocks of 128 columns pays are bound by their products: they gain nothing from a prefix that is read once
+    if (group == 1 || cache_attention_parts(n_tokens, n_seq, n_heads, n_kv, d, max_new, max_context, 0, all_bf16) > 0) return 1;
+    if (!pays(n_tokens, n_seq, group, n_heads, n_kv, max_new, max_context)) return 1;
+    return shared_grid(n_tokens, n_seq, group, n_heads, n_kv, d, max_new, max_context, all_bf16 != 0).prefix_wg > 0 ? 3 : 2;
+}
+
 size_t cache_attention_shared_ws(int n_tokens, int n_seq, int group, int n_heads, int n_kv, int d, int max_new, int max_context)
 {
     if (group == 1) return 0;
     // for either type, and for all smaller sizes: the most workgroups that any of them has, of the widest units
     const SharedGrid g = shared_grid(n_tokens, n_seq, group, n_heads, n_kv, d, max_new, max_context, true);
-    const size_t own = (size_t)kWorkgroups * 2 * 32 * (d + 4) * sizeof(float);
+    const size_t own = (size_t)kWorkgroups * 32 * (d + 4) * sizeof(float);
     return g.prefix_pieces + own + g.states;
 }
 
@@ -837,9 +900,8 @@ hipError_t launch_cache_attention_shared(SharedArgs h, hipStream_t s)
 {
     const AttentionArgs &a = h.a;
     const bool all_bf16 = a.q_bf16 && a.y_bf16;
-    // chunks for which the kernel for blocks of 128 columns pays are bound by their products: they gain nothing from a prefix that is read once
-    const int parts = cache_attention_parts(a.n_tokens, a.n_seq, a.n_heads, a.c.n_kv, a.c.d, a.max_new, a.max_context, 0, all_bf16);
-    if (h.group == 1 || parts > 0) return launch_cache_attention(a, s);
+    if (cache_attention_shared_kind(a.n_tokens, a.n_seq, h.group, a.n_heads, a.c.n_kv, a.c.d, a.max_new, a.max_context, all_bf16) < 2)
+        return launch_cache_attention(a, s);
     const SharedGrid g = shared_grid(a.n_tokens, a.n_seq, h.group, a.n_heads, a.c.n_kv, a.c.d, a.max_new, a.max_context, all_bf16);
     char *const ws = reinterpret_cast<char *>(a.ws);
     h.prefix_pieces = reinterpret_cast<float *>(ws), h.own_pieces = reinterpret_cast<float *>(ws + g.prefix_pieces);

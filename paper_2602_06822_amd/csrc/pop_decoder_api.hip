@@ -203,6 +203,15 @@ int pop_cache_attention_shared_workspace(int n_tokens, int n_seq, int group, int
     return POP_OK;
 }
 
+int pop_cache_attention_shared_kind(pop_dtype_t dtype, pop_dtype_t ydtype, int n_tokens, int n_seq, int group, int n_heads, int n_kv, int d, int max_new,
+                                    int max_context)
+{
+    const int rc = shared_sizes(n_tokens, n_seq, group, n_heads, n_kv, d, max_new, max_context);
+    if (rc != POP_OK) return rc;
+    if (!is_dtype(dtype) || !is_dtype(ydtype)) return POP_EINVAL;
+    return cache_attention_shared_kind(n_tokens, n_seq, group, n_heads, n_kv, d, max_new, max_context, dtype == POP_BF16 && ydtype == POP_BF16);
+}
+
 int pop_cache_attention_shared(const void *q, pop_dtype_t dtype, int n_tokens, const void *cache, int n_kv, int d, int page, int n_pages,
                                const int *block_table, int table_stride, const int *q_start, const int *context_len, int n_seq, int group,
                                const int *prefix_len, int n_heads, int max_new, int max_context, float scale, void *y, pop_dtype_t ydtype,
@@ -226,7 +235,7 @@ int pop_cache_attention_shared(const void *q, pop_dtype_t dtype, int n_tokens, c
     if (workspace_bytes < need) return POP_ESHAPE;
     SharedArgs h = {{q, dtype == POP_BF16, n_tokens, static_cast<const unsigned char *>(cache), c, block_table, table_stride, q_start, context_len, n_seq,
                      n_heads, max_new, max_context, scale, 0, y, ydtype == POP_BF16, static_cast<float *>(workspace), 0},
-                    group, prefix_len, nullptr, nullptr, nullptr, 0, 0};
+                    Divisor(n_heads / n_kv), Divisor(n_kv), Divisor(group), group, prefix_len, nullptr, nullptr, nullptr, 0, 0};
     POP_HIP(launch_cache_attention_shared(h, as_stream(stream)));
     return POP_OK;
 }

@@ -183,6 +183,22 @@ def test_shared_workspace(pop):
     assert pop.pop_cache_attention_shared_workspace(*_with(sizes, n_seq=0)) == 0
 
 
+def test_shared_kinds(pop):
+    sizes = dict(dtype=1, ydtype=1, n=8, n_seq=8, group=8, heads=32, n_kv=32, d=128, max_new=1, max_context=4096)
+
+    def kind(**change):
+        return pop.pop_cache_attention_shared_kind(*_with(sizes, **change))
+
+    assert kind(n=0) == 0 and kind(n_seq=0) == 0
+    assert kind() == 2 and kind(group=1) == 1 and kind(max_context=100) == 1 and kind(max_new=2048, n=8 * 2048) == 1
+    many = dict(n=64, n_seq=64, group=64, n_kv=8)
+    assert kind(**many) == 3 and kind(**many, dtype=0) == 2 and kind(**many, ydtype=0) == 2 and kind(**dict(many, group=8)) == 2
+    for status, change in (("POP_EINVAL", dict(dtype=2)), ("POP_ESHAPE", dict(group=3)), ("POP_ESHAPE", dict(heads=33)), ("POP_EUNSUPPORTED", dict(d=80))):
+        with pytest.raises(pop.PopError) as e:
+            kind(**change)
+        assert e.value.status == getattr(pop, status)
+
+
 def test_oracle_attention_with_first_tokens():
     g = np.random.default_rng(2)
     q, k, v = g.standard_normal((3, 2, 8)), g.standard_normal((20, 1, 8)), g.standard_normal((20, 1, 8))

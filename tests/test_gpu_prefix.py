@@ -277,19 +277,22 @@ class Grouped:
         torch.cuda.synchronize()
 
 
-def attend_shared(pop, c, q, start, dtype, ydtype, heads, scale, prefix=None, max_new=None, max_context=None, table=None, context=None, stream=None):
+LONG = 1 << 22  # a context for which sharing pays, whatever the sequences really have
+
+
+def attend_shared(pop, c, q, start, dtype, ydtype, heads, scale, prefix=None, max_new=None, max_context=LONG, table=None, context=None, stream=None, kinds=(2, 3)):
     table = c.table if table is None else table
     context = c.context if context is None else context
     n, n_seq = q.shape[0], len(context)
     max_new = max(int(np.diff(start).max()), 1) if max_new is None else max_new
-    max_context = max(max(context), 1) if max_context is None else max_context
+    sizes = (n, n_seq, c.group, heads, c.n_kv, c.d, max_new, max_context)
+    if 1 not in kinds and pop.pop_cache_attention_shared_kind(dtype, ydtype, *sizes) == 1:  # (a chunk that is bound by its products, by these sizes)
+        sizes = (n, n_seq, c.group, heads, c.n_kv, c.d, 1, max_context)
+    assert pop.pop_cache_attention_shared_kind(dtype, ydtype, *sizes) in kinds
     y = torch.full(q.shape, 7.0, dtype=DT[ydtype], device="cuda")
-    need = pop.pop_cache_attention_shared_workspace(n, n_seq, c.group, heads, c.n_kv, c.d, max_new, max_context)
-    # a chunk that blocks of 128 columns take reads each row's own pages: nothing of what these tests are for
-    assert pop.pop_cache_attention_kind(dtype, ydtype, n, n_seq, heads, c.n_kv, c.d, max_new, max_context)[0] < 2
-    ws = torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda")
+    ws = torch.full((pop.pop_cache_attention_shared_workspace(*sizes),), 0xFF, dtype=torch.uint8, device="cuda")
     args = (q, dtype, n, c.cache, c.n_kv, c.d, c.page, c.n_pages, i32(table), table.shape[1], i32(start), i32(context), n_seq, c.group,
-            i32(c.prefix if prefix is None else prefix), heads, max_new, max_context, scale, y, ydtype, ws)
+            i32(c.prefix if prefix is None else prefix), heads, *sizes[6:], scale, y, ydtype, ws)
     torch.cuda.synchronize()
     pop.pop_cache_attention_shared(*args, stream=stream)
     if stream is not None:
@@ -325,7 +328,7 @@ def test_shared_chunks(pop, dtype, ydtype, heads, n_kv, d, page):  # noqa: F811
     q = queries(rng, start[-1], heads, d, dtype)
     for scale in (0.07, -0.3, 0.0):
         check(c, attend_shared(pop, c, q, start, dtype, ydtype, heads, scale), q, start, ydtype, scale)
-    for change in (dict(max_new=1, max_context=1), dict(prefix=[399, 280]), dict(prefix=[0, -5]), dict(prefix=[-(1 << 31), 300]), dict(prefix=[400, 257])):
+    for change in (dict(max_new=1, max_context=1, kinds=(1,)), dict(max_new=1), dict(prefix=[399, 280]), dict(prefix=[0, -5]), dict(prefix=[-(1 << 31), 300]), dict(prefix=[400, 257])):
         check(c, attend_shared(pop, c, q, start, dtype, ydtype, heads, 0.07, **change), q, start, ydtype, 0.07)
     short = list(c.context)
     short[5] = 12  # of 33 new tokens
@@ -353,13 +356,33 @@ def test_shared_many_sequences(pop, group, n_groups, heads, n_kv, d, dtype):  # 
 @pytest.mark.parametrize("dtype,ydtype", [(BF16, BF16), (F32, F32)])
 @pytest.mark.parametrize("heads,n_kv,group", [(4, 2, 4), (8, 1, 8), (1, 1, 2)])
 def test_shared_long_prefixes(pop, dtype, ydtype, heads, n_kv, group):  # noqa: F811
-    """Units that many workgroups have."""
+    """Units that many workgroups have; sizes as they are, and longer ones."""
     rng = np.random.default_rng(heads)
     c = Grouped(pop, rng, [(20001, [20002 + 611 * i for i in range(group)])], n_kv, 128, 64)
     q = queries(rng, group, heads, 128, dtype)
-    y = attend_shared(pop, c, q, np.arange(group + 1), dtype, ydtype, heads, 0.08)
-    check(c, y, q, np.arange(group + 1), ydtype, 0.08)
+    for sizes in (dict(max_context=max(c.context), kinds=(1, 2)), {}):
+        y = attend_shared(pop, c, q, np.arange(group + 1), dtype, ydtype, heads, 0.08, **sizes)
+        check(c, y, q, np.arange(group + 1), ydtype, 0.08)
     assert torch.equal(y, attend_shared(pop, c, q, np.arange(group + 1), dtype, ydtype, heads, 0.08))
+
+
+@pytest.mark.parametrize("heads,n_kv,d,page,group,prefix", [(8, 2, 128, 64, 40, 4000), (6, 1, 64, 16, 17, 2999), (5, 1, 256, 32, 14, 1500), (16, 1, 128, 128, 9, 700)])
+def test_shared_prefixes_in_blocks_of_128_columns(pop, heads, n_kv, d, page, group, prefix):  # noqa: F811
+    """Blocks that are full and nearly empty, prefixes that end inside a tile, rows that are shorter and empty; pages that are none."""
+    rng = np.random.default_rng(d)
+    lengths = [prefix + int(rng.integers(1, 300)) for _ in range(group)]
+    lengths[3], lengths[5] = prefix // 2, 0
+    c = Grouped(pop, rng, [(prefix, lengths)], n_kv, d, page)
+    start = starts_of([0 if x == 0 else 1 for x in c.context])
+    q = queries(rng, start[-1], heads, d, BF16)
+    for scale in (d ** -0.5, -0.2):
+        y = attend_shared(pop, c, q, start, BF16, BF16, heads, scale, kinds=(3,))
+        check(c, y, q, start, BF16, scale)
+    assert torch.equal(y, attend_shared(pop, c, q, start, BF16, BF16, heads, scale, kinds=(3,)))
+    table = c.table.copy()
+    table[:, 2:4] = -1  # (of all rows: they share them)
+    there = [np.repeat((t >= 0) & (t < c.n_pages), page) for t in table]
+    check(c, attend_shared(pop, c, q, start, BF16, BF16, heads, 0.1, table=table, kinds=(3,)), q, start, BF16, 0.1, there=there)
 
 
 def test_shared_pages_that_are_none(pop):  # noqa: F811
@@ -393,7 +416,7 @@ def test_shared_starts_that_do_not_ascend(pop, dtype):  # noqa: F811
     q = queries(rng, n, 8, 64, dtype)
     for starts, kept in (([100, 140, 20, 60, 5000, 7000, -3], [0, 2]), ([150, 80, 149, 90, 2 ** 31 - 1, -2 ** 31, 0], [1]), ([-5, -1, 140, 3, 3, 10, 9], [4]),
                          ([0, 10, 20, 30, 40, 50, 60], [0, 1, 2, 3, 4, 5])):
-        h = f64(attend_shared(pop, c, q, starts, dtype, dtype, 8, 0.1, max_new=40, max_context=500))
+        h = f64(attend_shared(pop, c, q, starts, dtype, dtype, 8, 0.1, max_new=40))
         written = np.zeros(n, bool)
         for s in kept:
             a, b = starts[s], starts[s + 1]
@@ -422,7 +445,7 @@ def test_shared_group_of_one_is_plain_attention(pop):  # noqa: F811
     c = Cached(pop, rng, [700, 90], 2, 128, 16)
     c.group = 1
     q = queries(rng, 2, 8, 128, BF16)
-    y = attend_shared(pop, c, q, np.arange(3), BF16, BF16, 8, 0.1, prefix=[600, 50])
+    y = attend_shared(pop, c, q, np.arange(3), BF16, BF16, 8, 0.1, prefix=[600, 50], kinds=(1,))
     assert torch.equal(y, attend(pop, c, q, np.arange(3), BF16, BF16, 8, 0.1, 0, 0))
 
 
@@ -433,12 +456,8 @@ def test_shared_chunks_in_blocks_of_128_columns(pop, dtype):  # noqa: F811
     c = Grouped(pop, rng, [(300, [500, 450])], 2, 64, 16)
     start = starts_of([190, 150])
     q = queries(rng, start[-1], 4, 64, dtype)
-    sizes = dict(max_new=1 << 19, max_context=1 << 19)
     assert pop.pop_cache_attention_kind(BF16, BF16, len(q), 2, 4, 2, 64, 1 << 19, 1 << 19)[0] == 2
-    y = torch.zeros_like(q)
-    ws = torch.full((pop.pop_cache_attention_shared_workspace(len(q), 2, 2, 4, 2, 64, 1 << 19, 1 << 19),), 0xFF, dtype=torch.uint8, device="cuda")
-    pop.pop_cache_attention_shared(q, BF16, len(q), c.cache, 2, 64, 16, c.n_pages, i32(c.table), c.table.shape[1], i32(start), i32(c.context), 2, 2, i32([300]),
-                                   4, 1 << 19, 1 << 19, 0.1, y, BF16, ws)
+    y = attend_shared(pop, c, q, start, BF16, BF16, 4, 0.1, max_new=1 << 19, max_context=1 << 19, kinds=(1,))
     check(c, y, q, start, BF16, 0.1)
 
 
@@ -450,10 +469,10 @@ def test_shared_on_another_stream_and_in_a_replayed_graph(pop, heads, n_kv):  # 
     want = attend_shared(pop, c, q, np.arange(4), BF16, BF16, heads, 0.09)
     assert torch.equal(want, attend_shared(pop, c, q, np.arange(4), BF16, BF16, heads, 0.09, stream=torch.cuda.Stream()))
     y, table, start, context, prefix = torch.zeros_like(q), i32(c.table), i32([0, 1, 2, 3]), i32(c.context), i32([3000])
-    ws = torch.full((pop.pop_cache_attention_shared_workspace(3, 3, 3, heads, n_kv, 128, 1, 3100),), 0xFF, dtype=torch.uint8, device="cuda")
+    ws = torch.full((pop.pop_cache_attention_shared_workspace(3, 3, 3, heads, n_kv, 128, 1, LONG),), 0xFF, dtype=torch.uint8, device="cuda")
 
     def call():
-        pop.pop_cache_attention_shared(q, BF16, 3, c.cache, n_kv, 128, 16, c.n_pages, table, table.shape[1], start, context, 3, 3, prefix, heads, 1, 3100, 0.09,
+        pop.pop_cache_attention_shared(q, BF16, 3, c.cache, n_kv, 128, 16, c.n_pages, table, table.shape[1], start, context, 3, 3, prefix, heads, 1, LONG, 0.09,
                                        y, BF16, ws)
 
     call()
@@ -465,7 +484,7 @@ def test_shared_on_another_stream_and_in_a_replayed_graph(pop, heads, n_kv):  # 
     other = torch.cuda.CUDAGraph()  # of another size, over the same workspace
     y2 = torch.zeros_like(q)
     with torch.cuda.graph(other):
-        pop.pop_cache_attention_shared(q, BF16, 2, c.cache, n_kv, 128, 16, c.n_pages, table, table.shape[1], start, context, 2, 2, prefix, heads, 1, 3100, 0.09,
+        pop.pop_cache_attention_shared(q, BF16, 2, c.cache, n_kv, 128, 16, c.n_pages, table, table.shape[1], start, context, 2, 2, prefix, heads, 1, LONG, 0.09,
                                        y2, BF16, ws)
     for i in range(4):
         context.copy_(i32([3100 - i, 3001 - 7 * i, 3050 + i]))
