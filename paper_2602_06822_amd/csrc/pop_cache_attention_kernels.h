@@ -351,6 +351,31 @@ __device__ __forceinline__ bool nth_longest_block(const AttentionArgs &a, int q,
     return false;
 }
 
+// The q-th of all sequences' blocks of 128 columns, by sequence, the later block first: under a window that most blocks fill, all are about as long.
+__device__ __forceinline__ bool nth_block(const AttentionArgs &a, int q, int share, int lane, int *seq, int *block)
+{
+    const int per_lane = (a.n_seq + 63) / 64;
+    const auto blocks = [&](int s) {
+        Columns c;
+        if (s >= a.n_seq || !sequence_columns(a, a.start[s], a.start[s + 1], a.context[s], share, &c)) return 0;
+        return (c.n + 127) / 128;
+    };
+    int n = 0;
+    for (int i = 0; i < per_lane; ++i) n = __builtin_elementwise_add_sat(n, blocks(lane * per_lane + i));
+    const int upto = wave_scan(n), owner = __ffsll((unsigned long long)__ballot(upto > q)) - 1;
+    if (owner < 0) return false;
+    int rest = q - __builtin_amdgcn_readlane(upto - n, owner), s = owner * per_lane;
+    for (; s < a.n_seq; ++s) {
+        const int of = blocks(s);
+        if (rest < of) {
+            *seq = __builtin_amdgcn_readfirstlane(s), *block = __builtin_amdgcn_readfirstlane(of - 1 - rest);
+            return true;
+        }
+        rest -= of;
+    }
+    return false;
+}
+
 // Matrix-bound.  Workgroup: 4 waves, 32 columns each, of one kv head and sequence; 64 tokens at a time are converted to bf16 in LDS, a
 // tile of the cache by each wave, while the tokens before them are used.  A step is 32 tokens: S^T = K q^T (32 tokens x 32 columns),
 // softmax, O^T += V^T P^T; S^T of a step is asked for before the softmax of the one before, so that the matrix pipe has work
@@ -385,7 +410,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_prompt_kernel(Att
 
     for (int rank = blockIdx.x / n_kv;; rank += units, announced = false) {
         int seq, block;
-        if (!nth_longest_block(a, rank, share, lane, &seq, &block)) break;
+        if (!(SINKS ? nth_block(a, rank, share, lane, &seq, &block) : nth_longest_block(a, rank, share, lane, &seq, &block))) break;
         Columns cols;
         const int row0 = a.start[seq];
         sequence_columns(a, row0, a.start[seq + 1], a.context[seq], share, &cols);
