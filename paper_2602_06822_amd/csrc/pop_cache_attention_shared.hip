@@ -237,6 +237,7 @@ __device__ __forceinline__ int times(int a, int b) { return saturated((long long
 // w has items w, w + gridDim.x, ..: most have one.  (What had parts of several units a workgroup, in equal numbers of rounds: 8 sequences x 32 heads, 4000 tokens and 200 of
 // their own, 11.6 us; 64 sequences x 8 heads, 700 of their own, 13.6.)  Parts of units that have several have a place for their results each; there
 // are no more of those than workgroups.
+constexpr float kPartsOfRoot = 4.0f;
 struct Dealing {
     int all;
     float per_round;  // parts
@@ -248,6 +249,7 @@ struct Dealing {
         int n = all == 0x7fffffff ? 0 : (int)((float)rounds * per_round);
         if ((long long)(n + 1) * all <= share) ++n;
         if ((long long)n * all > share) --n;
+        n = min(n, (int)(kPartsOfRoot * __builtin_amdgcn_sqrtf((float)rounds)));
         return min(max(n, 1), max(rounds, 1));
     }
 };
@@ -512,14 +514,17 @@ __global__ __launch_bounds__(256, D == 256 || (D == 128 && NC == 2 && QT == 3) ?
 // tokens at a time are converted to bf16 in LDS, a tile of the cache by each wave, while the tokens before them are used.
 constexpr int kBlockColumns = 128;
 template <int D>
-__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void shared_blocks_kernel(SharedArgs h)
+constexpr int kHalves = D == 256 ? 1 : 2;
+template <int D>
+__global__ __launch_bounds__(256 * kHalves<D>, kHalves<D>) void shared_blocks_kernel(SharedArgs h)
 {
     constexpr int kTile = cache_tile_bytes(D), kCols = 32;
     extern __shared__ __align__(16) unsigned char s_raw[];
-    PromptTiles<D> &s_tiles = *reinterpret_cast<PromptTiles<D> *>(s_raw);
+    constexpr int H = kHalves<D>;
     const AttentionArgs &a = h.a;
-    const int lane_of_block = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane_of_block & 15, g = lane_of_block >> 4;
+    const int lane_of_block = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & 3, half = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), n = lane_of_block & 15, g = lane_of_block >> 4;
     const int lc = lane_of_block & 31, half_of = lane_of_block >> 5, token_row = lc ^ (lc & 4) << 1;  // (token_row: the token of S^T's row lc)
+    PromptTiles<D> &s_tiles = reinterpret_cast<PromptTiles<D> *>(s_raw)[half];
     const int share = a.n_heads / a.c.n_kv, n_kv = a.c.n_kv;
     const float scale = a.scale != 0.0f ? fabsf(a.scale) * kLog2e : 1.0f;
     const TileOffsets<D> offsets(n, g);
@@ -562,7 +567,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void shared_blocks_kernel(Sh
         const int owner = __ffsll((unsigned long long)__ballot(upto > item - items_before)) - 1;
         const int prefix = __builtin_amdgcn_readlane(own.prefix, owner), tiles = tiles_of(prefix), parts = dealing.parts(tiles);
         const PartOf of = part_of(item - items_before - (owner > 0 ? __builtin_amdgcn_readlane(upto, owner - 1) : 0), tiles, parts);
-        const int part = of.part, tile0 = of.begin, stop = of.stop, block = h.by_kv.of(of.unit), head = of.unit - block * n_kv;
+        // (the first half of the waves has the first half of the tiles)
+        const int part = of.part, most = (of.stop - of.begin + H - 1) / H, tile0 = of.begin + half * most, stop = min(tile0 + most, of.stop), block = h.by_kv.of(of.unit), head = of.unit - block * n_kv;
         place0 += (owner > 0 ? __builtin_amdgcn_readlane(places_upto, owner - 1) : 0) + of.unit * parts;
 
         const int pack0 = __builtin_amdgcn_readlane(own.pack0, owner), pack_n = __builtin_amdgcn_readlane(own.pack_n, owner);
@@ -678,12 +684,14 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void shared_blocks_kernel(Sh
                 }
         };
         bf16x8 p[2];
-        load(tile0);
-        convert(tile0);
-        if (tile0 + 1 < stop) load(tile0 + 1);
+        if (tile0 < stop) {
+            load(tile0);
+            convert(tile0);
+            if (tile0 + 1 < stop) load(tile0 + 1);
+        }
         __syncthreads();
         // (a wave whose columns see none of the piece only converts: with that as a branch within the loop registers do not suffice)
-        if (highest < lo) {
+        if (highest < lo || tile0 >= stop) {
             for (int tile = tile0; tile < stop; ++tile) {
                 if (tile + 1 < stop) {
                     convert(tile + 1);
@@ -708,9 +716,37 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void shared_blocks_kernel(Sh
                 values(p, tile, 1);
             }
         }
+        for (int i = max(stop - tile0, 0); i < most; ++i) __syncthreads();  // (a half with a tile less)
         l += __shfl_xor(l, 32, kWave);
+        m = by_scale(m, by, scale);
+        if constexpr (H == 2) {
+            // the halves' sums, joined by the first one
+            __syncthreads();
+            f32x4 *const s_o = reinterpret_cast<f32x4 *>(s_raw) + wave * (D / 8 + 1) * 64 + lc + 32 * half_of;
+            if (half == 1) {
+#pragma unroll
+                for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) s_o[(4 * j + b) * 64] = f32x4{o[j][4 * b], o[j][4 * b + 1], o[j][4 * b + 2], o[j][4 * b + 3]};
+                s_o[D / 8 * 64] = f32x4{m, l, 0.0f, 0.0f};
+            }
+            __syncthreads();
+            if (half == 0) {
+                const f32x4 ml = s_o[D / 8 * 64];
+                const float top = fmaxf(m, ml[0]), f = __builtin_amdgcn_exp2f(m - top), e = __builtin_amdgcn_exp2f(ml[0] - top);
+                m = top, l = f * l + e * ml[1];
+#pragma unroll
+                for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) {
+                        const f32x4 x = s_o[(4 * j + b) * 64];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[j][4 * b + i] = f * o[j][4 * b + i] + e * x[i];
+                    }
+            }
+        }
         const bool whole = parts == 1;
-        if (live) {
+        if (live && half == 0) {
             float *const state = state_of<D>(h, 0, y_row);
             float *const to = whole ? state : piece_of<D>(h.prefix_pieces, kBlockColumns, place0 + part) + (wave * kCols + lc) * (D + 4);
             // channels r D/16 .. of the lane's eight r: the places c 16 + r of all c
@@ -725,9 +761,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void shared_blocks_kernel(Sh
                             f32x4{o[e / 2][4 * b + i], o[e / 2][8 + 4 * b + i], o[e / 2 + 1][4 * b + i], o[e / 2 + 1][8 + 4 * b + i]};
                 }
             if (half_of == 0) {
-                const float most = by_scale(m, by, scale);
-                if (whole) *reinterpret_cast<float4 *>(state + D) = {most, l, __int_as_float(kWhole), 0.0f};
-                else *reinterpret_cast<float2 *>(to + D) = {most, l};
+                if (whole) *reinterpret_cast<float4 *>(state + D) = {m, l, __int_as_float(kWhole), 0.0f};
+                else *reinterpret_cast<float2 *>(to + D) = {m, l};
                 if (!whole && part == 0) *reinterpret_cast<int4 *>(state + D) = {place0, parts, kPieces, wave * kCols + lc};
             }
         }
@@ -822,13 +857,13 @@ SharedGrid shared_grid(int n_tokens, int n_seq, int group, int n_heads, int n_kv
     const bool in_blocks = all_bf16 && of_pack > kMostNarrow;
     if (in_blocks) {
         const long long units = packs * n_kv * ((of_pack + kBlockColumns - 1) / kBlockColumns);
-        g.prefix_wg = (int)std::min<long long>(units * 2 * rounds, d == 256 ? kWorkgroups / 2 : kWorkgroups);
+        g.prefix_wg = (int)std::min<long long>(units * 2 * rounds, kWorkgroups / 2);
         g.prefix_pieces = (size_t)g.prefix_wg * kBlockColumns * (d + 4) * sizeof(float);
     }
     if (d < 256 && (in_blocks ? of_seq : of_pack) > 16) g.nc = 2;
     const long long columns = 16 * g.nc, units = n_kv * (n_seq * ((of_seq + columns - 1) / columns) + (in_blocks ? 0 : packs * ((of_pack + columns - 1) / columns)));
     const long long per_unit = std::min(rounds + kUnitCost, std::max(32ll, (long long)(2.0 * sqrt((double)rounds))));
-    g.own_wg = (int)std::min(units * per_unit, units >= 128 && d < 256 ? (long long)kWorkgroups : kWorkgroups / 2ll);
+    g.own_wg = (int)std::min(units * per_unit, d < 256 ? (long long)kWorkgroups : kWorkgroups / 2ll);
     g.own_pieces = (size_t)g.own_wg * columns * (d + 4) * sizeof(float);
     g.states = 2 * (size_t)n_tokens * n_heads * (d + 4) * sizeof(float);
     return g;
@@ -849,10 +884,10 @@ hipError_t launch_units(const SharedArgs &h, const SharedGrid &g, hipStream_t s)
     if (g.prefix_wg == 0) {
         shared_attention_kernel<D, QT, PT, NC, kBoth><<<(unsigned)g.own_wg, 256, 0, s>>>(h);
     } else if constexpr (QT == 1 && PT == 1) {
-        constexpr int kBytes = (int)sizeof(PromptTiles<D>);
+        constexpr int kBytes = kHalves<D> * (int)sizeof(PromptTiles<D>);
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(shared_blocks_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, kBytes);
         if (e != hipSuccess) return e;
-        shared_blocks_kernel<D><<<(unsigned)g.prefix_wg, 256, kBytes, s>>>(h);
+        shared_blocks_kernel<D><<<(unsigned)g.prefix_wg, 256 * kHalves<D>, kBytes, s>>>(h);
         shared_attention_kernel<D, QT, PT, NC, kOwn><<<(unsigned)g.own_wg, 256, 0, s>>>(h);
     }
     const hipError_t e = hipGetLastError();
