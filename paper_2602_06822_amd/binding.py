@@ -324,6 +324,8 @@ def _rows(t, width, stride, n):
                     stride = max(row, width)
         return t.data_ptr(), stride
     steps, sizes = t.stride(), t.shape
+    if len(steps) == 2 and steps[1] == 1:  # (part of a projection's rows: the usual case)
+        return t.data_ptr(), (steps[0] if sizes[0] > 1 else width) if stride is None else stride
     inner = 1
     for step, size in zip(steps[:0:-1], sizes[:0:-1]):
         if size > 1 and step != inner:
