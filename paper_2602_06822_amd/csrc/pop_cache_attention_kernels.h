@@ -16,7 +16,7 @@ constexpr int kRound = 128;   // tokens of a round: a step of each of the four w
 // sequence's columns see.  All units stand in one row (sequence, block, head), and every workgroup takes the same number of rounds of
 // it, wherever units begin and end: ragged batches and single long sequences of single tokens load all compute units alike.  (Chunks less so: a
 // unit has the rounds of its whole sequence's columns, of which its own block may see few, under a window or where little is cached;
-// rounds behind what a block sees cost nothing, those in front of it, under a window, are gone over masked.)  A piece of a unit
+// rounds behind what a block sees cost nothing, those in front of it, under a window, are gone over masked; with first tokens a unit has its own.)  A piece of a unit
 // is what one workgroup has of it.  Where that gains less than pieces cost, workgroups take units.
 struct SequenceWork {
     int rounds;  // of a unit
@@ -33,7 +33,12 @@ __device__ __forceinline__ SequenceWork sequence_work(const AttentionArgs &a, in
     if (!sequence_columns(a, start, next, context, share, &w.cols)) return w;
     w.blocks = (w.cols.n + 15) / 16;
     w.seen = seen_tokens<SINKS>(w.cols, 0, w.cols.n, a.sinks);
-    w.rounds = max((w.seen.hi - w.seen.begin + kRound - 1) / kRound, 1);
+    int places = w.seen.hi - w.seen.begin;
+    if (SINKS) {  // of no block are there more than this; each goes over its own
+        const int kept = (min(a.sinks, kMostTokens) + 31) & ~31;
+        places = min(places, __builtin_elementwise_add_sat(__builtin_elementwise_add_sat(w.cols.window, kept), 15 / share + 1 + 31));
+    }
+    w.rounds = max((places + kRound - 1) / kRound, 1);
     return w;
 }
 
@@ -140,7 +145,9 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_kernel(
         const int pos = live ? cols.first_pos + token : -1;  // a column that is not there sees nothing
         WaveSums<D, QT, PT> sums;
         {
-            const int t1 = min(seen.hi, w.seen.begin + stop * kRound), first = w.seen.begin + begin * kRound + wave * 32;
+            // (the places that the unit's rounds are of)
+            const SeenTokens &of = SINKS ? seen : w.seen;
+            const int t1 = min(seen.hi, of.begin + stop * kRound), first = of.begin + begin * kRound + wave * 32;
             const unsigned char *const cache = a.cache + (size_t)(head * (a.c.page >> 4)) * kTile;
             TileRegs<D> r[kBuffers][2];
             int limit[kBuffers][2], page[2];
@@ -148,15 +155,15 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_kernel(
             auto look_up = [&](int t0) {
                 if (a.c.page == 16) {
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) page[u] = table[w.seen.template token<SINKS>(min(t0 + 16 * u, t1 - 1)) >> 4];
+                    for (int u = 0; u < 2; ++u) page[u] = table[of.template token<SINKS>(min(t0 + 16 * u, t1 - 1)) >> 4];
                 } else {  // one page holds both
-                    page[0] = page[1] = table[w.seen.template token<SINKS>(min(t0, t1 - 1)) >> a.c.log_page];
+                    page[0] = page[1] = table[of.template token<SINKS>(min(t0, t1 - 1)) >> a.c.log_page];
                 }
             };
             auto load = [&](TileRegs<D> (&to)[2], int (&lim)[2], int t0) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const int t = w.seen.template token<SINKS>(t0 + 16 * u);
+                    const int t = of.template token<SINKS>(t0 + 16 * u);
                     lim[u] = (unsigned)page[u] < (unsigned)a.c.n_pages ? t1 - (t0 + 16 * u - t) : 0;
                     const unsigned char *tile = cache + (size_t)(lim[u] ? (unsigned)page[u] : 0u) * page_bytes + ((t & (a.c.page - 1)) >> 4) * kTile;
                     load_tile<D, PAST>(to[u], tile, t < lim[u], offsets);
@@ -207,12 +214,10 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_attention_kernel(
                     constexpr int kAhead = kBuffers - 1;
                     load(r[(i + kAhead) % kBuffers], limit[(i + kAhead) % kBuffers], t0 + kRound * kAhead);
                     look_up(t0 + kRound * kBuffers);
-                    const int t = w.seen.template token<SINKS>(t0);
+                    const int t = of.template token<SINKS>(t0);
                     const bool all = t + 32 <= min(limit[i][0], limit[i][1]) && t + 31 <= seen.first_pos &&
                                      (seen.last_pos - t < cols.window || (SINKS && t + 32 <= a.sinks));
-                    // (with first tokens, what lies between them and the block's window is passed over)
-                    const bool none = SINKS && seen.first_pos - (t + 31) >= cols.window && t >= a.sinks;
-                    if (t0 < t1 && !none) sums.template step<SINKS>(r[i], limit[i], !all, t, pos, cols.window, a.sinks, g, scale);
+                    if (t0 < t1) sums.template step<SINKS>(r[i], limit[i], !all, t, pos, cols.window, a.sinks, g, scale);
                     t0 += kRound;
                 }
             }
