@@ -480,7 +480,7 @@ int pop_rotary_frequencies(int rotary_dim, double base, int scaling, double fact
  * Angles are products in 64 bits, sines and cosines float32.
  * Errors: NULL or misaligned pointers, bad dtype or layout, an amplitude that is not finite, outputs that are inputs with another stride
  * -> POP_EINVAL; sizes, rotary_dim odd or above head_dim, strides below a row -> POP_ESHAPE; rotary_dim > 1024, (n_heads + n_kv_heads) * head_dim
- * >= 2^30, 2^22 tokens or more -> POP_EUNSUPPORTED. */
+ * >= 2^26, 2^22 tokens or more -> POP_EUNSUPPORTED. */
 int pop_rotary(const void *q, const void *k, pop_dtype_t dtype, int n_tokens, int n_heads, int n_kv_heads, int head_dim, int rotary_dim, int layout,
                long long q_stride, long long k_stride, const int *positions, const double *turns, float amplitude, void *q_out, void *k_out,
                long long q_out_stride, long long k_out_stride, void *stream);

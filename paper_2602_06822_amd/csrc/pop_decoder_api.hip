@@ -389,7 +389,7 @@ int pop_rotary(const void *q, const void *k, pop_dtype_t dtype, int n_tokens, in
 {
     if (n_tokens < 0 || n_heads < 1 || (k && n_kv < 1) || d < 1 || rotary_dim < 2 || rotary_dim % 2 || rotary_dim > d) return POP_ESHAPE;
     const int of_k = k ? n_kv : 0;
-    if (rotary_dim > kMostRotary || ((long long)n_heads + of_k) * d >= 1 << 30 || n_tokens >= kMostTokenRows) return POP_EUNSUPPORTED;
+    if (rotary_dim > kMostRotary || ((long long)n_heads + of_k) * d >= 1 << 26 || n_tokens >= kMostTokenRows) return POP_EUNSUPPORTED;
     if (!is_dtype(dtype) || (layout != POP_ROTARY_HALVES && layout != POP_ROTARY_PAIRS) || !isfinite(amplitude)) return POP_EINVAL;
     if (q_stride < (long long)n_heads * d || q_out_stride < (long long)n_heads * d) return POP_ESHAPE;
     if (k && (k_stride < (long long)n_kv * d || k_out_stride < (long long)n_kv * d)) return POP_ESHAPE;

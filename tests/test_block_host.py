@@ -65,7 +65,7 @@ ROTARY = dict(q=A, k=2 * A, dtype=1, n=4, n_heads=8, n_kv=2, d=64, r=64, layout=
     ("POP_ESHAPE", dict(r=66)), ("POP_ESHAPE", dict(q_stride=511)), ("POP_ESHAPE", dict(k_stride=127)), ("POP_ESHAPE", dict(q_out_stride=0)),
     ("POP_ESHAPE", dict(k_out_stride=-128)),
     ("POP_EUNSUPPORTED", dict(d=2048, r=1026, q_stride=1 << 20, k_stride=1 << 20)), ("POP_EUNSUPPORTED", dict(n=1 << 22)),
-    ("POP_EUNSUPPORTED", dict(n_heads=1 << 24, q_stride=1 << 30)), ("POP_OK", dict(n=0)), ("POP_OK", dict(n=0, k=None, n_kv=0))])
+    ("POP_EUNSUPPORTED", dict(n_heads=1 << 24, q_stride=1 << 30)), ("POP_EUNSUPPORTED", dict(n_heads=(1 << 20) - 2, q_stride=1 << 26)), ("POP_OK", dict(n=0)), ("POP_OK", dict(n=0, k=None, n_kv=0))])
 def test_rotary_refuses(pop, status, change):
     _refused(pop, status, "pop_rotary", _with(ROTARY, **change))
 

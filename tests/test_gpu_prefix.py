@@ -234,6 +234,40 @@ def test_sinks_on_another_stream_and_in_a_replayed_graph(pop):  # noqa: F811
         assert torch.equal(got, y) and bool(y.any())
 
 
+@pytest.mark.parametrize("window,sinks", [(90, 20), (30, 70)])
+@pytest.mark.parametrize("n_seq,heads,n_kv,d", [(65, 4, 1, 64), (150, 8, 2, 64), (129, 16, 4, 128)])
+def test_sinks_many_sequences_in_blocks_of_128_columns(pop, n_seq, heads, n_kv, d, window, sinks):  # noqa: F811
+    """Several sequences to a lane; empty ones, ones without new tokens."""
+    rng = np.random.default_rng(n_seq + window)
+    context = [int(x) for x in rng.integers(0, 300, n_seq)]
+    new = [int(rng.integers(0, c + 1)) if i % 9 else 0 for i, c in enumerate(context)]
+    c = Cached(pop, rng, context, n_kv, d, 16)
+    start = starts_of(new)
+    q = queries(rng, start[-1], heads, d, BF16)
+    assert_in_blocks(pop, c, len(q), heads, window)
+    y = attend(pop, c, q, start, BF16, BF16, heads, 0.1, window, sinks, table=given_back(c, start, window, sinks), **IN_BLOCKS)
+    check(c, y, q, start, BF16, 0.1, window, sinks)
+
+
+@pytest.mark.parametrize("dtype,blocks", [(F32, False), (BF16, False), (BF16, True)])
+def test_sinks_starts_that_do_not_ascend(pop, dtype, blocks):  # noqa: F811
+    """Sequences whose rows are none or leave the tensors are left out; the others' rows, wherever they stand, are right; rows of none stay."""
+    rng = np.random.default_rng(15)
+    c = Cached(pop, rng, [300, 200, 90, 64, 500, 7], 2, 64, 16)
+    n = 150
+    q = queries(rng, n, 8, 64, dtype)
+    for starts, kept in (([100, 140, 20, 60, 5000, 7000, -3], [0, 2]), ([150, 80, 149, 90, 2 ** 31 - 1, -2 ** 31, 0], [1]), ([-5, -1, 140, 3, 3, 10, 9], [4])):
+        h = f64(attend(pop, c, q, starts, dtype, dtype, 8, 0.1, 50, 40, **(IN_BLOCKS if blocks else dict(max_new=40, max_context=500))))
+        written = np.zeros(n, bool)
+        for s in kept:
+            a, b = starts[s], starts[s + 1]
+            written[a:b] = True
+            sizes = []
+            want = orc.attention(f64(q[a:b]), c.k[s], c.v[s], 0.1, c.context[s] - (b - a), 50, None, sizes, 40)
+            assert (np.abs(h[a:b] - want) <= bound_of(want, sizes, 64, c.context[s], dtype) + 1e-30).all(), (starts, s)
+        assert (h[~written] == 7.0).all()
+
+
 # ---------------------------------------------------------------- a prefix that is shared
 
 class Grouped:
@@ -500,3 +534,23 @@ def test_shared_on_another_stream_and_in_a_replayed_graph(pop, heads, n_kv):  # 
         torch.cuda.synchronize()
         # (the third row is said to be longer than what was written: what stands there is no number, and comes out as none, the same every time)
         assert torch.equal(got.view(torch.int16), y.view(torch.int16)) and bool(y.any()) and bool(y2[:2].any())
+
+
+def test_shared_calls_at_once(pop):  # noqa: F811
+    """Calls on two streams, each with a workspace of its own, over one cache."""
+    rng = np.random.default_rng(20)
+    c = Grouped(pop, rng, [(2000, [2100, 2050, 2001, 2300])], 2, 128, 64)
+    cases = []
+    for heads in (4, 64):  # narrow blocks, blocks of 128
+        q = queries(rng, 4, heads, 128, BF16)
+        sizes = (4, 4, 4, heads, 2, 128, 1, LONG)
+        ws = torch.full((pop.pop_cache_attention_shared_workspace(*sizes),), 0xFF, dtype=torch.uint8, device="cuda")
+        cases.append((q, heads, ws, torch.zeros_like(q), torch.cuda.Stream(), attend_shared(pop, c, q, np.arange(5), BF16, BF16, heads, 0.1)))
+    table, start, context, prefix = i32(c.table), i32(np.arange(5)), i32(c.context), i32(c.prefix)
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for q, heads, ws, y, stream, _ in cases:
+            pop.pop_cache_attention_shared(q, BF16, 4, c.cache, 2, 128, 64, c.n_pages, table, table.shape[1], start, context, 4, 4, prefix, heads, 1, LONG, 0.1, y,
+                                           BF16, ws, stream=stream)
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, want) for _, _, _, y, _, want in cases)
