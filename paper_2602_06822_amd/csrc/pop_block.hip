@@ -61,13 +61,14 @@ __device__ __forceinline__ void store_one(void *p, long long at, float x)
 
 // ---------------------------------------------------------------- residual sums and norms
 
-// Sum over the workgroup, the same in every thread.
-__device__ __forceinline__ float workgroup_sum(float v, float *s_sums)
+// Sum over a row's threads, the same in all of them: L lanes, or (0) the workgroup.
+template <int L>
+__device__ __forceinline__ float row_sum(float v, float *s_sums)
 {
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, kWave);
+    for (int off = (L ? L : kWave) / 2; off > 0; off >>= 1) v += __shfl_xor(v, off, kWave);
     const int waves = blockDim.x / kWave;
-    if (waves == 1) return v;
+    if (L || waves == 1) return v;
     if (threadIdx.x % kWave == 0) s_sums[threadIdx.x / kWave] = v;
     __syncthreads();
     v = 0.0f;
@@ -75,9 +76,9 @@ __device__ __forceinline__ float workgroup_sum(float v, float *s_sums)
     return v;
 }
 
-// Eight of a row's channels: those from `at` on (V8), or every blockDim-th one.
+// Eight of a row's channels: those from `at` on (V8), or every `apart`-th one.
 template <bool BF16, bool V8>
-__device__ __forceinline__ void row_load(const void *p, long long row, int at, int d, float (&x)[8])
+__device__ __forceinline__ void row_load(const void *p, long long row, int at, int apart, int d, float (&x)[8])
 {
     if constexpr (V8) {
         Eight<BF16> e;
@@ -87,39 +88,45 @@ __device__ __forceinline__ void row_load(const void *p, long long row, int at, i
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int c = at + i * (int)blockDim.x;
+            const int c = at + i * apart;
             x[i] = c < d ? load_one<BF16>(p, row + c) : 0.0f;
         }
     }
 }
 template <bool BF16, bool V8>
-__device__ __forceinline__ void row_store(void *p, long long row, int at, int d, const float (&x)[8])
+__device__ __forceinline__ void row_store(void *p, long long row, int at, int apart, int d, const float (&x)[8])
 {
     if constexpr (V8) {
         store_eight<BF16>(p, row + at, x);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int c = at + i * (int)blockDim.x;
+            const int c = at + i * apart;
             if (c < d) store_one<BF16>(p, row + c, x[i]);
         }
     }
 }
 
-// A workgroup has a row, a thread N eights of its channels in registers: everything is read once and written once.  The sums of squares
-// are float32: a thread's up to 8 N terms one by one, the rest a tree.
-template <bool XBF16, bool BF16, bool V8, int N>
-__global__ __launch_bounds__(1024) void block_norm_kernel(BlockNormArgs a)
+// A row has a workgroup (L = 0) or L lanes, a thread N eights of its channels in registers: everything is read once and written once.  The sums of
+// squares are float32: a thread's up to 8 N terms one by one, the rest a tree.
+//
+// Bound by memory: 4096 rows of 5120, float32 stream, bf16 block and gate, both norms 59 us (294 MB at 5.0 TB/s, where a copy has 4.8); 2047 rows
+// of 4096 in bf16 12.4 us (67 MB at 5.4).  A step's few rows: 2.8 us on the device, less than the call.  Narrow rows (heads' norms) by lanes, several to a wave:
+// 58205 rows of 160 in bf16 22.7 us, with a wave to each 34.7.
+template <bool XBF16, bool BF16, bool V8, int N, int L>
+__global__ __launch_bounds__(L ? 256 : 1024) void block_norm_kernel(BlockNormArgs a)
 {
     __shared__ float s_sums[2][16];
-    const long long row = blockIdx.x;
-    const int step = V8 ? (int)blockDim.x * 8 : (int)blockDim.x * 8, first = V8 ? (int)threadIdx.x * 8 : (int)threadIdx.x;
+    const int lanes = L ? L : (int)blockDim.x, lane = L ? threadIdx.x % L : threadIdx.x;
+    const long long row = L ? (long long)blockIdx.x * (256 / (L ? L : 1)) + threadIdx.x / (L ? L : 1) : blockIdx.x;
+    if (L && row >= a.n) return;  // (a row's lanes leave together, and nobody waits for them)
+    const int step = lanes * 8, first = V8 ? lane * 8 : lane;
     float v[N][8];
 #pragma unroll
     for (int j = 0; j < N; ++j) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[j][i] = 0.0f;
-        if (a.u && first + j * step < a.d) row_load<BF16, V8>(a.u, row * a.u_stride, first + j * step, a.d, v[j]);
+        if (a.u && first + j * step < a.d) row_load<BF16, V8>(a.u, row * a.u_stride, first + j * step, lanes, a.d, v[j]);
     }
     if (a.post) {
         float sum = 0.0f;
@@ -127,12 +134,12 @@ __global__ __launch_bounds__(1024) void block_norm_kernel(BlockNormArgs a)
         for (int j = 0; j < N; ++j)
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum = fmaf(v[j][i], v[j][i], sum);
-        const float by = 1.0f / sqrtf(workgroup_sum(sum, s_sums[0]) / (float)a.d + a.eps);
+        const float by = 1.0f / sqrtf(row_sum<L>(sum, s_sums[0]) / (float)a.d + a.eps);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             if (first + j * step >= a.d) continue;
             float w[8] = {1, 1, 1, 1, 1, 1, 1, 1};
-            if (a.w_post) row_load<BF16, V8>(a.w_post, 0, first + j * step, a.d, w);
+            if (a.w_post) row_load<BF16, V8>(a.w_post, 0, first + j * step, lanes, a.d, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[j][i] = v[j][i] * by * (a.w_post ? w[i] + a.offset : 1.0f);
         }
@@ -142,10 +149,10 @@ __global__ __launch_bounds__(1024) void block_norm_kernel(BlockNormArgs a)
     for (int j = 0; j < N; ++j) {
         if (first + j * step >= a.d) continue;
         float x[8];
-        row_load<XBF16, V8>(a.x, row * a.x_stride, first + j * step, a.d, x);
+        row_load<XBF16, V8>(a.x, row * a.x_stride, first + j * step, lanes, a.d, x);
         if (a.gate) {
             float g[8];
-            row_load<BF16, V8>(a.gate, row * a.gate_stride, first + j * step, a.d, g);
+            row_load<BF16, V8>(a.gate, row * a.gate_stride, first + j * step, lanes, a.d, g);
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[j][i] *= g[i];
         }
@@ -154,18 +161,18 @@ __global__ __launch_bounds__(1024) void block_norm_kernel(BlockNormArgs a)
             v[j][i] = a.u ? fmaf(a.x_scale, x[i], a.u_scale * v[j][i]) : a.x_scale * x[i];
             sum = fmaf(v[j][i], v[j][i], sum);
         }
-        if (a.x_out) row_store<XBF16, V8>(a.x_out, row * a.x_out_stride, first + j * step, a.d, v[j]);
+        if (a.x_out) row_store<XBF16, V8>(a.x_out, row * a.x_out_stride, first + j * step, lanes, a.d, v[j]);
     }
     if (!a.z) return;
-    const float by = 1.0f / sqrtf(workgroup_sum(sum, s_sums[1]) / (float)a.d + a.eps);
+    const float by = 1.0f / sqrtf(row_sum<L>(sum, s_sums[1]) / (float)a.d + a.eps);
 #pragma unroll
     for (int j = 0; j < N; ++j) {
         if (first + j * step >= a.d) continue;
         float w[8] = {1, 1, 1, 1, 1, 1, 1, 1};
-        if (a.w_pre) row_load<BF16, V8>(a.w_pre, 0, first + j * step, a.d, w);
+        if (a.w_pre) row_load<BF16, V8>(a.w_pre, 0, first + j * step, lanes, a.d, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[j][i] = v[j][i] * by * (a.w_pre ? w[i] + a.offset : 1.0f);
-        row_store<BF16, V8>(a.z, row * a.z_stride, first + j * step, a.d, v[j]);
+        row_store<BF16, V8>(a.z, row * a.z_stride, first + j * step, lanes, a.d, v[j]);
     }
 }
 
@@ -175,13 +182,19 @@ template <bool XBF16, bool BF16, bool V8>
 hipError_t launch_norm(const BlockNormArgs &a, hipStream_t s)
 {
     const int eights = (a.d + 7) / 8;
-    const int n = eights <= 1024 ? 1 : eights <= 2048 ? 2 : eights <= 4096 ? 4 : 8;
-    const unsigned threads = (unsigned)(((eights + n - 1) / n + 63) / 64 * 64);
-    switch (n) {
-        case 1: block_norm_kernel<XBF16, BF16, V8, 1><<<a.n, threads, 0, s>>>(a); break;
-        case 2: block_norm_kernel<XBF16, BF16, V8, 2><<<a.n, threads, 0, s>>>(a); break;
-        case 4: block_norm_kernel<XBF16, BF16, V8, 4><<<a.n, threads, 0, s>>>(a); break;
-        default: block_norm_kernel<XBF16, BF16, V8, 8><<<a.n, threads, 0, s>>>(a); break;
+    const auto rows_in = [&](int lanes) { return (unsigned)((a.n + 256 / lanes - 1) / (256 / lanes)); };
+    if (eights <= 8) block_norm_kernel<XBF16, BF16, V8, 1, 8><<<rows_in(8), 256, 0, s>>>(a);
+    else if (eights <= 16) block_norm_kernel<XBF16, BF16, V8, 1, 16><<<rows_in(16), 256, 0, s>>>(a);
+    else if (eights <= 32) block_norm_kernel<XBF16, BF16, V8, 1, 32><<<rows_in(32), 256, 0, s>>>(a);
+    else {
+        const int n = eights <= 1024 ? 1 : eights <= 2048 ? 2 : eights <= 4096 ? 4 : 8;
+        const unsigned threads = (unsigned)(((eights + n - 1) / n + 63) / 64 * 64);
+        switch (n) {
+            case 1: block_norm_kernel<XBF16, BF16, V8, 1, 0><<<a.n, threads, 0, s>>>(a); break;
+            case 2: block_norm_kernel<XBF16, BF16, V8, 2, 0><<<a.n, threads, 0, s>>>(a); break;
+            case 4: block_norm_kernel<XBF16, BF16, V8, 4, 0><<<a.n, threads, 0, s>>>(a); break;
+            default: block_norm_kernel<XBF16, BF16, V8, 8, 0><<<a.n, threads, 0, s>>>(a); break;
+        }
     }
     return hipGetLastError();
 }

@@ -94,7 +94,7 @@ def test_norm_widths(pop, d, xdtype, dtype):
 
 
 @pytest.mark.parametrize("n", [1, 2, 33, 700, 3001])
-@pytest.mark.parametrize("d", [64, 520, 1003])
+@pytest.mark.parametrize("d", [64, 65, 128, 129, 160, 256, 257, 520, 1003])
 def test_norm_rows(pop, n, d):
     run_norm(pop, n, d, BF16, BF16)
     run_norm(pop, n, d, F32, BF16, post=True, gate="channels")
