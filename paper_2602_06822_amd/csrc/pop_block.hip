@@ -1,5 +1,6 @@
 // What stands between a decoder layer's blocks: residual sums with the norms around a block, rotary positions.
 #include <algorithm>
+#include <type_traits>
 
 #include "pop_block.h"
 
@@ -212,16 +213,25 @@ __device__ __forceinline__ float2 turn_of(int position, double per_token, float 
 }
 
 // A workgroup has a run of tokens (`tokens`) and of each the same part of its heads' eights of channels; sines and cosines stand in LDS, a thread
-// computes some and all heads use them.  Halves: an eight and the one it is turned with together; pairs: an eight by itself; eights behind the
-// turned part are copied.  A thread asks for kTogether of them before it waits, the first ones before the angles are computed.
+// computes some and all heads use them.  kHalves: an eight and the one it is turned with together; kPairs: an eight by itself; kStaged: halves that are
+// no whole eights, where the other channels come out of LDS; eights behind the turned part are copied.  A thread asks for kTogether of them before
+// it waits, the first ones before the angles are computed (kStaged: all of them).
+//
+// Bound by memory: 8191 tokens of 32 + 32 heads of 128 in bf16, out of a projection's rows, 55 us (268 MB at 4.9 TB/s, where a copy has 4.8); channel by
+// channel, as in the kernel below, 80.  4000 tokens of 32 + 8 heads, 46 of 128 channels turned: 25 us staged, channel by channel 41.  A step's eight tokens: 3.5 us
+// on the device, less than the call.
+enum { kHalves = 0, kPairs = 1, kStaged = 2 };
 constexpr int kTogether = 4, kMostTurns = 1024;
-template <bool BF16, bool PAIRS>
+template <bool BF16, int FORM>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, int tokens, int part)
 {
-    __shared__ float2 s_turn[kMostTurns];
-    __shared__ int s_position[kMostTurns];
+    constexpr bool PAIRS = FORM == kPairs;
+    typedef typename std::conditional<BF16, uint16_t, float>::type Stored;
+    __shared__ float2 s_turn[kMostTurns + 4];
+    __shared__ int s_position[64];
+    __shared__ __align__(16) Stored s_eights[FORM == kStaged ? 256 * kTogether * 8 : 8];
     const int token0 = blockIdx.x * tokens, here = min(tokens, a.n - token0), half = a.r / 2;
-    const int turned = PAIRS ? a.r / 8 : a.r / 16, per_head = turned + (a.d - a.r) / 8, per_token = (a.n_heads + a.n_kv) * per_head;
+    const int turned = FORM == kHalves ? a.r / 16 : (a.r + 7) / 8, per_head = FORM == kHalves ? turned + (a.d - a.r) / 8 : a.d / 8, per_token = (a.n_heads + a.n_kv) * per_head;
     const int first = blockIdx.y * part, mine = min(part, per_token - first), total = here * mine;
     struct Place {
         const void *from;
@@ -236,7 +246,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, int tokens, i
         p.chunk = i - head * per_head;
         const bool of_k = head >= a.n_heads;
         const long long row = token0 + p.token, h = of_k ? head - a.n_heads : head;
-        const int ch = p.chunk < turned ? 8 * p.chunk : a.r + 8 * (p.chunk - turned);
+        const int ch = FORM != kHalves || p.chunk < turned ? 8 * p.chunk : a.r + 8 * (p.chunk - turned);
         p.from = of_k ? a.k : a.q, p.to = of_k ? a.k_out : a.q_out;
         p.in = row * (of_k ? a.k_stride : a.q_stride) + h * a.d + ch;
         p.out = row * (of_k ? a.k_out_stride : a.q_out_stride) + h * a.d + ch;
@@ -250,7 +260,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, int tokens, i
             if (e < total) {
                 const Place p = place(e);
                 x[u].load(p.from, p.in);
-                if (!PAIRS && p.chunk < turned) y[u].load(p.from, p.in + half);
+                if (FORM == kHalves && p.chunk < turned) y[u].load(p.from, p.in + half);
             }
         }
     };
@@ -260,6 +270,15 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, int tokens, i
         s_turn[i] = turn_of(a.positions[token0 + token], a.turns[i - token * half], a.amplitude);
     }
     if (threadIdx.x < here) s_position[threadIdx.x] = a.positions[token0 + threadIdx.x];
+    if constexpr (FORM == kStaged) {  // (whole heads, no more than a thread's kTogether: checked by the launcher)
+#pragma unroll
+        for (int u = 0; u < kTogether; ++u) {
+            const int e = threadIdx.x + 256 * u;
+#pragma unroll
+            for (int i = 0; i < (BF16 ? 1 : 2); ++i)
+                if (e < total) reinterpret_cast<u32x4 *>(s_eights)[(BF16 ? 1 : 2) * e + i] = x[u].raw[i];
+        }
+    }
     __syncthreads();
     for (int e0 = threadIdx.x; e0 < total; e0 += 256 * kTogether) {
 #pragma unroll
@@ -278,8 +297,21 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a, int tokens, i
                 float v[8];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    v[2 * i] = x[u][2 * i] * t[i].x - x[u][2 * i + 1] * t[i].y;
-                    v[2 * i + 1] = x[u][2 * i] * t[i].y + x[u][2 * i + 1] * t[i].x;
+                    const bool turns = 8 * p.chunk + 2 * i < a.r;
+                    v[2 * i] = turns ? x[u][2 * i] * t[i].x - x[u][2 * i + 1] * t[i].y : x[u][2 * i];
+                    v[2 * i + 1] = turns ? x[u][2 * i] * t[i].y + x[u][2 * i + 1] * t[i].x : x[u][2 * i + 1];
+                }
+                store_eight<BF16>(p.to, p.out, v);
+            } else if constexpr (FORM == kStaged) {
+                const float2 *const t = s_turn + p.token * half;
+                const Stored *const of_head = s_eights + (e - p.chunk) * 8;
+                float v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int c = 8 * p.chunk + i;
+                    v[i] = x[u][i];
+                    if (c < half) v[i] = v[i] * t[c].x - load_one<BF16>(of_head, c + half) * t[c].y;
+                    else if (c < a.r) v[i] = load_one<BF16>(of_head, c - half) * t[c - half].y + v[i] * t[c - half].x;
                 }
                 store_eight<BF16>(p.to, p.out, v);
             } else {
@@ -332,19 +364,22 @@ __global__ __launch_bounds__(256) void rotary_any_kernel(RotaryArgs a)
 template <bool BF16>
 hipError_t launch_rotary_as(const RotaryArgs &a, hipStream_t s)
 {
-    const bool v8 = a.d % 8 == 0 && a.r % (a.pairs ? 8 : 16) == 0 && (a.q_stride | a.k_stride | a.q_out_stride | a.k_out_stride) % 8 == 0 && aligned16(a.q) &&
-                    aligned16(a.k) && aligned16(a.q_out) && aligned16(a.k_out);
-    if (!v8) {
+    const bool v8 = a.d % 8 == 0 && (a.q_stride | a.k_stride | a.q_out_stride | a.k_out_stride) % 8 == 0 && aligned16(a.q) && aligned16(a.k) &&
+                    aligned16(a.q_out) && aligned16(a.k_out);
+    const int form = a.pairs ? kPairs : a.r % 16 == 0 ? kHalves : kStaged, most = 256 * kTogether;
+    const int per_head = form == kHalves ? a.r / 16 + (a.d - a.r) / 8 : a.d / 8, per_token = (a.n_heads + a.n_kv) * per_head;
+    if (!v8 || (form == kStaged && per_head > most)) {
         rotary_any_kernel<BF16><<<a.n, 256, 0, s>>>(a);
         return hipGetLastError();
     }
-    const int per_token = (a.n_heads + a.n_kv) * (a.r / (a.pairs ? 8 : 16) + (a.d - a.r) / 8);
     // full threads where there is work for all compute units, else as many workgroups as there are eights for
-    const int at_once = 256 * ((long long)a.n * per_token >= 512ll * 256 * kTogether ? kTogether : 1);
-    const int tokens = std::max(1, std::min({at_once / per_token, kMostTurns / (a.r / 2), 64})), part = std::min(per_token, at_once);
+    const int at_once = (long long)a.n * per_token >= 512ll * most || (form == kStaged && per_head > 256) ? most : 256;
+    const int tokens = std::max(1, std::min({at_once / per_token, kMostTurns / (a.r / 2), 64}));
+    const int part = std::min(per_token, form == kStaged ? at_once / per_head * per_head : at_once);
     const dim3 grid((unsigned)((a.n + tokens - 1) / tokens), (unsigned)((per_token + part - 1) / part));
-    if (a.pairs) rotary_kernel<BF16, true><<<grid, 256, 0, s>>>(a, tokens, part);
-    else rotary_kernel<BF16, false><<<grid, 256, 0, s>>>(a, tokens, part);
+    if (form == kPairs) rotary_kernel<BF16, kPairs><<<grid, 256, 0, s>>>(a, tokens, part);
+    else if (form == kHalves) rotary_kernel<BF16, kHalves><<<grid, 256, 0, s>>>(a, tokens, part);
+    else rotary_kernel<BF16, kStaged><<<grid, 256, 0, s>>>(a, tokens, part);
     return hipGetLastError();
 }
 

@@ -201,7 +201,7 @@ def some_positions(rng, n, most):
     return p
 
 
-@pytest.mark.parametrize("d,r", [(64, 64), (80, 40), (80, 80), (128, 128), (128, 46), (128, 64), (96, 2), (3, 2), (256, 256), (33, 32), (1100, 1024)])
+@pytest.mark.parametrize("d,r", [(64, 64), (80, 40), (80, 80), (128, 128), (128, 46), (128, 64), (96, 2), (3, 2), (256, 256), (33, 32), (1100, 1024), (128, 2), (128, 126), (64, 6), (1024, 1000), (2400, 500), (4096, 34), (8200, 20)])
 @pytest.mark.parametrize("pairs", [False, True])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_rotary_shapes(pop, d, r, pairs, dtype):
@@ -224,7 +224,7 @@ def test_rotary_rows_apart_misaligned_and_in_place(pop, pad, at, in_place, pairs
     run_rotary(pop, 19, 5, 2, 64, 48, pairs, dtype, some_positions(np.random.default_rng(3), 19, 1 << 17), pad=pad, at=at, in_place=in_place)
 
 
-@pytest.mark.parametrize("n,heads,n_kv,d,r", [(3000, 32, 8, 128, 128), (1500, 7, 1, 80, 20), (300, 71, 1, 64, 64), (2, 128, 128, 128, 128)])
+@pytest.mark.parametrize("n,heads,n_kv,d,r", [(3000, 32, 8, 128, 128), (1500, 7, 1, 80, 20), (300, 71, 1, 64, 64), (2, 128, 128, 128, 128), (3000, 32, 8, 128, 46), (2000, 8, 8, 256, 250), (700, 2, 1, 2048, 1000)])
 @pytest.mark.parametrize("pairs", [False, True])
 def test_rotary_many_tokens(pop, n, heads, n_kv, d, r, pairs):
     run_rotary(pop, n, heads, n_kv, d, r, pairs, BF16, some_positions(np.random.default_rng(n), n, 1 << 20))
