@@ -376,7 +376,7 @@ int pop_cache_attention_sinks(const void *q, pop_dtype_t dtype, int n_tokens, co
  * the shorter of prefix_len and its context, each row's table names pages that hold the same keys and values there, the same pages or copies, as
  * pop_cache_reorder leaves them.  Tokens of the prefix are read from any of the rows that have new tokens, once for all of them; rows may be
  * shorter than the prefix, and new tokens may stand in it.  prefix_len that is negative or 0 shares nothing.
- * Where that does not pay (pop_cache_attention_shared_kind; prefixes of less than 256 tokens) each row reads its own pages.
+ * Where that does not pay (pop_cache_attention_shared_kind; prefixes of less than 1024 tokens) each row reads its own pages.
  * Rows, types, limits and errors otherwise as pop_cache_attention (of the rounds: < 2^30); group < 1 or n_seq no multiple of it -> POP_ESHAPE.
  * workspace: dev, of pop_cache_attention_shared_workspace bytes for the same group and the same or larger other sizes; any content, for this call
  * alone. */
@@ -389,8 +389,8 @@ int pop_cache_attention_shared(const void *q, pop_dtype_t dtype, int n_tokens, c
 int pop_cache_attention_shared_workspace(int n_tokens, int n_seq, int group, int n_heads, int n_kv_heads, int head_dim,
                                          int max_new, int max_context, size_t *bytes);
 /* Host only.  Which implementation a call of these sizes runs: 0 = none (nothing to do), 1 = that of pop_cache_attention, each row for itself (chunks that
- * are bound by their products, and calls too small to gain by sharing, by max_context), 2 = prefixes by blocks of 16 or 32 columns (new tokens x
- * query heads of a kv head, of up to 64 rows of a group), 3 = by blocks of 128.  Errors: as pop_cache_attention_shared. */
+ * are bound by their products, and calls too small to gain by sharing were all of max_context shared), 2 = prefixes by blocks of 16 or 32 columns (new
+ * tokens x query heads of a kv head, of up to 64 rows of a group), 3 = by blocks of 128.  Errors: as pop_cache_attention_shared. */
 int pop_cache_attention_shared_kind(pop_dtype_t dtype, pop_dtype_t ydtype, int n_tokens, int n_seq, int group, int n_heads, int n_kv_heads,
                                     int head_dim, int max_new, int max_context);
 

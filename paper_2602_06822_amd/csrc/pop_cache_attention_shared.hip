@@ -19,8 +19,10 @@ constexpr int kRound = 128;  // tokens of a round: a step of each of the four wa
 constexpr int kWorkgroups = 512;
 // What a unit costs its workgroup beside its rounds (its columns, q and table, the waves' sums), in rounds.
 constexpr int kUnitCost = 4;
-// A prefix shorter than this is read by each sequence for itself.
-constexpr int kLeastPrefix = 256;
+// A prefix shorter than this is read by each sequence for itself, also in a call that could share longer ones: units of its own and joining cost more. (Microseconds,
+// shared / not: 8 sequences x 32 heads 512 tokens 14.4 / 14.0, 1024 15.5 / 16.2; 16 x 32 over 8 512 tokens 15.1 / 13.2, 1024 15.9 / 14.8; 4 groups of 4 x 32
+// 512 tokens 16.6 / 14.8, 1024 19.0 / 17.4.)
+constexpr int kLeastPrefix = 1024;
 
 // One step of a wave: 32 tokens of one kv head against NC blocks of 16 columns, whose keys and values are converted once.
 template <int D, int QT, int PT, int NC>
@@ -513,14 +515,12 @@ __global__ __launch_bounds__(256, D == 256 || (D == 128 && NC == 2 && QT == 3) ?
 // The prefix where a pack has many columns: matrix-bound, in blocks of 128 columns (as cache_prompt_kernel).  Workgroup: 4 waves, 32 columns each; 64
 // tokens at a time are converted to bf16 in LDS, a tile of the cache by each wave, while the tokens before them are used.
 constexpr int kBlockColumns = 128;
+constexpr int kHalves = 2;
 template <int D>
-constexpr int kHalves = D == 256 ? 1 : 2;
-template <int D>
-__global__ __launch_bounds__(256 * kHalves<D>, kHalves<D>) void shared_blocks_kernel(SharedArgs h)
+__global__ __launch_bounds__(256 * kHalves, kHalves) void shared_blocks_kernel(SharedArgs h)
 {
     constexpr int kTile = cache_tile_bytes(D), kCols = 32;
     extern __shared__ __align__(16) unsigned char s_raw[];
-    constexpr int H = kHalves<D>;
     const AttentionArgs &a = h.a;
     const int lane_of_block = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & 3, half = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), n = lane_of_block & 15, g = lane_of_block >> 4;
     const int lc = lane_of_block & 31, half_of = lane_of_block >> 5, token_row = lc ^ (lc & 4) << 1;  // (token_row: the token of S^T's row lc)
@@ -568,7 +568,7 @@ __global__ __launch_bounds__(256 * kHalves<D>, kHalves<D>) void shared_blocks_ke
         const int prefix = __builtin_amdgcn_readlane(own.prefix, owner), tiles = tiles_of(prefix), parts = dealing.parts(tiles);
         const PartOf of = part_of(item - items_before - (owner > 0 ? __builtin_amdgcn_readlane(upto, owner - 1) : 0), tiles, parts);
         // (the first half of the waves has the first half of the tiles)
-        const int part = of.part, most = (of.stop - of.begin + H - 1) / H, tile0 = of.begin + half * most, stop = min(tile0 + most, of.stop), block = h.by_kv.of(of.unit), head = of.unit - block * n_kv;
+        const int part = of.part, most = (of.stop - of.begin + kHalves - 1) / kHalves, tile0 = of.begin + half * most, stop = min(tile0 + most, of.stop), block = h.by_kv.of(of.unit), head = of.unit - block * n_kv;
         place0 += (owner > 0 ? __builtin_amdgcn_readlane(places_upto, owner - 1) : 0) + of.unit * parts;
 
         const int pack0 = __builtin_amdgcn_readlane(own.pack0, owner), pack_n = __builtin_amdgcn_readlane(own.pack_n, owner);
@@ -719,7 +719,7 @@ __global__ __launch_bounds__(256 * kHalves<D>, kHalves<D>) void shared_blocks_ke
         for (int i = max(stop - tile0, 0); i < most; ++i) __syncthreads();  // (a half with a tile less)
         l += __shfl_xor(l, 32, kWave);
         m = by_scale(m, by, scale);
-        if constexpr (H == 2) {
+        {
             // the halves' sums, joined by the first one
             __syncthreads();
             f32x4 *const s_o = reinterpret_cast<f32x4 *>(s_raw) + wave * (D / 8 + 1) * 64 + lc + 32 * half_of;
@@ -840,21 +840,29 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs h)
     }
 }
 
-// How a call is launched.  Columns of a pack (new tokens x query heads to a kv head) in blocks of 128 from kMostNarrow on, where all is bf16; else in one or two blocks
-// of 16 that share a conversion, as many as they fill, as far as registers go.
-constexpr int kMostNarrow = 64;
+// How a call is launched: all units by the first kernel, or prefixes by the one for blocks of 128 columns, where a pack's columns (new tokens x query heads to a kv
+// head) and the prefix are long enough, and own tokens by the first.
 struct SharedGrid {
     int prefix_wg, own_wg;  // workgroups of the kernel for blocks of 128 (0: the other one has all units), and of the other one
     int nc;
     size_t prefix_pieces, own_pieces, states;  // bytes
     size_t bytes() const { return prefix_pieces + own_pieces + states; }
 };
+// Microseconds that a round of 128 tokens takes all compute units together, for 16 columns: measured for D = 128, the others in proportion.
+double round_cost(int d, bool all_bf16) { return (d == 64 ? 0.0015 : d == 128 ? 0.0022 : 0.0054) * (all_bf16 ? 1.0 : 1.45); }
+
 SharedGrid shared_grid(int n_tokens, int n_seq, int group, int n_heads, int n_kv, int d, int max_new, int max_context, bool all_bf16)
 {
     const long long share = n_heads / n_kv, rounds = (max_context + (long long)kRound - 1) / kRound, packs = (long long)n_seq / group * ((group + 63) / 64);
     const long long of_pack = std::min<long long>(n_tokens, (long long)std::min(group, 64) * max_new) * share, of_seq = std::min(n_tokens, max_new) * share;
     SharedGrid g = {0, 0, 1, 0, 0, 0};
-    const bool in_blocks = all_bf16 && of_pack > kMostNarrow;
+    // Blocks of 128 columns take a round in 0.0069 us, blocks of 32 in 0.0027 each, but a third launch and larger results cost 11 (D = 64: 0.0035, 0.0022, 8).
+    // Microseconds, blocks of 32 / of 128.  D 128, 32 heads over 8, prefixes of 8000 tokens: 64 columns 21.4 / 29.5, 128 26.3 / 35.6, 256 33.3 / 40.5; of 32000: 64
+    // columns 29.6 / 39.8; of 32768: 256 columns 75.0 / 69.6; 20000 tokens, 32 heads over 2, 1024 columns 96.5 / 78.5.  D 64, 256 columns over 8 kv heads, 16000 tokens 42.9 / 37.5.
+    // D 256, 80 columns over 4 kv heads, 8000 tokens 22.0 / 42.6: never.
+    const double narrow = d == 64 ? 0.0022 : 0.0027, wide = d == 64 ? 0.0035 : 0.0069, launch = d == 64 ? 8.0 : 11.0;
+    const double saved = (double)(packs * n_kv) * (double)rounds * (narrow * (double)((of_pack + 31) / 32) - wide * (double)((of_pack + 127) / 128));
+    const bool in_blocks = all_bf16 && d < 256 && saved > launch;
     if (in_blocks) {
         const long long units = packs * n_kv * ((of_pack + kBlockColumns - 1) / kBlockColumns);
         g.prefix_wg = (int)std::min<long long>(units * 2 * rounds, kWorkgroups / 2);
@@ -869,13 +877,18 @@ SharedGrid shared_grid(int n_tokens, int n_seq, int group, int n_heads, int n_kv
     return g;
 }
 
-// Whether reading the prefix once can save more than the second launch and its joining cost: with rounds of 128 tokens for 256 compute units at 0.57 us as in
-// cache_attention_kernel, where the prefix is most of the context.
-bool pays(int n_tokens, int n_seq, int group, int n_heads, int n_kv, int max_new, int max_context)
+// Whether reading the prefix once can pay, were it all of the context.  Each row for itself takes a round's cost for every 16 columns of a sequence and 5.4 us (10
+// where units are fewer than compute units, whose parts have to be joined); shared, as many rounds as a pack has blocks of columns, and 12.4 us in two launches (14.5
+// with 32 columns to a block, or float32; 19.5 with both).  (Microseconds, each for itself / shared, D 128, own tokens up to 200.  8 sequences x 32 heads, prefix 1000 10.9 / 12.9, 2000 15.6 / 13.5,
+// 4000 24.3 / 14.2; 2 x 32, 4000 15.3 / 14.4, 8000 20.1 / 16.0; 4 x 32, 1000 10.6 / 12.4, 2000 15.6 / 12.9; 8 x 32 over 8, 4000 15.8 / 16.1, 8000 20.0 / 17.4;
+// float32, 8 x 32, 1000 14.2 / 15.1, 2000 20.9 / 15.0, 8 x 16 over 4, 8000 19.1 / 21.3; D 256, 8 x 8, 4000 24.5 / 16.1.)
+bool pays(int n_tokens, int n_seq, int group, int n_heads, int n_kv, int d, int max_new, int max_context, bool all_bf16)
 {
-    const long long columns = std::min<long long>(n_tokens, max_new) * (n_heads / n_kv);
-    const double rounds = (double)((max_context + (long long)kRound - 1) / kRound) * n_seq * n_kv * (double)((columns + 15) / 16);
-    return rounds * (1.0 - 1.0 / group) * 0.57 / 256 > 5.0;
+    const long long share = n_heads / n_kv, of_seq = std::min<long long>(n_tokens, max_new) * share;
+    const long long of_pack = std::min<long long>(n_tokens, (long long)std::min(group, 64) * max_new) * share, packs = (long long)n_seq / group * ((group + 63) / 64);
+    const double cost = round_cost(d, all_bf16) * (double)((max_context + (long long)kRound - 1) / kRound);
+    const double units = (double)n_seq * n_kv * (double)((of_seq + 15) / 16), of_prefix = (double)packs * n_kv * (of_pack > 16 && d < 256 ? 1.23 * (double)((of_pack + 31) / 32) : (double)((of_pack + 15) / 16));
+    return cost * units + (units >= 256 ? 5.4 : 10.0) > cost * of_prefix + (of_pack > 16 && !all_bf16 ? 19.5 : of_pack > 16 || !all_bf16 ? 14.5 : 12.4);
 }
 
 template <int D, int QT, int PT, int NC>
@@ -883,11 +896,11 @@ hipError_t launch_units(const SharedArgs &h, const SharedGrid &g, hipStream_t s)
 {
     if (g.prefix_wg == 0) {
         shared_attention_kernel<D, QT, PT, NC, kBoth><<<(unsigned)g.own_wg, 256, 0, s>>>(h);
-    } else if constexpr (QT == 1 && PT == 1) {
-        constexpr int kBytes = kHalves<D> * (int)sizeof(PromptTiles<D>);
+    } else if constexpr (QT == 1 && PT == 1 && D < 256) {
+        constexpr int kBytes = kHalves * (int)sizeof(PromptTiles<D>);
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(shared_blocks_kernel<D>), hipFuncAttributeMaxDynamicSharedMemorySize, kBytes);
         if (e != hipSuccess) return e;
-        shared_blocks_kernel<D><<<(unsigned)g.prefix_wg, 256 * kHalves<D>, kBytes, s>>>(h);
+        shared_blocks_kernel<D><<<(unsigned)g.prefix_wg, 256 * kHalves, kBytes, s>>>(h);
         shared_attention_kernel<D, QT, PT, NC, kOwn><<<(unsigned)g.own_wg, 256, 0, s>>>(h);
     }
     const hipError_t e = hipGetLastError();
@@ -918,17 +931,19 @@ int cache_attention_shared_kind(int n_tokens, int n_seq, int group, int n_heads,
     if (n_seq == 0 || n_tokens == 0) return 0;
     // chunks for which the kernel for blocks of 128 columns pays are bound by their products: they gain nothing from a prefix that is read once
     if (group == 1 || cache_attention_parts(n_tokens, n_seq, n_heads, n_kv, d, max_new, max_context, 0, all_bf16) > 0) return 1;
-    if (!pays(n_tokens, n_seq, group, n_heads, n_kv, max_new, max_context)) return 1;
+    if (!pays(n_tokens, n_seq, group, n_heads, n_kv, d, max_new, max_context, all_bf16 != 0)) return 1;
     return shared_grid(n_tokens, n_seq, group, n_heads, n_kv, d, max_new, max_context, all_bf16 != 0).prefix_wg > 0 ? 3 : 2;
 }
 
 size_t cache_attention_shared_ws(int n_tokens, int n_seq, int group, int n_heads, int n_kv, int d, int max_new, int max_context)
 {
     if (group == 1) return 0;
-    // for either type, and for all smaller sizes: the most workgroups that any of them has, of the widest units
+    // for either type, and for all smaller sizes: the most workgroups that any of them has, of the widest units, and blocks of 128 where some of
+    // them may have a pack of more than 64 columns
     const SharedGrid g = shared_grid(n_tokens, n_seq, group, n_heads, n_kv, d, max_new, max_context, true);
-    const size_t own = (size_t)kWorkgroups * 32 * (d + 4) * sizeof(float);
-    return g.prefix_pieces + own + g.states;
+    const long long of_pack = std::min<long long>(n_tokens, (long long)std::min(group, 64) * max_new) * (n_heads / n_kv);
+    const size_t row = (d + 4) * sizeof(float), own = (size_t)kWorkgroups * 32 * row;
+    return own + (d < 256 && of_pack > 64 ? (size_t)kWorkgroups / 2 * kBlockColumns * row : 0) + g.states;
 }
 
 hipError_t launch_cache_attention_shared(SharedArgs h, hipStream_t s)

@@ -177,6 +177,10 @@ def test_shared_workspace(pop):
     need = pop.pop_cache_attention_shared_workspace(*_with(chunks))
     for change in (dict(max_new=1), dict(max_new=3), dict(max_new=39), dict(n=64, max_new=1), dict(n=1999), dict(n_seq=8), dict(max_context=70)):
         assert pop.pop_cache_attention_shared_workspace(*_with(chunks, **change)) <= need
+    wide = dict(sizes, n=160, n_seq=160, group=160, n_kv=32, max_context=200000)  # (a block of 128 columns, and a second one that is nearly empty)
+    need = pop.pop_cache_attention_shared_workspace(*_with(wide))
+    for n in range(1, 160, 7):
+        assert pop.pop_cache_attention_shared_workspace(*_with(wide, n=n)) <= need
     with pytest.raises(pop.PopError) as e:
         pop.pop_cache_attention_shared_workspace(*_with(sizes, group=5))
     assert e.value.status == pop.POP_ESHAPE
@@ -191,8 +195,9 @@ def test_shared_kinds(pop):
 
     assert kind(n=0) == 0 and kind(n_seq=0) == 0
     assert kind() == 2 and kind(group=1) == 1 and kind(max_context=100) == 1 and kind(max_new=2048, n=8 * 2048) == 1
-    many = dict(n=64, n_seq=64, group=64, n_kv=8)
-    assert kind(**many) == 3 and kind(**many, dtype=0) == 2 and kind(**many, ydtype=0) == 2 and kind(**dict(many, group=8)) == 2
+    assert kind(group=2, n_seq=2, n=2, max_context=1000) == 1 and kind(group=2, n_seq=2, n=2, max_context=9000) == 2
+    many = dict(n=64, n_seq=64, group=64, n_kv=8, max_context=40000)
+    assert kind(**many) == 3 and kind(**many, dtype=0) == 2 and kind(**many, ydtype=0) == 2 and kind(**dict(many, group=8)) == 2 and kind(**dict(many, max_context=5000)) == 2
     for status, change in (("POP_EINVAL", dict(dtype=2)), ("POP_ESHAPE", dict(group=3)), ("POP_ESHAPE", dict(heads=33)), ("POP_EUNSUPPORTED", dict(d=80))):
         with pytest.raises(pop.PopError) as e:
             kind(**change)

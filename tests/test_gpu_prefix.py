@@ -270,6 +270,14 @@ def test_sinks_starts_that_do_not_ascend(pop, dtype, blocks):  # noqa: F811
 
 # ---------------------------------------------------------------- a prefix that is shared
 
+LIFT = 1024  # prefixes that are shorter are not shared
+
+
+def lifted(groups):
+    """Groups whose prefixes are all longer by that; rows that are not much shorter than their prefix with them."""
+    return [(p + LIFT, [c + LIFT if c >= p - 50 and c else c for c in lengths]) if p > 0 else (p, lengths) for p, lengths in groups]
+
+
 class Grouped:
     """Groups of sequences whose first tokens are the same: (prefix, [context ..]).  Full pages of the prefix are shared by all rows, the page that it ends in is
     copied; a row that is shorter than the prefix has what it reaches.  The cache's other bytes are all ones (a scale of all ones is no number)."""
@@ -343,7 +351,7 @@ def test_shared_single_tokens(pop, d, dtype, ydtype):  # noqa: F811
             (2, 2, 16, [(700, [701, 730, 900])]), (8, 1, 32, [(257, [300, 257, 258, 1000, 289, 290, 256, 400])]),
             (4, 2, 64, [(300, [333, 0, 350, 301]), (0, [40, 1, 17, 500]), (1000, [1001, 1064, 999, 200])]),
             (5, 1, 16, [(515, [516 + 7 * i for i in range(9)])]), (6, 2, 128, [(290, [300, 310]), (100, [130, 120]), (640, [700, 641])])):
-        c = Grouped(pop, rng, groups, n_kv, d, page)
+        c = Grouped(pop, rng, lifted(groups), n_kv, d, page)
         start = starts_of([0 if x == 0 else 1 for x in c.context])
         q = queries(rng, start[-1], heads, d, dtype)
         y = attend_shared(pop, c, q, start, dtype, ydtype, heads, d ** -0.5)
@@ -357,12 +365,13 @@ def test_shared_chunks(pop, dtype, ydtype, heads, n_kv, d, page):  # noqa: F811
     """Several new tokens to a sequence, some of them in the prefix, rows without any, a context shorter than its new tokens; sizes that the caller
     underestimates, and prefix lengths that say less, more and nothing."""
     rng = np.random.default_rng(d)
-    c = Grouped(pop, rng, [(400, [401, 420, 395, 500, 30]), (300, [330, 299, 0, 310, 700])], n_kv, d, page)
+    c = Grouped(pop, rng, lifted([(400, [401, 420, 395, 500, 30]), (300, [330, 299, 0, 310, 700])]), n_kv, d, page)
     start = starts_of([1, 5, 4, 0, 17, 33, 9, 0, 2, 64])
     q = queries(rng, start[-1], heads, d, dtype)
     for scale in (0.07, -0.3, 0.0):
         check(c, attend_shared(pop, c, q, start, dtype, ydtype, heads, scale), q, start, ydtype, scale)
-    for change in (dict(max_new=1, max_context=1, kinds=(1,)), dict(max_new=1), dict(prefix=[399, 280]), dict(prefix=[0, -5]), dict(prefix=[-(1 << 31), 300]), dict(prefix=[400, 257])):
+    for change in (dict(max_new=1, max_context=1, kinds=(1,)), dict(max_new=1), dict(prefix=[LIFT + 399, LIFT + 280]), dict(prefix=[0, -5]),
+                   dict(prefix=[-(1 << 31), LIFT + 300]), dict(prefix=[LIFT + 400, LIFT + 1]), dict(prefix=[LIFT, LIFT - 1])):
         check(c, attend_shared(pop, c, q, start, dtype, ydtype, heads, 0.07, **change), q, start, ydtype, 0.07)
     short = list(c.context)
     short[5] = 12  # of 33 new tokens
@@ -380,7 +389,7 @@ def test_shared_many_sequences(pop, group, n_groups, heads, n_kv, d, dtype):  # 
     for g in range(n_groups):
         p = int(rng.integers(250, 600))
         groups.append((p, [0 if rng.random() < 0.1 else p + int(rng.integers(-20, 60)) for _ in range(group)]))
-    c = Grouped(pop, rng, groups, n_kv, d, 16)
+    c = Grouped(pop, rng, lifted(groups), n_kv, d, 16)
     start = starts_of([0 if x == 0 else int(rng.integers(1, 3)) for x in c.context])
     q = queries(rng, start[-1], heads, d, dtype)
     y = attend_shared(pop, c, q, start, dtype, dtype, heads, 0.1)
@@ -400,7 +409,7 @@ def test_shared_long_prefixes(pop, dtype, ydtype, heads, n_kv, group):  # noqa: 
     assert torch.equal(y, attend_shared(pop, c, q, np.arange(group + 1), dtype, ydtype, heads, 0.08))
 
 
-@pytest.mark.parametrize("heads,n_kv,d,page,group,prefix", [(8, 2, 128, 64, 40, 4000), (6, 1, 64, 16, 17, 2999), (5, 1, 256, 32, 14, 1500), (16, 1, 128, 128, 9, 700)])
+@pytest.mark.parametrize("heads,n_kv,d,page,group,prefix", [(8, 1, 128, 64, 40, 4000), (6, 1, 64, 16, 17, 2999), (16, 1, 128, 128, 9, 1700)])
 def test_shared_prefixes_in_blocks_of_128_columns(pop, heads, n_kv, d, page, group, prefix):  # noqa: F811
     """Blocks that are full and nearly empty, prefixes that end inside a tile, rows that are shorter and empty; pages that are none."""
     rng = np.random.default_rng(d)
@@ -422,10 +431,10 @@ def test_shared_prefixes_in_blocks_of_128_columns(pop, heads, n_kv, d, page, gro
 def test_shared_pages_that_are_none(pop):  # noqa: F811
     """Pages of the prefix that no row has, pages behind it that one has not, nothing at all: what is not there is not seen."""
     rng = np.random.default_rng(12)
-    c = Grouped(pop, rng, [(512, [540, 530, 600])], 2, 128, 16)
+    c = Grouped(pop, rng, [(1536, [1564, 1554, 1624])], 2, 128, 16)
     start = starts_of([2, 1, 1])
     q = queries(rng, 4, 4, 128, BF16)
-    for blocks, of in (([3, 4, 20], [0, 1, 2]), ([32], [1]), (range(33, 38), [2])):
+    for blocks, of in (([3, 4, 20], [0, 1, 2]), ([96], [1]), (range(97, 102), [2])):
         table = c.table.copy()
         for s in of:
             table[s, list(blocks)] = -1 if s % 2 else c.n_pages
@@ -435,17 +444,17 @@ def test_shared_pages_that_are_none(pop):  # noqa: F811
     y = attend_shared(pop, c, q, start, BF16, BF16, 4, 0.1, table=np.full_like(c.table, -1))
     assert (f64(y) == 0).all()
     # contexts beyond the table
-    c = Grouped(pop, rng, [(320, [320, 320])], 2, 64, 16, spare=0)
+    c = Grouped(pop, rng, [(1344, [1344, 1344])], 2, 64, 16, spare=0)
     q = queries(rng, 2, 4, 64, BF16)
-    y = attend_shared(pop, c, q, np.arange(3), BF16, BF16, 4, 0.1, context=[900, 320], prefix=[1 << 30])
-    check(c, y, q, np.arange(3), BF16, 0.1, context=[900, 320])
+    y = attend_shared(pop, c, q, np.arange(3), BF16, BF16, 4, 0.1, context=[1900, 1344], prefix=[1 << 30])
+    check(c, y, q, np.arange(3), BF16, 0.1, context=[1900, 1344])
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_shared_starts_that_do_not_ascend(pop, dtype):  # noqa: F811
     """Sequences whose rows are none or leave the tensors are left out; the others' rows, wherever they stand, are right; rows of none stay."""
     rng = np.random.default_rng(15)
-    c = Grouped(pop, rng, [(300, [310, 320, 330]), (400, [420, 500, 401])], 2, 64, 16)
+    c = Grouped(pop, rng, lifted([(300, [310, 320, 330]), (400, [420, 500, 401])]), 2, 64, 16)
     n = 150
     q = queries(rng, n, 8, 64, dtype)
     for starts, kept in (([100, 140, 20, 60, 5000, 7000, -3], [0, 2]), ([150, 80, 149, 90, 2 ** 31 - 1, -2 ** 31, 0], [1]), ([-5, -1, 140, 3, 3, 10, 9], [4]),
@@ -465,7 +474,7 @@ def test_shared_starts_that_do_not_ascend(pop, dtype):  # noqa: F811
 def test_shared_scores_far_from_zero(pop, dtype):  # noqa: F811
     """Scores of 2^34 in the prefix or behind it: the part that holds the largest decides, and equal ones share."""
     rng = np.random.default_rng(16)
-    c = Grouped(pop, rng, [(300, [340, 310])], 1, 64, 16)
+    c = Grouped(pop, rng, lifted([(300, [340, 310])]), 1, 64, 16)
     q = queries(rng, 2, 2, 64, dtype)
     for scale in (2.0 ** 28, -(2.0 ** 30), 2.0 ** 34):
         h = f64(attend_shared(pop, c, q, np.arange(3), dtype, dtype, 2, scale))
