@@ -239,6 +239,8 @@ __device__ __forceinline__ int times(int a, int b) { return saturated((long long
 // w has items w, w + gridDim.x, ..: most have one.  (What had parts of several units a workgroup, in equal numbers of rounds: 8 sequences x 32 heads, 4000 tokens and 200 of
 // their own, 11.6 us; 64 sequences x 8 heads, 700 of their own, 13.6.)  Parts of units that have several have a place for their results each; there
 // are no more of those than workgroups.
+// A unit has no more parts than kPartsOfRoot roots of its rounds: each costs its columns' joining about a thirtieth of a microsecond. (3, 5, 8: 2 kv heads x 32 columns
+// over 32768 tokens 19.1, 18.9, 20.4 us, 8 chunks of 5 over 8000 31.4, 31.2, 34.3.)
 constexpr float kPartsOfRoot = 4.0f;
 struct Dealing {
     int all;
@@ -290,6 +292,10 @@ __device__ __forceinline__ float *state_of(const SharedArgs &h, int own, size_t 
 }
 
 // Workgroup: 4 waves; in a round of 128 tokens each has 32.
+//
+// Bound by its chain of latencies: 8 sequences x 32 heads, D 128, a prefix of 4000 tokens and up to 200 of their own, 11.1 us (21 MB, which memory gives in
+// 3.3): the launch 0.5, lengths and dealing 1.7, the item and its columns 1.0, table, codes and q 1.2, up to six rounds 4, the waves' sums 1.1. Codes are asked
+// for ahead of all that the columns need (12.2 behind it); three workgroups to a compute unit instead of two 11.1.
 template <int D, int QT, int PT, int NC, int UNITS>
 __global__ __launch_bounds__(256, D == 256 || (D == 128 && NC == 2 && QT == 3) ? 1 : 2) void shared_attention_kernel(SharedArgs h)
 {
@@ -513,7 +519,12 @@ __global__ __launch_bounds__(256, D == 256 || (D == 128 && NC == 2 && QT == 3) ?
 }
 
 // The prefix where a pack has many columns: matrix-bound, in blocks of 128 columns (as cache_prompt_kernel).  Workgroup: 4 waves, 32 columns each; 64
-// tokens at a time are converted to bf16 in LDS, a tile of the cache by each wave, while the tokens before them are used.
+// tokens at a time are converted to bf16 in LDS, a tile of the cache by each wave, while the tokens before them are used. A
+// workgroup has two such sets of waves, each with half of the part's tiles, and joins their sums in LDS: half as many results in memory as with a workgroup for each
+// (64 sequences of 32768 tokens, 256 columns over 8 kv heads: 76.9 -> 71.4 us in all three launches). Products 0.87 PFLOP/s in the loop (39.5 of its 52 us); the
+// sequences' lengths, columns and first tiles take 6.4 in front of it, the results behind it 5 (17 MB at 4.2 TB/s; halves that write half of the channels each: the same).
+// Registers decide here: a wave that sees nothing of a part has a loop of its own, and what can be computed of the lane's number ahead of the loop is kept from being
+// so (76 registers in scratch memory and 104 us with both as the compiler had them).
 constexpr int kBlockColumns = 128;
 constexpr int kHalves = 2;
 template <int D>
@@ -771,7 +782,8 @@ __global__ __launch_bounds__(256 * kHalves, kHalves) void shared_blocks_kernel(S
 }
 
 // y of the columns whose results stand in the workspace.  Workgroup: one (token, head); a group of D/4 lanes for a row of results, four channels to
-// a lane, rows in the order of the tokens.
+// a lane, rows in the order of the tokens. A launch of its own costs 3 to 4 us (8 x 32 rows; 2048 rows of 17 parts 7.8); the first kernel's workgroups, counting
+// themselves and joining what they are the last of, took 10 us longer (25.4 -> 14.5 in all).
 template <int D>
 __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs h)
 {
