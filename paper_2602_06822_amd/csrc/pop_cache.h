@@ -164,7 +164,7 @@ struct SharedArgs {
     const int *prefix;  // [n_seq / group] tokens that a group's sequences share
     // set by the launcher
     float *prefix_pieces, *own_pieces, *states;
-    int prefix_columns, own_columns;
+    int prefix_columns, own_columns, prefix_places, own_places;
 };
 // 0: nothing to do, 1: each sequence for itself (launch_cache_attention), 2: the prefix by blocks of 16 or 32 columns of a group, 3: by blocks of 128.
 int cache_attention_shared_kind(int n_tokens, int n_seq, int group, int n_heads, int n_kv, int d, int max_new, int max_context, int all_bf16);

@@ -170,8 +170,10 @@ struct Sequence {
                 local = before + token - (lane_value(fresh_upto, max(lo - 1, 0)) & (lo > 0 ? -1 : 0));
             }
         }
-        *row = lane_value(start, of) + local;
-        *pos = lane_value(context, of) - lane_value(fresh, of) + local;
+        // (within the sequence's rows whatever sums that have saturated say)
+        const int rows = lane_value(fresh, of), at = max(min(local, rows - 1), 0);
+        *row = lane_value(start, of) + at;
+        *pos = lane_value(context, of) - rows + at;
     }
     // The lane of the longest of the pack's sequences, whose row of the table the prefix is read from.
     __device__ __forceinline__ int source(int pack0, int pack_n, int lane) const
@@ -335,19 +337,19 @@ __global__ __launch_bounds__(256, D == 256 || (D == 128 && NC == 2 && QT == 3) ?
     deal();
     const size_t page_bytes = cache_page_bytes(a.c);
 
-    for (int item = blockIdx.x;;) {
+    for (unsigned item = blockIdx.x;;) {
         const int of_look = __builtin_amdgcn_readlane(upto, 63);
-        if ((unsigned)item >= (unsigned)items_before + (unsigned)of_look) {
+        if (item >= (unsigned)items_before + (unsigned)of_look) {
             if (++look >= looks) break;
             items_before += of_look, places_before += __builtin_amdgcn_readlane(places_upto, 63);
             own = look_at<kColumns, UNITS>(h, packs, look, lane);
             deal();
             continue;
         }
-        const int owner = __ffsll((unsigned long long)__ballot(upto > item - items_before)) - 1;
+        const int of_item = (int)(item - (unsigned)items_before), owner = __ffsll((unsigned long long)__ballot(upto > of_item)) - 1;
         const int prefix = __builtin_amdgcn_readlane(own.prefix, owner), prefix_rounds = __builtin_amdgcn_readlane(own.prefix_rounds, owner);
         const int of_prefix = __builtin_amdgcn_readlane(items1, owner);
-        int at = item - items_before - (owner > 0 ? __builtin_amdgcn_readlane(upto, owner - 1) : 0);
+        int at = of_item - (owner > 0 ? __builtin_amdgcn_readlane(upto, owner - 1) : 0);
         int place0 = places_before + (owner > 0 ? __builtin_amdgcn_readlane(places_upto, owner - 1) : 0);
         const bool shared = at < of_prefix;
         const int rounds = shared ? prefix_rounds : __builtin_amdgcn_readlane(own.rounds, owner);
@@ -549,7 +551,7 @@ __global__ __launch_bounds__(256 * kHalves, kHalves) void shared_blocks_kernel(S
     bool dealt = false;
     // (what the lanes know of the sequences is looked up anew for every item: it does not fit next to a block's registers, and nor does what
     // could be computed of the lane's number ahead of the loop)
-    for (int item = blockIdx.x;; item += gridDim.x) {
+    for (unsigned item = blockIdx.x;; item += gridDim.x) {
         int lane = lane_of_block;
         asm volatile("" : "+v"(lane));
         int look = 0, items_before = 0, place0 = 0;  // the look that `own` is of, and items and places in front of it
@@ -569,15 +571,15 @@ __global__ __launch_bounds__(256 * kHalves, kHalves) void shared_blocks_kernel(S
             upto = wave_scan(items), places_upto = wave_scan(parts > 1 ? items : 0);
         };
         deal();
-        while ((unsigned)item >= (unsigned)items_before + (unsigned)__builtin_amdgcn_readlane(upto, 63)) {
+        while (item >= (unsigned)items_before + (unsigned)__builtin_amdgcn_readlane(upto, 63)) {
             if (++look >= looks) return;
             items_before += __builtin_amdgcn_readlane(upto, 63), place0 += __builtin_amdgcn_readlane(places_upto, 63);
             own = look_up(look, lane);
             deal();
         }
-        const int owner = __ffsll((unsigned long long)__ballot(upto > item - items_before)) - 1;
+        const int of_item = (int)(item - (unsigned)items_before), owner = __ffsll((unsigned long long)__ballot(upto > of_item)) - 1;
         const int prefix = __builtin_amdgcn_readlane(own.prefix, owner), tiles = tiles_of(prefix), parts = dealing.parts(tiles);
-        const PartOf of = part_of(item - items_before - (owner > 0 ? __builtin_amdgcn_readlane(upto, owner - 1) : 0), tiles, parts);
+        const PartOf of = part_of(of_item - (owner > 0 ? __builtin_amdgcn_readlane(upto, owner - 1) : 0), tiles, parts);
         // (the first half of the waves has the first half of the tiles)
         const int part = of.part, most = (of.stop - of.begin + kHalves - 1) / kHalves, tile0 = of.begin + half * most, stop = min(tile0 + most, of.stop), block = h.by_kv.of(of.unit), head = of.unit - block * n_kv;
         place0 += (owner > 0 ? __builtin_amdgcn_readlane(places_upto, owner - 1) : 0) + of.unit * parts;
@@ -795,7 +797,7 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs h)
     const size_t rows = (size_t)a.n_tokens * a.n_heads;
     for (size_t row = blockIdx.x; row < rows; row += gridDim.x) {
         const float *const of_own = state_of<D>(h, 1, row), *const of_prefix = state_of<D>(h, 0, row);
-        const int4 own = *reinterpret_cast<const int4 *>(of_own + D), prefix = *reinterpret_cast<const int4 *>(of_prefix + D);
+        int4 own = *reinterpret_cast<const int4 *>(of_own + D), prefix = *reinterpret_cast<const int4 *>(of_prefix + D);
         // is it some sequence's row? (of one that is not, the workspace says nothing)
         const int token = (int)(row / a.n_heads);
         bool found = false;
@@ -804,6 +806,11 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs h)
             found |= start >= 0 && start <= token && token < next && next <= a.n_tokens;
         }
         if (!__syncthreads_or(found) || own.z == kDone) continue;
+        // (sequences whose rows overlap may have left out some: what stands there then names no places beyond those that there are)
+        const auto within = [](int4 &e, int places, int columns) {
+            if (e.z == kPieces && ((unsigned)e.x > (unsigned)places || (unsigned)e.y > (unsigned)(places - e.x) || (e.w & 255) >= columns)) e.y = 0;
+        };
+        within(own, h.own_places, h.own_columns), within(prefix, h.prefix_places, h.prefix_columns);
         // (a sequence with a prefix leaves kWhole or kPieces of its own tokens, and so does one whose own unit several workgroups have)
         const bool shares = own.w >= 0;
         const int n1 = !shares ? 0 : prefix.z == kPieces ? prefix.y : 1, n = n1 + (own.z == kPieces ? own.y : 1);
@@ -969,6 +976,7 @@ hipError_t launch_cache_attention_shared(SharedArgs h, hipStream_t s)
     h.prefix_pieces = reinterpret_cast<float *>(ws), h.own_pieces = reinterpret_cast<float *>(ws + g.prefix_pieces);
     h.states = reinterpret_cast<float *>(ws + g.prefix_pieces + g.own_pieces);
     h.own_columns = 16 * g.nc, h.prefix_columns = g.prefix_wg ? kBlockColumns : h.own_columns;
+    h.own_places = g.own_wg, h.prefix_places = g.prefix_wg ? g.prefix_wg : g.own_wg;
     if (!g.prefix_wg) h.prefix_pieces = h.own_pieces;
     if (a.c.d == 64) return launch_shared_d<64>(h, g, s);
     if (a.c.d == 128) return launch_shared_d<128>(h, g, s);

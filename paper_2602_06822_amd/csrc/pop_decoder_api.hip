@@ -235,7 +235,7 @@ int pop_cache_attention_shared(const void *q, pop_dtype_t dtype, int n_tokens, c
     if (workspace_bytes < need) return POP_ESHAPE;
     SharedArgs h = {{q, dtype == POP_BF16, n_tokens, static_cast<const unsigned char *>(cache), c, block_table, table_stride, q_start, context_len, n_seq,
                      n_heads, max_new, max_context, scale, 0, y, ydtype == POP_BF16, static_cast<float *>(workspace), 0},
-                    Divisor(n_heads / n_kv), Divisor(n_kv), Divisor(group), group, prefix_len, nullptr, nullptr, nullptr, 0, 0};
+                    Divisor(n_heads / n_kv), Divisor(n_kv), Divisor(group), group, prefix_len, nullptr, nullptr, nullptr, 0, 0, 0, 0};
     POP_HIP(launch_cache_attention_shared(h, as_stream(stream)));
     return POP_OK;
 }

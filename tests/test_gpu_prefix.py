@@ -504,7 +504,25 @@ def test_shared_chunks_in_blocks_of_128_columns(pop, dtype):  # noqa: F811
     check(c, y, q, start, BF16, 0.1)
 
 
-@pytest.mark.parametrize("heads,n_kv", [(4, 2), (16, 1)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_shared_rows_of_several_sequences(pop, dtype):  # noqa: F811
+    """Rows that two sequences say are theirs are undefined; the others' are right, and nothing beyond the rows is written."""
+    rng = np.random.default_rng(21)
+    c = Grouped(pop, rng, lifted([(300, [340, 330, 320]), (310, [340, 330, 320])]), 2, 64, 16)
+    q = queries(rng, 40, 8, 64, dtype)
+    starts = [0, 10, 5, 20, 3, 15, 32]  # sequences 0, 2, 4 and 5: rows 0-9, 5-19, 3-14, 15-31
+    h = f64(attend_shared(pop, c, q, starts, dtype, dtype, 8, 0.1, max_new=20))
+    for rows, s in ((range(0, 3), 0), (range(20, 32), 5)):
+        a, b = starts[s], starts[s + 1]
+        sizes = []
+        want = orc.attention(f64(q[a:b]), c.k[s], c.v[s], 0.1, c.context[s] - (b - a), 0, None, sizes)
+        bound = bound_of(want, sizes, 64, c.context[s], dtype)
+        for r in rows:
+            assert (np.abs(h[r] - want[r - a]) <= bound[r - a] + 1e-30).all(), (s, r)
+    assert (h[32:] == 7.0).all()
+
+
+@pytest.mark.parametrize("heads,n_kv", [(4, 2), (16, 1), (64, 1)])
 def test_shared_on_another_stream_and_in_a_replayed_graph(pop, heads, n_kv):  # noqa: F811
     rng = np.random.default_rng(19)
     c = Grouped(pop, rng, [(3000, [3100, 3001, 3050])], n_kv, 128, 16)
