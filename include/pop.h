@@ -388,6 +388,9 @@ int pop_cache_attention_shared(const void *q, pop_dtype_t dtype, int n_tokens, c
 /* Host only. */
 int pop_cache_attention_shared_workspace(int n_tokens, int n_seq, int group, int n_heads, int n_kv_heads, int head_dim,
                                          int max_new, int max_context, size_t *bytes);
+/* Host only.  Bytes of that which a call of just these types and sizes uses, from the workspace's beginning on. */
+int pop_cache_attention_shared_used(pop_dtype_t dtype, pop_dtype_t ydtype, int n_tokens, int n_seq, int group, int n_heads, int n_kv_heads,
+                                    int head_dim, int max_new, int max_context, size_t *bytes);
 /* Host only.  Which implementation a call of these sizes runs: 0 = none (nothing to do), 1 = that of pop_cache_attention, each row for itself (chunks that
  * are bound by their products, and calls too small to gain by sharing were all of max_context shared), 2 = prefixes by blocks of 16 or 32 columns (new
  * tokens x query heads of a kv head, of up to 64 rows of a group), 3 = by blocks of 128.  Errors: as pop_cache_attention_shared. */

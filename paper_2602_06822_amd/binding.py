@@ -71,6 +71,7 @@ _SIGS = {
     "pop_cache_attention_shared": (_i, [_vp, _i, _i, _vp, _i, _i, _i, _i, _vp, _i, _vp, _vp, _i, _i, _vp, _i, _i, _i, C.c_float, _vp, _i,
                                         _vp, C.c_size_t, _vp]),
     "pop_cache_attention_shared_kind": (_i, [_i] * 10),
+    "pop_cache_attention_shared_used": (_i, [_i] * 10 + [_szp]),
     "pop_cache_attention_shared_workspace": (_i, [_i, _i, _i, _i, _i, _i, _i, _i, _szp]),
     "pop_cache_attention_workspace": (_i, [_i, _i, _i, _i, _i, _i, _i, _szp]),
     "pop_cache_attention_kind": (_i, [_i, _i, _i, _i, _i, _i, _i, _i, _i, _i, _ip]),
@@ -402,6 +403,11 @@ def pop_cache_attention_shared_kind(dtype, ydtype, n_tokens, n_seq, group, n_hea
 
 def pop_cache_attention_shared_workspace(n_tokens, n_seq, group, n_heads, n_kv_heads, head_dim, max_new, max_context) -> int:
     return _size(_lib.pop_cache_attention_shared_workspace, "pop_cache_attention_shared_workspace", n_tokens, n_seq, group, n_heads,
+                 n_kv_heads, head_dim, max_new, max_context)
+
+
+def pop_cache_attention_shared_used(dtype, ydtype, n_tokens, n_seq, group, n_heads, n_kv_heads, head_dim, max_new, max_context) -> int:
+    return _size(_lib.pop_cache_attention_shared_used, "pop_cache_attention_shared_used", dtype, ydtype, n_tokens, n_seq, group, n_heads,
                  n_kv_heads, head_dim, max_new, max_context)
 
 

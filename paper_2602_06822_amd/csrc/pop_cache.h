@@ -162,13 +162,17 @@ struct SharedArgs {
     Divisor by_share, by_kv, by_group;  // query heads to a kv head, kv heads, sequences of a group
     int group;          // sequences of a group
     const int *prefix;  // [n_seq / group] tokens that a group's sequences share
+    size_t ws_bytes;    // of the caller's workspace
     // set by the launcher
     float *prefix_pieces, *own_pieces, *states;
     int prefix_columns, own_columns, prefix_places, own_places;
 };
 // 0: nothing to do, 1: each sequence for itself (launch_cache_attention), 2: the prefix by blocks of 16 or 32 columns of a group, 3: by blocks of 128.
 int cache_attention_shared_kind(int n_tokens, int n_seq, int group, int n_heads, int n_kv, int d, int max_new, int max_context, int all_bf16);
+// Bytes for calls of these sizes, or smaller n_tokens, n_seq, max_new and max_context, of any types.
 size_t cache_attention_shared_ws(int n_tokens, int n_seq, int group, int n_heads, int n_kv, int d, int max_new, int max_context);
+// Bytes that a call of these types and sizes lays out in its workspace.
+size_t cache_attention_shared_used(int n_tokens, int n_seq, int group, int n_heads, int n_kv, int d, int max_new, int max_context, int all_bf16);
 hipError_t launch_cache_attention_shared(SharedArgs h, hipStream_t s);  // (pop_cache_attention_shared.hip)
 
 struct BeamArgs {

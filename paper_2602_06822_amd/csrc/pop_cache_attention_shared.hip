@@ -864,35 +864,52 @@ __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs h)
 struct SharedGrid {
     int prefix_wg, own_wg;  // workgroups of the kernel for blocks of 128 (0: the other one has all units), and of the other one
     int nc;
-    size_t prefix_pieces, own_pieces, states;  // bytes
-    size_t bytes() const { return prefix_pieces + own_pieces + states; }
+    size_t row, states;  // bytes of a row of the workspace, and of all results of (token, head)
+    size_t prefix_pieces() const { return (size_t)prefix_wg * kBlockColumns * row; }
+    size_t own_pieces() const { return (size_t)own_wg * 16 * nc * row; }
+    size_t bytes() const { return prefix_pieces() + own_pieces() + states; }
 };
+long long columns_of_pack(int n_tokens, int group, int n_heads, int n_kv, int max_new)
+{
+    return std::min<long long>(n_tokens, (long long)std::min(group, 64) * max_new) * (n_heads / n_kv);
+}
+// Microseconds that a round takes a block of 32 and one of 128 columns, and what a third launch and larger results cost (measured: see shared_grid).
+struct BlockCosts {
+    double narrow, wide, launch;
+    explicit BlockCosts(int d) : narrow(d == 64 ? 0.0022 : 0.0027), wide(d == 64 ? 0.0035 : 0.0069), launch(d == 64 ? 8.0 : 11.0) {}
+    double saved_a_round(long long columns) const { return narrow * (double)((columns + 31) / 32) - wide * (double)((columns + 127) / 128); }
+};
+// The most that a call of these sizes and any types, or of smaller ones, has: its workspace.  shared_grid takes its grids from this one, so that what a call lays out is
+// never more.  (A pack has room for blocks of 128 if any number of its columns, or fewer, may take them: the first block decides.)
+SharedGrid most_grid(int n_tokens, int group, int n_heads, int n_kv, int d, int max_new)
+{
+    const BlockCosts costs(d);
+    const long long of_pack = std::min(columns_of_pack(n_tokens, group, n_heads, n_kv, max_new), (long long)kBlockColumns);
+    SharedGrid g = {0, d < 256 ? kWorkgroups : kWorkgroups / 2, d < 256 ? 2 : 1, (d + 4) * sizeof(float), 0};
+    if (d < 256 && costs.saved_a_round(of_pack) > 0.0) g.prefix_wg = kWorkgroups / 2;
+    g.states = 2 * (size_t)n_tokens * n_heads * g.row;
+    return g;
+}
 // Microseconds that a round of 128 tokens takes all compute units together, for 16 columns: measured for D = 128, the others in proportion.
 double round_cost(int d, bool all_bf16) { return (d == 64 ? 0.0015 : d == 128 ? 0.0022 : 0.0054) * (all_bf16 ? 1.0 : 1.45); }
 
 SharedGrid shared_grid(int n_tokens, int n_seq, int group, int n_heads, int n_kv, int d, int max_new, int max_context, bool all_bf16)
 {
+    const SharedGrid most = most_grid(n_tokens, group, n_heads, n_kv, d, max_new);
     const long long share = n_heads / n_kv, rounds = (max_context + (long long)kRound - 1) / kRound, packs = (long long)n_seq / group * ((group + 63) / 64);
-    const long long of_pack = std::min<long long>(n_tokens, (long long)std::min(group, 64) * max_new) * share, of_seq = std::min(n_tokens, max_new) * share;
-    SharedGrid g = {0, 0, 1, 0, 0, 0};
+    const long long of_pack = columns_of_pack(n_tokens, group, n_heads, n_kv, max_new), of_seq = std::min(n_tokens, max_new) * share;
+    SharedGrid g = most;
     // Blocks of 128 columns take a round in 0.0069 us, blocks of 32 in 0.0027 each, but a third launch and larger results cost 11 (D = 64: 0.0035, 0.0022, 8).
     // Microseconds, blocks of 32 / of 128.  D 128, 32 heads over 8, prefixes of 8000 tokens: 64 columns 21.4 / 29.5, 128 26.3 / 35.6, 256 33.3 / 40.5; of 32000: 64
     // columns 29.6 / 39.8; of 32768: 256 columns 75.0 / 69.6; 20000 tokens, 32 heads over 2, 1024 columns 96.5 / 78.5.  D 64, 256 columns over 8 kv heads, 16000 tokens 42.9 / 37.5.
     // D 256, 80 columns over 4 kv heads, 8000 tokens 22.0 / 42.6: never.
-    const double narrow = d == 64 ? 0.0022 : 0.0027, wide = d == 64 ? 0.0035 : 0.0069, launch = d == 64 ? 8.0 : 11.0;
-    const double saved = (double)(packs * n_kv) * (double)rounds * (narrow * (double)((of_pack + 31) / 32) - wide * (double)((of_pack + 127) / 128));
-    const bool in_blocks = all_bf16 && d < 256 && saved > launch;
-    if (in_blocks) {
-        const long long units = packs * n_kv * ((of_pack + kBlockColumns - 1) / kBlockColumns);
-        g.prefix_wg = (int)std::min<long long>(units * 2 * rounds, kWorkgroups / 2);
-        g.prefix_pieces = (size_t)g.prefix_wg * kBlockColumns * (d + 4) * sizeof(float);
-    }
-    if (d < 256 && (in_blocks ? of_seq : of_pack) > 16) g.nc = 2;
+    const BlockCosts costs(d);
+    const bool in_blocks = all_bf16 && most.prefix_wg > 0 && (double)(packs * n_kv) * (double)rounds * costs.saved_a_round(of_pack) > costs.launch;
+    g.prefix_wg = in_blocks ? (int)std::min<long long>(packs * n_kv * ((of_pack + kBlockColumns - 1) / kBlockColumns) * 2 * rounds, most.prefix_wg) : 0;
+    g.nc = (in_blocks ? of_seq : of_pack) > 16 ? most.nc : 1;
     const long long columns = 16 * g.nc, units = n_kv * (n_seq * ((of_seq + columns - 1) / columns) + (in_blocks ? 0 : packs * ((of_pack + columns - 1) / columns)));
     const long long per_unit = std::min(rounds + kUnitCost, std::max(32ll, (long long)(2.0 * sqrt((double)rounds))));
-    g.own_wg = (int)std::min(units * per_unit, d < 256 ? (long long)kWorkgroups : kWorkgroups / 2ll);
-    g.own_pieces = (size_t)g.own_wg * columns * (d + 4) * sizeof(float);
-    g.states = 2 * (size_t)n_tokens * n_heads * (d + 4) * sizeof(float);
+    g.own_wg = (int)std::min<long long>(units * per_unit, most.own_wg);
     return g;
 }
 
@@ -904,7 +921,7 @@ SharedGrid shared_grid(int n_tokens, int n_seq, int group, int n_heads, int n_kv
 bool pays(int n_tokens, int n_seq, int group, int n_heads, int n_kv, int d, int max_new, int max_context, bool all_bf16)
 {
     const long long share = n_heads / n_kv, of_seq = std::min<long long>(n_tokens, max_new) * share;
-    const long long of_pack = std::min<long long>(n_tokens, (long long)std::min(group, 64) * max_new) * share, packs = (long long)n_seq / group * ((group + 63) / 64);
+    const long long of_pack = columns_of_pack(n_tokens, group, n_heads, n_kv, max_new), packs = (long long)n_seq / group * ((group + 63) / 64);
     const double cost = round_cost(d, all_bf16) * (double)((max_context + (long long)kRound - 1) / kRound);
     const double units = (double)n_seq * n_kv * (double)((of_seq + 15) / 16), of_prefix = (double)packs * n_kv * (of_pack > 16 && d < 256 ? 1.23 * (double)((of_pack + 31) / 32) : (double)((of_pack + 15) / 16));
     return cost * units + (units >= 256 ? 5.4 : 10.0) > cost * of_prefix + (of_pack > 16 && !all_bf16 ? 19.5 : of_pack > 16 || !all_bf16 ? 14.5 : 12.4);
@@ -956,13 +973,16 @@ int cache_attention_shared_kind(int n_tokens, int n_seq, int group, int n_heads,
 
 size_t cache_attention_shared_ws(int n_tokens, int n_seq, int group, int n_heads, int n_kv, int d, int max_new, int max_context)
 {
-    if (group == 1) return 0;
-    // for either type, and for all smaller sizes: the most workgroups that any of them has, of the widest units, and blocks of 128 where some of
-    // them may have a pack of more than 64 columns
-    const SharedGrid g = shared_grid(n_tokens, n_seq, group, n_heads, n_kv, d, max_new, max_context, true);
-    const long long of_pack = std::min<long long>(n_tokens, (long long)std::min(group, 64) * max_new) * (n_heads / n_kv);
-    const size_t row = (d + 4) * sizeof(float), own = (size_t)kWorkgroups * 32 * row;
-    return own + (d < 256 && of_pack > 64 ? (size_t)kWorkgroups / 2 * kBlockColumns * row : 0) + g.states;
+    const size_t each = cache_attention_ws(n_tokens, n_seq, n_heads, n_kv, d, max_new, max_context);
+    return group == 1 ? each : std::max(each, most_grid(n_tokens, group, n_heads, n_kv, d, max_new).bytes());
+}
+
+size_t cache_attention_shared_used(int n_tokens, int n_seq, int group, int n_heads, int n_kv, int d, int max_new, int max_context, int all_bf16)
+{
+    const int kind = cache_attention_shared_kind(n_tokens, n_seq, group, n_heads, n_kv, d, max_new, max_context, all_bf16);
+    if (kind == 0) return 0;
+    if (kind == 1) return cache_attention_ws(n_tokens, n_seq, n_heads, n_kv, d, max_new, max_context);
+    return shared_grid(n_tokens, n_seq, group, n_heads, n_kv, d, max_new, max_context, all_bf16 != 0).bytes();
 }
 
 hipError_t launch_cache_attention_shared(SharedArgs h, hipStream_t s)
@@ -972,9 +992,10 @@ hipError_t launch_cache_attention_shared(SharedArgs h, hipStream_t s)
     if (cache_attention_shared_kind(a.n_tokens, a.n_seq, h.group, a.n_heads, a.c.n_kv, a.c.d, a.max_new, a.max_context, all_bf16) < 2)
         return launch_cache_attention(a, s);
     const SharedGrid g = shared_grid(a.n_tokens, a.n_seq, h.group, a.n_heads, a.c.n_kv, a.c.d, a.max_new, a.max_context, all_bf16);
+    if (g.bytes() > h.ws_bytes) return hipErrorInvalidValue;  // (never: see most_grid)
     char *const ws = reinterpret_cast<char *>(a.ws);
-    h.prefix_pieces = reinterpret_cast<float *>(ws), h.own_pieces = reinterpret_cast<float *>(ws + g.prefix_pieces);
-    h.states = reinterpret_cast<float *>(ws + g.prefix_pieces + g.own_pieces);
+    h.prefix_pieces = reinterpret_cast<float *>(ws), h.own_pieces = reinterpret_cast<float *>(ws + g.prefix_pieces());
+    h.states = reinterpret_cast<float *>(ws + g.prefix_pieces() + g.own_pieces());
     h.own_columns = 16 * g.nc, h.prefix_columns = g.prefix_wg ? kBlockColumns : h.own_columns;
     h.own_places = g.own_wg, h.prefix_places = g.prefix_wg ? g.prefix_wg : g.own_wg;
     if (!g.prefix_wg) h.prefix_pieces = h.own_pieces;

@@ -197,9 +197,18 @@ int pop_cache_attention_shared_workspace(int n_tokens, int n_seq, int group, int
     if (!bytes) return POP_EINVAL;
     const int rc = shared_sizes(n_tokens, n_seq, group, n_heads, n_kv, d, max_new, max_context);
     if (rc != POP_OK) return rc;
-    *bytes = n_seq ? std::max(cache_attention_ws(n_tokens, n_seq, n_heads, n_kv, d, max_new, max_context),
-                              cache_attention_shared_ws(n_tokens, n_seq, group, n_heads, n_kv, d, max_new, max_context))
-                   : 0;
+    *bytes = n_seq ? cache_attention_shared_ws(n_tokens, n_seq, group, n_heads, n_kv, d, max_new, max_context) : 0;
+    return POP_OK;
+}
+
+int pop_cache_attention_shared_used(pop_dtype_t dtype, pop_dtype_t ydtype, int n_tokens, int n_seq, int group, int n_heads, int n_kv, int d, int max_new,
+                                    int max_context, size_t *bytes)
+{
+    if (!bytes) return POP_EINVAL;
+    const int rc = shared_sizes(n_tokens, n_seq, group, n_heads, n_kv, d, max_new, max_context);
+    if (rc != POP_OK) return rc;
+    if (!is_dtype(dtype) || !is_dtype(ydtype)) return POP_EINVAL;
+    *bytes = cache_attention_shared_used(n_tokens, n_seq, group, n_heads, n_kv, d, max_new, max_context, dtype == POP_BF16 && ydtype == POP_BF16);
     return POP_OK;
 }
 
@@ -229,13 +238,12 @@ int pop_cache_attention_shared(const void *q, pop_dtype_t dtype, int n_tokens, c
     if (n_seq == 0 || n_tokens == 0) return POP_OK;
     if (!q || !cache || !block_table || !q_start || !context_len || !prefix_len || !y) return POP_EINVAL;
     if (!aligned16(q) || !aligned16(cache) || !aligned16(y) || !aligned16(workspace)) return POP_EINVAL;
-    const size_t need = std::max(cache_attention_ws(n_tokens, n_seq, n_heads, n_kv, d, max_new, max_context),
-                                 cache_attention_shared_ws(n_tokens, n_seq, group, n_heads, n_kv, d, max_new, max_context));
+    const size_t need = cache_attention_shared_ws(n_tokens, n_seq, group, n_heads, n_kv, d, max_new, max_context);
     if (need && !workspace) return POP_EINVAL;
     if (workspace_bytes < need) return POP_ESHAPE;
     SharedArgs h = {{q, dtype == POP_BF16, n_tokens, static_cast<const unsigned char *>(cache), c, block_table, table_stride, q_start, context_len, n_seq,
                      n_heads, max_new, max_context, scale, 0, y, ydtype == POP_BF16, static_cast<float *>(workspace), 0},
-                    Divisor(n_heads / n_kv), Divisor(n_kv), Divisor(group), group, prefix_len, nullptr, nullptr, nullptr, 0, 0, 0, 0};
+                    Divisor(n_heads / n_kv), Divisor(n_kv), Divisor(group), group, prefix_len, workspace_bytes, nullptr, nullptr, nullptr, 0, 0, 0, 0};
     POP_HIP(launch_cache_attention_shared(h, as_stream(stream)));
     return POP_OK;
 }
