@@ -237,9 +237,11 @@ __device__ __forceinline__ Sequence look_at(const SharedArgs &h, const Packs &pa
 __device__ __forceinline__ int times(int a, int b) { return saturated((long long)a * b); }
 
 // How the work is dealt.  A unit is one kv head's block of columns over the prefix (of a pack) or over its own tokens (of a sequence), so many rounds; with what
-// it costs beside them all units make up `all`, and a unit is split into as many parts as it has of that, in workgroups, but at least one.  A part is an item; workgroup
-// w has items w, w + gridDim.x, ..: most have one.  (What had parts of several units a workgroup, in equal numbers of rounds: 8 sequences x 32 heads, 4000 tokens and 200 of
-// their own, 11.6 us; 64 sequences x 8 heads, 700 of their own, 13.6.)  Parts of units that have several have a place for their results each; there
+// it costs beside them all units make up `all`, and a unit is split into as many parts as it has of that, in workgroups, but at least one.  A part is an item; items
+// of prefixes, which are long, and own ones are dealt each by themselves, in turn to all workgroups: most have one.  (Both in one row: where a group's items are a whole part of
+// the workgroups, the prefixes of all groups fall to the same few.  Microseconds, in one row / each by themselves / each sequence for itself: 16 groups of 14 rows, 32 heads over 8, D 64,
+// 30229 tokens 893 / 190 / 534, D 128, 8000 tokens 338 / 91 / 228; 3 groups of 10, 40 heads over 8, 9000 tokens 28.5 / 29.5 / 47; one group, the same.) (What had parts of several units a workgroup, in equal
+// numbers of rounds: 8 sequences x 32 heads, 4000 tokens and 200 of their own, 11.6 us; 64 sequences x 8 heads, 700 of their own, 13.6.)  Parts of units that have several have a place for their results each; there
 // are no more of those than workgroups.
 // A unit has no more parts than kPartsOfRoot roots of its rounds: each costs its columns' joining about a thirtieth of a microsecond. (3, 5, 8: 2 kv heads x 32 columns
 // over 32768 tokens 19.1, 18.9, 20.4 us, 8 chunks of 5 over 8000 31.4, 31.2, 34.3.)
@@ -323,43 +325,46 @@ __global__ __launch_bounds__(256, D == 256 || (D == 128 && NC == 2 && QT == 3) ?
         all = __builtin_elementwise_add_sat(all, __builtin_amdgcn_readlane(wave_scan(cost), 63));
     }
     const Dealing dealing(all);
-    int upto = 0, places_upto = 0;  // items and places of the look's sequences up to the lane's
-    int look = 0, items_before = 0, places_before = 0;  // the look that `own` is of, and items and places in front of it
+    int upto1 = 0, upto2 = 0, places_upto = 0;  // items (of prefixes, own) and places of the look's sequences up to the lane's
+    int look = 0, before1 = 0, before2 = 0, places_before = 0;  // the look that `own` is of, and items and places in front of it
     int parts1 = 1, parts2 = 1, items1 = 0;  // parts of a unit of the prefix and of an own one, items of the former
     const auto deal = [&]() {
         parts1 = dealing.parts(own.prefix_rounds), parts2 = dealing.parts(own.rounds);
         items1 = times(times(own.prefix_blocks, n_kv), parts1);
         const int items2 = times(times(own.blocks, n_kv), parts2);
-        upto = wave_scan(__builtin_elementwise_add_sat(items1, items2));
+        upto1 = wave_scan(items1), upto2 = wave_scan(items2);
         places_upto = wave_scan((parts1 > 1 ? items1 : 0) + (parts2 > 1 ? items2 : 0));
     };
     if (looks > 1) own = look_at<kColumns, UNITS>(h, packs, 0, lane);
     deal();
     const size_t page_bytes = cache_page_bytes(a.c);
 
-    for (unsigned item = blockIdx.x;;) {
-        const int of_look = __builtin_amdgcn_readlane(upto, 63);
-        if (item >= (unsigned)items_before + (unsigned)of_look) {
+    // the workgroup's next items: own ones go on where those of prefixes end, or (several looks: that is not known yet) begin with the last workgroup
+    const unsigned of_prefixes = (unsigned)__builtin_amdgcn_readlane(upto1, 63) % gridDim.x;
+    unsigned next1 = blockIdx.x, next2 = looks > 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x + (blockIdx.x < of_prefixes ? gridDim.x : 0u) - of_prefixes;
+    for (;;) {
+        const int of_look1 = __builtin_amdgcn_readlane(upto1, 63), of_look2 = __builtin_amdgcn_readlane(upto2, 63);
+        const bool shared = next1 < (unsigned)before1 + (unsigned)of_look1;
+        if (!shared && next2 >= (unsigned)before2 + (unsigned)of_look2) {
             if (++look >= looks) break;
-            items_before += of_look, places_before += __builtin_amdgcn_readlane(places_upto, 63);
+            before1 += of_look1, before2 += of_look2, places_before += __builtin_amdgcn_readlane(places_upto, 63);
             own = look_at<kColumns, UNITS>(h, packs, look, lane);
             deal();
             continue;
         }
-        const int of_item = (int)(item - (unsigned)items_before), owner = __ffsll((unsigned long long)__ballot(upto > of_item)) - 1;
-        const int prefix = __builtin_amdgcn_readlane(own.prefix, owner), prefix_rounds = __builtin_amdgcn_readlane(own.prefix_rounds, owner);
-        const int of_prefix = __builtin_amdgcn_readlane(items1, owner);
-        int at = of_item - (owner > 0 ? __builtin_amdgcn_readlane(upto, owner - 1) : 0);
+        const int of_item = (int)(shared ? next1 - (unsigned)before1 : next2 - (unsigned)before2), upto = shared ? upto1 : upto2;
+        const int owner = __ffsll((unsigned long long)__ballot(upto > of_item)) - 1;
+        const int prefix = __builtin_amdgcn_readlane(own.prefix, owner);
+        const int rounds = __builtin_amdgcn_readlane(shared ? own.prefix_rounds : own.rounds, owner), parts = __builtin_amdgcn_readlane(shared ? parts1 : parts2, owner);
+        const int at = of_item - (owner > 0 ? __builtin_amdgcn_readlane(upto, owner - 1) : 0);
         int place0 = places_before + (owner > 0 ? __builtin_amdgcn_readlane(places_upto, owner - 1) : 0);
-        const bool shared = at < of_prefix;
-        const int rounds = shared ? prefix_rounds : __builtin_amdgcn_readlane(own.rounds, owner);
-        const int parts = __builtin_amdgcn_readlane(shared ? parts1 : parts2, owner);
-        if (!shared) at -= of_prefix, place0 += __builtin_amdgcn_readlane(parts1, owner) > 1 ? of_prefix : 0;
+        if (!shared) place0 += __builtin_amdgcn_readlane(parts1 > 1 ? items1 : 0, owner);  // (a sequence's places of the prefix come first)
+        if (shared) next1 += gridDim.x;
+        else next2 += gridDim.x;
         const PartOf of = part_of(at, rounds, parts);
         const int unit = of.unit, part = of.part, begin = of.begin, stop = of.stop;
         const int block = h.by_kv.of(unit), head = unit - block * n_kv;
         place0 += unit * parts;  // (of parts that have places)
-        item += gridDim.x;
 
         // tokens, and the row of the table that names their pages: for the prefix that of the longest sequence
         const int pack0 = __builtin_amdgcn_readlane(own.pack0, owner), pack_n = __builtin_amdgcn_readlane(own.pack_n, owner);
