@@ -881,7 +881,7 @@ long long columns_of_pack(int n_tokens, int group, int n_heads, int n_kv, int ma
 // Microseconds that a round takes a block of 32 and one of 128 columns, and what a third launch and larger results cost (measured: see shared_grid).
 struct BlockCosts {
     double narrow, wide, launch;
-    explicit BlockCosts(int d) : narrow(d == 64 ? 0.0022 : 0.0027), wide(d == 64 ? 0.0035 : 0.0069), launch(d == 64 ? 8.0 : 11.0) {}
+    explicit BlockCosts(int d) : narrow(d == 64 ? 0.0022 : 0.0027), wide(d == 64 ? 0.0056 : 0.0069), launch(d == 64 ? 8.0 : 11.0) {}
     double saved_a_round(long long columns) const { return narrow * (double)((columns + 31) / 32) - wide * (double)((columns + 127) / 128); }
 };
 // The most that a call of these sizes and any types, or of smaller ones, has: its workspace.  shared_grid takes its grids from this one, so that what a call lays out is
@@ -904,9 +904,12 @@ SharedGrid shared_grid(int n_tokens, int n_seq, int group, int n_heads, int n_kv
     const long long share = n_heads / n_kv, rounds = (max_context + (long long)kRound - 1) / kRound, packs = (long long)n_seq / group * ((group + 63) / 64);
     const long long of_pack = columns_of_pack(n_tokens, group, n_heads, n_kv, max_new), of_seq = std::min(n_tokens, max_new) * share;
     SharedGrid g = most;
-    // Blocks of 128 columns take a round in 0.0069 us, blocks of 32 in 0.0027 each, but a third launch and larger results cost 11 (D = 64: 0.0035, 0.0022, 8).
+    // Blocks of 128 columns take a round in 0.0069 us, blocks of 32 in 0.0027 each, but a third launch and larger results cost 11 (D = 64: 0.0056, 0.0022, 8).
     // Microseconds, blocks of 32 / of 128.  D 128, 32 heads over 8, prefixes of 8000 tokens: 64 columns 21.4 / 29.5, 128 26.3 / 35.6, 256 33.3 / 40.5; of 32000: 64
-    // columns 29.6 / 39.8; of 32768: 256 columns 75.0 / 69.6; 20000 tokens, 32 heads over 2, 1024 columns 96.5 / 78.5.  D 64, 256 columns over 8 kv heads, 16000 tokens 42.9 / 37.5.
+    // columns 29.6 / 39.8; of 32768: 256 columns 75.0 / 69.6; 20000 tokens, 32 heads over 2, 1024 columns 96.5 / 78.5.  D 64, one group over 8 kv heads: 96 columns, 40000
+    // tokens 32.1 / 37.3, 128 columns, 57492 tokens 51.3 / 45.5, 256 columns, 8000 tokens 28.2 / 33.6, 16000 42.7 / 39.3; 33 to 64 columns: 32 kv heads, 65536 tokens, 33
+    // columns 86.1 / 114.4, 64 columns 124.4 / 122.2, 12 groups of 16 rows, 8 kv heads, 37128 tokens, 64 columns 171 / 248, and so 58 of 60 calls of any sizes.
+    // (Several groups' own tokens take longer behind the blocks than between them: 152 columns over 16 kv heads, 6 groups of 5877 tokens 113 / 145; 256 over 8, 4 of 28796 191 / 145.)
     // D 256, 80 columns over 4 kv heads, 8000 tokens 22.0 / 42.6: never.
     const BlockCosts costs(d);
     const bool in_blocks = all_bf16 && most.prefix_wg > 0 && (double)(packs * n_kv) * (double)rounds * costs.saved_a_round(of_pack) > costs.launch;

@@ -44,6 +44,20 @@ def test_every_number_of_columns(pop, d):
     assert kinds >= ({2, 3} if d < 256 else {2})
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_blocks_that_are_at_most_half_full_are_not_taken(pop, d):
+    """Blocks of 128 columns need more than 64; what they would use is not asked for then."""
+    for rows in (33, 40, 48, 64):
+        for groups, n_kv, context in ((1, 32, 1 << 22), (1, 32, 65536), (12, 8, 37128), (8, 8, 20000), (16, 16, 40000)):
+            sizes = (groups * rows, groups * rows, rows, n_kv, n_kv, d, 1, context)
+            assert pop.pop_cache_attention_shared_kind(BF16, BF16, *sizes) == 2, sizes
+            row = 4 * (d + 4)
+            assert pop.pop_cache_attention_shared_workspace(*sizes) <= max(512 * 32 * row + 2 * groups * rows * n_kv * row,
+                                                                           pop.pop_cache_attention_workspace(*sizes[:2], *sizes[3:]))
+    sizes = (96, 96, 48, 64, 32, d, 1, 1 << 20)
+    assert pop.pop_cache_attention_shared_kind(BF16, BF16, *sizes) == 3
+
+
 def test_random_sizes_and_all_smaller_ones(pop):
     rng = random.Random(7)
 
