@@ -370,6 +370,9 @@ int pop_cache_attention_sinks(const void *q, pop_dtype_t dtype, int n_tokens, co
                               const int *q_start, const int *context_len, int n_seq, int n_heads, int max_new,
                               int max_context, float scale, int window, int sinks, void *y, pop_dtype_t ydtype,
                               void *workspace, size_t workspace_bytes, void *stream);
+/* Host only.  As pop_cache_attention_kind, which knows of no first tokens (they add to what a window sees). */
+int pop_cache_attention_sinks_kind(pop_dtype_t dtype, pop_dtype_t ydtype, int n_tokens, int n_seq, int n_heads, int n_kv_heads,
+                                   int head_dim, int max_new, int max_context, int window, int sinks, int *parts);
 
 /* pop_cache_attention (without a window) for sequences that share a prefix: n_seq rows in groups of `group` sequences (beams of a prompt, or questions
  * about one document), whose first prefix_len[g] tokens (dev [n_seq / group]) are the same in all rows of group g.  The caller sees to that: up to

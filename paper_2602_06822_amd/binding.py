@@ -75,6 +75,7 @@ _SIGS = {
     "pop_cache_attention_shared_workspace": (_i, [_i, _i, _i, _i, _i, _i, _i, _i, _szp]),
     "pop_cache_attention_workspace": (_i, [_i, _i, _i, _i, _i, _i, _i, _szp]),
     "pop_cache_attention_kind": (_i, [_i, _i, _i, _i, _i, _i, _i, _i, _i, _i, _ip]),
+    "pop_cache_attention_sinks_kind": (_i, [_i, _i, _i, _i, _i, _i, _i, _i, _i, _i, _i, _ip]),
     "pop_beam_select": (_i, [_vp, _i, _vp, _vp, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp, C.c_size_t, _vp]),
     "pop_beam_workspace": (_i, [_i, _i, _i, _i, _szp]),
     "pop_cache_reorder": (_i, [_vp, _vp, _vp, _i, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _vp, _vp, _vp, C.c_size_t, _vp, _vp]),
@@ -423,6 +424,16 @@ def pop_cache_attention_kind(dtype, ydtype, n_tokens, n_seq, n_heads, n_kv_heads
                                          C.byref(parts))
     if kind < 0:
         raise PopError(kind, "pop_cache_attention_kind")
+    return kind, parts.value
+
+
+def pop_cache_attention_sinks_kind(dtype, ydtype, n_tokens, n_seq, n_heads, n_kv_heads, head_dim, max_new, max_context, window, sinks):
+    """(kind, parts), as pop_cache_attention_kind, of pop_cache_attention_sinks."""
+    parts = C.c_int()
+    kind = _lib.pop_cache_attention_sinks_kind(dtype, ydtype, n_tokens, n_seq, n_heads, n_kv_heads, head_dim, max_new, max_context, window,
+                                               sinks, C.byref(parts))
+    if kind < 0:
+        raise PopError(kind, "pop_cache_attention_sinks_kind")
     return kind, parts.value
 
 

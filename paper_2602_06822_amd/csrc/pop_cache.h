@@ -143,7 +143,7 @@ struct AttentionLaunch {
 hipError_t launch_attention_sinks(const AttentionArgs &a, const AttentionLaunch &l, hipStream_t s);  // (pop_cache_attention_sinks.hip)
 size_t cache_attention_ws(int n_tokens, int n_seq, int n_heads, int n_kv, int d, int max_new, int max_context);
 // Parts that the prompt kernel splits the tokens of a block of 128 columns into, 0 where the general kernel takes the call.
-int cache_attention_parts(int n_tokens, int n_seq, int n_heads, int n_kv, int d, int max_new, int max_context, int window, int all_bf16);
+int cache_attention_parts(int n_tokens, int n_seq, int n_heads, int n_kv, int d, int max_new, int max_context, int window, int sinks, int all_bf16);
 hipError_t launch_cache_attention(const AttentionArgs &a, hipStream_t s);
 
 // Division of numbers below 2^31 by one that the host knows: ceil(2^(31 + l) / d) with 2^l >= d is off by less than 2^l / d parts of a quotient.

@@ -96,9 +96,9 @@ size_t cache_attention_ws(int n_tokens, int n_seq, int n_heads, int n_kv, int d,
     return std::max((size_t)prompt, (size_t)attention_workgroups(n_seq, n_heads, n_kv, d, max_new, max_context) * (2 * 16 * (d + 4) * sizeof(float) + 8));
 }
 
-int cache_attention_parts(int n_tokens, int n_seq, int n_heads, int n_kv, int d, int max_new, int max_context, int window, int all_bf16)
+int cache_attention_parts(int n_tokens, int n_seq, int n_heads, int n_kv, int d, int max_new, int max_context, int window, int sinks, int all_bf16)
 {
-    const PromptGrid g = prompt_of(n_tokens, n_seq, n_heads, n_kv, d, max_new, longest_seen(max_new, max_context, window, 0), all_bf16 != 0);
+    const PromptGrid g = prompt_of(n_tokens, n_seq, n_heads, n_kv, d, max_new, longest_seen(max_new, max_context, window, sinks), all_bf16 != 0);
     return g.blocks > 0 ? g.splits : 0;
 }
 

@@ -974,7 +974,7 @@ int cache_attention_shared_kind(int n_tokens, int n_seq, int group, int n_heads,
 {
     if (n_seq == 0 || n_tokens == 0) return 0;
     // chunks for which the kernel for blocks of 128 columns pays are bound by their products: they gain nothing from a prefix that is read once
-    if (group == 1 || cache_attention_parts(n_tokens, n_seq, n_heads, n_kv, d, max_new, max_context, 0, all_bf16) > 0) return 1;
+    if (group == 1 || cache_attention_parts(n_tokens, n_seq, n_heads, n_kv, d, max_new, max_context, 0, 0, all_bf16) > 0) return 1;
     if (!pays(n_tokens, n_seq, group, n_heads, n_kv, d, max_new, max_context, all_bf16 != 0)) return 1;
     return shared_grid(n_tokens, n_seq, group, n_heads, n_kv, d, max_new, max_context, all_bf16 != 0).prefix_wg > 0 ? 3 : 2;
 }

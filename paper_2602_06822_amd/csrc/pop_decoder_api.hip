@@ -135,18 +135,24 @@ int pop_cache_attention_workspace(int n_tokens, int n_seq, int n_heads, int n_kv
     return POP_OK;
 }
 
-int pop_cache_attention_kind(pop_dtype_t dtype, pop_dtype_t ydtype, int n_tokens, int n_seq, int n_heads, int n_kv, int d, int max_new,
-                             int max_context, int window, int *parts)
+int pop_cache_attention_sinks_kind(pop_dtype_t dtype, pop_dtype_t ydtype, int n_tokens, int n_seq, int n_heads, int n_kv, int d, int max_new,
+                                   int max_context, int window, int sinks, int *parts)
 {
     const int rc = attention_sizes(n_tokens, n_seq, n_heads, n_kv, d, max_new, max_context);
     if (rc != POP_OK) return rc;
-    if (window < 0) return POP_ESHAPE;
+    if (window < 0 || sinks < 0) return POP_ESHAPE;
     if (!is_dtype(dtype) || !is_dtype(ydtype)) return POP_EINVAL;
     const bool none = n_seq == 0 || n_tokens == 0;
     const int of_blocks =
-        none ? 0 : cache_attention_parts(n_tokens, n_seq, n_heads, n_kv, d, max_new, max_context, window, dtype == POP_BF16 && ydtype == POP_BF16);
+        none ? 0 : cache_attention_parts(n_tokens, n_seq, n_heads, n_kv, d, max_new, max_context, window, sinks, dtype == POP_BF16 && ydtype == POP_BF16);
     if (parts) *parts = of_blocks;
     return none ? 0 : of_blocks > 0 ? 2 : 1;
+}
+
+int pop_cache_attention_kind(pop_dtype_t dtype, pop_dtype_t ydtype, int n_tokens, int n_seq, int n_heads, int n_kv, int d, int max_new,
+                             int max_context, int window, int *parts)
+{
+    return pop_cache_attention_sinks_kind(dtype, ydtype, n_tokens, n_seq, n_heads, n_kv, d, max_new, max_context, window, 0, parts);
 }
 
 int pop_cache_attention_sinks(const void *q, pop_dtype_t dtype, int n_tokens, const void *cache, int n_kv, int d, int page, int n_pages,
