@@ -441,8 +441,8 @@ int pop_cache_copy_pages(void *cache, int n_kv_heads, int head_dim, int page_tok
 
 /* ---- between a layer's blocks ----
  *
- * Residual sums with the norms around a block, and rotary positions, on rows of any length and alignment (of their elements); rows whose length,
- * distance and address are multiples of 16 bytes are faster.  Strides are in elements, from row to row. */
+ * Residual sums with the norms around a block, and rotary positions, on rows of any length and alignment (of their elements).  Calls are faster where all
+ * widths (d, head_dim) and strides are multiples of 8 elements and all addresses of 16 bytes.  Strides are in elements, from row to row. */
 
 /* The residual stream after a block, and the next block's input, in one pass:
  *     u' = u r(u) (w_post + weight_offset)  if post_norm, else u;       r(v) = 1 / sqrt(sum of squares of v / d + eps)
