@@ -364,7 +364,7 @@ int pop_cache_attention_kind(pop_dtype_t dtype, pop_dtype_t ydtype, int n_tokens
 
 /* The same with first tokens that stay visible: with window > 0 a token at position p sees token t <= p if p - t < window or t < sinks.  Without a
  * window, or with sinks = 0, it is pop_cache_attention.  Pages that no token sees may be none (given back to the pool).
- * workspace: as for pop_cache_attention.  Errors: as pop_cache_attention; sinks < 0 -> POP_ESHAPE. */
+ * workspace, the rounding of the softmax weights: as for pop_cache_attention.  Errors: as pop_cache_attention; sinks < 0 -> POP_ESHAPE. */
 int pop_cache_attention_sinks(const void *q, pop_dtype_t dtype, int n_tokens, const void *cache, int n_kv_heads,
                               int head_dim, int page_tokens, int n_pages, const int *block_table, int table_stride,
                               const int *q_start, const int *context_len, int n_seq, int n_heads, int max_new,
@@ -380,9 +380,9 @@ int pop_cache_attention_sinks_kind(pop_dtype_t dtype, pop_dtype_t ydtype, int n_
  * pop_cache_reorder leaves them.  Tokens of the prefix are read from any of the rows that have new tokens, once for all of them; rows may be
  * shorter than the prefix, and new tokens may stand in it.  prefix_len that is negative or 0 shares nothing.
  * Where that does not pay (pop_cache_attention_shared_kind; prefixes of less than 1024 tokens) each row reads its own pages.
- * Rows, types, limits and errors otherwise as pop_cache_attention (of the rounds: < 2^30); group < 1 or n_seq no multiple of it -> POP_ESHAPE.
- * workspace: dev, of pop_cache_attention_shared_workspace bytes for the same group and the same or larger other sizes; any content, for this call
- * alone. */
+ * Rows, types, the rounding of the softmax weights, limits and errors otherwise as pop_cache_attention (of the rounds: < 2^30); group < 1 or n_seq no multiple of it -> POP_ESHAPE.
+ * workspace: dev, of pop_cache_attention_shared_workspace bytes for the same sizes, or for larger n_tokens, n_seq, max_new or max_context; any content,
+ * for this call alone. */
 int pop_cache_attention_shared(const void *q, pop_dtype_t dtype, int n_tokens, const void *cache, int n_kv_heads,
                                int head_dim, int page_tokens, int n_pages, const int *block_table, int table_stride,
                                const int *q_start, const int *context_len, int n_seq, int group, const int *prefix_len,
