@@ -453,11 +453,10 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void cache_prompt_kernel(Att
         // next to what is seen counted too 890 us, so 521)
         int full = seen.hi;
         const int window0 = cols.window == kNoWindow ? 0 : max(seen.first_pos - cols.window + 1, 0);
-        const auto seen_page = [&](int i) { return (i + 1) << a.c.log_page > window0 || (SINKS && i << a.c.log_page < a.sinks); };
-        for (int i = (seen.lo >> a.c.log_page) + lane; i << a.c.log_page < seen.hi; i += 64)
-            if ((unsigned)table[i] >= (unsigned)a.c.n_pages && seen_page(i)) full = 0;
+        for (int i = (max(seen.lo, window0) >> a.c.log_page) + lane; i << a.c.log_page < seen.hi; i += 64)
+            if ((unsigned)table[i] >= (unsigned)a.c.n_pages) full = 0;
         if (SINKS)
-            for (int i = lane; i << a.c.log_page < min(a.sinks, seen.lo - seen.begin); i += 64)
+            for (int i = lane; i << a.c.log_page < min(a.sinks, seen.hi); i += 64)
                 if ((unsigned)table[i] >= (unsigned)a.c.n_pages) full = 0;
         full = __any(full == 0) ? 0 : full;
         const int first = seen.begin, all_tiles = (seen.hi - seen.begin + kPromptTile - 1) / kPromptTile;
