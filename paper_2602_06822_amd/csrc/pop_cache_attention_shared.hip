@@ -20,8 +20,8 @@ constexpr int kWorkgroups = 512;
 // What a unit costs its workgroup beside its rounds (its columns, q and table, the waves' sums), in rounds.
 constexpr int kUnitCost = 4;
 // A prefix shorter than this is read by each sequence for itself, also in a call that could share longer ones: units of its own and joining cost more. (Microseconds,
-// shared / not: 8 sequences x 32 heads 512 tokens 14.4 / 14.0, 1024 15.5 / 16.2; 16 x 32 over 8 512 tokens 15.1 / 13.2, 1024 15.9 / 14.8; 4 groups of 4 x 32
-// 512 tokens 16.6 / 14.8, 1024 19.0 / 17.4.)
+// shared / not: 8 sequences x 32 heads 512 tokens 13.7 / 13.6, 1024 14.9 / 15.9; 16 x 32 over 8 512 tokens 12.9 / 12.7, 1024 15.5 / 14.5; 4 groups of 4 x 32
+// 512 tokens 14.4 / 14.4, 1024 18.6 / 16.7, 1500 17.1 / 18.3.)
 constexpr int kLeastPrefix = 1024;
 
 // One step of a wave: 32 tokens of one kv head against NC blocks of 16 columns, whose keys and values are converted once.
@@ -238,10 +238,10 @@ __device__ __forceinline__ int times(int a, int b) { return saturated((long long
 
 // How the work is dealt.  A unit is one kv head's block of columns over the prefix (of a pack) or over its own tokens (of a sequence), so many rounds; with what
 // it costs beside them all units make up `all`, and a unit is split into as many parts as it has of that, in workgroups, but at least one.  A part is an item; items
-// of prefixes, which are long, and own ones are dealt each by themselves, in turn to all workgroups: most have one.  (Both in one row: where a group's items are a whole part of
-// the workgroups, the prefixes of all groups fall to the same few.  Microseconds, in one row / each by themselves / each sequence for itself: 16 groups of 14 rows, 32 heads over 8, D 64,
-// 30229 tokens 893 / 190 / 534, D 128, 8000 tokens 338 / 91 / 228; 3 groups of 10, 40 heads over 8, 9000 tokens 28.5 / 29.5 / 47; one group, the same.) (What had parts of several units a workgroup, in equal
-// numbers of rounds: 8 sequences x 32 heads, 4000 tokens and 200 of their own, 11.6 us; 64 sequences x 8 heads, 700 of their own, 13.6.)  Parts of units that have several have a place for their results each; there
+// of prefixes, which are long, and own ones are dealt each by themselves, in turn to all workgroups: most have one.  (Both in one row: where a group's items are a whole
+// part of the workgroups, the prefixes of all groups fall to the same few.  Microseconds, in one row / each by themselves / each sequence for itself, 32 heads over 8: 16 groups of 14
+// rows, D 64, 30229 tokens 893 / 186 / 534, D 128, 8000 tokens 338 / 91 / 228; 4 groups of 8, D 128, 8000 tokens 25.5 / 25.2 / 43.5, one of 64 32.7 / 29.5 / 65.)  (What had parts of
+// several units a workgroup, in equal numbers of rounds: 8 sequences x 32 heads, 4000 tokens and 200 of their own, 11.6 us; 64 sequences x 8 heads, 700 of their own, 13.6.)  Parts of units that have several have a place for their results each; there
 // are no more of those than workgroups.
 // A unit has no more parts than kPartsOfRoot roots of its rounds: each costs its columns' joining about a thirtieth of a microsecond. (3, 5, 8: 2 kv heads x 32 columns
 // over 32768 tokens 19.1, 18.9, 20.4 us, 8 chunks of 5 over 8000 31.4, 31.2, 34.3.)
@@ -339,9 +339,14 @@ __global__ __launch_bounds__(256, D == 256 || (D == 128 && NC == 2 && QT == 3) ?
     deal();
     const size_t page_bytes = cache_page_bytes(a.c);
 
-    // the workgroup's next items: own ones go on where those of prefixes end, or (several looks: that is not known yet) begin with the last workgroup
-    const unsigned of_prefixes = (unsigned)__builtin_amdgcn_readlane(upto1, 63) % gridDim.x;
-    unsigned next1 = blockIdx.x, next2 = looks > 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x + (blockIdx.x < of_prefixes ? gridDim.x : 0u) - of_prefixes;
+    // the workgroup's next items.  Own ones go on where those of prefixes end, and there again after the last workgroup: who has one more of a prefix has two fewer own ones
+    // (4 groups of 4 x 32 heads, 1500 tokens: with one fewer 20.9, so 17.1).  Of several looks that place is not known yet: they begin with the last workgroup.
+    const unsigned longer = (unsigned)__builtin_amdgcn_readlane(upto1, 63) % gridDim.x, others = gridDim.x - longer;
+    unsigned next1 = blockIdx.x, next2 = gridDim.x - 1 - blockIdx.x, step2 = gridDim.x;
+    if (looks == 1) {
+        if (blockIdx.x < longer) next2 = 2 * others + blockIdx.x;
+        else next2 = blockIdx.x - longer, step2 = others;
+    }
     for (;;) {
         const int of_look1 = __builtin_amdgcn_readlane(upto1, 63), of_look2 = __builtin_amdgcn_readlane(upto2, 63);
         const bool shared = next1 < (unsigned)before1 + (unsigned)of_look1;
@@ -360,7 +365,7 @@ __global__ __launch_bounds__(256, D == 256 || (D == 128 && NC == 2 && QT == 3) ?
         int place0 = places_before + (owner > 0 ? __builtin_amdgcn_readlane(places_upto, owner - 1) : 0);
         if (!shared) place0 += __builtin_amdgcn_readlane(parts1 > 1 ? items1 : 0, owner);  // (a sequence's places of the prefix come first)
         if (shared) next1 += gridDim.x;
-        else next2 += gridDim.x;
+        else next2 += step2, step2 = gridDim.x;
         const PartOf of = part_of(at, rounds, parts);
         const int unit = of.unit, part = of.part, begin = of.begin, stop = of.stop;
         const int block = h.by_kv.of(unit), head = unit - block * n_kv;
@@ -905,11 +910,11 @@ SharedGrid shared_grid(int n_tokens, int n_seq, int group, int n_heads, int n_kv
     const long long of_pack = columns_of_pack(n_tokens, group, n_heads, n_kv, max_new), of_seq = std::min(n_tokens, max_new) * share;
     SharedGrid g = most;
     // Blocks of 128 columns take a round in 0.0069 us, blocks of 32 in 0.0027 each, but a third launch and larger results cost 11 (D = 64: 0.0056, 0.0022, 8).
-    // Microseconds, blocks of 32 / of 128.  D 128, 32 heads over 8, prefixes of 8000 tokens: 64 columns 21.4 / 29.5, 128 26.3 / 35.6, 256 33.3 / 40.5; of 32000: 64
-    // columns 29.6 / 39.8; of 32768: 256 columns 75.0 / 69.6; 20000 tokens, 32 heads over 2, 1024 columns 96.5 / 78.5.  D 64, one group over 8 kv heads: 96 columns, 40000
-    // tokens 32.1 / 37.3, 128 columns, 57492 tokens 51.3 / 45.5, 256 columns, 8000 tokens 28.2 / 33.6, 16000 42.7 / 39.3; 33 to 64 columns: 32 kv heads, 65536 tokens, 33
-    // columns 86.1 / 114.4, 64 columns 124.4 / 122.2, 12 groups of 16 rows, 8 kv heads, 37128 tokens, 64 columns 171 / 248, and so 58 of 60 calls of any sizes.
-    // (Several groups' own tokens take longer behind the blocks than between them: 152 columns over 16 kv heads, 6 groups of 5877 tokens 113 / 145; 256 over 8, 4 of 28796 191 / 145.)
+    // Microseconds, blocks of 32 / of 128.  D 128, 32 heads over 8, prefixes of 8000 tokens: 64 columns 21.9 / 30.2, 128 26.3 / 35.9, 256 29.3 / 41.2; of 32000: 64
+    // columns 29.1 / 39.7; of 32768: 256 columns 72.3 / 69.7; 20000 tokens, 32 heads over 2, 1024 columns 93.7 / 84.2.  D 64, one group over 8 kv heads: 96 columns, 40000
+    // tokens 30.9 / 36.6, 128 columns, 57492 tokens 50.9 / 45.8, 256 columns, 8000 tokens 24.4 / 33.0, 16000 39.1 / 39.0; 33 to 64 columns: 32 kv heads, 65536 tokens, 33
+    // columns 83.8 / 114.0, 64 columns 118.3 / 122.0, 12 groups of 16 rows, 8 kv heads, 37128 tokens, 64 columns 168 / 247, and so 59 of 60 calls of any sizes.
+    // (Several groups' own tokens take longer behind the blocks than between them: 152 columns over 16 kv heads, 6 groups of 5877 tokens 115 / 148; 256 over 8, 4 of 28796 179 / 138.)
     // D 256, 80 columns over 4 kv heads, 8000 tokens 22.0 / 42.6: never.
     const BlockCosts costs(d);
     const bool in_blocks = all_bf16 && most.prefix_wg > 0 && (double)(packs * n_kv) * (double)rounds * costs.saved_a_round(of_pack) > costs.launch;
