@@ -262,6 +262,22 @@ struct Dealing {
     }
 };
 
+// A workgroup's items of a row of them: one of every gridDim.x, in each run of those 40 / 512 of the workgroups further on, so that items which are longer than others at regular
+// distances (the first row of every group, every eighth prefix) do not all fall to the same workgroups; 40 of them are five on every XCD, which so keeps its kv heads.  (Microseconds,
+// without that / with it / each sequence for itself, D 128: 64 groups of 8 rows, 32 heads over 8, 1024 tokens, 8000 of the first rows' own 548 / 190 / 207 (37 of 512: 234); 64 groups of 4 x
+// 16 heads, 1024 tokens, of every eighth group 8192, 169 / 122 / 188; 64 rows x 32 heads, 2000 tokens, up to 700 of their own 44.5 / 49.1 / 86.)
+struct Turns {
+    unsigned slot, row, items;  // the place in the run, the run's first item, items of the run
+    __device__ __forceinline__ explicit Turns(unsigned first) : slot(first), row(0), items(gridDim.x) {}
+    __device__ __forceinline__ unsigned item() const { return row + slot; }
+    __device__ __forceinline__ void next()
+    {
+        row += items;
+        if (items == gridDim.x) slot += gridDim.x * 40u >> 9, slot -= slot >= gridDim.x ? gridDim.x : 0u;
+        items = gridDim.x;
+    }
+};
+
 // Item `at` of units of so many rounds: its unit, and which part of it, rounds [begin, stop).
 struct PartOf {
     int unit, part, begin, stop;
@@ -327,10 +343,10 @@ __global__ __launch_bounds__(256, D == 256 || (D == 128 && NC == 2 && QT == 3) ?
     const Dealing dealing(all);
     int upto1 = 0, upto2 = 0, places_upto = 0;  // items (of prefixes, own) and places of the look's sequences up to the lane's
     int look = 0, before1 = 0, before2 = 0, places_before = 0;  // the look that `own` is of, and items and places in front of it
-    int parts1 = 1, parts2 = 1, items1 = 0;  // parts of a unit of the prefix and of an own one, items of the former
+    int parts1 = 1, parts2 = 1;  // parts of a unit of the prefix and of an own one
     const auto deal = [&]() {
         parts1 = dealing.parts(own.prefix_rounds), parts2 = dealing.parts(own.rounds);
-        items1 = times(times(own.prefix_blocks, n_kv), parts1);
+        const int items1 = times(times(own.prefix_blocks, n_kv), parts1);
         const int items2 = times(times(own.blocks, n_kv), parts2);
         upto1 = wave_scan(items1), upto2 = wave_scan(items2);
         places_upto = wave_scan((parts1 > 1 ? items1 : 0) + (parts2 > 1 ? items2 : 0));
@@ -342,30 +358,32 @@ __global__ __launch_bounds__(256, D == 256 || (D == 128 && NC == 2 && QT == 3) ?
     // the workgroup's next items.  Own ones go on where those of prefixes end, and there again after the last workgroup: who has one more of a prefix has two fewer own ones
     // (4 groups of 4 x 32 heads, 1500 tokens: with one fewer 20.9, so 17.1).  Of several looks that place is not known yet: they begin with the last workgroup.
     const unsigned longer = (unsigned)__builtin_amdgcn_readlane(upto1, 63) % gridDim.x, others = gridDim.x - longer;
-    unsigned next1 = blockIdx.x, next2 = gridDim.x - 1 - blockIdx.x, step2 = gridDim.x;
+    Turns of_prefixes(blockIdx.x), of_own(gridDim.x - 1 - blockIdx.x);
     if (looks == 1) {
-        if (blockIdx.x < longer) next2 = 2 * others + blockIdx.x;
-        else next2 = blockIdx.x - longer, step2 = others;
+        if (blockIdx.x < longer) of_own = Turns(others + blockIdx.x), of_own.row = others;
+        else of_own = Turns(blockIdx.x - longer), of_own.items = others;
     }
     for (;;) {
         const int of_look1 = __builtin_amdgcn_readlane(upto1, 63), of_look2 = __builtin_amdgcn_readlane(upto2, 63);
-        const bool shared = next1 < (unsigned)before1 + (unsigned)of_look1;
-        if (!shared && next2 >= (unsigned)before2 + (unsigned)of_look2) {
+        const bool shared = of_prefixes.item() < (unsigned)before1 + (unsigned)of_look1;
+        if (!shared && of_own.item() >= (unsigned)before2 + (unsigned)of_look2) {
             if (++look >= looks) break;
             before1 += of_look1, before2 += of_look2, places_before += __builtin_amdgcn_readlane(places_upto, 63);
             own = look_at<kColumns, UNITS>(h, packs, look, lane);
             deal();
             continue;
         }
-        const int of_item = (int)(shared ? next1 - (unsigned)before1 : next2 - (unsigned)before2), upto = shared ? upto1 : upto2;
+        const int of_item = (int)(shared ? of_prefixes.item() - (unsigned)before1 : of_own.item() - (unsigned)before2), upto = shared ? upto1 : upto2;
         const int owner = __ffsll((unsigned long long)__ballot(upto > of_item)) - 1;
         const int prefix = __builtin_amdgcn_readlane(own.prefix, owner);
         const int rounds = __builtin_amdgcn_readlane(shared ? own.prefix_rounds : own.rounds, owner), parts = __builtin_amdgcn_readlane(shared ? parts1 : parts2, owner);
-        const int at = of_item - (owner > 0 ? __builtin_amdgcn_readlane(upto, owner - 1) : 0);
-        int place0 = places_before + (owner > 0 ? __builtin_amdgcn_readlane(places_upto, owner - 1) : 0);
-        if (!shared) place0 += __builtin_amdgcn_readlane(parts1 > 1 ? items1 : 0, owner);  // (a sequence's places of the prefix come first)
-        if (shared) next1 += gridDim.x;
-        else next2 += step2, step2 = gridDim.x;
+        const auto in_front = [&](int v) { return owner > 0 ? __builtin_amdgcn_readlane(v, owner - 1) : 0; };  // (of sums up to the lane's sequence)
+        const int at = of_item - in_front(upto);
+        int place0 = places_before + in_front(places_upto);
+        // (a sequence's places of the prefix come first)
+        if (!shared && __builtin_amdgcn_readlane(parts1, owner) > 1) place0 += __builtin_amdgcn_readlane(upto1, owner) - in_front(upto1);
+        if (shared) of_prefixes.next();
+        else of_own.next();
         const PartOf of = part_of(at, rounds, parts);
         const int unit = of.unit, part = of.part, begin = of.begin, stop = of.stop;
         const int block = h.by_kv.of(unit), head = unit - block * n_kv;
@@ -561,7 +579,8 @@ __global__ __launch_bounds__(256 * kHalves, kHalves) void shared_blocks_kernel(S
     bool dealt = false;
     // (what the lanes know of the sequences is looked up anew for every item: it does not fit next to a block's registers, and nor does what
     // could be computed of the lane's number ahead of the loop)
-    for (unsigned item = blockIdx.x;; item += gridDim.x) {
+    for (Turns turns(blockIdx.x);; turns.next()) {
+        const unsigned item = turns.item();
         int lane = lane_of_block;
         asm volatile("" : "+v"(lane));
         int look = 0, items_before = 0, place0 = 0;  // the look that `own` is of, and items and places in front of it
